@@ -22,9 +22,8 @@
 // 4 KB of the next linear's image (32 rows x 64 columns are contiguous there) or as a 32 x 32 fp32 block that the copy
 // itself adds into the residual stream, so that x is never read here.
 #pragma once
-#include <cuda.h>
-#include <cudaTypedefs.h>
 #include "gemm_tc.cuh"
+#include "tensor_map.cuh"
 
 namespace ttsgpt {
 
@@ -470,22 +469,9 @@ inline PwPlan pw_plan(int N, int K, int rows, bool resid, int n_sm, int fixed_ks
 
 inline cudaError_t pw_encode(CUtensorMap *map, CUtensorMapDataType type, const void *base, size_t cols, size_t rows, size_t pitch_bytes, int box_cols,
                              int box_rows, CUtensorMapSwizzle swizzle) {
-  static std::atomic<PFN_cuTensorMapEncodeTiled> known{nullptr};   // the same address whoever looks it up first
-  PFN_cuTensorMapEncodeTiled encode = known.load(std::memory_order_acquire);
-  if (!encode) {
-    void *fn = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
-    if (e != cudaSuccess) return e;
-    if (found != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
-    encode = (PFN_cuTensorMapEncodeTiled)fn;
-    known.store(encode, std::memory_order_release);
-  }
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch_bytes};
-  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, step[2] = {1, 1};
-  return encode(map, type, 2, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
-             ? cudaSuccess : cudaErrorInvalidValue;
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+  return tensor_map_encode(map, type, base, 2, dims, strides, box, swizzle);
 }
 // an operand image of `blocks` blocks of 128 rows x 128 bytes, as the source of pw_copy_rows
 inline cudaError_t pw_image_map(CUtensorMap *map, const void *img, size_t blocks) {

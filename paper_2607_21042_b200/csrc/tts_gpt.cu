@@ -13,6 +13,7 @@
 #include <string>
 #include <vector>
 
+#include "host.cuh"
 #include "common.cuh"
 #include "linear.cuh"
 #include "attention.cuh"
@@ -142,13 +143,6 @@ struct tts_gpt {
 
 namespace {
 
-// SMs of the current device
-int device_sms() {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && sms > 0) return sms;
-  return 148;
-}
-
 int fail(tts_gpt *h, int code, const char *fmt, ...) {
   char buf[512];
   va_list ap;
@@ -159,6 +153,20 @@ int fail(tts_gpt *h, int code, const char *fmt, ...) {
   g_last_error = buf;
   return code;
 }
+
+}  // namespace
+
+int ttsgpt::fail_op(int code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_last_error = buf;
+  return code;
+}
+
+namespace {
 
 #define CUDA_TRY(h, expr)                                                                      \
   do {                                                                                         \
