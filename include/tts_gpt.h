@@ -48,6 +48,9 @@ enum {
                               k = 8w+j as u = q+8; bf16 scales [N,K/128]: W = s[n,k/128]*(u-8) */
 };
 
+/* Element types of the arguments of the single-kernel entry points that take more than one. */
+enum { TTS_GPT_T_F32 = 0, TTS_GPT_T_BF16 = 1, TTS_GPT_T_F16 = 2 };
+
 enum {
   TTS_GPT_OK = 0,
   TTS_GPT_E_ARG = -1,          /* invalid argument or configuration */
@@ -363,6 +366,75 @@ int32_t tts_gpt_op_layernorm(int32_t R, int32_t d, const float *x, const void *g
 int32_t tts_gpt_op_sample(int32_t R, int32_t V, const float *logits, int32_t top_k,
                           float temperature, const float *uniforms, int32_t *tokens,
                           void *cuda_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Serving many requests from one paged cache without the engine: a program that assembles its own step has the page
+ * lists built (op_page_tables), writes the pass's K and V rows (op_kv_append) and attends over them, the pages that all
+ * requests begin with read once (op_attention_shared); op_attention_cross reads an encoder's states instead.  The layer's
+ * pool is that of the engine: bf16 [n_pages][2 (K,V)][heads][64 tokens][64], or with TTS_GPT_KV_FP8_E4M3 blocks of 4352 bytes
+ * [n_pages][2][heads]: 64 tokens x 64 codes, then the 64 fp32 scales.  All index arrays DEVICE int32.  Each call is one
+ * kernel, allocates nothing, does not wait for the GPU and can be captured into a CUDA graph.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Page lists and slot maps of a pass.  Request i (of n) adds new_len[i] >= 0 tokens to stream stream_ids[i] (NULL: i), which
+ * holds ctx_len[stream].  A stream that holds nothing and is given tokens opens: the first n_shared entries of its page list
+ * become shared_pages[0 .. n_shared-1] and its tokens begin at position 64 n_shared.  Pages are taken from the top of the stack
+ * free_pages (of n_pages places, *free_top of them filled), request by request in the order of the call.  Rows are numbered
+ * request by request too: row r of request i, its k-th, has
+ *   row_stream[r] = stream, row_pos[r] = first position + k, row_slot[r] = page * 64 + position % 64,
+ * row_start[i] (n + 1 of them) is the number of request i's first row; places behind the last row are left as they were.
+ * page_table [max_streams][pages_per_stream] receives the new entries, ctx_len_out[stream] the new lengths of the call's
+ * streams, *free_top_out the new height; ctx_len_out and free_top_out may be ctx_len and free_top.  info: int32 [8], zero before
+ * its first use: {status, rows, pages taken, height of the stack, ...}.  The lengths live on the device, so their
+ * errors do too: info[0] is TTS_GPT_OK, or E_ARG (a negative length, a height outside 0..n_pages), E_STREAM (an id outside
+ * 0..max_streams-1, or one that comes twice), E_CTX_OVERFLOW, E_WORKSPACE (more than max_rows rows) or E_NO_PAGES, and then
+ * nothing but info is written.  Limits: n <= 4096, max_streams <= 32768, pages_per_stream <= 32768 (E_UNSUPPORTED).  Two
+ * calls that share info or update the same streams must be ordered. */
+int32_t tts_gpt_op_page_tables(int32_t n, const int32_t *stream_ids, const int32_t *new_len, int32_t max_streams,
+                               const int32_t *ctx_len, int32_t *ctx_len_out, int32_t n_pages, const int32_t *free_pages,
+                               const int32_t *free_top, int32_t *free_top_out, int32_t n_shared, const int32_t *shared_pages,
+                               int32_t pages_per_stream, int32_t *page_table, int32_t max_rows, int32_t *row_start,
+                               int32_t *row_stream, int32_t *row_pos, int32_t *row_slot, int32_t *info, void *cuda_stream);
+
+/* K and V rows of a pass into their slots: k, v TTS_GPT_T_F32 or TTS_GPT_T_BF16, n_head heads of 64 contiguous values a row, rows
+ * k_stride / v_stride elements apart (so that both may be parts of one QKV array); rows and pool 16-byte aligned.  The bf16 cache
+ * takes each value rounded once, the 8-bit cache codes e4m3(x / s) with s = max|x| / 448 over a head's 64 values (1 if all are
+ * zero).  A row whose row_slot lies outside 0 .. 64 n_pages - 1 is left out.  Slots must be distinct: of two rows with the same
+ * slot either may be kept, for each 16 bytes anew.  Values must be finite in the 8-bit format. */
+int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void *k, int64_t k_stride, const void *v,
+                             int64_t v_stride, const int32_t *row_slot, int32_t kv_fmt, int32_t n_pages, void *kv_layer,
+                             void *cuda_stream);
+
+/* Attention of a batch whose streams begin with the same pages: as tts_gpt_op_attention (row r attends over keys
+ * 0..row_pos[r] of stream row_stream[r], o = softmax(q.K^T / 8) V per head), where the first n_shared entries of the page lists of
+ * all R rows are the same pages, which are read once for all rows and not once for each.  n_shared may be 0.  Query head
+ * h reads the keys of head h / (n_head / n_kv_head), at most 16 to one.  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements
+ * apart; out bf16 [R][n_head*64].  A row with row_pos -1 has no keys: its output is zero.  Several rows may belong to one stream.
+ * Keys on a page outside 0..n_pages-1 are left out, as are those behind the list's pages_per_stream pages.  K and V of the shared
+ * pages must be finite.  fp32 queries enter with 16 bits, the softmax weights are rounded to bf16, sums are fp32; results do
+ * not depend on timing.  R <= 4096, R * n_kv_head <= 262144.
+ * scratch (256-byte aligned, >= scratch_bytes; zero before its first use, by this call or op_attention_cross, in any size)
+ * belongs to one call at a time: calls that may overlap, replays of captured graphs among them, need one each.  Its first
+ * word is set to 1 if a bounded wait inside a kernel ran out; outputs are then incomplete and the scratch must be zeroed. */
+int32_t tts_gpt_op_attention_shared_scratch_bytes(int32_t R, int32_t n_head, int32_t n_kv_head, size_t *bytes);
+int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head, int32_t type, const void *q, int64_t q_stride,
+                                    int32_t kv_fmt, int32_t n_pages, const void *kv_layer, int32_t n_shared,
+                                    const int32_t *page_table, int32_t pages_per_stream, const int32_t *row_stream,
+                                    const int32_t *row_pos, void *out, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/* Attention to an encoder's states: n sequences, queries q_start[i] .. q_start[i+1]-1 (rows of q) over keys
+ * k_start[i] .. k_start[i+1]-1 (rows of k and v), all of them, o = softmax(scale q.K^T) V per head.  Lengths are ragged and
+ * independent; a sequence without keys has zero outputs, rows outside every sequence are left as they were.  q_start, k_start:
+ * ascending, n + 1 each, at most q_rows and k_rows; q_max: at least the longest sequence of queries (rows beyond it are not
+ * computed).  q, k, v, out of one type, TTS_GPT_T_BF16 or TTS_GPT_T_F16; q rows q_stride elements apart with contiguous heads, k and v with
+ * strides of rows and of heads (so both [rows][heads][64], parts of one array, and [heads][rows][64]); out [q_rows][n_head*64].
+ * Heads, roundings and scratch as for op_attention_shared (scratch size independent of the call).  n <= 4096. */
+int32_t tts_gpt_op_attention_cross_scratch_bytes(size_t *bytes);
+int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head, int32_t type, int32_t q_rows, const void *q,
+                                   int64_t q_stride, int32_t k_rows, const void *k, int64_t k_stride, int64_t k_head_stride,
+                                   const void *v, int64_t v_stride, int64_t v_head_stride, const int32_t *q_start,
+                                   const int32_t *k_start, int32_t q_max, float scale, void *out, void *scratch,
+                                   size_t scratch_bytes, void *cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -29,7 +29,20 @@ EXPORTS = [
     "tts_gpt_op_linear_tc_scratch_bytes", "tts_gpt_op_linear_tc", "tts_gpt_op_attention_scratch_bytes", "tts_gpt_op_attention", "tts_gpt_op_attention_static", "tts_gpt_op_attention_cluster",
     "tts_gpt_op_layernorm",
     "tts_gpt_op_sample",
+    "tts_gpt_op_page_tables", "tts_gpt_op_kv_append", "tts_gpt_op_attention_shared_scratch_bytes", "tts_gpt_op_attention_shared",
+    "tts_gpt_op_attention_cross_scratch_bytes", "tts_gpt_op_attention_cross",
 ]
+T_F32, T_BF16, T_F16 = 0, 1, 2
+_TYPES = {torch.float32: T_F32, torch.bfloat16: T_BF16, torch.int16: T_BF16, torch.float16: T_F16}   # int16: bf16 bits
+# Argument types of the calls below that are made once a step or more: declared, ctypes converts plain numbers itself, several
+# times faster than from objects made for each argument.
+_i, _l, _p = C.c_int32, C.c_int64, C.c_void_p  # noqa: E741
+_ARGTYPES = {
+    "tts_gpt_op_page_tables": [_i, _p, _p, _i, _p, _p, _i, _p, _p, _p, _i, _p, _i, _p, _i, _p, _p, _p, _p, _p, _p],
+    "tts_gpt_op_kv_append": [_i, _i, _i, _p, _l, _p, _l, _p, _i, _i, _p, _p],
+    "tts_gpt_op_attention_shared": [_i, _i, _i, _i, _p, _l, _i, _i, _p, _i, _p, _i, _p, _p, _p, _p, C.c_size_t, _p],
+    "tts_gpt_op_attention_cross": [_i, _i, _i, _i, _i, _p, _l, _i, _p, _l, _l, _p, _l, _l, _p, _p, _i, C.c_float, _p, _p, C.c_size_t, _p],
+}
 
 
 class TtsGptError(RuntimeError):
@@ -71,6 +84,8 @@ def load() -> C.CDLL:
         for name in EXPORTS:
             if name != "tts_gpt_last_error":
                 getattr(lib, name).restype = C.c_int32
+        for name, types in _ARGTYPES.items():
+            getattr(lib, name).argtypes = types
         _lib = lib
     return _lib
 
@@ -415,6 +430,149 @@ def op_sample(logits, top_k=0, temperature=1.0, uniforms=None, stream=None):
     out = torch.empty(R, dtype=torch.int32, device=logits.device)
     _check(load().tts_gpt_op_sample(C.c_int32(R), C.c_int32(V), _ptr(logits), C.c_int32(top_k),
                                     C.c_float(temperature), _ptr(uniforms), _ptr(out), _stream_ptr(stream)))
+    return out
+
+
+# ---------------------------------------------------------------------------------------------
+# serving many requests from one paged cache
+# ---------------------------------------------------------------------------------------------
+def _refuse(what):
+    raise TtsGptError(E_ARG, what)
+
+
+def _index(t, name, dev, numel=None):
+    """The address of a contiguous int32 tensor on `dev` (of at least `numel` values)."""
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.device != dev or (numel is not None and t.numel() < numel):
+        _refuse("%s must be a contiguous int32 tensor on %s%s" % (name, dev, "" if numel is None else " with at least %d values" % numel))
+    return t.data_ptr()
+
+
+def _launch(name, dev, stream, *args):
+    """Calls a C entry point with `dev` current, on `stream` or torch's current one of that device."""
+    if dev.type != "cuda":
+        _refuse("%s: tensors must be on a CUDA device" % name)
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _launch(name, dev, stream, *args)
+    st = torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
+    rc = getattr(load(), name)(*args, st)
+    if rc != OK:
+        _check(rc)
+
+
+def _pool(kv_layer, dev):
+    """(format, pages, heads) of one layer's pool: bf16 [pages, 2, heads, 64, 64], or bytes [pages, 2, heads, 4352]."""
+    sh = kv_layer.shape
+    if kv_layer.device != dev or not kv_layer.is_contiguous() or len(sh) < 4 or sh[1] != 2:
+        _refuse("kv_layer must be a contiguous tensor [pages, 2, heads, ...] on %s" % dev)
+    if kv_layer.dtype in (torch.bfloat16, torch.int16) and sh[3:] == (64, 64):
+        return 0, sh[0], sh[2]
+    if kv_layer.dtype == torch.uint8 and sh[3:] == (4352,):
+        return 1, sh[0], sh[2]
+    _refuse("kv_layer must be bf16 [pages, 2, heads, 64, 64] or uint8 [pages, 2, heads, 4352]")
+
+
+def op_page_tables(new_len, ctx_len, page_table, free_pages, free_top, row_start, row_stream, row_pos, row_slot, info,
+                   stream_ids=None, shared_pages=None, ctx_len_out=None, free_top_out=None, stream=None):
+    """Page lists and slot maps of a pass from the requests' lengths; everything int32 on one device, written in place.  row_stream,
+    row_pos and row_slot hold as many rows as the pass may have.  ctx_len_out, free_top_out: None updates ctx_len, free_top.
+    info: 8 values, zero at first; info[0] is the status the lengths lead to, which lives on the device like they do."""
+    dev, n = new_len.device, new_len.numel()
+    if page_table.dim() != 2 or page_table.shape[0] != ctx_len.numel():
+        _refuse("page_table must be [streams, pages of a stream], ctx_len [streams]")
+    if row_pos.numel() != row_stream.numel() or row_slot.numel() != row_stream.numel():
+        _refuse("row_stream, row_pos and row_slot must have the same length")
+    streams = ctx_len.numel()
+    _launch("tts_gpt_op_page_tables", dev, stream, n, None if stream_ids is None else _index(stream_ids, "stream_ids", dev, n), _index(new_len, "new_len", dev),
+            streams, _index(ctx_len, "ctx_len", dev), _index(ctx_len if ctx_len_out is None else ctx_len_out, "ctx_len_out", dev, streams),
+            free_pages.numel(), _index(free_pages, "free_pages", dev), _index(free_top, "free_top", dev, 1),
+            _index(free_top if free_top_out is None else free_top_out, "free_top_out", dev, 1), 0 if shared_pages is None else shared_pages.numel(),
+            None if shared_pages is None else _index(shared_pages, "shared_pages", dev), page_table.shape[1], _index(page_table, "page_table", dev),
+            row_stream.numel(), _index(row_start, "row_start", dev, n + 1), _index(row_stream, "row_stream", dev), _index(row_pos, "row_pos", dev),
+            _index(row_slot, "row_slot", dev), _index(info, "info", dev, 8))
+
+
+def op_kv_append(k, v, kv_layer, row_slot, stream=None):
+    """K and V rows [R, heads * 64] (fp32 or bf16; rows may be strided) into their slots of the pool."""
+    dev = k.device
+    fmt, pages, heads = _pool(kv_layer, dev)
+    if k.dtype != v.dtype or k.dtype not in _TYPES or k.dtype == torch.float16 or k.shape != v.shape or k.dim() != 2 or k.shape[1] != heads * 64 \
+            or v.device != dev or k.stride(1) != 1 or v.stride(1) != 1:
+        _refuse("k and v must be [R, %d] of one type, fp32 or bf16, on %s, with contiguous rows" % (heads * 64, dev))
+    R = k.shape[0]
+    # the stride of a single row addresses nothing
+    ks, vs = (k.stride(0), v.stride(0)) if R > 1 else (heads * 64, heads * 64)
+    _launch("tts_gpt_op_kv_append", dev, stream, R, heads, _TYPES[k.dtype], k.data_ptr(), ks, v.data_ptr(), vs, _index(row_slot, "row_slot", dev, R),
+            fmt, pages, kv_layer.data_ptr())
+
+
+def _scratch(scratch, dev):
+    if scratch.dtype != torch.uint8 or scratch.device != dev or not scratch.is_contiguous():
+        _refuse("scratch must be a contiguous uint8 tensor on %s" % dev)
+    return scratch.data_ptr(), scratch.numel()
+
+
+def op_attention_shared_scratch(R, n_head, n_kv_head, device):
+    n = C.c_size_t(0)
+    _check(load().tts_gpt_op_attention_shared_scratch_bytes(C.c_int32(R), C.c_int32(n_head), C.c_int32(n_kv_head), C.byref(n)))
+    return torch.zeros(n.value, dtype=torch.uint8, device=device)
+
+
+def op_attention_shared(q, kv_layer, page_table, row_stream, row_pos, n_shared, scratch=None, out=None, stream=None):
+    """Attention of rows q [R, heads * 64] (fp32 or bf16) over a paged cache whose page lists all begin with the same n_shared
+    pages.  The pool may have fewer heads than q.  Returns bf16 bits [R, heads * 64], or `out`."""
+    dev = q.device
+    fmt, pages, kv_heads = _pool(kv_layer, dev)
+    if q.dim() != 2 or q.dtype not in _TYPES or q.dtype == torch.float16 or q.shape[1] % 64 or q.stride(1) != 1:
+        _refuse("q must be [R, heads * 64], fp32 or bf16, with contiguous rows")
+    if page_table.dim() != 2:
+        _refuse("page_table must be [streams, pages of a stream]")
+    R, heads = q.shape[0], q.shape[1] // 64
+    if out is None:
+        out = torch.empty((R, heads * 64), dtype=torch.int16, device=dev)
+    elif out.shape != q.shape or out.dtype not in (torch.int16, torch.bfloat16) or out.device != dev or not out.is_contiguous():
+        _refuse("out must be a contiguous bf16 tensor of q's shape")
+    if scratch is None:
+        scratch = op_attention_shared_scratch(R, heads, kv_heads, dev)
+    sp, sn = _scratch(scratch, dev)
+    _launch("tts_gpt_op_attention_shared", dev, stream, R, heads, kv_heads, _TYPES[q.dtype], q.data_ptr(), q.stride(0) if R > 1 else heads * 64, fmt, pages,
+            kv_layer.data_ptr(), n_shared, _index(page_table, "page_table", dev), page_table.shape[1], _index(row_stream, "row_stream", dev, R),
+            _index(row_pos, "row_pos", dev, R), out.data_ptr(), sp, sn)
+    return out
+
+
+def op_attention_cross_scratch(device):
+    n = C.c_size_t(0)
+    _check(load().tts_gpt_op_attention_cross_scratch_bytes(C.byref(n)))
+    return torch.zeros(n.value, dtype=torch.uint8, device=device)
+
+
+def op_attention_cross(q, k, v, q_start, k_start, q_max, scale=0.125, scratch=None, out=None, stream=None):
+    """Attention of ragged sequences of queries q [rows, heads, 64] to keys and values k, v [rows, kv heads, 64] of other lengths, bf16
+    or fp16; sequence i has rows q_start[i] .. q_start[i+1]-1 of q and k_start[i] .. k_start[i+1]-1 of k and v, whose rows and heads
+    may be strided.  q_max: at least the longest sequence of queries.  Returns [rows, heads, 64] (rows of no sequence undefined), or `out`
+    (in which they are left as they were)."""
+    dev = q.device
+    if q.dim() != 3 or k.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16) or k.dtype != q.dtype or v.dtype != q.dtype or q.shape[2] != 64 or k.shape[2] != 64 \
+            or v.shape != k.shape or k.device != dev or v.device != dev or q.stride(2) != 1 or k.stride(2) != 1 or v.stride(2) != 1 or (q.shape[1] > 1 and q.stride(1) != 64):
+        _refuse("q must be [rows, heads, 64] with contiguous heads, k and v [rows, kv heads, 64], all bf16 or all fp16, on one device")
+    n = q_start.numel() - 1
+    if n < 1 or k_start.numel() != n + 1:
+        _refuse("q_start and k_start must have one value more than there are sequences")
+    rows, heads = q.shape[0], q.shape[1]
+    if out is None:
+        out = torch.empty((rows, heads, 64), dtype=q.dtype, device=dev)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or not out.is_contiguous():
+        _refuse("out must be a contiguous tensor of q's shape and type")
+    if scratch is None:
+        scratch = op_attention_cross_scratch(dev)
+    sp, sn = _scratch(scratch, dev)
+    # strides of a single row or head address nothing
+    kr, vr = (k.stride(0), v.stride(0)) if k.shape[0] > 1 else (64, 64)
+    kh, vh = (k.stride(1), v.stride(1)) if k.shape[1] > 1 else (64, 64)
+    _launch("tts_gpt_op_attention_cross", dev, stream, n, heads, k.shape[1], _TYPES[q.dtype], rows, q.data_ptr(), q.stride(0) if rows > 1 else heads * 64,
+            k.shape[0], k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, _index(q_start, "q_start", dev), _index(k_start, "k_start", dev), q_max, scale,
+            out.data_ptr(), sp, sn)
     return out
 
 

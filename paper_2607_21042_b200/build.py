@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtts_gpt.so")
 EXTRA = os.environ.get("TTS_EXTRA_NVCC", "").split()
-SOURCES = [os.path.join(CSRC, "tts_gpt.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("tts_gpt.cu", "serving_ops.cu")]
 
 
 def _deps():
@@ -41,7 +41,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
     cmd = [nvcc_path(), "-std=c++17", "-O3", "-lineinfo", "-shared", "-Xcompiler", "-fPIC",
-           "-gencode", "arch=compute_100a,code=sm_100a", "-o", LIB] + EXTRA + SOURCES
+           "-gencode", "arch=compute_100a,code=sm_100a", "--threads", "2", "-o", LIB] + EXTRA + SOURCES
     if verbose:
         cmd.insert(1, "-Xptxas")
         cmd.insert(2, "-v")

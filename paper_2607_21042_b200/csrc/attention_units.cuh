@@ -1,0 +1,647 @@
+// Attention of query tiles of up to 16 rows over units of 32 keys, on the warp-level tensor pipe: the batch that shares a long
+// prefix, and cross attention with few queries a sequence (Section I: the decode engine's attention kernels).
+//
+// A tile is up to 16 query rows that read the same keys: the heads of a group for one row (its own pages), as many rows
+// as fit for the shared pages, or neighbouring rows of a sequence.  For every tile, with scores s_j = scale q.k_j,
+//     m = max s_j,   l = sum 2^(s_j - m),   o = sum 2^(s_j - m) v_j          (log2 units)
+// over a range of its keys; the results of a tile's ranges, and of a row's two tiles, meet as
+//     O = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p,   M = max m_p,
+// with M, the sums and o in fp32; zero where no key is left.
+//
+// Work split.  The units of all tiles are laid end to end and cut into one range a warp, equal to within a unit whatever the
+// lengths are.  A tile inside one range is finished by its warp.  Parts of the others go to scratch, and the warp that
+// arrives last at the tile's ticket (for the shared prefix: at that of each row and group) adds them in the order of
+// their keys: no warp waits for another, and results do not depend on timing.
+//
+// Instructions.  Queries are the 16-row operand of m16n8k16, keys the 8-wide one, so the scores come out in the layout in which
+// P enters P V.  Queries in fp32 enter as two bf16 parts (16 bits), P is rounded to the cache's type (half a step of it: as
+// much again as the rounding of the output).  A unit is copied two or four ahead per warp, as 16-key boxes of K and of V with the
+// 128-byte swizzle; of the 8-bit cache as plain rows, whose codes become bf16 in registers (exact).
+#pragma once
+#include <cuda_fp16.h>
+#include "page_tables.cuh"
+#include "tcgen05.cuh"
+#include "tensor_map.cuh"
+
+namespace ttsgpt {
+
+constexpr int kUnWarps = 12;
+constexpr int kUnKeys = 32;                 // keys of a unit: two to a page
+constexpr int kUnBox = 16;                  // keys of one copy
+constexpr int kUnTile = 16;                 // query rows of a tile
+constexpr int kUnMaxSeq = 4096;             // rows (shared) or sequences (cross) of a call
+constexpr int kUnMaxCtas = 160;
+constexpr int kUnMaxWarps = kUnMaxCtas * kUnWarps;
+constexpr int kUnPitch = 68;                // floats of a partial row: o[64], m, l, and two to keep 16-byte rows
+constexpr unsigned long long kUnWaitNs = 2000000000ull;
+
+enum { KV_BF16 = 0, KV_F16 = 1, KV_E4M3 = 2 };   // what the keys and values are stored as
+
+struct UnitArgs {
+  const void *q;
+  uint16_t *out;                // [rows][H * 64]
+  long long q_stride;           // elements between query rows
+  int q_rows, H, Hkv, G;        // G = H / Hkv query heads share a head of keys
+  int rpt;                      // query rows of a tile: 16 / G
+  float scale;                  // of the scores, in log2 units
+  // shared prefix: pages
+  const int *page_table, *row_stream, *row_pos;
+  const unsigned char *pool;
+  int pps, n_shared, n_pages;
+  // cross: sequences
+  const int *q_start, *k_start;
+  int n_seq, q_max, k_rows;
+  int k_tokens_first, v_tokens_first;   // the map's middle dimension is the token, not the head
+  // scratch
+  int *err;                     // [0]: set when a wait ran out
+  unsigned *tickets;
+  float *part;
+  int suffix_part0;             // partial row at which those of the rows' own tiles begin
+};
+
+template <int KV> struct UnitLayout {
+  static constexpr int kStages = KV == KV_E4M3 ? 4 : 2;
+  static constexpr int kHalf = KV == KV_E4M3 ? kUnKeys * kHeadDim : kUnKeys * kHeadDim * 2;   // K (or V) of a unit
+  static constexpr int kStage = KV == KV_E4M3 ? 2 * kHalf + 2 * kUnKeys * 4 : 2 * kHalf;   // codes of K and V, scales of K and V
+};
+template <int KV> inline size_t units_smem_bytes(int n) {
+  return (size_t)kUnWarps * UnitLayout<KV>::kStages * UnitLayout<KV>::kStage + 1024 + kUnWarps * UnitLayout<KV>::kStages * 8 + (size_t)(n + 1) * 4 + 64;
+}
+
+__device__ __forceinline__ void un_box(const CUtensorMap *map, int c1, int c2, unsigned char *dst, uint64_t *bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(0), "r"(c1), "r"(c2), "r"(smem_u32(bar)) : "memory");
+}
+template <bool F16>
+__device__ __forceinline__ void un_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (F16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else mma_bf16_16816(c, a[0], a[1], a[2], a[3], b0, b1);
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t un_pack(float lo, float hi) {
+  if constexpr (F16) { const __half2 v = __floats2half2_rn(lo, hi); return *reinterpret_cast<const uint32_t *>(&v); }
+  else return pack_bf16x2(lo, hi);
+}
+// Two e4m3 codes, in the upper bytes of the halves of x (the lower bytes are ignored), as bf16: the bits moved into place are the
+// value times 2^-120, exactly (denormals too).  The NaN code reads as 480.
+__device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t x) {
+  const uint32_t y = (x & 0x80008000u) | ((x >> 4) & 0x07F007F0u);
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(y), "r"(0x7B807B80u));   // 2^120
+  return r;
+}
+
+// what a unit is; one per lane, 32 units at a time
+struct UnitDesc {
+  int c1, c2;      // where its keys lie: token of the page and block of the pool, or head and token row
+  int n;           // keys that exist (0: nothing is copied)
+  int u0, nu;      // first unit and units of its tile
+  int row0;        // first query row of the tile
+  int hn;          // head of keys | query rows times heads of the tile << 16
+  int own;         // shared prefix: 1: the keys are the row's own
+};
+
+// SHARED: pages, common ones first; otherwise sequences of their own.  KV: KV_*.  QF32: queries in fp32, else of the keys' type
+// (bf16 for the 8-bit cache).
+template <bool SHARED, int KV, bool QF32>
+__global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                                                                           const UnitArgs a) {
+  using L = UnitLayout<KV>;
+  constexpr bool F16 = KV == KV_F16;
+  extern __shared__ __align__(16) unsigned char un_smem_raw[];
+  unsigned char *stages = un_smem_raw + ((1024u - (smem_u32(un_smem_raw) & 1023u)) & 1023u);
+  uint64_t *bars = reinterpret_cast<uint64_t *>(stages + (size_t)kUnWarps * L::kStages * L::kStage);
+  int *first = reinterpret_cast<int *>(bars + kUnWarps * L::kStages);   // running sums of units: of a head of each row, or of all tiles of each sequence
+  __shared__ int warp_tot[kUnWarps];
+  __shared__ unsigned long long lead_s;   // keys of the longest row, and that row: its list names the shared pages
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int n_items = SHARED ? a.q_rows : a.n_seq;
+
+  if (lane < L::kStages) mbar_init(&bars[warp * L::kStages + lane], 1);
+  if (tid == 0) lead_s = 0;
+  __syncthreads();
+  // ---- running sums ----
+  auto q_span = [&](int i, int &b, int &e) {   // query rows of a sequence
+    b = min(max(a.q_start[i], 0), a.q_rows);
+    e = min(min(max(a.q_start[i + 1], b), a.q_rows), b + a.q_max);
+  };
+  auto k_span = [&](int i, int &b, int &e) {
+    b = min(max(a.k_start[i], 0), a.k_rows);
+    e = min(max(a.k_start[i + 1], b), a.k_rows);
+  };
+  const int prefix_keys = SHARED ? a.n_shared * kPageTokens : 0;
+  auto own_keys = [&](int r) { return min(max(a.row_pos[r] + 1, 0), a.pps * kPageTokens) - prefix_keys; };   // may be negative
+  int carry = 0;
+  for (int base = 0; base < n_items; base += kUnWarps * 32) {
+    const int i = base + tid;
+    int u = 0;
+    if (i < n_items) {
+      if (SHARED) {
+        const int n = own_keys(i);
+        atomicMax(&lead_s, ((unsigned long long)(unsigned)(n + prefix_keys) << 32) | (unsigned)i);
+        u = n > 0 ? (n + kUnKeys - 1) / kUnKeys : (a.n_shared == 0 ? 1 : 0);   // a row without any key still gets its zeros
+      } else {
+        int qb, qe, kb, ke;
+        q_span(i, qb, qe);
+        k_span(i, kb, ke);
+        u = a.Hkv * ((qe - qb + a.rpt - 1) / a.rpt) * max(1, (ke - kb + kUnKeys - 1) / kUnKeys);
+      }
+    }
+    int incl = u;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    __syncthreads();
+    if (lane == 31) warp_tot[warp] = incl;
+    __syncthreads();
+    int before = carry, all = carry;
+#pragma unroll
+    for (int w = 0; w < kUnWarps; ++w) { if (w < warp) before += warp_tot[w]; all += warp_tot[w]; }
+    if (i < n_items) first[i] = before + incl - u;
+    carry = all;
+  }
+  if (tid == 0) first[n_items] = carry;
+  __syncthreads();
+  const int lead = (int)(lead_s & 0xFFFFFFFFu), lead_keys = (int)(lead_s >> 32);
+  const int tiles_head = SHARED && a.n_shared > 0 ? (a.q_rows + a.rpt - 1) / a.rpt : 0;   // prefix tiles of a head
+  const int prefix_nu = SHARED ? 2 * a.n_shared : 0;                                      // units of each of them
+  const int U_prefix = a.Hkv * tiles_head * prefix_nu;
+  const long long T = (long long)U_prefix + (long long)carry * (SHARED ? a.Hkv : 1);
+  // W ranges, none of them empty; range j goes to CTA j % grid, so that few units reach every CTA
+  const int W = (int)min(T, (long long)gridDim.x * kUnWarps);
+  const int w = warp * gridDim.x + blockIdx.x;
+  const int u_begin = w < W ? (int)(T * w / W) : 0, u_end = w < W ? (int)(T * (w + 1) / W) : 0;
+  auto warp_of = [&](int u) { return (int)((((long long)u + 1) * W - 1) / T); };
+
+  auto find = [&](int x) {   // last item that begins at or before x
+    int lo = 0, hi = n_items - 1;
+    while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (first[m] <= x) lo = m; else hi = m - 1; }
+    return lo;
+  };
+  auto describe = [&](int u) {
+    UnitDesc d = {0, 0, 0, u, 1, 0, 0, 0};
+    if (u >= u_end) return d;
+    if constexpr (SHARED) {
+      int r, kvh, page, n, list;
+      if (u < U_prefix) {
+        const int tile = u / prefix_nu, k = u - tile * prefix_nu;
+        kvh = tile / tiles_head;
+        r = (tile - kvh * tiles_head) * a.rpt;
+        d.u0 = u - k; d.nu = prefix_nu;
+        d.hn = kvh | (min(a.rpt, a.q_rows - r) * a.G << 16);
+        page = k >> 1; list = lead;
+        n = min(kUnKeys, lead_keys - k * kUnKeys);   // a page of the shared ones holds 64 keys, unless no row is that long
+        d.c1 = (k & 1) * kUnKeys;
+      } else {
+        const int v = u - U_prefix;
+        r = find(v / a.Hkv);
+        const int nu = first[r + 1] - first[r], x = v - first[r] * a.Hkv;
+        kvh = x / nu;
+        const int k = x - kvh * nu;
+        d.u0 = u - k; d.nu = nu; d.own = 1;
+        d.hn = kvh | (a.G << 16);
+        page = a.n_shared + (k >> 1); list = r;
+        n = min(kUnKeys, own_keys(r) - k * kUnKeys);
+        d.c1 = (k & 1) * kUnKeys;
+      }
+      d.row0 = r;
+      if (n > 0) {
+        const int phys = a.page_table[(size_t)a.row_stream[list] * a.pps + page];
+        if (phys >= 0 && phys < a.n_pages) { d.n = n; d.c2 = phys * 2 * a.Hkv + kvh; }   // a page that is none has no keys
+      }
+    } else {
+      const int s = find(u), x = u - first[s];
+      int qb, qe, kb, ke;
+      q_span(s, qb, qe);
+      k_span(s, kb, ke);
+      const int nu = max(1, (ke - kb + kUnKeys - 1) / kUnKeys), tile = x / nu, k = x - tile * nu;
+      const int blocks = (qe - qb + a.rpt - 1) / a.rpt, kvh = tile / blocks;
+      d.row0 = qb + (tile - kvh * blocks) * a.rpt;
+      d.u0 = u - k; d.nu = nu;
+      d.hn = kvh | (min(a.rpt, qe - d.row0) * a.G << 16);
+      d.c1 = kvh; d.c2 = kb + k * kUnKeys;
+      d.n = min(kUnKeys, max(0, ke - d.c2));
+    }
+    return d;
+  };
+
+  unsigned char *stage0 = stages + (size_t)warp * L::kStages * L::kStage;
+  uint64_t *bar = bars + warp * L::kStages;
+  UnitDesc nxt, cur;                          // descriptions of the units being copied, and of those being computed
+  auto issue = [&](int i) {                   // unit u_begin + i into stage i % kStages
+    if ((i & 31) == 0) nxt = describe(u_begin + i + lane);
+    const int c1 = __shfl_sync(0xFFFFFFFFu, nxt.c1, i & 31), c2 = __shfl_sync(0xFFFFFFFFu, nxt.c2, i & 31), n = __shfl_sync(0xFFFFFFFFu, nxt.n, i & 31);
+    unsigned char *st = stage0 + (size_t)(i % L::kStages) * L::kStage;
+    uint64_t *b = &bar[i % L::kStages];
+    if (elect_one()) {
+      if constexpr (KV == KV_E4M3) {
+        const uint32_t codes = (uint32_t)n * kHeadDim, scales = (uint32_t)(n + 3) / 4 * 16;
+        mbar_expect_tx(b, 2 * (codes + scales));
+        if (n > 0) {
+          const unsigned char *kp = a.pool + (size_t)c2 * kE4m3BlockBytes, *vp = kp + (size_t)a.Hkv * kE4m3BlockBytes;
+          bulk_copy_g2s(st, kp + c1 * kHeadDim, codes, b);
+          bulk_copy_g2s(st + 2 * L::kHalf, kp + kPageTokens * kHeadDim + 4 * c1, scales, b);
+          bulk_copy_g2s(st + L::kHalf, vp + c1 * kHeadDim, codes, b);
+          bulk_copy_g2s(st + 2 * L::kHalf + kUnKeys * 4, vp + kPageTokens * kHeadDim + 4 * c1, scales, b);
+        }
+      } else {
+        const int boxes = (n + kUnBox - 1) / kUnBox;
+        mbar_expect_tx(b, (uint32_t)boxes * 2 * kUnBox * 128);
+#pragma unroll
+        for (int x = 0; x < kUnKeys / kUnBox; ++x)
+          if (x < boxes) {
+            const int o = x * kUnBox;
+            if constexpr (SHARED) {
+              un_box(&k_map, c1 + o, c2, st + o * 128, b);
+              un_box(&v_map, c1 + o, c2 + a.Hkv, st + L::kHalf + o * 128, b);
+            } else {
+              un_box(&k_map, a.k_tokens_first ? c2 + o : c1, a.k_tokens_first ? c1 : c2 + o, st + o * 128, b);
+              un_box(&v_map, a.v_tokens_first ? c2 + o : c1, a.v_tokens_first ? c1 : c2 + o, st + L::kHalf + o * 128, b);
+            }
+          }
+      }
+    }
+    __syncwarp();
+  };
+
+  const int n_mine = u_end - u_begin;
+  int issued = 0;
+  for (; issued < min(n_mine, L::kStages); ++issued) issue(issued);
+
+  // ---- state of the tile ----
+  uint32_t qa[4][4], qlo[QF32 ? 4 : 1][4];    // query fragments by 16 dimensions; fp32: what the first part leaves
+  float o[8][4], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;   // rows g and g + 8
+  int tile_u0 = -1, tile_nu = 0, row0 = 0, kvh = 0, n_i = 0, own = 0, vis0 = 0, vis1 = 0;
+  bool whole = true, dead = false;
+
+  // dimension of accumulator column e (0, 1) of fragment j
+  auto dim_of = [&](int j, int e) { return KV == KV_E4M3 ? 16 * t + 8 * e + j : 8 * j + 2 * t + e; };
+  auto q_ptr = [&](int i) { return (size_t)(row0 + i / a.G) * a.q_stride + (size_t)(kvh * a.G + i % a.G) * kHeadDim; };
+  auto load_q = [&]() {
+    const bool h0 = g < n_i, h1 = g + 8 < n_i;
+    const size_t p0 = h0 ? q_ptr(g) : 0, p1 = h1 ? q_ptr(g + 8) : 0;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {           // fragment f: row g + 8 (f & 1), upper half of the dimensions where f >= 2
+        const int dim = KV == KV_E4M3 ? 16 * t + 4 * ks + 2 * (f >> 1) : 16 * ks + 2 * t + 8 * (f >> 1);
+        const bool have = f & 1 ? h1 : h0;
+        const size_t p = (f & 1 ? p1 : p0) + dim;
+        if constexpr (QF32) {
+          const float2 x = have ? *reinterpret_cast<const float2 *>(reinterpret_cast<const float *>(a.q) + p) : make_float2(0.f, 0.f);
+          const float hx = __uint_as_float(__float_as_uint(x.x) & 0xFFFF0000u), hy = __uint_as_float(__float_as_uint(x.y) & 0xFFFF0000u);
+          qa[ks][f] = pack_bf16x2(hx, hy);
+          qlo[ks][f] = pack_bf16x2(x.x - hx, x.y - hy);
+        } else {
+          qa[ks][f] = have ? *reinterpret_cast<const uint32_t *>(reinterpret_cast<const uint16_t *>(a.q) + p) : 0u;
+        }
+      }
+  };
+  auto out_ptr = [&](int i) { return a.out + ((size_t)(row0 + i / a.G) * a.H + kvh * a.G + i % a.G) * kHeadDim; };
+
+  // ---- the parts of up to 16 query rows, added in the order of their keys: lanes 2 i and 2 i + 1 take row i, half the dimensions each ----
+  // n0 parts from partial row s0 on, each `pitch0` rows behind the other, then n1 from s1
+  auto merge = [&](bool mine, int i, int n0, const float *s0, size_t step0, const float *s1b, int n1, const float *s1, size_t step1) {
+    const int half = (lane & 1) * 32;
+    float M = -INFINITY;
+    auto part = [&](int p) { return p < n0 ? (p == 0 ? s0 : s1b + (size_t)(p - 1) * step0) : s1 + (size_t)(p - n0) * step1; };
+    const int n = mine ? n0 + n1 : 0;
+    for (int p = 0; p < n; ++p) M = fmaxf(M, __ldcg(part(p) + 64));
+    float acc[32], den = 0.f;
+#pragma unroll
+    for (int c = 0; c < 32; ++c) acc[c] = 0.f;
+    for (int p = 0; p < n; ++p) {
+      const float *x = part(p);
+      const float mp = __ldcg(x + 64), f = mp == -INFINITY ? 0.f : exp2f(mp - M);
+      den = fmaf(f, __ldcg(x + 65), den);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const float4 v = __ldcg(reinterpret_cast<const float4 *>(x + half) + c);
+        if (f > 0.f) {
+          acc[4 * c] = fmaf(f, v.x, acc[4 * c]); acc[4 * c + 1] = fmaf(f, v.y, acc[4 * c + 1]);
+          acc[4 * c + 2] = fmaf(f, v.z, acc[4 * c + 2]); acc[4 * c + 3] = fmaf(f, v.w, acc[4 * c + 3]);
+        }
+      }
+    }
+    const float inv = den > 0.f || den != den ? 1.0f / den : 0.f;
+    if (mine && !*reinterpret_cast<volatile int *>(a.err)) {
+      uint16_t *dst = out_ptr(i) + half;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<uint4 *>(dst + 8 * c) =
+            make_uint4(un_pack<F16>(acc[8 * c] * inv, acc[8 * c + 1] * inv), un_pack<F16>(acc[8 * c + 2] * inv, acc[8 * c + 3] * inv),
+                       un_pack<F16>(acc[8 * c + 4] * inv, acc[8 * c + 5] * inv), un_pack<F16>(acc[8 * c + 6] * inv, acc[8 * c + 7] * inv));
+    }
+  };
+
+  auto finish = [&]() {                       // the warp leaves its tile
+    l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 1); l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 2);
+    l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 1); l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 2);
+    const int last = tile_u0 + tile_nu - 1;
+    const int w0 = warp_of(tile_u0), w1 = warp_of(last);
+    // does anything else feed this tile's rows?
+    int prefix_tile = 0, p_w0 = 0, p_n = 0;   // parts of the prefix tile of this row and group
+    if constexpr (SHARED) {
+      if (own && tiles_head > 0) {
+        prefix_tile = kvh * tiles_head + row0 / a.rpt;
+        p_w0 = warp_of(prefix_tile * prefix_nu);
+        p_n = warp_of(prefix_tile * prefix_nu + prefix_nu - 1) - p_w0 + 1;
+      }
+    }
+    const bool alone = w0 == w1 && (!SHARED || (own && p_n == 0));
+    if (alone) {
+      const float i0 = l0 > 0.f || l0 != l0 ? 1.0f / l0 : 0.f, i1 = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
+      if (!dead) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (g + 8 * e < n_i) {
+            uint16_t *dst = out_ptr(g + 8 * e);
+            const float inv = e ? i1 : i0;
+            if constexpr (KV == KV_E4M3) {
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf)
+                *reinterpret_cast<uint4 *>(dst + 16 * t + 8 * hf) =
+                    make_uint4(un_pack<F16>(o[0][2 * e + hf] * inv, o[1][2 * e + hf] * inv), un_pack<F16>(o[2][2 * e + hf] * inv, o[3][2 * e + hf] * inv),
+                               un_pack<F16>(o[4][2 * e + hf] * inv, o[5][2 * e + hf] * inv), un_pack<F16>(o[6][2 * e + hf] * inv, o[7][2 * e + hf] * inv));
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) *reinterpret_cast<uint32_t *>(dst + 8 * j + 2 * t) = un_pack<F16>(o[j][2 * e] * inv, o[j][2 * e + 1] * inv);
+            }
+          }
+        }
+      }
+      return;
+    }
+    // ---- this part into scratch.  Slots: a tile's parts are numbered tile + warp, which never repeats along the units; sequences
+    // (whose tiles meet only where a range ends) have two slots a warp ----
+    auto prefix_slot = [&](int tile, int wp) { return a.part + (size_t)(tile + wp) * kUnTile * kUnPitch; };
+    auto own_slot = [&](int r, int h, int wp) { return a.part + ((size_t)a.suffix_part0 + (size_t)(r * a.Hkv + h + wp) * a.G) * kUnPitch; };
+    auto seq_slot = [&](int wp, bool begins) { return a.part + (size_t)(2 * wp + (begins ? 1 : 0)) * kUnTile * kUnPitch; };
+    float *dst = SHARED ? (own ? own_slot(row0, kvh, w) : prefix_slot(tile_u0 / max(1, prefix_nu), w)) : seq_slot(w, w == w0);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (g + 8 * e < n_i) {
+        float *p = dst + (g + 8 * e) * kUnPitch;
+        if constexpr (KV == KV_E4M3) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<float4 *>(p + 16 * t + 4 * q) = make_float4(o[4 * (q & 1)][2 * e + (q >> 1)], o[4 * (q & 1) + 1][2 * e + (q >> 1)],
+                                                                          o[4 * (q & 1) + 2][2 * e + (q >> 1)], o[4 * (q & 1) + 3][2 * e + (q >> 1)]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) *reinterpret_cast<float2 *>(p + 8 * j + 2 * t) = make_float2(o[j][2 * e], o[j][2 * e + 1]);
+        }
+        if (t == 0) { p[64] = e ? m1 : m0; p[65] = e ? l1 : l0; }
+      }
+    __threadfence();
+    __syncwarp();
+    const int i = lane >> 1;
+    if constexpr (SHARED) {
+      // every row and group of the tile has a ticket that counts the parts of its prefix tile and of its own keys
+      const int rows = n_i / a.G;
+      unsigned want = 0, got = 0;
+      int my_r = row0 + min(lane, rows - 1), own_nu = 0, o_w0 = 0, o_n = 0;
+      if (own) { o_w0 = w0; o_n = w1 - w0 + 1; }
+      else {
+        p_w0 = w0; p_n = w1 - w0 + 1;
+        prefix_tile = tile_u0 / prefix_nu;
+        own_nu = first[my_r + 1] - first[my_r];
+        if (own_nu > 0) {
+          const int b = U_prefix + first[my_r] * a.Hkv + kvh * own_nu;
+          o_w0 = warp_of(b);
+          o_n = warp_of(b + own_nu - 1) - o_w0 + 1;
+        }
+      }
+      want = (unsigned)(p_n + o_n);
+      bool done = false;
+      if (lane < rows) {
+        unsigned *tk = a.tickets + (size_t)my_r * a.Hkv + kvh;
+        got = atomicAdd(tk, 1u) + 1u;
+        done = got == want;
+        if (done) *tk = 0u;
+      }
+      const unsigned mask = __ballot_sync(0xFFFFFFFFu, done);
+      if (mask) {
+        __threadfence();
+        const int li = i / a.G;                 // row of the tile that lanes 2 i, 2 i + 1 work for
+        const int src = min(li, 31);
+        const int ow0 = __shfl_sync(0xFFFFFFFFu, o_w0, src), on = __shfl_sync(0xFFFFFFFFu, o_n, src);
+        const bool mine = i < n_i && ((mask >> li) & 1u);
+        const int r = row0 + li, gi = i - li * a.G;
+        const int pi = (r % a.rpt) * a.G + gi;  // place in the prefix tile
+        const float *pp = prefix_slot(prefix_tile, p_w0) + pi * kUnPitch;
+        const float *op = own_slot(r, kvh, ow0) + gi * kUnPitch;
+        merge(mine, i, p_n, pp, (size_t)kUnTile * kUnPitch, pp + (size_t)kUnTile * kUnPitch, on, op, (size_t)a.G * kUnPitch);
+      }
+    } else {
+      unsigned got = 0;
+      if (lane == 0) {
+        got = atomicAdd(a.tickets + w0, 1u) + 1u;
+        if (got == (unsigned)(w1 - w0 + 1)) a.tickets[w0] = 0u;
+      }
+      got = __shfl_sync(0xFFFFFFFFu, got, 0);
+      if (got == (unsigned)(w1 - w0 + 1)) {
+        __threadfence();
+        merge(i < n_i, i, w1 - w0 + 1, seq_slot(w0, true) + i * kUnPitch, (size_t)2 * kUnTile * kUnPitch, seq_slot(w0 + 1, false) + i * kUnPitch, 0, nullptr, 0);
+      }
+    }
+  };
+
+#pragma unroll 1
+  for (int idx = 0; idx < n_mine; ++idx) {
+    if ((idx & 31) == 0) cur = nxt;            // copies run at most four units ahead: `nxt` still describes these
+    const int u0 = __shfl_sync(0xFFFFFFFFu, cur.u0, idx & 31), n = __shfl_sync(0xFFFFFFFFu, cur.n, idx & 31);
+    if (u0 != tile_u0) {
+      if (tile_u0 >= 0) finish();
+      tile_u0 = u0;
+      tile_nu = __shfl_sync(0xFFFFFFFFu, cur.nu, idx & 31);
+      row0 = __shfl_sync(0xFFFFFFFFu, cur.row0, idx & 31);
+      const int hn = __shfl_sync(0xFFFFFFFFu, cur.hn, idx & 31);
+      own = __shfl_sync(0xFFFFFFFFu, cur.own, idx & 31);
+      kvh = hn & 0xffff; n_i = hn >> 16;
+      load_q();
+      whole = true;
+      if constexpr (SHARED) {
+        if (!own) {                            // a row may end inside the shared pages
+          vis0 = g < n_i ? a.row_pos[row0 + g / a.G] + 1 : prefix_keys;
+          vis1 = g + 8 < n_i ? a.row_pos[row0 + (g + 8) / a.G] + 1 : prefix_keys;
+          whole = __all_sync(0xFFFFFFFFu, vis0 >= prefix_keys && vis1 >= prefix_keys);
+        }
+      }
+      m0 = m1 = -INFINITY; l0 = l1 = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+    }
+    const int s = idx % L::kStages;
+    unsigned char *st = stage0 + (size_t)s * L::kStage;
+    if (!dead && !mbar_wait_bounded(&bar[s], (uint32_t)(idx / L::kStages) & 1u, kUnWaitNs)) {
+      atomicExch(a.err, 1);
+      dead = true;
+    }
+    dead = __any_sync(0xFFFFFFFFu, dead);
+    if (n > 0 && !dead) {
+      const uint32_t k_base = smem_u32(st), v_base = k_base + L::kHalf;
+      float sc[4][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
+      if constexpr (KV == KV_E4M3) {
+        const float *ks = reinterpret_cast<const float *>(st + 2 * L::kHalf);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {          // eight keys: lane (g, t) holds dimensions 16 t .. 16 t + 15 of key g
+          const uint4 c = *reinterpret_cast<const uint4 *>(st + (8 * j + g) * kHeadDim + 16 * t);
+          const uint32_t cw[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+          for (int k4 = 0; k4 < 4; ++k4) {
+            const uint32_t b0 = e4m3x2_to_bf16x2(__byte_perm(cw[k4], 0u, 0x1404)), b1 = e4m3x2_to_bf16x2(__byte_perm(cw[k4], 0u, 0x3424));
+            un_mma<false>(sc[j], qa[k4], b0, b1);
+            if constexpr (QF32) un_mma<false>(sc[j], qlo[k4], b0, b1);
+          }
+          const float2 f = *reinterpret_cast<const float2 *>(ks + 8 * j + 2 * t);
+          sc[j][0] *= f.x; sc[j][1] *= f.y; sc[j][2] *= f.x; sc[j][3] *= f.y;
+        }
+      } else {
+        // V rows without a key may hold NaN, and 0 * NaN must not reach O
+        if (n < kUnKeys) {
+          const int zero_to = min(kUnKeys, (n + kUnBox - 1) / kUnBox * kUnBox);
+          for (int i = n * 8 + lane; i < zero_to * 8; i += 32) *reinterpret_cast<uint4 *>(st + L::kHalf + i * 16) = make_uint4(0, 0, 0, 0);
+          __syncwarp();
+        }
+#pragma unroll
+        for (int np = 0; np < 2; ++np) {
+          if (np * kUnBox >= n) break;
+          const int key = 16 * np + 8 * (lane >> 4) + (lane & 7);
+#pragma unroll
+          for (int k4 = 0; k4 < 4; ++k4) {
+            uint32_t f[4];
+            ldmatrix_x4(f, k_base + key * 128 + (((2 * k4 + ((lane >> 3) & 1)) ^ (key & 7)) << 4));
+            un_mma<F16>(sc[2 * np], qa[k4], f[0], f[1]);
+            un_mma<F16>(sc[2 * np + 1], qa[k4], f[2], f[3]);
+            if constexpr (QF32) {
+              un_mma<F16>(sc[2 * np], qlo[k4], f[0], f[1]);
+              un_mma<F16>(sc[2 * np + 1], qlo[k4], f[2], f[3]);
+            }
+          }
+        }
+      }
+      if (n < kUnKeys || !whole) {
+        const int k0 = (u_begin + idx - tile_u0) * kUnKeys;
+        const int lim0 = whole ? n : min(n, vis0 - k0), lim1 = whole ? n : min(n, vis1 - k0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = 8 * j + 2 * t;
+          if (c >= lim0) sc[j][0] = -INFINITY;
+          if (c + 1 >= lim0) sc[j][1] = -INFINITY;
+          if (c >= lim1) sc[j][2] = -INFINITY;
+          if (c + 1 >= lim1) sc[j][3] = -INFINITY;
+        }
+      }
+      float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { x0 = fmaxf(x0, fmaxf(sc[j][0], sc[j][1])); x1 = fmaxf(x1, fmaxf(sc[j][2], sc[j][3])); }
+      x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 1)); x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2));
+      x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1)); x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
+      const float n0 = fmaxf(m0, x0 * a.scale), n1 = fmaxf(m1, x1 * a.scale);
+      const float r0 = n0 == -INFINITY ? 0.f : n0, r1 = n1 == -INFINITY ? 0.f : n1;   // a row that has seen nothing keeps -inf
+      const float f0 = pt_exp2(m0 - r0), f1 = pt_exp2(m1 - r1);
+      m0 = n0; m1 = n1;
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sc[j][0] = pt_exp2(fmaf(sc[j][0], a.scale, -r0)); sc[j][1] = pt_exp2(fmaf(sc[j][1], a.scale, -r0));
+        sc[j][2] = pt_exp2(fmaf(sc[j][2], a.scale, -r1)); sc[j][3] = pt_exp2(fmaf(sc[j][3], a.scale, -r1));
+        s0 += sc[j][0] + sc[j][1];
+        s1 += sc[j][2] + sc[j][3];
+      }
+      l0 = fmaf(l0, f0, s0); l1 = fmaf(l1, f1, s1);
+      if (__any_sync(0xFFFFFFFFu, f0 != 1.0f || f1 != 1.0f)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
+      }
+      if constexpr (KV == KV_E4M3) {
+        const float *vs = reinterpret_cast<const float *>(st + 2 * L::kHalf + kUnKeys * 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {          // the values' scales belong to P; a key that is none may have any
+          const float2 f = *reinterpret_cast<const float2 *>(vs + 8 * j + 2 * t);
+          const float fx = 8 * j + 2 * t < n ? f.x : 0.f, fy = 8 * j + 2 * t + 1 < n ? f.y : 0.f;
+          sc[j][0] *= fx; sc[j][1] *= fy; sc[j][2] *= fx; sc[j][3] *= fy;
+        }
+      }
+#pragma unroll
+      for (int np = 0; np < 2; ++np) {
+        if (np * kUnBox >= n) break;
+        const uint32_t pa[4] = {un_pack<F16>(sc[2 * np][0], sc[2 * np][1]), un_pack<F16>(sc[2 * np][2], sc[2 * np][3]),
+                                un_pack<F16>(sc[2 * np + 1][0], sc[2 * np + 1][1]), un_pack<F16>(sc[2 * np + 1][2], sc[2 * np + 1][3])};
+        if constexpr (KV == KV_E4M3) {
+          const unsigned char *vp = st + L::kHalf + (16 * np + 2 * t) * kHeadDim + 8 * g;   // dimensions 8 g .. 8 g + 7 of four keys
+          const uint2 v0 = *reinterpret_cast<const uint2 *>(vp), v1 = *reinterpret_cast<const uint2 *>(vp + kHeadDim);
+          const uint2 v8 = *reinterpret_cast<const uint2 *>(vp + 8 * kHeadDim), v9 = *reinterpret_cast<const uint2 *>(vp + 9 * kHeadDim);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {        // byte j of the first key below, of the second above
+            constexpr uint32_t sel[4] = {0x4000, 0x5010, 0x6020, 0x7030};
+            const uint32_t b0 = e4m3x2_to_bf16x2(__byte_perm(j < 4 ? v0.x : v0.y, j < 4 ? v1.x : v1.y, sel[j & 3]));
+            const uint32_t b1 = e4m3x2_to_bf16x2(__byte_perm(j < 4 ? v8.x : v8.y, j < 4 ? v9.x : v9.y, sel[j & 3]));
+            un_mma<false>(o[j], pa, b0, b1);
+          }
+        } else {
+          const int key = 16 * np + 8 * ((lane >> 3) & 1) + (lane & 7);
+#pragma unroll
+          for (int dp = 0; dp < 4; ++dp) {
+            uint32_t f[4];
+            ldmatrix_x4_trans(f, v_base + key * 128 + (((2 * dp + (lane >> 4)) ^ (key & 7)) << 4));
+            un_mma<F16>(o[2 * dp], pa, f[0], f[1]);
+            un_mma<F16>(o[2 * dp + 1], pa, f[2], f[3]);
+          }
+        }
+      }
+    }
+    // every lane has read the stage: refill it
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (issued < n_mine && !dead) { issue(issued); ++issued; }
+  }
+  if (tile_u0 >= 0) finish();
+  if (dead) {   // copies of the warp may still be in flight, and none may land in a CTA that has left
+    const unsigned long long t0 = global_timer_ns();
+    while (global_timer_ns() - t0 <= 10000000ull) {}
+  }
+}
+
+// partial rows of the shared form: prefix tiles (their number + warps slots of 16), then the rows' own (rows x heads + warps slots of G)
+inline long long shared_prefix_part_rows(int R, int Hkv, int G) {
+  const int rpt = kUnTile / G;
+  return ((long long)Hkv * ((R + rpt - 1) / rpt) + kUnMaxWarps) * kUnTile;
+}
+inline long long shared_part_rows(int R, int Hkv, int G) { return shared_prefix_part_rows(R, Hkv, G) + ((long long)R * Hkv + kUnMaxWarps) * G; }
+inline long long cross_part_rows() { return 2ll * kUnMaxWarps * kUnTile; }
+
+template <bool SHARED, int KV, bool QF32>
+inline cudaError_t launch_units_as(const CUtensorMap &k_map, const CUtensorMap &v_map, const UnitArgs &a, int n_sm, cudaStream_t st) {
+  static SmemOptIn opt_in;
+  if (const cudaError_t e = opt_in(attention_units_kernel<SHARED, KV, QF32>, units_smem_bytes<KV>(kUnMaxSeq))) return e;
+  return launch_kernel(attention_units_kernel<SHARED, KV, QF32>, dim3(std::min(n_sm, kUnMaxCtas)), dim3(kUnWarps * 32),
+                       units_smem_bytes<KV>(SHARED ? a.q_rows : a.n_seq), st, false, k_map, v_map, a);
+}
+
+// The maps of K and V: 16 keys of one head a copy, with the 128-byte swizzle.  A pool of 16-bit pages: [64, 64 tokens, blocks].
+inline cudaError_t units_pool_map(CUtensorMap *map, const void *pool, size_t blocks) {
+  const cuuint64_t dims[3] = {kHeadDim, kPageTokens, blocks}, strides[2] = {kHeadDim * 2, kPageElems * 2};
+  const cuuint32_t box[3] = {kHeadDim, kUnBox, 1};
+  return tensor_map_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, pool, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// Rows of 64 values: heads and tokens `head` and `row` bytes apart, in whichever order; `box_rows` tokens of one head a copy.  The
+// dimension with the smaller stride comes first: *tokens_first says whether that is the token.
+inline cudaError_t units_rows_map(CUtensorMap *map, int *tokens_first, bool f16, const void *base, size_t heads, size_t rows, size_t head, size_t row, int box_rows) {
+  if (heads == 1) head = std::max(row, (size_t)(kHeadDim * 2)) * rows;   // strides that nothing is addressed with
+  if (rows == 1) row = head * heads;
+  const bool tf = row < head;
+  *tokens_first = tf;
+  const cuuint64_t dims[3] = {kHeadDim, tf ? rows : heads, tf ? heads : rows}, strides[2] = {tf ? row : head, tf ? head : row};
+  const cuuint32_t box[3] = {kHeadDim, tf ? (cuuint32_t)box_rows : 1u, tf ? 1u : (cuuint32_t)box_rows};
+  return tensor_map_encode(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+}  // namespace ttsgpt

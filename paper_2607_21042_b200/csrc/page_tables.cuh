@@ -1,0 +1,271 @@
+// Page lists and slot maps of a pass, built on the GPU from the requests' lengths, and the pass's K and V rows into those
+// slots (Section I: KV-cache management of the decode engine).
+//
+// Tables.  Request i adds n_i = new_len[i] tokens to stream s_i, which holds c_i.  With b_i = c_i, or 64 n_shared where a
+// stream opens behind shared pages, the request's rows are positions b_i .. b_i + n_i - 1 and it takes
+//     p_i = ceil((b_i + n_i) / 64) - ceil(b_i / 64)
+// pages from the top of the stack: page number j of the request is free_pages[top - 1 - (p_0 + .. + p_(i-1)) - j].  Row
+// r = n_0 + .. + n_(i-1) + k has slot page(pos / 64) * 64 + pos % 64.
+//
+// Every CTA computes both running sums over all requests for itself (at most 4096 of them, out of L2) and then writes its share
+// of the rows and of the list entries, which it finds by bisection: one launch, no CTA waits for another.  What a caller may
+// update in place (contexts, stack height) is written by the CTA that leaves last, when every CTA has read it.
+// Bound: two dependent reads (ids, contexts), one of the page stack, the launch; 12 bytes a row where there are many.
+#pragma once
+#include <cuda_fp8.h>
+#include <algorithm>
+#include "../../include/tts_gpt.h"
+#include "common.cuh"
+
+namespace ttsgpt {
+
+constexpr int kTabMaxRequests = 4096;
+constexpr int kTabMaxStreams = 32768;     // a bit each in shared memory, where an id that comes twice is found
+constexpr int kTabMaxListPages = 32768;   // pages of a list: keeps a pass's rows below 2^36 and its pages below 2^28, as packed in one sum
+constexpr int kTabPageBits = 28;
+
+struct TableArgs {
+  int n, max_streams, pps, n_pages, n_shared, max_rows;
+  const int *stream_ids, *new_len, *ctx_len, *free_pages, *free_top, *shared_pages;
+  int *ctx_len_out, *free_top_out, *page_table, *row_start, *row_stream, *row_pos, *row_slot;
+  int *info;   // {status, rows, pages taken, stack height, 0, 0, 0, CTAs that have left}
+  int vec;     // the three row arrays are 16-byte aligned
+};
+
+enum { kTabBadArg = 1, kTabBadStream = 2, kTabOverflow = 4, kTabRows = 8, kTabNoPages = 16 };
+
+inline size_t page_tables_smem_bytes(int n, int max_streams) { return (size_t)(5 * n + 2 + (max_streams + 31) / 32) * sizeof(int); }
+
+// THREADS * ITEMS requests at most
+template <int THREADS, int ITEMS>
+__global__ void __launch_bounds__(THREADS) page_tables_kernel(const TableArgs a) {
+  extern __shared__ int tab_smem[];
+  int *row_s = tab_smem, *page_s = row_s + a.n + 1;              // running sums, one more than requests
+  int *base_s = page_s + a.n + 1, *held_s = base_s + a.n, *id_s = held_s + a.n;
+  unsigned *seen = reinterpret_cast<unsigned *>(id_s + a.n);
+  __shared__ unsigned long long warp_sum_s[THREADS / 32];
+  __shared__ int bad_s, last_s;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int id[ITEMS], add[ITEMS], ctx[ITEMS];
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int i = k * THREADS + tid;
+    id[k] = i < a.n ? (a.stream_ids ? a.stream_ids[i] : i) : -1;
+    add[k] = i < a.n ? a.new_len[i] : 0;
+  }
+  const int top = *a.free_top;
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) ctx[k] = id[k] >= 0 && id[k] < a.max_streams ? a.ctx_len[id[k]] : 0;
+  for (int w = tid; w < (a.max_streams + 31) / 32; w += THREADS) seen[w] = 0u;
+  if (tid == 0) bad_s = top < 0 || top > a.n_pages ? kTabBadArg : 0;
+  __syncthreads();
+  int bad = 0;
+  unsigned long long carry = 0;
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int i = k * THREADS + tid;
+    unsigned long long mine = 0;
+    int base = 0, held = 0;
+    if (i < a.n) {
+      if (id[k] < 0 || id[k] >= a.max_streams || (atomicOr(&seen[id[k] >> 5], 1u << (id[k] & 31)) >> (id[k] & 31) & 1u)) bad |= kTabBadStream;
+      else if (add[k] < 0 || ctx[k] < 0) bad |= kTabBadArg;
+      else {
+        base = ctx[k] == 0 && add[k] > 0 ? a.n_shared * kPageTokens : ctx[k];
+        if ((long long)base + add[k] > (long long)a.pps * kPageTokens) bad |= kTabOverflow;
+        else {
+          held = (base + kPageTokens - 1) / kPageTokens;
+          const int taken = (base + add[k] + kPageTokens - 1) / kPageTokens - held;
+          mine = ((unsigned long long)add[k] << kTabPageBits) + (unsigned long long)taken;
+        }
+      }
+    }
+    // inclusive sum over the block, behind those of the rounds before
+    unsigned long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    if (k > 0) __syncthreads();   // the sums of the round before have been read
+    if (lane == 31) warp_sum_s[warp] = incl;
+    __syncthreads();
+    unsigned long long before = carry, all = carry;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+      const unsigned long long v = warp_sum_s[w];
+      if (w < warp) before += v;
+      all += v;
+    }
+    carry = all;
+    if (i < a.n) {
+      const unsigned long long e = before + incl - mine;
+      row_s[i] = (int)(e >> kTabPageBits);   // beyond 2^31 rows the pass is refused below
+      page_s[i] = (int)(e & ((1u << kTabPageBits) - 1));
+      base_s[i] = base; held_s[i] = held; id_s[i] = id[k];
+    }
+  }
+  const long long rows = (long long)(carry >> kTabPageBits);
+  const int pages = (int)(carry & ((1u << kTabPageBits) - 1));
+  if (tid == 0) { row_s[a.n] = (int)rows; page_s[a.n] = pages; }
+  if (rows > a.max_rows) bad |= kTabRows;
+  if (pages > top) bad |= kTabNoPages;
+  if (bad) atomicOr(&bad_s, bad);
+  __syncthreads();
+  bad = bad_s;
+  if (bad == 0) {
+    auto request_of = [&](const int *start, int x) {   // last request that starts at or before x
+      int lo = 0, hi = a.n - 1;
+      while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (start[m] <= x) lo = m; else hi = m - 1; }
+      return lo;
+    };
+    const int me = blockIdx.x * THREADS + tid, all = gridDim.x * THREADS;
+    for (int r0 = 4 * me; r0 < (int)rows; r0 += 4 * all) {   // four rows at a time
+      int i = request_of(row_s, r0);
+      int s4[4], p4[4], t4[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = min(r0 + e, (int)rows - 1);
+        while (row_s[i + 1] <= r) ++i;
+        const int pos = base_s[i] + r - row_s[i], pg = pos / kPageTokens;
+        const int page = pg < held_s[i] ? a.page_table[(size_t)id_s[i] * a.pps + pg] : a.free_pages[top - 1 - (page_s[i] + pg - held_s[i])];
+        s4[e] = id_s[i]; p4[e] = pos; t4[e] = page * kPageTokens + pos % kPageTokens;
+      }
+      if (a.vec && r0 + 4 <= (int)rows) {
+        *reinterpret_cast<int4 *>(a.row_stream + r0) = make_int4(s4[0], s4[1], s4[2], s4[3]);
+        *reinterpret_cast<int4 *>(a.row_pos + r0) = make_int4(p4[0], p4[1], p4[2], p4[3]);
+        *reinterpret_cast<int4 *>(a.row_slot + r0) = make_int4(t4[0], t4[1], t4[2], t4[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (r0 + e < (int)rows) { a.row_stream[r0 + e] = s4[e]; a.row_pos[r0 + e] = p4[e]; a.row_slot[r0 + e] = t4[e]; }
+      }
+    }
+    for (int k = me; k < pages; k += all) {                  // new entries of the page lists
+      const int i = request_of(page_s, k);
+      a.page_table[(size_t)id_s[i] * a.pps + held_s[i] + k - page_s[i]] = a.free_pages[top - 1 - k];
+    }
+    if (a.n_shared > 0) {                                    // the shared pages of the streams that open
+      const long long entries = (long long)a.n * a.n_shared;
+      for (long long k = me; k < entries; k += all) {
+        const int i = (int)(k / a.n_shared), j = (int)(k - (long long)i * a.n_shared);
+        if (row_s[i + 1] > row_s[i] && a.ctx_len[id_s[i]] == 0) a.page_table[(size_t)id_s[i] * a.pps + j] = a.shared_pages[j];
+      }
+    }
+    if (blockIdx.x == 0)
+      for (int i = tid; i <= a.n; i += THREADS) a.row_start[i] = row_s[i];
+  }
+  __syncthreads();
+  if (tid == 0) {
+    last_s = 1;
+    if (gridDim.x > 1) { __threadfence(); last_s = atomicAdd(a.info + 7, 1) == (int)gridDim.x - 1; }
+  }
+  __syncthreads();
+  if (!last_s) return;
+  if (bad == 0)
+    for (int i = tid; i < a.n; i += THREADS) {
+      const int len = row_s[i + 1] - row_s[i];
+      a.ctx_len_out[id_s[i]] = base_s[i] + len;
+    }
+  if (tid == 0) {
+    const int code = bad & kTabBadArg ? TTS_GPT_E_ARG : bad & kTabBadStream ? TTS_GPT_E_STREAM : bad & kTabOverflow ? TTS_GPT_E_CTX_OVERFLOW
+                     : bad & kTabRows ? TTS_GPT_E_WORKSPACE : bad ? TTS_GPT_E_NO_PAGES : TTS_GPT_OK;
+    a.info[0] = code;
+    a.info[1] = bad ? 0 : (int)rows;
+    a.info[2] = bad ? 0 : pages;
+    a.info[3] = bad ? top : top - pages;
+    if (!bad) *a.free_top_out = top - pages;
+    a.info[7] = 0;
+  }
+}
+
+inline cudaError_t launch_page_tables(const TableArgs &a, int n_sm, cudaStream_t st) {
+  const size_t smem = page_tables_smem_bytes(a.n, a.max_streams);
+  // a CTA writes 4 rows a thread at a time; more CTAs than hold a few thousand rows each only repeat the sums
+  if (a.n <= 256) {
+    static SmemOptIn opt_in;
+    if (const cudaError_t e = opt_in(page_tables_kernel<256, 1>, page_tables_smem_bytes(256, kTabMaxStreams))) return e;
+    const int grid = std::max(1, std::min(n_sm, (a.max_rows + 2047) / 2048));
+    return launch_kernel(page_tables_kernel<256, 1>, dim3(grid), dim3(256), smem, st, false, a);
+  }
+  static SmemOptIn opt_in;
+  if (const cudaError_t e = opt_in(page_tables_kernel<1024, 4>, page_tables_smem_bytes(kTabMaxRequests, kTabMaxStreams))) return e;
+  const int grid = std::max(1, std::min(n_sm, (a.max_rows + 4095) / 4096));
+  return launch_kernel(page_tables_kernel<1024, 4>, dim3(grid), dim3(1024), smem, st, false, a);
+}
+
+// ---------------------------------------------------------------------------------------------
+// K and V rows into their slots
+// ---------------------------------------------------------------------------------------------
+constexpr int kE4m3BlockBytes = kPageTokens * kHeadDim + kPageTokens * 4;   // codes, then the tokens' fp32 scales
+
+struct AppendArgs {
+  const void *k, *v;
+  long long k_stride, v_stride;   // elements between rows
+  const int *row_slot;
+  unsigned char *pool;
+  int R, H, n_slots;              // slots of the pool: 64 n_pages
+};
+
+__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
+  const float4 lo = *reinterpret_cast<const float4 *>(p), hi = *reinterpret_cast<const float4 *>(p + 4);
+  x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w; x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+}
+__device__ __forceinline__ void load8(const uint16_t *p, float (&x)[8]) {
+  const uint4 w = *reinterpret_cast<const uint4 *>(p);
+  const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(ww[i]); x[2 * i + 1] = bf16_hi(ww[i]); }
+}
+
+// Eight lanes take the 64 values of one (row, K|V, head), eight values each.  16-bit cache: each value rounded once.  8-bit cache:
+// s = max|x| / 448 over the 64 (1 if all are zero), codes e4m3(x / s).  Bound: bytes in and out.
+constexpr int kAppendThreads = 256;
+template <typename Src, bool E4M3>
+__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const AppendArgs a) {
+  const long long unit = (long long)blockIdx.x * kAppendThreads + threadIdx.x;
+  const int e = (int)(unit & 7);
+  const long long item = unit >> 3;
+  const bool live = item < (long long)a.R * 2 * a.H;   // the same for the eight lanes of an item
+  const int r = live ? (int)(item / (2 * a.H)) : 0, rem = live ? (int)(item - (long long)r * 2 * a.H) : 0;
+  const int which = rem >= a.H ? 1 : 0, h = rem - which * a.H;
+  const int slot = live ? a.row_slot[r] : -1;
+  float x[8];
+  const Src *src = reinterpret_cast<const Src *>(which ? a.v : a.k) + (size_t)r * (which ? a.v_stride : a.k_stride) + h * kHeadDim + 8 * e;
+  load8(src, x);
+  const bool there = slot >= 0 && slot < a.n_slots;
+  const int page = there ? slot / kPageTokens : 0, off = there ? slot % kPageTokens : 0;
+  const size_t block = ((size_t)page * 2 + which) * a.H + h;
+  if constexpr (E4M3) {
+    float m = fabsf(x[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    const float s = m > 0.f ? m / 448.0f : 1.0f;
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(__fdiv_rn(x[4 * i], s), __fdiv_rn(x[4 * i + 1], s)), __NV_SATFINITE, __NV_E4M3);
+      const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(__fdiv_rn(x[4 * i + 2], s), __fdiv_rn(x[4 * i + 3], s)), __NV_SATFINITE, __NV_E4M3);
+      w[i] = lo | (hi << 16);
+    }
+    if (there) {
+      unsigned char *blk = a.pool + block * kE4m3BlockBytes;
+      *reinterpret_cast<uint2 *>(blk + off * kHeadDim + 8 * e) = make_uint2(w[0], w[1]);
+      if (e == 0) *reinterpret_cast<float *>(blk + kPageTokens * kHeadDim + 4 * off) = s;
+    }
+  } else if (there) {
+    *reinterpret_cast<uint4 *>(a.pool + block * (kPageElems * 2) + off * (kHeadDim * 2) + 16 * e) =
+        make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+  }
+}
+
+inline cudaError_t launch_kv_append(const AppendArgs &a, bool src_f32, bool e4m3, cudaStream_t st) {
+  const long long units = (long long)a.R * 2 * a.H * 8;
+  const dim3 grid((unsigned)((units + kAppendThreads - 1) / kAppendThreads)), block(kAppendThreads);
+  auto kernel = src_f32 ? (e4m3 ? kv_append_kernel<float, true> : kv_append_kernel<float, false>)
+                        : (e4m3 ? kv_append_kernel<uint16_t, true> : kv_append_kernel<uint16_t, false>);
+  return launch_kernel(kernel, grid, block, 0, st, false, a);
+}
+
+}  // namespace ttsgpt

@@ -1,0 +1,183 @@
+// Single-kernel entry points of a program that assembles its own step over a paged cache: page lists and slot maps, K/V rows
+// into their slots, attention of a batch that shares a prefix, attention to an encoder's states.  A translation unit of its
+// own: the engine's kernels keep their places in its module, which decide how their code is fetched.
+#include <algorithm>
+#include <cmath>
+
+#include "host.cuh"
+#include "page_tables.cuh"
+#include "attention_units.cuh"
+
+using namespace ttsgpt;
+
+namespace {
+
+#define OP_TRY(expr)                                                                                   \
+  do {                                                                                                 \
+    cudaError_t e_ = (expr);                                                                           \
+    if (e_ != cudaSuccess) return fail_op(TTS_GPT_E_CUDA, "%s: %s", #expr, cudaGetErrorString(e_));   \
+  } while (0)
+
+// Scratch of the two attentions: [error word][tickets][partial rows], the first two of the same size in every call, so that calls
+// of other sizes, of either kind, find the tickets at zero where the call before left them.
+constexpr size_t kOpMaxTickets = 262144;
+constexpr size_t kOpHeaderBytes = 256 + kOpMaxTickets * sizeof(unsigned);
+size_t scratch_bytes(long long part_rows) { return kOpHeaderBytes + (size_t)part_rows * kUnPitch * sizeof(float); }
+
+bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
+
+int check_heads(const char *op, int32_t n_head, int32_t n_kv_head) {
+  if (n_head < 1 || n_kv_head < 1 || n_head % n_kv_head) return fail_op(TTS_GPT_E_ARG, "%s: n_head must be a multiple of n_kv_head", op);
+  if (n_head / n_kv_head > kUnTile || n_head > 1024)
+    return fail_op(TTS_GPT_E_UNSUPPORTED, "%s: at most %d query heads to a head of keys, and 1024 in all", op, kUnTile);
+  return TTS_GPT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t tts_gpt_op_page_tables(int32_t n, const int32_t *stream_ids, const int32_t *new_len, int32_t max_streams, const int32_t *ctx_len,
+                               int32_t *ctx_len_out, int32_t n_pages, const int32_t *free_pages, const int32_t *free_top, int32_t *free_top_out,
+                               int32_t n_shared, const int32_t *shared_pages, int32_t pages_per_stream, int32_t *page_table, int32_t max_rows,
+                               int32_t *row_start, int32_t *row_stream, int32_t *row_pos, int32_t *row_slot, int32_t *info, void *cuda_stream) {
+  if (!new_len || !ctx_len || !ctx_len_out || !free_pages || !free_top || !free_top_out || !page_table || !row_start || !row_stream || !row_pos ||
+      !row_slot || !info || (n_shared > 0 && !shared_pages))
+    return fail_op(TTS_GPT_E_ARG, "op_page_tables: null argument");
+  const void *all[] = {stream_ids, new_len, ctx_len, ctx_len_out, free_pages, free_top, free_top_out, shared_pages, page_table, row_start, row_stream, row_pos,
+                       row_slot, info};
+  for (const void *p : all)
+    if (!aligned(p, 4)) return fail_op(TTS_GPT_E_ARG, "op_page_tables: index arrays must be 4-byte aligned");
+  if (n < 1 || max_streams < 1 || (!stream_ids && n > max_streams) || n_pages < 1 || n_pages > INT32_MAX / kPageTokens || max_rows < 1 || n_shared < 0 ||
+      pages_per_stream < 1 || n_shared > pages_per_stream)
+    return fail_op(TTS_GPT_E_ARG, "op_page_tables: bad argument");
+  if (n > kTabMaxRequests || max_streams > kTabMaxStreams || pages_per_stream > kTabMaxListPages)
+    return fail_op(TTS_GPT_E_UNSUPPORTED, "op_page_tables: at most %d requests, %d streams, %d pages to a stream", kTabMaxRequests, kTabMaxStreams, kTabMaxListPages);
+  TableArgs a;
+  a.n = n; a.max_streams = max_streams; a.pps = pages_per_stream; a.n_pages = n_pages; a.n_shared = n_shared; a.max_rows = max_rows;
+  a.stream_ids = stream_ids; a.new_len = new_len; a.ctx_len = ctx_len; a.free_pages = free_pages; a.free_top = free_top; a.shared_pages = shared_pages;
+  a.ctx_len_out = ctx_len_out; a.free_top_out = free_top_out; a.page_table = page_table; a.row_start = row_start; a.row_stream = row_stream;
+  a.row_pos = row_pos; a.row_slot = row_slot; a.info = info;
+  a.vec = aligned(row_stream, 16) && aligned(row_pos, 16) && aligned(row_slot, 16);
+  OP_TRY(launch_page_tables(a, device_sms(), (cudaStream_t)cuda_stream));
+  return TTS_GPT_OK;
+}
+
+int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                             const int32_t *row_slot, int32_t kv_fmt, int32_t n_pages, void *kv_layer, void *cuda_stream) {
+  if (R < 1 || n_head < 1 || !k || !v || !row_slot || !kv_layer || n_pages < 1 || n_pages > INT32_MAX / kPageTokens || (type != TTS_GPT_T_F32 && type != TTS_GPT_T_BF16) ||
+      (kv_fmt != TTS_GPT_KV_BF16 && kv_fmt != TTS_GPT_KV_FP8_E4M3) || k_stride < (int64_t)n_head * kHeadDim || v_stride < (int64_t)n_head * kHeadDim)
+    return fail_op(TTS_GPT_E_ARG, "op_kv_append: bad argument");
+  const int per16 = type == TTS_GPT_T_F32 ? 4 : 8;
+  if (!aligned(k, 16) || !aligned(v, 16) || k_stride % per16 || v_stride % per16 || !aligned(kv_layer, 16) || !aligned(row_slot, 4))
+    return fail_op(TTS_GPT_E_ARG, "op_kv_append: K and V rows and the pool must be 16-byte aligned, slots 4-byte");
+  if ((long long)R * n_head > (1ll << 31)) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_kv_append: R * n_head must be at most 2^31");
+  AppendArgs a;
+  a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride; a.row_slot = row_slot; a.pool = (unsigned char *)kv_layer;
+  a.R = R; a.H = n_head; a.n_slots = n_pages * kPageTokens;
+  OP_TRY(launch_kv_append(a, type == TTS_GPT_T_F32, kv_fmt == TTS_GPT_KV_FP8_E4M3, (cudaStream_t)cuda_stream));
+  return TTS_GPT_OK;
+}
+
+static int check_shared(int32_t R, int32_t n_head, int32_t n_kv_head) {
+  if (const int rc = check_heads("op_attention_shared", n_head, n_kv_head)) return rc;
+  if (R < 1) return fail_op(TTS_GPT_E_ARG, "op_attention_shared: R must be positive");
+  if (R > kUnMaxSeq || (long long)R * n_kv_head > (long long)kOpMaxTickets)
+    return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_shared: at most %d rows, and R * n_kv_head at most %d", kUnMaxSeq, (int)kOpMaxTickets);
+  return TTS_GPT_OK;
+}
+
+int32_t tts_gpt_op_attention_shared_scratch_bytes(int32_t R, int32_t n_head, int32_t n_kv_head, size_t *bytes) {
+  if (!bytes) return fail_op(TTS_GPT_E_ARG, "op_attention_shared: null argument");
+  if (const int rc = check_shared(R, n_head, n_kv_head)) return rc;
+  *bytes = scratch_bytes(shared_part_rows(R, n_kv_head, n_head / n_kv_head));
+  return TTS_GPT_OK;
+}
+
+int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head, int32_t type, const void *q, int64_t q_stride, int32_t kv_fmt,
+                                    int32_t n_pages, const void *kv_layer, int32_t n_shared, const int32_t *page_table, int32_t pages_per_stream,
+                                    const int32_t *row_stream, const int32_t *row_pos, void *out, void *scratch, size_t scratch_size, void *cuda_stream) {
+  if (const int rc = check_shared(R, n_head, n_kv_head)) return rc;
+  if (!q || !kv_layer || !page_table || !row_stream || !row_pos || !out || !scratch || (type != TTS_GPT_T_F32 && type != TTS_GPT_T_BF16) ||
+      (kv_fmt != TTS_GPT_KV_BF16 && kv_fmt != TTS_GPT_KV_FP8_E4M3) || n_pages < 1 || pages_per_stream < 1 || n_shared < 0 || n_shared > pages_per_stream ||
+      q_stride < (int64_t)n_head * kHeadDim)
+    return fail_op(TTS_GPT_E_ARG, "op_attention_shared: bad argument");
+  if (!aligned(q, 16) || q_stride % (type == TTS_GPT_T_F32 ? 4 : 8) || !aligned(kv_layer, 16) || !aligned(out, 16) || !aligned(scratch, 256) ||
+      !aligned(page_table, 4) || !aligned(row_stream, 4) || !aligned(row_pos, 4))
+    return fail_op(TTS_GPT_E_ARG, "op_attention_shared: q rows, out and the KV pool must be 16-byte aligned, scratch 256-byte, index arrays 4-byte");
+  // units of 32 keys are numbered in 31 bits, blocks of the pool too
+  const int G = n_head / n_kv_head;
+  const long long tiles = (long long)n_kv_head * ((R + kUnTile / G - 1) / (kUnTile / G));
+  if (pages_per_stream > (1 << 24) || 2ll * tiles * n_shared + 2ll * R * n_kv_head * (pages_per_stream - n_shared) + (long long)R * n_kv_head >= (1ll << 31) ||
+      2ll * n_pages * n_kv_head >= (1ll << 31))
+    return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_shared: too many pages");
+  if (scratch_size < scratch_bytes(shared_part_rows(R, n_kv_head, G)))
+    return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_shared: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(shared_part_rows(R, n_kv_head, G)));
+  UnitArgs a = {};
+  a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = R; a.H = n_head; a.Hkv = n_kv_head; a.G = G; a.rpt = kUnTile / G;
+  a.scale = 0.125f * 1.4426950408889634f;
+  a.page_table = page_table; a.row_stream = row_stream; a.row_pos = row_pos; a.pool = (const unsigned char *)kv_layer; a.pps = pages_per_stream;
+  a.n_shared = n_shared; a.n_pages = n_pages;
+  a.err = (int *)scratch;
+  a.tickets = (unsigned *)((char *)scratch + 256);
+  a.part = (float *)((char *)scratch + kOpHeaderBytes);
+  a.suffix_part0 = (int)shared_prefix_part_rows(R, n_kv_head, G);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  const int n_sm = device_sms();
+  CUtensorMap map = {};
+  if (kv_fmt == TTS_GPT_KV_BF16) {
+    OP_TRY(units_pool_map(&map, kv_layer, (size_t)n_pages * 2 * n_kv_head));
+    OP_TRY((type == TTS_GPT_T_F32 ? launch_units_as<true, KV_BF16, true> : launch_units_as<true, KV_BF16, false>)(map, map, a, n_sm, st));
+  } else {
+    OP_TRY((type == TTS_GPT_T_F32 ? launch_units_as<true, KV_E4M3, true> : launch_units_as<true, KV_E4M3, false>)(map, map, a, n_sm, st));
+  }
+  return TTS_GPT_OK;
+}
+
+int32_t tts_gpt_op_attention_cross_scratch_bytes(size_t *bytes) {
+  if (!bytes) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: null argument");
+  *bytes = scratch_bytes(cross_part_rows());
+  return TTS_GPT_OK;
+}
+
+int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head, int32_t type, int32_t q_rows, const void *q, int64_t q_stride,
+                                   int32_t k_rows, const void *k, int64_t k_stride, int64_t k_head_stride, const void *v, int64_t v_stride,
+                                   int64_t v_head_stride, const int32_t *q_start, const int32_t *k_start, int32_t q_max, float scale, void *out,
+                                   void *scratch, size_t scratch_size, void *cuda_stream) {
+  if (const int rc = check_heads("op_attention_cross", n_head, n_kv_head)) return rc;
+  if (n < 1 || q_rows < 1 || k_rows < 0 || q_max < 1 || !q || (k_rows > 0 && (!k || !v)) || !q_start || !k_start || !out || !scratch ||
+      (type != TTS_GPT_T_BF16 && type != TTS_GPT_T_F16) || q_stride < (int64_t)n_head * kHeadDim || !std::isfinite(scale))
+    return fail_op(TTS_GPT_E_ARG, "op_attention_cross: bad argument");
+  if (!(scale > 0.f)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: scale must be positive");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(scratch, 256) || !aligned(q_start, 4) || !aligned(k_start, 4) || q_stride % 8 ||
+      k_stride % 8 || v_stride % 8 || k_head_stride % 8 || v_head_stride % 8)
+    return fail_op(TTS_GPT_E_ARG, "op_attention_cross: rows of q, K, V and out must be 16-byte aligned, scratch 256-byte, index arrays 4-byte");
+  if (k_rows > 1 && (k_stride < kHeadDim || v_stride < kHeadDim)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: rows of K or V overlap");
+  if (n_kv_head > 1 && k_rows > 0 && (k_head_stride < kHeadDim || v_head_stride < kHeadDim)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: heads of K or V overlap");
+  if (n > kUnMaxSeq) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: at most %d sequences", kUnMaxSeq);
+  if (q_max > q_rows) q_max = q_rows;
+  const int G = n_head / n_kv_head, rpt = kUnTile / G;
+  const long long blocks = std::min((long long)n * ((q_max + rpt - 1) / rpt), (long long)q_rows / rpt + n);
+  if ((long long)n_kv_head * blocks * ((long long)k_rows / kUnKeys + 1) >= (1ll << 31) &&
+      (long long)n_kv_head * ((q_max + rpt - 1) / rpt) * ((long long)k_rows / kUnKeys + n) >= (1ll << 31))
+    return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: too many queries times keys");
+  if (scratch_size < scratch_bytes(cross_part_rows()))
+    return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_cross: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(cross_part_rows()));
+  UnitArgs a = {};
+  a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = q_rows; a.H = n_head; a.Hkv = n_kv_head; a.G = G; a.rpt = rpt;
+  a.scale = scale * 1.4426950408889634f;
+  a.q_start = q_start; a.k_start = k_start; a.n_seq = n; a.q_max = q_max; a.k_rows = k_rows;
+  a.err = (int *)scratch;
+  a.tickets = (unsigned *)((char *)scratch + 256);
+  a.part = (float *)((char *)scratch + kOpHeaderBytes);
+  CUtensorMap k_map = {}, v_map = {};
+  const bool f16 = type == TTS_GPT_T_F16;
+  if (k_rows > 0) {
+    OP_TRY(units_rows_map(&k_map, &a.k_tokens_first, f16, k, n_kv_head, k_rows, k_head_stride * 2, k_stride * 2, kUnBox));
+    OP_TRY(units_rows_map(&v_map, &a.v_tokens_first, f16, v, n_kv_head, k_rows, v_head_stride * 2, v_stride * 2, kUnBox));
+  }
+  OP_TRY((f16 ? launch_units_as<false, KV_F16, false> : launch_units_as<false, KV_BF16, false>)(k_map, v_map, a, device_sms(), (cudaStream_t)cuda_stream));
+  return TTS_GPT_OK;
+}
+
+}  // extern "C"
