@@ -372,8 +372,8 @@ int32_t tts_gpt_op_sample(int32_t R, int32_t V, const float *logits, int32_t top
  * lists built (op_page_tables), writes the pass's K and V rows (op_kv_append) and attends over them, the pages that all
  * requests begin with read once (op_attention_shared); op_attention_cross reads an encoder's states instead.  The layer's
  * pool is that of the engine: bf16 [n_pages][2 (K,V)][heads][64 tokens][64], or with TTS_GPT_KV_FP8_E4M3 blocks of 4352 bytes
- * [n_pages][2][heads]: 64 tokens x 64 codes, then the 64 fp32 scales.  All index arrays DEVICE int32.  Each call is one
- * kernel, allocates nothing, does not wait for the GPU and can be captured into a CUDA graph.
+ * [n_pages][2][heads]: 64 tokens x 64 codes, then the 64 fp32 scales.  All index arrays DEVICE int32.  A call
+ * allocates nothing, does not wait for the GPU and can be captured into a CUDA graph.
  * ------------------------------------------------------------------------------------------- */
 
 /* Page lists and slot maps of a pass.  Request i (of n) adds new_len[i] >= 0 tokens to stream stream_ids[i] (NULL: i), which
@@ -412,10 +412,10 @@ int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void
  * apart; out bf16 [R][n_head*64].  A row with row_pos -1 has no keys: its output is zero.  Several rows may belong to one stream.
  * Keys on a page outside 0..n_pages-1 are left out, as are those behind the list's pages_per_stream pages.  K and V of the shared
  * pages must be finite.  fp32 queries enter with 16 bits, the softmax weights are rounded to bf16, sums are fp32; results do
- * not depend on timing.  R <= 4096, R * n_kv_head <= 262144.
- * scratch (256-byte aligned, >= scratch_bytes; zero before its first use, by this call or op_attention_cross, in any size)
- * belongs to one call at a time: calls that may overlap, replays of captured graphs among them, need one each.  Its first
- * word is set to 1 if a bounded wait inside a kernel ran out; outputs are then incomplete and the scratch must be zeroed. */
+ * not depend on timing.  R <= 4096.
+ * scratch (256-byte aligned, >= scratch_bytes; its first word zero before its first use, by this call or op_attention_cross, in
+ * any size) belongs to one call at a time: calls that may overlap, replays of captured graphs among them, need one each.  That
+ * word is set to 1 if a bounded wait inside a kernel ran out; outputs are then incomplete, until it is zeroed. */
 int32_t tts_gpt_op_attention_shared_scratch_bytes(int32_t R, int32_t n_head, int32_t n_kv_head, size_t *bytes);
 int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head, int32_t type, const void *q, int64_t q_stride,
                                     int32_t kv_fmt, int32_t n_pages, const void *kv_layer, int32_t n_shared,

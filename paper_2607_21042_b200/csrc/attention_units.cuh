@@ -9,9 +9,10 @@
 // with M, the sums and o in fp32; zero where no key is left.
 //
 // Work split.  The units of all tiles are laid end to end and cut into one range a warp, equal to within a unit whatever the
-// lengths are.  A tile inside one range is finished by its warp.  Parts of the others go to scratch, and the warp that
-// arrives last at the tile's ticket (for the shared prefix: at that of each row and group) adds them in the order of
-// their keys: no warp waits for another, and results do not depend on timing.
+// lengths are.  A tile inside one range, whose rows read no other keys, is finished by its warp.  The others' parts go to
+// scratch, and a second kernel, launched behind the first's start, adds a row's parts in the order of their keys: no warp waits for
+// another, and results do not depend on timing.  (Tickets, with the merge by the warp that comes last, took 5 us a tile in a
+// chain of fence, atomic and reads: a warp with twenty short rows ended 100 us behind the others.)
 //
 // Instructions.  Queries are the 16-row operand of m16n8k16, keys the 8-wide one, so the scores come out in the layout in which
 // P enters P V.  Queries in fp32 enter as two bf16 parts (16 bits), P is rounded to the cache's type (half a step of it: as
@@ -54,18 +55,18 @@ struct UnitArgs {
   int k_tokens_first, v_tokens_first;   // the map's middle dimension is the token, not the head
   // scratch
   int *err;                     // [0]: set when a wait ran out
-  unsigned *tickets;
+  int *plan;                    // shared: {units of a range, ranges with one more, running sums of units}; cross: an int4 a range
   float *part;
   int suffix_part0;             // partial row at which those of the rows' own tiles begin
 };
 
 template <int KV> struct UnitLayout {
-  static constexpr int kStages = KV == KV_E4M3 ? 4 : 2;
+  static constexpr int kStages = KV == KV_E4M3 ? 3 : 2;
   static constexpr int kHalf = KV == KV_E4M3 ? kUnKeys * kHeadDim : kUnKeys * kHeadDim * 2;   // K (or V) of a unit
   static constexpr int kStage = KV == KV_E4M3 ? 2 * kHalf + 2 * kUnKeys * 4 : 2 * kHalf;   // codes of K and V, scales of K and V
 };
 template <int KV> inline size_t units_smem_bytes(int n) {
-  return (size_t)kUnWarps * UnitLayout<KV>::kStages * UnitLayout<KV>::kStage + 1024 + kUnWarps * UnitLayout<KV>::kStages * 8 + (size_t)(n + 1) * 4 + 64;
+  return (size_t)kUnWarps * UnitLayout<KV>::kStages * UnitLayout<KV>::kStage + 1024 + kUnWarps * UnitLayout<KV>::kStages * 8 + (size_t)(2 * n + 1) * 4 + 64;
 }
 
 __device__ __forceinline__ void un_box(const CUtensorMap *map, int c1, int c2, unsigned char *dst, uint64_t *bar) {
@@ -93,6 +94,17 @@ __device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t x) {
   return r;
 }
 
+// the range that unit u lies in: the first `rem` ranges have size + 1 units, the others size
+__device__ __forceinline__ int unit_range(int u, int size, int rem) {
+  const int t = rem * (size + 1);
+  return u < t ? u / (size + 1) : rem + (u - t) / size;
+}
+// First partial row of a part.  A tile's parts are numbered tile + range, which never repeats along the units; sequences, whose
+// tiles only meet where a range ends, have two places a range: for the tile that goes on behind it, and the one that began before.
+__device__ __forceinline__ size_t prefix_part(int tile, int range) { return (size_t)(tile + range) * kUnTile; }
+__device__ __forceinline__ size_t own_part(const UnitArgs &a, int row, int kvh, int range) { return (size_t)a.suffix_part0 + (size_t)(row * a.Hkv + kvh + range) * a.G; }
+__device__ __forceinline__ size_t seq_part(int range, bool begins) { return (size_t)(2 * range + (begins ? 1 : 0)) * kUnTile; }
+
 // what a unit is; one per lane, 32 units at a time
 struct UnitDesc {
   int c1, c2;      // where its keys lie: token of the page and block of the pool, or head and token row
@@ -114,13 +126,20 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   unsigned char *stages = un_smem_raw + ((1024u - (smem_u32(un_smem_raw) & 1023u)) & 1023u);
   uint64_t *bars = reinterpret_cast<uint64_t *>(stages + (size_t)kUnWarps * L::kStages * L::kStage);
   int *first = reinterpret_cast<int *>(bars + kUnWarps * L::kStages);   // running sums of units: of a head of each row, or of all tiles of each sequence
+  int *stream_s = first + (SHARED ? a.q_rows : a.n_seq) + 1;             // shared: the rows' streams
   __shared__ int warp_tot[kUnWarps];
   __shared__ unsigned long long lead_s;   // keys of the longest row, and that row: its list names the shared pages
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int n_items = SHARED ? a.q_rows : a.n_seq;
 
   if (lane < L::kStages) mbar_init(&bars[warp * L::kStages + lane], 1);
-  if (tid == 0) lead_s = 0;
+  if (tid == 0) {
+    lead_s = 0;
+    if constexpr (KV != KV_E4M3) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+      if (!SHARED) asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+    }
+  }
   __syncthreads();
   // ---- running sums ----
   auto q_span = [&](int i, int &b, int &e) {   // query rows of a sequence
@@ -140,13 +159,14 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
     if (i < n_items) {
       if (SHARED) {
         const int n = own_keys(i);
+        stream_s[i] = a.row_stream[i];
         atomicMax(&lead_s, ((unsigned long long)(unsigned)(n + prefix_keys) << 32) | (unsigned)i);
-        u = n > 0 ? (n + kUnKeys - 1) / kUnKeys : (a.n_shared == 0 ? 1 : 0);   // a row without any key still gets its zeros
+        u = n > 0 ? 1 + (n + kUnKeys - 1) / kUnKeys : (a.n_shared == 0 ? 1 : 0);   // a row without any key still gets its zeros
       } else {
         int qb, qe, kb, ke;
         q_span(i, qb, qe);
         k_span(i, kb, ke);
-        u = a.Hkv * ((qe - qb + a.rpt - 1) / a.rpt) * max(1, (ke - kb + kUnKeys - 1) / kUnKeys);
+        u = a.Hkv * ((qe - qb + a.rpt - 1) / a.rpt) * (1 + (ke - kb + kUnKeys - 1) / kUnKeys);
       }
     }
     int incl = u;
@@ -168,14 +188,20 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   __syncthreads();
   const int lead = (int)(lead_s & 0xFFFFFFFFu), lead_keys = (int)(lead_s >> 32);
   const int tiles_head = SHARED && a.n_shared > 0 ? (a.q_rows + a.rpt - 1) / a.rpt : 0;   // prefix tiles of a head
-  const int prefix_nu = SHARED ? 2 * a.n_shared : 0;                                      // units of each of them
+  const int prefix_nu = SHARED ? 2 * a.n_shared + 1 : 0;                                     // units of each of them
   const int U_prefix = a.Hkv * tiles_head * prefix_nu;
-  const long long T = (long long)U_prefix + (long long)carry * (SHARED ? a.Hkv : 1);
-  // W ranges, none of them empty; range j goes to CTA j % grid, so that few units reach every CTA
-  const int W = (int)min(T, (long long)gridDim.x * kUnWarps);
+  const int T = U_prefix + carry * (SHARED ? a.Hkv : 1);
+  // W ranges of at least two units; range j goes to CTA j % grid, so that few units reach every CTA
+  const int W = min((T + 1) / 2, (int)gridDim.x * kUnWarps), size = T / max(1, W), rem = T - size * W;
   const int w = warp * gridDim.x + blockIdx.x;
-  const int u_begin = w < W ? (int)(T * w / W) : 0, u_end = w < W ? (int)(T * (w + 1) / W) : 0;
-  auto warp_of = [&](int u) { return (int)((((long long)u + 1) * W - 1) / T); };
+  const int u_begin = w * size + min(w, rem), n_mine = w < W ? size + (w < rem ? 1 : 0) : 0;
+  auto warp_of = [&](int u) { return unit_range(u, size, rem); };
+  if (SHARED && blockIdx.x == 0) {
+    for (int i = tid; i <= n_items; i += kUnWarps * 32) a.plan[2 + i] = first[i];
+    if (tid == 0) { a.plan[0] = size; a.plan[1] = rem; }
+  }
+  if (!SHARED && lane == 0) reinterpret_cast<int4 *>(a.plan)[w] = make_int4(0, 0, 0, 0);
+  pdl_launch_dependents();
 
   auto find = [&](int x) {   // last item that begins at or before x
     int lo = 0, hi = n_items - 1;
@@ -184,18 +210,18 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   };
   auto describe = [&](int u) {
     UnitDesc d = {0, 0, 0, u, 1, 0, 0, 0};
-    if (u >= u_end) return d;
+    if (u >= u_begin + n_mine) return d;
     if constexpr (SHARED) {
-      int r, kvh, page, n, list;
+      int r, kvh, page, n, list, kk;            // unit 0 of a tile has no keys: it stands for what a tile costs besides them
       if (u < U_prefix) {
         const int tile = u / prefix_nu, k = u - tile * prefix_nu;
         kvh = tile / tiles_head;
         r = (tile - kvh * tiles_head) * a.rpt;
         d.u0 = u - k; d.nu = prefix_nu;
         d.hn = kvh | (min(a.rpt, a.q_rows - r) * a.G << 16);
-        page = k >> 1; list = lead;
-        n = min(kUnKeys, lead_keys - k * kUnKeys);   // a page of the shared ones holds 64 keys, unless no row is that long
-        d.c1 = (k & 1) * kUnKeys;
+        kk = k - 1;
+        page = kk >> 1; list = lead;
+        n = min(kUnKeys, lead_keys - kk * kUnKeys);   // a page of the shared ones holds 64 keys, unless no row is that long
       } else {
         const int v = u - U_prefix;
         r = find(v / a.Hkv);
@@ -204,34 +230,35 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         const int k = x - kvh * nu;
         d.u0 = u - k; d.nu = nu; d.own = 1;
         d.hn = kvh | (a.G << 16);
-        page = a.n_shared + (k >> 1); list = r;
-        n = min(kUnKeys, own_keys(r) - k * kUnKeys);
-        d.c1 = (k & 1) * kUnKeys;
+        kk = k - 1;
+        page = a.n_shared + (kk >> 1); list = r;
+        n = kk < 0 ? 0 : min(kUnKeys, own_keys(r) - kk * kUnKeys);
       }
       d.row0 = r;
-      if (n > 0) {
-        const int phys = a.page_table[(size_t)a.row_stream[list] * a.pps + page];
-        if (phys >= 0 && phys < a.n_pages) { d.n = n; d.c2 = phys * 2 * a.Hkv + kvh; }   // a page that is none has no keys
+      d.c1 = (kk & 1) * kUnKeys;
+      if (kk >= 0 && stream_s[list] >= 0) {
+        const int phys = a.page_table[(size_t)stream_s[list] * a.pps + page];
+        if (n > 0 && phys >= 0 && phys < a.n_pages) { d.n = n; d.c2 = phys * 2 * a.Hkv + kvh; }   // a page that is none has no keys
       }
     } else {
       const int s = find(u), x = u - first[s];
       int qb, qe, kb, ke;
       q_span(s, qb, qe);
       k_span(s, kb, ke);
-      const int nu = max(1, (ke - kb + kUnKeys - 1) / kUnKeys), tile = x / nu, k = x - tile * nu;
+      const int nu = 1 + (ke - kb + kUnKeys - 1) / kUnKeys, tile = x / nu, k = x - tile * nu;
       const int blocks = (qe - qb + a.rpt - 1) / a.rpt, kvh = tile / blocks;
       d.row0 = qb + (tile - kvh * blocks) * a.rpt;
       d.u0 = u - k; d.nu = nu;
       d.hn = kvh | (min(a.rpt, qe - d.row0) * a.G << 16);
-      d.c1 = kvh; d.c2 = kb + k * kUnKeys;
-      d.n = min(kUnKeys, max(0, ke - d.c2));
+      d.c1 = kvh; d.c2 = kb + (k - 1) * kUnKeys;
+      d.n = k == 0 ? 0 : min(kUnKeys, ke - d.c2);
     }
     return d;
   };
 
   unsigned char *stage0 = stages + (size_t)warp * L::kStages * L::kStage;
   uint64_t *bar = bars + warp * L::kStages;
-  UnitDesc nxt, cur;                          // descriptions of the units being copied, and of those being computed
+  UnitDesc nxt = {}, cur = {};                          // descriptions of the units being copied, and of those being computed
   auto issue = [&](int i) {                   // unit u_begin + i into stage i % kStages
     if ((i & 31) == 0) nxt = describe(u_begin + i + lane);
     const int c1 = __shfl_sync(0xFFFFFFFFu, nxt.c1, i & 31), c2 = __shfl_sync(0xFFFFFFFFu, nxt.c2, i & 31), n = __shfl_sync(0xFFFFFFFFu, nxt.n, i & 31);
@@ -268,18 +295,12 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
     __syncwarp();
   };
 
-  const int n_mine = u_end - u_begin;
-  int issued = 0;
-  for (; issued < min(n_mine, L::kStages); ++issued) issue(issued);
-
   // ---- state of the tile ----
   uint32_t qa[4][4], qlo[QF32 ? 4 : 1][4];    // query fragments by 16 dimensions; fp32: what the first part leaves
   float o[8][4], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;   // rows g and g + 8
   int tile_u0 = -1, tile_nu = 0, row0 = 0, kvh = 0, n_i = 0, own = 0, vis0 = 0, vis1 = 0;
   bool whole = true, dead = false;
 
-  // dimension of accumulator column e (0, 1) of fragment j
-  auto dim_of = [&](int j, int e) { return KV == KV_E4M3 ? 16 * t + 8 * e + j : 8 * j + 2 * t + e; };
   auto q_ptr = [&](int i) { return (size_t)(row0 + i / a.G) * a.q_stride + (size_t)(kvh * a.G + i % a.G) * kHeadDim; };
   auto load_q = [&]() {
     const bool h0 = g < n_i, h1 = g + 8 < n_i;
@@ -303,56 +324,13 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   };
   auto out_ptr = [&](int i) { return a.out + ((size_t)(row0 + i / a.G) * a.H + kvh * a.G + i % a.G) * kHeadDim; };
 
-  // ---- the parts of up to 16 query rows, added in the order of their keys: lanes 2 i and 2 i + 1 take row i, half the dimensions each ----
-  // n0 parts from partial row s0 on, each `pitch0` rows behind the other, then n1 from s1
-  auto merge = [&](bool mine, int i, int n0, const float *s0, size_t step0, const float *s1b, int n1, const float *s1, size_t step1) {
-    const int half = (lane & 1) * 32;
-    float M = -INFINITY;
-    auto part = [&](int p) { return p < n0 ? (p == 0 ? s0 : s1b + (size_t)(p - 1) * step0) : s1 + (size_t)(p - n0) * step1; };
-    const int n = mine ? n0 + n1 : 0;
-    for (int p = 0; p < n; ++p) M = fmaxf(M, __ldcg(part(p) + 64));
-    float acc[32], den = 0.f;
-#pragma unroll
-    for (int c = 0; c < 32; ++c) acc[c] = 0.f;
-    for (int p = 0; p < n; ++p) {
-      const float *x = part(p);
-      const float mp = __ldcg(x + 64), f = mp == -INFINITY ? 0.f : exp2f(mp - M);
-      den = fmaf(f, __ldcg(x + 65), den);
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const float4 v = __ldcg(reinterpret_cast<const float4 *>(x + half) + c);
-        if (f > 0.f) {
-          acc[4 * c] = fmaf(f, v.x, acc[4 * c]); acc[4 * c + 1] = fmaf(f, v.y, acc[4 * c + 1]);
-          acc[4 * c + 2] = fmaf(f, v.z, acc[4 * c + 2]); acc[4 * c + 3] = fmaf(f, v.w, acc[4 * c + 3]);
-        }
-      }
-    }
-    const float inv = den > 0.f || den != den ? 1.0f / den : 0.f;
-    if (mine && !*reinterpret_cast<volatile int *>(a.err)) {
-      uint16_t *dst = out_ptr(i) + half;
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        *reinterpret_cast<uint4 *>(dst + 8 * c) =
-            make_uint4(un_pack<F16>(acc[8 * c] * inv, acc[8 * c + 1] * inv), un_pack<F16>(acc[8 * c + 2] * inv, acc[8 * c + 3] * inv),
-                       un_pack<F16>(acc[8 * c + 4] * inv, acc[8 * c + 5] * inv), un_pack<F16>(acc[8 * c + 6] * inv, acc[8 * c + 7] * inv));
-    }
-  };
-
   auto finish = [&]() {                       // the warp leaves its tile
     l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 1); l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 2);
     l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 1); l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 2);
     const int last = tile_u0 + tile_nu - 1;
     const int w0 = warp_of(tile_u0), w1 = warp_of(last);
-    // does anything else feed this tile's rows?
-    int prefix_tile = 0, p_w0 = 0, p_n = 0;   // parts of the prefix tile of this row and group
-    if constexpr (SHARED) {
-      if (own && tiles_head > 0) {
-        prefix_tile = kvh * tiles_head + row0 / a.rpt;
-        p_w0 = warp_of(prefix_tile * prefix_nu);
-        p_n = warp_of(prefix_tile * prefix_nu + prefix_nu - 1) - p_w0 + 1;
-      }
-    }
-    const bool alone = w0 == w1 && (!SHARED || (own && p_n == 0));
+    // does nothing else feed this tile's rows?
+    const bool alone = w0 == w1 && (!SHARED || (own && tiles_head == 0));
     if (alone) {
       const float i0 = l0 > 0.f || l0 != l0 ? 1.0f / l0 : 0.f, i1 = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
       if (!dead) {
@@ -376,12 +354,8 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
       }
       return;
     }
-    // ---- this part into scratch.  Slots: a tile's parts are numbered tile + warp, which never repeats along the units; sequences
-    // (whose tiles meet only where a range ends) have two slots a warp ----
-    auto prefix_slot = [&](int tile, int wp) { return a.part + (size_t)(tile + wp) * kUnTile * kUnPitch; };
-    auto own_slot = [&](int r, int h, int wp) { return a.part + ((size_t)a.suffix_part0 + (size_t)(r * a.Hkv + h + wp) * a.G) * kUnPitch; };
-    auto seq_slot = [&](int wp, bool begins) { return a.part + (size_t)(2 * wp + (begins ? 1 : 0)) * kUnTile * kUnPitch; };
-    float *dst = SHARED ? (own ? own_slot(row0, kvh, w) : prefix_slot(tile_u0 / max(1, prefix_nu), w)) : seq_slot(w, w == w0);
+    // this part into scratch
+    float *dst = a.part + (SHARED ? (own ? own_part(a, row0, kvh, w) : prefix_part(tile_u0 / max(1, prefix_nu), w)) : seq_part(w, w == w0)) * kUnPitch;
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       if (g + 8 * e < n_i) {
@@ -397,66 +371,24 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         }
         if (t == 0) { p[64] = e ? m1 : m0; p[65] = e ? l1 : l0; }
       }
-    __threadfence();
-    __syncwarp();
-    const int i = lane >> 1;
-    if constexpr (SHARED) {
-      // every row and group of the tile has a ticket that counts the parts of its prefix tile and of its own keys
-      const int rows = n_i / a.G;
-      unsigned want = 0, got = 0;
-      int my_r = row0 + min(lane, rows - 1), own_nu = 0, o_w0 = 0, o_n = 0;
-      if (own) { o_w0 = w0; o_n = w1 - w0 + 1; }
-      else {
-        p_w0 = w0; p_n = w1 - w0 + 1;
-        prefix_tile = tile_u0 / prefix_nu;
-        own_nu = first[my_r + 1] - first[my_r];
-        if (own_nu > 0) {
-          const int b = U_prefix + first[my_r] * a.Hkv + kvh * own_nu;
-          o_w0 = warp_of(b);
-          o_n = warp_of(b + own_nu - 1) - o_w0 + 1;
-        }
-      }
-      want = (unsigned)(p_n + o_n);
-      bool done = false;
-      if (lane < rows) {
-        unsigned *tk = a.tickets + (size_t)my_r * a.Hkv + kvh;
-        got = atomicAdd(tk, 1u) + 1u;
-        done = got == want;
-        if (done) *tk = 0u;
-      }
-      const unsigned mask = __ballot_sync(0xFFFFFFFFu, done);
-      if (mask) {
-        __threadfence();
-        const int li = i / a.G;                 // row of the tile that lanes 2 i, 2 i + 1 work for
-        const int src = min(li, 31);
-        const int ow0 = __shfl_sync(0xFFFFFFFFu, o_w0, src), on = __shfl_sync(0xFFFFFFFFu, o_n, src);
-        const bool mine = i < n_i && ((mask >> li) & 1u);
-        const int r = row0 + li, gi = i - li * a.G;
-        const int pi = (r % a.rpt) * a.G + gi;  // place in the prefix tile
-        const float *pp = prefix_slot(prefix_tile, p_w0) + pi * kUnPitch;
-        const float *op = own_slot(r, kvh, ow0) + gi * kUnPitch;
-        merge(mine, i, p_n, pp, (size_t)kUnTile * kUnPitch, pp + (size_t)kUnTile * kUnPitch, on, op, (size_t)a.G * kUnPitch);
-      }
-    } else {
-      unsigned got = 0;
-      if (lane == 0) {
-        got = atomicAdd(a.tickets + w0, 1u) + 1u;
-        if (got == (unsigned)(w1 - w0 + 1)) a.tickets[w0] = 0u;
-      }
-      got = __shfl_sync(0xFFFFFFFFu, got, 0);
-      if (got == (unsigned)(w1 - w0 + 1)) {
-        __threadfence();
-        merge(i < n_i, i, w1 - w0 + 1, seq_slot(w0, true) + i * kUnPitch, (size_t)2 * kUnTile * kUnPitch, seq_slot(w0 + 1, false) + i * kUnPitch, 0, nullptr, 0);
-      }
-    }
+    // the merge finds a cut tile at the range that begins it
+    if (!SHARED && w == w0 && lane == 0) reinterpret_cast<int4 *>(a.plan)[w] = make_int4(row0, kvh | (n_i << 16), w1 - w0 + 1, 0);
   };
 
+  // turn i copies unit i and computes unit i - kStages, whose stage it frees; one place for each in the code, which is fetched cold
 #pragma unroll 1
-  for (int idx = 0; idx < n_mine; ++idx) {
-    if ((idx & 31) == 0) cur = nxt;            // copies run at most four units ahead: `nxt` still describes these
-    const int u0 = __shfl_sync(0xFFFFFFFFu, cur.u0, idx & 31), n = __shfl_sync(0xFFFFFFFFu, cur.n, idx & 31);
+  for (int turn = 0;; ++turn) {
+    const int idx = turn - L::kStages;
+    if (idx < 0) {
+      if (turn < n_mine) issue(turn);
+      continue;
+    }
+    if ((idx & 31) == 0) cur = nxt;            // copies run a few units ahead: `nxt` still describes these
+    const bool end = idx >= n_mine;
+    const int u0 = end ? -2 : __shfl_sync(0xFFFFFFFFu, cur.u0, idx & 31), n = __shfl_sync(0xFFFFFFFFu, cur.n, idx & 31);
     if (u0 != tile_u0) {
       if (tile_u0 >= 0) finish();
+      if (end) break;
       tile_u0 = u0;
       tile_nu = __shfl_sync(0xFFFFFFFFu, cur.nu, idx & 31);
       row0 = __shfl_sync(0xFFFFFFFFu, cur.row0, idx & 31);
@@ -528,7 +460,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         }
       }
       if (n < kUnKeys || !whole) {
-        const int k0 = (u_begin + idx - tile_u0) * kUnKeys;
+        const int k0 = (u_begin + idx - tile_u0 - 1) * kUnKeys;
         const int lim0 = whole ? n : min(n, vis0 - k0), lim1 = whole ? n : min(n, vis1 - k0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -601,16 +533,94 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
     // every lane has read the stage: refill it
     fence_proxy_async_smem();
     __syncwarp();
-    if (issued < n_mine && !dead) { issue(issued); ++issued; }
+    if (turn < n_mine && !dead) issue(turn);
   }
-  if (tile_u0 >= 0) finish();
   if (dead) {   // copies of the warp may still be in flight, and none may land in a CTA that has left
     const unsigned long long t0 = global_timer_ns();
     while (global_timer_ns() - t0 <= 10000000ull) {}
   }
 }
 
-// partial rows of the shared form: prefix tiles (their number + warps slots of 16), then the rows' own (rows x heads + warps slots of G)
+// The parts of a query row, added in the order of their keys by 8 PG lanes: lane group pg takes every PG-th part, a lane eight
+// dimensions.  part(p): the p-th of n partial rows.
+template <int PG, bool F16, typename Part>
+__device__ __forceinline__ void merge_parts(int n, Part part, uint16_t *out, bool store) {
+  const int sub = threadIdx.x & 7, pg = (threadIdx.x >> 3) & (PG - 1);
+  float M = -INFINITY, l = 0.f, acc[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) acc[c] = 0.f;
+  auto add = [&](float m, float pl, const float (&v)[8]) {
+    if (pl == 0.f) return;                     // no key in it; a sum that is NaN goes in
+    const float Mn = fmaxf(M, m), fo = M == Mn ? 1.f : pt_exp2(M - Mn), fn = pt_exp2(m - Mn);
+    M = Mn;
+    l = fmaf(l, fo, pl * fn);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[c] = fmaf(acc[c], fo, v[c] * fn);
+  };
+#pragma unroll 2
+  for (int p = pg; p < n; p += PG) {
+    const float *x = part(p);
+    const float2 ml = __ldcg(reinterpret_cast<const float2 *>(x + kHeadDim));
+    const float4 a = __ldcg(reinterpret_cast<const float4 *>(x + 8 * sub)), b = __ldcg(reinterpret_cast<const float4 *>(x + 8 * sub + 4));
+    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    add(ml.x, ml.y, v);
+  }
+#pragma unroll
+  for (int o = 8; o < 8 * PG; o <<= 1) {       // the groups' sums, the lower group's first
+    const float m2 = __shfl_down_sync(0xFFFFFFFFu, M, o), l2 = __shfl_down_sync(0xFFFFFFFFu, l, o);
+    float v[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] = __shfl_down_sync(0xFFFFFFFFu, acc[c], o);
+    add(m2, l2, v);
+  }
+  if (store && pg == 0) {
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    *reinterpret_cast<uint4 *>(out + 8 * sub) = make_uint4(un_pack<F16>(acc[0] * inv, acc[1] * inv), un_pack<F16>(acc[2] * inv, acc[3] * inv),
+                                                           un_pack<F16>(acc[4] * inv, acc[5] * inv), un_pack<F16>(acc[6] * inv, acc[7] * inv));
+  }
+}
+
+constexpr int kMergeWarps = 8;
+// a warp per query row and head: the parts of the prefix tile, then those of the row's own keys
+__global__ void __launch_bounds__(kMergeWarps * 32) merge_shared_kernel(const UnitArgs a) {
+  pdl_wait();
+  const int item = blockIdx.x * kMergeWarps + (threadIdx.x >> 5);
+  if (item >= a.q_rows * a.H) return;          // whole warps
+  const int r = item / a.H, h = item - r * a.H, kvh = h / a.G, gi = h - kvh * a.G;
+  const int size = a.plan[0], rem = a.plan[1], f0 = a.plan[2 + r], nu = a.plan[3 + r] - f0;
+  const int tiles_head = a.n_shared > 0 ? (a.q_rows + a.rpt - 1) / a.rpt : 0, prefix_nu = 2 * a.n_shared + 1;
+  int p_n = 0, o_n = 0;
+  const float *pp = a.part, *op = a.part;
+  if (tiles_head > 0) {
+    const int tile = kvh * tiles_head + r / a.rpt, w0 = unit_range(tile * prefix_nu, size, rem);
+    p_n = unit_range(tile * prefix_nu + prefix_nu - 1, size, rem) - w0 + 1;
+    pp += (prefix_part(tile, w0) + (r % a.rpt) * a.G + gi) * kUnPitch;
+  }
+  if (nu > 0) {
+    const int u0 = a.Hkv * tiles_head * prefix_nu + f0 * a.Hkv + kvh * nu, w0 = unit_range(u0, size, rem);
+    o_n = unit_range(u0 + nu - 1, size, rem) - w0 + 1;
+    op += (own_part(a, r, kvh, w0) + gi) * kUnPitch;
+  }
+  if (p_n == 0 && o_n == 1) return;            // finished by its warp
+  merge_parts<4, false>(p_n + o_n, [&](int p) { return p < p_n ? pp + (size_t)p * kUnTile * kUnPitch : op + (size_t)(p - p_n) * a.G * kUnPitch; },
+                        a.out + ((size_t)r * a.H + h) * kHeadDim, *a.err == 0);
+}
+
+// four warps per range: the rows of the tile that begins in it and goes on behind it, four a warp
+template <bool F16>
+__global__ void __launch_bounds__(kMergeWarps * 32) merge_ranges_kernel(const UnitArgs a, int ranges) {
+  pdl_wait();
+  const int w = blockIdx.x * (kMergeWarps / 4) + (threadIdx.x >> 7);
+  if (w >= ranges) return;
+  const int4 c = __ldcg(reinterpret_cast<const int4 *>(a.plan) + w);
+  const int kvh = c.y & 0xffff, n_i = c.y >> 16, i = (threadIdx.x >> 3) & 15, ic = min(i, n_i - 1);
+  if (c.z == 0 || (i & ~3) >= n_i) return;     // whole warps
+  merge_parts<1, F16>(c.z, [&](int p) { return a.part + (seq_part(w + p, p == 0) + ic) * kUnPitch; },
+                      a.out + ((size_t)(c.x + ic / a.G) * a.H + kvh * a.G + ic % a.G) * kHeadDim, i < n_i && *a.err == 0);
+}
+
+// partial rows of the shared form: prefix tiles (their number + ranges places of 16), then the rows' own (rows x heads + ranges
+// places of G)
 inline long long shared_prefix_part_rows(int R, int Hkv, int G) {
   const int rpt = kUnTile / G;
   return ((long long)Hkv * ((R + rpt - 1) / rpt) + kUnMaxWarps) * kUnTile;
@@ -622,8 +632,12 @@ template <bool SHARED, int KV, bool QF32>
 inline cudaError_t launch_units_as(const CUtensorMap &k_map, const CUtensorMap &v_map, const UnitArgs &a, int n_sm, cudaStream_t st) {
   static SmemOptIn opt_in;
   if (const cudaError_t e = opt_in(attention_units_kernel<SHARED, KV, QF32>, units_smem_bytes<KV>(kUnMaxSeq))) return e;
-  return launch_kernel(attention_units_kernel<SHARED, KV, QF32>, dim3(std::min(n_sm, kUnMaxCtas)), dim3(kUnWarps * 32),
-                       units_smem_bytes<KV>(SHARED ? a.q_rows : a.n_seq), st, false, k_map, v_map, a);
+  const int grid = std::min(n_sm, kUnMaxCtas);
+  if (const cudaError_t e = launch_kernel(attention_units_kernel<SHARED, KV, QF32>, dim3(grid), dim3(kUnWarps * 32),
+                                          units_smem_bytes<KV>(SHARED ? a.q_rows : a.n_seq), st, false, k_map, v_map, a)) return e;
+  if (SHARED) return launch_kernel(merge_shared_kernel, dim3((a.q_rows * a.H + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), 0, st, true, a);
+  const int ranges = grid * kUnWarps;
+  return launch_kernel(merge_ranges_kernel<KV == KV_F16>, dim3((ranges + kMergeWarps / 4 - 1) / (kMergeWarps / 4)), dim3(kMergeWarps * 32), 0, st, true, a, ranges);
 }
 
 // The maps of K and V: 16 keys of one head a copy, with the 128-byte swizzle.  A pool of 16-bit pages: [64, 64 tokens, blocks].

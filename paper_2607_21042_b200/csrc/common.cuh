@@ -17,7 +17,7 @@ constexpr int kMaxPassRows = 4096;                  // rows (streams x positions
 constexpr int kMaxSplitRows = 1024;                 // rows up to which every pass may leave four k-range partial sums (or attend over e4m3 codes)
 constexpr int kMaxOrderedRows = 2688;               // rows of a sampled pass, all of which leave up to four partial sums: 55 MB of them at width 1280
 
-inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+constexpr size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }

@@ -18,10 +18,9 @@ namespace {
     if (e_ != cudaSuccess) return fail_op(TTS_GPT_E_CUDA, "%s: %s", #expr, cudaGetErrorString(e_));   \
   } while (0)
 
-// Scratch of the two attentions: [error word][tickets][partial rows], the first two of the same size in every call, so that calls
-// of other sizes, of either kind, find the tickets at zero where the call before left them.
-constexpr size_t kOpMaxTickets = 262144;
-constexpr size_t kOpHeaderBytes = 256 + kOpMaxTickets * sizeof(unsigned);
+// Scratch of the two attentions: [error word][plan][partial rows]; only the error word outlives a call.
+constexpr size_t kOpPlanBytes = align256(kUnMaxWarps * sizeof(int4) + (kUnMaxSeq + 3) * sizeof(int));
+constexpr size_t kOpHeaderBytes = 256 + kOpPlanBytes;
 size_t scratch_bytes(long long part_rows) { return kOpHeaderBytes + (size_t)part_rows * kUnPitch * sizeof(float); }
 
 bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
@@ -82,8 +81,7 @@ int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void
 static int check_shared(int32_t R, int32_t n_head, int32_t n_kv_head) {
   if (const int rc = check_heads("op_attention_shared", n_head, n_kv_head)) return rc;
   if (R < 1) return fail_op(TTS_GPT_E_ARG, "op_attention_shared: R must be positive");
-  if (R > kUnMaxSeq || (long long)R * n_kv_head > (long long)kOpMaxTickets)
-    return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_shared: at most %d rows, and R * n_kv_head at most %d", kUnMaxSeq, (int)kOpMaxTickets);
+  if (R > kUnMaxSeq) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_shared: at most %d rows", kUnMaxSeq);
   return TTS_GPT_OK;
 }
 
@@ -108,7 +106,7 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
   // units of 32 keys are numbered in 31 bits, blocks of the pool too
   const int G = n_head / n_kv_head;
   const long long tiles = (long long)n_kv_head * ((R + kUnTile / G - 1) / (kUnTile / G));
-  if (pages_per_stream > (1 << 24) || 2ll * tiles * n_shared + 2ll * R * n_kv_head * (pages_per_stream - n_shared) + (long long)R * n_kv_head >= (1ll << 31) ||
+  if (pages_per_stream > (1 << 24) || tiles * (2ll * n_shared + 1) + (long long)R * n_kv_head * (2ll * (pages_per_stream - n_shared) + 1) >= (1ll << 31) ||
       2ll * n_pages * n_kv_head >= (1ll << 31))
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_shared: too many pages");
   if (scratch_size < scratch_bytes(shared_part_rows(R, n_kv_head, G)))
@@ -119,7 +117,7 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
   a.page_table = page_table; a.row_stream = row_stream; a.row_pos = row_pos; a.pool = (const unsigned char *)kv_layer; a.pps = pages_per_stream;
   a.n_shared = n_shared; a.n_pages = n_pages;
   a.err = (int *)scratch;
-  a.tickets = (unsigned *)((char *)scratch + 256);
+  a.plan = (int *)((char *)scratch + 256);
   a.part = (float *)((char *)scratch + kOpHeaderBytes);
   a.suffix_part0 = (int)shared_prefix_part_rows(R, n_kv_head, G);
   cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -158,8 +156,8 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   if (q_max > q_rows) q_max = q_rows;
   const int G = n_head / n_kv_head, rpt = kUnTile / G;
   const long long blocks = std::min((long long)n * ((q_max + rpt - 1) / rpt), (long long)q_rows / rpt + n);
-  if ((long long)n_kv_head * blocks * ((long long)k_rows / kUnKeys + 1) >= (1ll << 31) &&
-      (long long)n_kv_head * ((q_max + rpt - 1) / rpt) * ((long long)k_rows / kUnKeys + n) >= (1ll << 31))
+  if ((long long)n_kv_head * blocks * ((long long)k_rows / kUnKeys + 2) >= (1ll << 31) &&
+      (long long)n_kv_head * ((q_max + rpt - 1) / rpt) * ((long long)k_rows / kUnKeys + 2 * n) >= (1ll << 31))
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: too many queries times keys");
   if (scratch_size < scratch_bytes(cross_part_rows()))
     return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_cross: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(cross_part_rows()));
@@ -168,7 +166,7 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   a.scale = scale * 1.4426950408889634f;
   a.q_start = q_start; a.k_start = k_start; a.n_seq = n; a.q_max = q_max; a.k_rows = k_rows;
   a.err = (int *)scratch;
-  a.tickets = (unsigned *)((char *)scratch + 256);
+  a.plan = (int *)((char *)scratch + 256);
   a.part = (float *)((char *)scratch + kOpHeaderBytes);
   CUtensorMap k_map = {}, v_map = {};
   const bool f16 = type == TTS_GPT_T_F16;

@@ -60,7 +60,7 @@ def _shared(**kw):
 
 @pytest.mark.parametrize("code,kw", [
     (B.E_ARG, dict(R=0)), (B.E_ARG, dict(heads=0)), (B.E_ARG, dict(kv=0)), (B.E_ARG, dict(kv=3)), (B.E_UNSUPPORTED, dict(heads=34, qs=34 * 64)),
-    (B.E_UNSUPPORTED, dict(R=4097)), (B.E_UNSUPPORTED, dict(R=4096, heads=65, kv=65, qs=65 * 64)), (B.E_ARG, dict(type=B.T_F16)), (B.E_ARG, dict(q=0)), (B.E_ARG, dict(pool=0)),
+    (B.E_UNSUPPORTED, dict(R=4097)), (B.E_UNSUPPORTED, dict(heads=1040, kv=65, qs=1040 * 64)), (B.E_ARG, dict(type=B.T_F16)), (B.E_ARG, dict(q=0)), (B.E_ARG, dict(pool=0)),
     (B.E_ARG, dict(table=0)), (B.E_ARG, dict(rs=0)), (B.E_ARG, dict(rp=0)), (B.E_ARG, dict(out=0)), (B.E_ARG, dict(scratch=0)), (B.E_ARG, dict(fmt=3)), (B.E_ARG, dict(pages=0)),
     (B.E_ARG, dict(n_shared=-1)), (B.E_ARG, dict(n_shared=5)), (B.E_ARG, dict(pps=0)), (B.E_ARG, dict(qs=255)), (B.E_ARG, dict(qs=258)), (B.E_ARG, dict(q=P + 8)),
     (B.E_ARG, dict(out=P + 2)), (B.E_ARG, dict(scratch=P + 128)), (B.E_ARG, dict(table=P + 2)), (B.E_UNSUPPORTED, dict(pages=2 ** 30)), (B.E_UNSUPPORTED, dict(pps=2 ** 25)),
