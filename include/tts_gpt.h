@@ -413,9 +413,9 @@ int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void
  * Keys on a page outside 0..n_pages-1 are left out, as are those behind the list's pages_per_stream pages.  K and V of the shared
  * pages must be finite.  fp32 queries enter with 16 bits, the softmax weights are rounded to bf16, sums are fp32; results do
  * not depend on timing.  R <= 4096.
- * scratch (256-byte aligned, >= scratch_bytes; its first word zero before its first use, by this call or op_attention_cross, in
- * any size) belongs to one call at a time: calls that may overlap, replays of captured graphs among them, need one each.  That
- * word is set to 1 if a bounded wait inside a kernel ran out; outputs are then incomplete, until it is zeroed. */
+ * scratch (256-byte aligned, >= scratch_bytes; zero before its first use, by this call or op_attention_cross, in any size)
+ * belongs to one call at a time: calls that may overlap, replays of captured graphs among them, need one each.  Its first
+ * word is set to 1 if a bounded wait inside a kernel ran out; outputs are then incomplete and the scratch must be zeroed. */
 int32_t tts_gpt_op_attention_shared_scratch_bytes(int32_t R, int32_t n_head, int32_t n_kv_head, size_t *bytes);
 int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head, int32_t type, const void *q, int64_t q_stride,
                                     int32_t kv_fmt, int32_t n_pages, const void *kv_layer, int32_t n_shared,

@@ -436,40 +436,46 @@ def op_sample(logits, top_k=0, temperature=1.0, uniforms=None, stream=None):
 # ---------------------------------------------------------------------------------------------
 # serving many requests from one paged cache
 # ---------------------------------------------------------------------------------------------
+# These calls are made every step, so their checks are written for speed: one condition over all tensors, attribute by attribute
+# (0.05 us each), and a search for the culprit only where it fails.
+_I32, _F32, _F16, _BF16, _I16, _U8 = torch.int32, torch.float32, torch.float16, torch.bfloat16, torch.int16, torch.uint8
+
+
 def _refuse(what):
     raise TtsGptError(E_ARG, what)
 
 
-def _index(t, name, dev, numel=None):
-    """The address of a contiguous int32 tensor on `dev` (of at least `numel` values)."""
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.device != dev or (numel is not None and t.numel() < numel):
-        _refuse("%s must be a contiguous int32 tensor on %s%s" % (name, dev, "" if numel is None else " with at least %d values" % numel))
-    return t.data_ptr()
+def _refuse_index(d, **tensors):
+    """Says which of the tensors is not a contiguous int32 tensor on device number d, if one is."""
+    for name, t in tensors.items():
+        if t is not None and (t.dtype is not _I32 or t.get_device() != d or not t.is_contiguous()):
+            _refuse("%s must be a contiguous int32 tensor on the same device as the others" % name)
 
 
-def _launch(name, dev, stream, *args):
-    """Calls a C entry point with `dev` current, on `stream` or torch's current one of that device."""
-    if dev.type != "cuda":
-        _refuse("%s: tensors must be on a CUDA device" % name)
-    if dev.index != torch.cuda.current_device():
-        with torch.cuda.device(dev):
-            return _launch(name, dev, stream, *args)
-    st = torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
-    rc = getattr(load(), name)(*args, st)
-    if rc != OK:
+def _run(fn, d, stream, *args):
+    """Calls a C entry point with device number d current, on `stream` or torch's current one of that device."""
+    if d < 0:
+        _refuse("tensors must be on a CUDA device")
+    st = torch._C._cuda_getCurrentRawStream(d) if stream is None else stream.cuda_stream
+    if d == torch._C._cuda_getDevice():
+        rc = fn(*args, st)
+    else:
+        with torch.cuda.device(d):
+            rc = fn(*args, st)
+    if rc:
         _check(rc)
 
 
-def _pool(kv_layer, dev):
+def _pool(kv_layer, d):
     """(format, pages, heads) of one layer's pool: bf16 [pages, 2, heads, 64, 64], or bytes [pages, 2, heads, 4352]."""
     sh = kv_layer.shape
-    if kv_layer.device != dev or not kv_layer.is_contiguous() or len(sh) < 4 or sh[1] != 2:
-        _refuse("kv_layer must be a contiguous tensor [pages, 2, heads, ...] on %s" % dev)
-    if kv_layer.dtype in (torch.bfloat16, torch.int16) and sh[3:] == (64, 64):
-        return 0, sh[0], sh[2]
-    if kv_layer.dtype == torch.uint8 and sh[3:] == (4352,):
-        return 1, sh[0], sh[2]
-    _refuse("kv_layer must be bf16 [pages, 2, heads, 64, 64] or uint8 [pages, 2, heads, 4352]")
+    if kv_layer.get_device() == d and kv_layer.is_contiguous():
+        t = kv_layer.dtype
+        if (t is _BF16 or t is _I16) and len(sh) == 5 and sh[1] == 2 and sh[3] == 64 and sh[4] == 64:
+            return 0, sh[0], sh[2]
+        if t is _U8 and len(sh) == 4 and sh[1] == 2 and sh[3] == 4352:
+            return 1, sh[0], sh[2]
+    _refuse("kv_layer must be a contiguous bf16 tensor [pages, 2, heads, 64, 64] or uint8 tensor [pages, 2, heads, 4352] on the same device as the others")
 
 
 def op_page_tables(new_len, ctx_len, page_table, free_pages, free_top, row_start, row_stream, row_pos, row_slot, info,
@@ -477,38 +483,59 @@ def op_page_tables(new_len, ctx_len, page_table, free_pages, free_top, row_start
     """Page lists and slot maps of a pass from the requests' lengths; everything int32 on one device, written in place.  row_stream,
     row_pos and row_slot hold as many rows as the pass may have.  ctx_len_out, free_top_out: None updates ctx_len, free_top.
     info: 8 values, zero at first; info[0] is the status the lengths lead to, which lives on the device like they do."""
-    dev, n = new_len.device, new_len.numel()
-    if page_table.dim() != 2 or page_table.shape[0] != ctx_len.numel():
-        _refuse("page_table must be [streams, pages of a stream], ctx_len [streams]")
-    if row_pos.numel() != row_stream.numel() or row_slot.numel() != row_stream.numel():
-        _refuse("row_stream, row_pos and row_slot must have the same length")
-    streams = ctx_len.numel()
-    _launch("tts_gpt_op_page_tables", dev, stream, n, None if stream_ids is None else _index(stream_ids, "stream_ids", dev, n), _index(new_len, "new_len", dev),
-            streams, _index(ctx_len, "ctx_len", dev), _index(ctx_len if ctx_len_out is None else ctx_len_out, "ctx_len_out", dev, streams),
-            free_pages.numel(), _index(free_pages, "free_pages", dev), _index(free_top, "free_top", dev, 1),
-            _index(free_top if free_top_out is None else free_top_out, "free_top_out", dev, 1), 0 if shared_pages is None else shared_pages.numel(),
-            None if shared_pages is None else _index(shared_pages, "shared_pages", dev), page_table.shape[1], _index(page_table, "page_table", dev),
-            row_stream.numel(), _index(row_start, "row_start", dev, n + 1), _index(row_stream, "row_stream", dev), _index(row_pos, "row_pos", dev),
-            _index(row_slot, "row_slot", dev), _index(info, "info", dev, 8))
+    d, n, streams, rows = new_len.get_device(), new_len.numel(), ctx_len.numel(), row_stream.numel()
+    if ctx_len_out is None:
+        ctx_len_out = ctx_len
+    if free_top_out is None:
+        free_top_out = free_top
+    ids = shared = None
+    n_shared = 0
+    fine = (new_len.dtype is ctx_len.dtype is page_table.dtype is free_pages.dtype is free_top.dtype is row_start.dtype is row_stream.dtype is row_pos.dtype
+            is row_slot.dtype is info.dtype is ctx_len_out.dtype is free_top_out.dtype is _I32
+            and ctx_len.get_device() == page_table.get_device() == free_pages.get_device() == free_top.get_device() == row_start.get_device()
+            == row_stream.get_device() == row_pos.get_device() == row_slot.get_device() == info.get_device() == ctx_len_out.get_device()
+            == free_top_out.get_device() == d
+            and new_len.is_contiguous() and ctx_len.is_contiguous() and page_table.is_contiguous() and free_pages.is_contiguous() and row_start.is_contiguous()
+            and row_stream.is_contiguous() and row_pos.is_contiguous() and row_slot.is_contiguous() and info.is_contiguous() and ctx_len_out.is_contiguous())
+    if stream_ids is not None:
+        fine = fine and stream_ids.dtype is _I32 and stream_ids.get_device() == d and stream_ids.is_contiguous() and stream_ids.numel() == n
+        ids = stream_ids.data_ptr()
+    if shared_pages is not None:
+        fine = fine and shared_pages.dtype is _I32 and shared_pages.get_device() == d and shared_pages.is_contiguous()
+        shared, n_shared = shared_pages.data_ptr(), shared_pages.numel()
+    shape = page_table.shape
+    if not (fine and len(shape) == 2 and shape[0] == streams == ctx_len_out.numel() and row_pos.numel() == rows == row_slot.numel() and row_start.numel() > n
+            and info.numel() >= 8 and free_top.numel() and free_top_out.numel()):
+        _refuse_index(d, new_len=new_len, ctx_len=ctx_len, page_table=page_table, free_pages=free_pages, free_top=free_top, row_start=row_start,
+                      row_stream=row_stream, row_pos=row_pos, row_slot=row_slot, info=info, stream_ids=stream_ids, shared_pages=shared_pages,
+                      ctx_len_out=ctx_len_out, free_top_out=free_top_out)
+        _refuse("page_table must be [streams, pages of a stream], ctx_len [streams], stream_ids as long as new_len, row_start longer, "
+                "row_stream, row_pos and row_slot of one length, info 8 long")
+    _run((_lib or load()).tts_gpt_op_page_tables, d, stream, n, ids, new_len.data_ptr(), streams, ctx_len.data_ptr(), ctx_len_out.data_ptr(), free_pages.numel(),
+         free_pages.data_ptr(), free_top.data_ptr(), free_top_out.data_ptr(), n_shared, shared, shape[1], page_table.data_ptr(), rows, row_start.data_ptr(),
+         row_stream.data_ptr(), row_pos.data_ptr(), row_slot.data_ptr(), info.data_ptr())
 
 
 def op_kv_append(k, v, kv_layer, row_slot, stream=None):
     """K and V rows [R, heads * 64] (fp32 or bf16; rows may be strided) into their slots of the pool."""
-    dev = k.device
-    fmt, pages, heads = _pool(kv_layer, dev)
-    if k.dtype != v.dtype or k.dtype not in _TYPES or k.dtype == torch.float16 or k.shape != v.shape or k.dim() != 2 or k.shape[1] != heads * 64 \
-            or v.device != dev or k.stride(1) != 1 or v.stride(1) != 1:
-        _refuse("k and v must be [R, %d] of one type, fp32 or bf16, on %s, with contiguous rows" % (heads * 64, dev))
-    R = k.shape[0]
-    # the stride of a single row addresses nothing
-    ks, vs = (k.stride(0), v.stride(0)) if R > 1 else (heads * 64, heads * 64)
-    _launch("tts_gpt_op_kv_append", dev, stream, R, heads, _TYPES[k.dtype], k.data_ptr(), ks, v.data_ptr(), vs, _index(row_slot, "row_slot", dev, R),
-            fmt, pages, kv_layer.data_ptr())
+    d, t, shape = k.get_device(), k.dtype, k.shape
+    fmt, pages, heads = _pool(kv_layer, d)
+    if v.dtype is not t or t is _F16 or t not in _TYPES or v.shape != shape or len(shape) != 2 or shape[1] != heads * 64 or v.get_device() != d:
+        _refuse("k and v must be [R, %d] of one type, fp32 or bf16, on one device" % (heads * 64))
+    (ks, k1), (vs, v1), R = k.stride(), v.stride(), shape[0]
+    if k1 != 1 or v1 != 1:
+        _refuse("rows of k and v must be contiguous")
+    if R == 1:
+        ks = vs = heads * 64                   # the stride of a single row addresses nothing
+    if row_slot.dtype is not _I32 or row_slot.get_device() != d or not row_slot.is_contiguous() or row_slot.numel() < R:
+        _refuse("row_slot must be a contiguous int32 tensor of at least R values on the same device")
+    _run((_lib or load()).tts_gpt_op_kv_append, d, stream, R, heads, _TYPES[t], k.data_ptr(), ks, v.data_ptr(), vs, row_slot.data_ptr(), fmt, pages,
+         kv_layer.data_ptr())
 
 
-def _scratch(scratch, dev):
-    if scratch.dtype != torch.uint8 or scratch.device != dev or not scratch.is_contiguous():
-        _refuse("scratch must be a contiguous uint8 tensor on %s" % dev)
+def _scratch(scratch, d):
+    if scratch.dtype is not _U8 or scratch.get_device() != d or not scratch.is_contiguous():
+        _refuse("scratch must be a contiguous uint8 tensor on the same device")
     return scratch.data_ptr(), scratch.numel()
 
 
@@ -521,23 +548,30 @@ def op_attention_shared_scratch(R, n_head, n_kv_head, device):
 def op_attention_shared(q, kv_layer, page_table, row_stream, row_pos, n_shared, scratch=None, out=None, stream=None):
     """Attention of rows q [R, heads * 64] (fp32 or bf16) over a paged cache whose page lists all begin with the same n_shared
     pages.  The pool may have fewer heads than q.  Returns bf16 bits [R, heads * 64], or `out`."""
-    dev = q.device
-    fmt, pages, kv_heads = _pool(kv_layer, dev)
-    if q.dim() != 2 or q.dtype not in _TYPES or q.dtype == torch.float16 or q.shape[1] % 64 or q.stride(1) != 1:
-        _refuse("q must be [R, heads * 64], fp32 or bf16, with contiguous rows")
-    if page_table.dim() != 2:
-        _refuse("page_table must be [streams, pages of a stream]")
-    R, heads = q.shape[0], q.shape[1] // 64
+    d, t, shape = q.get_device(), q.dtype, q.shape
+    fmt, pages, kv_heads = _pool(kv_layer, d)
+    if len(shape) != 2 or shape[1] % 64 or t is _F16 or t not in _TYPES:
+        _refuse("q must be [R, heads * 64], fp32 or bf16")
+    (qs, q1), R, heads = q.stride(), shape[0], shape[1] // 64
+    if q1 != 1:
+        _refuse("rows of q must be contiguous")
+    if R == 1:
+        qs = heads * 64                        # the stride of a single row addresses nothing
+    lists = page_table.shape
+    if not (page_table.dtype is row_stream.dtype is row_pos.dtype is _I32 and page_table.get_device() == row_stream.get_device() == row_pos.get_device() == d
+            and page_table.is_contiguous() and row_stream.is_contiguous() and row_pos.is_contiguous() and len(lists) == 2 and row_stream.numel() >= R
+            and row_pos.numel() >= R):
+        _refuse_index(d, page_table=page_table, row_stream=row_stream, row_pos=row_pos)
+        _refuse("page_table must be [streams, pages of a stream], row_stream and row_pos at least R long")
     if out is None:
-        out = torch.empty((R, heads * 64), dtype=torch.int16, device=dev)
-    elif out.shape != q.shape or out.dtype not in (torch.int16, torch.bfloat16) or out.device != dev or not out.is_contiguous():
-        _refuse("out must be a contiguous bf16 tensor of q's shape")
+        out = torch.empty(shape, dtype=_I16, device=q.device)
+    elif out.shape != shape or (out.dtype is not _BF16 and out.dtype is not _I16) or out.get_device() != d or not out.is_contiguous():
+        _refuse("out must be a contiguous bf16 tensor of q's shape on the same device")
     if scratch is None:
-        scratch = op_attention_shared_scratch(R, heads, kv_heads, dev)
-    sp, sn = _scratch(scratch, dev)
-    _launch("tts_gpt_op_attention_shared", dev, stream, R, heads, kv_heads, _TYPES[q.dtype], q.data_ptr(), q.stride(0) if R > 1 else heads * 64, fmt, pages,
-            kv_layer.data_ptr(), n_shared, _index(page_table, "page_table", dev), page_table.shape[1], _index(row_stream, "row_stream", dev, R),
-            _index(row_pos, "row_pos", dev, R), out.data_ptr(), sp, sn)
+        scratch = op_attention_shared_scratch(R, heads, kv_heads, q.device)
+    sp, sn = _scratch(scratch, d)
+    _run((_lib or load()).tts_gpt_op_attention_shared, d, stream, R, heads, kv_heads, _TYPES[t], q.data_ptr(), qs, fmt, pages, kv_layer.data_ptr(), n_shared,
+         page_table.data_ptr(), lists[1], row_stream.data_ptr(), row_pos.data_ptr(), out.data_ptr(), sp, sn)
     return out
 
 
@@ -552,27 +586,36 @@ def op_attention_cross(q, k, v, q_start, k_start, q_max, scale=0.125, scratch=No
     or fp16; sequence i has rows q_start[i] .. q_start[i+1]-1 of q and k_start[i] .. k_start[i+1]-1 of k and v, whose rows and heads
     may be strided.  q_max: at least the longest sequence of queries.  Returns [rows, heads, 64] (rows of no sequence undefined), or `out`
     (in which they are left as they were)."""
-    dev = q.device
-    if q.dim() != 3 or k.dim() != 3 or q.dtype not in (torch.bfloat16, torch.float16) or k.dtype != q.dtype or v.dtype != q.dtype or q.shape[2] != 64 or k.shape[2] != 64 \
-            or v.shape != k.shape or k.device != dev or v.device != dev or q.stride(2) != 1 or k.stride(2) != 1 or v.stride(2) != 1 or (q.shape[1] > 1 and q.stride(1) != 64):
-        _refuse("q must be [rows, heads, 64] with contiguous heads, k and v [rows, kv heads, 64], all bf16 or all fp16, on one device")
-    n = q_start.numel() - 1
-    if n < 1 or k_start.numel() != n + 1:
-        _refuse("q_start and k_start must have one value more than there are sequences")
-    rows, heads = q.shape[0], q.shape[1]
-    if out is None:
-        out = torch.empty((rows, heads, 64), dtype=q.dtype, device=dev)
-    elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or not out.is_contiguous():
-        _refuse("out must be a contiguous tensor of q's shape and type")
-    if scratch is None:
-        scratch = op_attention_cross_scratch(dev)
-    sp, sn = _scratch(scratch, dev)
+    d, t, shape, kshape = q.get_device(), q.dtype, q.shape, k.shape
+    if (t is not _BF16 and t is not _F16) or not (k.dtype is v.dtype is t) or len(shape) != 3 or len(kshape) != 3 or v.shape != kshape or shape[2] != 64 \
+            or kshape[2] != 64 or k.get_device() != d or v.get_device() != d:
+        _refuse("q must be [rows, heads, 64], k and v [rows, kv heads, 64], all bf16 or all fp16, on one device")
+    (qs, qh, q1), (kr, kh, k1), (vr, vh, v1) = q.stride(), k.stride(), v.stride()
+    rows, heads, _ = shape
+    k_rows, kv_heads, _ = kshape
+    if q1 != 1 or k1 != 1 or v1 != 1 or (heads > 1 and qh != 64):
+        _refuse("heads of q, and the 64 values of a head of k and v, must be contiguous")
     # strides of a single row or head address nothing
-    kr, vr = (k.stride(0), v.stride(0)) if k.shape[0] > 1 else (64, 64)
-    kh, vh = (k.stride(1), v.stride(1)) if k.shape[1] > 1 else (64, 64)
-    _launch("tts_gpt_op_attention_cross", dev, stream, n, heads, k.shape[1], _TYPES[q.dtype], rows, q.data_ptr(), q.stride(0) if rows > 1 else heads * 64,
-            k.shape[0], k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, _index(q_start, "q_start", dev), _index(k_start, "k_start", dev), q_max, scale,
-            out.data_ptr(), sp, sn)
+    if rows == 1:
+        qs = heads * 64
+    if k_rows <= 1:
+        kr = vr = 64
+    if kv_heads == 1:
+        kh = vh = 64
+    n = q_start.numel() - 1
+    if not (q_start.dtype is k_start.dtype is _I32 and q_start.get_device() == k_start.get_device() == d and q_start.is_contiguous() and k_start.is_contiguous()
+            and n >= 1 and k_start.numel() == n + 1):
+        _refuse_index(d, q_start=q_start, k_start=k_start)
+        _refuse("q_start and k_start must have one value more than there are sequences")
+    if out is None:
+        out = torch.empty(shape, dtype=t, device=q.device)
+    elif out.shape != shape or out.dtype is not t or out.get_device() != d or not out.is_contiguous():
+        _refuse("out must be a contiguous tensor of q's shape and type on the same device")
+    if scratch is None:
+        scratch = op_attention_cross_scratch(q.device)
+    sp, sn = _scratch(scratch, d)
+    _run((_lib or load()).tts_gpt_op_attention_cross, d, stream, n, heads, kv_heads, _TYPES[t], rows, q.data_ptr(), qs, k_rows, k.data_ptr(), kr, kh,
+         v.data_ptr(), vr, vh, q_start.data_ptr(), k_start.data_ptr(), q_max, scale, out.data_ptr(), sp, sn)
     return out
 
 

@@ -1,0 +1,413 @@
+// Attention of query tiles of 128 rows over blocks of 128 keys on the 5th-generation tensor cores: cross attention where a
+// sequence has more queries than a tile of the warp-level kernel (Section I: the decode engine's attention kernels).
+//
+// A tile is 128 (row, head of the group) pairs of one sequence and one head of keys; thread t of the softmax warps owns row t =
+// accumulator lane t.  For each block of 128 keys
+//     S = Q K^T     tcgen05.mma M=128 x N=128 x K=64, S (fp32) in tensor memory
+//     softmax       S out of tensor memory, running reference m and sum l in fp32, P = 2^(S scale - m) rounded to the inputs' type
+//                   back into tensor memory.  The reference moves, and O with it, only where a score exceeds it by 2^8: weights
+//                   stay below 256 and the rounding of a weight is relative, so nothing is lost
+//     O += P V      M=128 x N=64 x K=128, P as the operand in tensor memory, V as stored
+// S takes 128 columns, P 64 and O 64: half of an SM's tensor memory, so that two CTAs share an SM and one's softmax runs while
+// the other's products do.  What bounds it is the softmax's exponentials: 16384 of them a block, 16 a cycle and SM.
+//
+// Work split.  The blocks of all tiles are laid end to end and cut into one range a CTA, equal to within a block; a tile counts
+// one block more than its keys have.  The parts of a tile that several CTAs share meet as in the warp-level kernel: in scratch,
+// added in the order of their keys by the CTA that arrives last at the tile's ticket.  Every wait on a copy or a product is bounded.
+#pragma once
+#include "attention_units.cuh"
+
+namespace ttsgpt {
+
+constexpr int kTlRows = 128, kTlKeys = 128;
+constexpr int kTlThreads = 192;             // warps 0-3: softmax, 4: copies, 5: products
+constexpr int kTlHalf = kTlKeys * 128;      // K or V of a block: 16 KB
+constexpr int kTlRing = 4;                  // places for K and V blocks in turn
+constexpr int kTlMaxSeq = 2048;
+constexpr int kTlMaxCtas = 2 * kUnMaxCtas;
+constexpr float kTlSlack = 8.0f;            // log2 by which a score may exceed the reference
+
+struct TileShared {
+  uint64_t full[kTlRing], empty[kTlRing];   // K and V blocks
+  uint64_t q_full[2], q_free[2];
+  uint64_t s_full, s_free, p_full, pv_done;
+  uint32_t tmem;
+  int failed;
+  Div size;
+  int warp_tot[kTlThreads / 32];
+};
+inline size_t tiles_smem_bytes(int n) { return 1024 + (size_t)(kTlRing + 2) * kTlHalf + sizeof(TileShared) + (size_t)(n + 1) * sizeof(int); }
+
+// 32 lanes x 16 or 32 columns of 32 bits into tensor memory, of which the caller waits for all at once
+__device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+                 "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// A in tensor memory (row = lane, two 16-bit values of consecutive k a column), B in shared memory
+__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
+}
+
+template <bool F16>
+__global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                                                                        const __grid_constant__ CUtensorMap v_map, const UnitArgs a) {
+  extern __shared__ __align__(16) unsigned char tl_smem_raw[];
+  unsigned char *base = tl_smem_raw + ((1024u - (smem_u32(tl_smem_raw) & 1023u)) & 1023u);
+  unsigned char *ring = base, *Qs = base + kTlRing * kTlHalf;      // [2] 128 rows x 64 values, K-major, 128-byte swizzle
+  TileShared &sh = *reinterpret_cast<TileShared *>(Qs + 2 * kTlHalf);
+  int *first = reinterpret_cast<int *>(&sh + 1);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  volatile int *failed = &sh.failed;
+
+  if (tid == 0) {
+    for (int i = 0; i < kTlRing; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_free[i], 1); }
+    mbar_init(&sh.s_full, 1); mbar_init(&sh.s_free, kTlRows); mbar_init(&sh.p_full, kTlRows); mbar_init(&sh.pv_done, 1);
+    sh.failed = 0;
+  }
+  if (warp == 4) {
+    if (lane < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &q_map : lane == 1 ? &k_map : &v_map) : "memory");
+    __syncwarp();
+  }
+  if (warp == 5) tmem_alloc(&sh.tmem, 256);   // S: columns 0 .. 127, P: 128 .. 191, O: 192 .. 255
+  // ---- running sums of blocks over the sequences ----
+  auto q_span = [&](int i, int &b, int &e) {
+    b = min(max(a.q_start[i], 0), a.q_rows);
+    e = min(min(max(a.q_start[i + 1], b), a.q_rows), b + a.q_max);
+  };
+  auto k_span = [&](int i, int &b, int &e) {
+    b = min(max(a.k_start[i], 0), a.k_rows);
+    e = min(max(a.k_start[i + 1], b), a.k_rows);
+  };
+  int carry = 0;
+  for (int i0 = 0; i0 < a.n_seq; i0 += kTlThreads) {
+    const int i = i0 + tid;
+    int u = 0;
+    if (i < a.n_seq) {
+      int qb, qe, kb, ke;
+      q_span(i, qb, qe);
+      k_span(i, kb, ke);
+      u = a.Hkv * a.by_rpt.of(qe - qb + a.rpt - 1) * (1 + (ke - kb + kTlKeys - 1) / kTlKeys);
+    }
+    int incl = u;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    __syncthreads();
+    if (lane == 31) sh.warp_tot[warp] = incl;
+    __syncthreads();
+    int before = carry, all = carry;
+#pragma unroll
+    for (int w = 0; w < kTlThreads / 32; ++w) { if (w < warp) before += sh.warp_tot[w]; all += sh.warp_tot[w]; }
+    if (i < a.n_seq) first[i] = before + incl - u;
+    carry = all;
+  }
+  const int T = carry;
+  if (tid == 0) {
+    first[a.n_seq] = T;
+    sh.size.set(max(2, (T + (int)gridDim.x - 1) / (int)gridDim.x));
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = sh.tmem;
+  const Div size = sh.size;
+  const int u_begin = blockIdx.x * (int)size.d, u_end = min(T, u_begin + (int)size.d);
+
+  // the part of a tile that lies in this CTA's range, from unit u on
+  struct Part {
+    int row0, n_i, kvh, u0, nu;     // first query row, rows times heads, head of keys; the tile's units
+    int j0, j1, key0, keys;         // its blocks here; first key row and number of keys of the sequence
+  };
+  auto part_at = [&](int u) {
+    Part p;
+    int lo = 0, hi = a.n_seq - 1;
+    while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (first[m] <= u) lo = m; else hi = m - 1; }
+    int qb, qe, kb, ke;
+    q_span(lo, qb, qe);
+    k_span(lo, kb, ke);
+    p.key0 = kb; p.keys = ke - kb;
+    p.nu = 1 + (p.keys + kTlKeys - 1) / kTlKeys;
+    const int x = u - first[lo], tile = (int)((unsigned)x / (unsigned)p.nu), blocks = a.by_rpt.of(qe - qb + a.rpt - 1);
+    p.u0 = first[lo] + tile * p.nu;
+    p.kvh = (int)((unsigned)tile / (unsigned)blocks);
+    p.row0 = qb + (tile - p.kvh * blocks) * a.rpt;
+    p.n_i = min(a.rpt, qe - p.row0) * a.G;
+    p.j0 = max(u - p.u0 - 1, 0);
+    p.j1 = min(u_end - p.u0, p.nu) - 1;
+    return p;
+  };
+  auto wait = [&](uint64_t *bar, uint32_t parity) {   // the whole warp; false: some wait of the CTA has run out
+    if (mbar_try_wait(bar, parity)) return true;
+    const unsigned long long t0 = global_timer_ns();
+    while (!mbar_try_wait(bar, parity)) {
+      if (*failed) return false;
+      if (global_timer_ns() - t0 > kUnWaitNs) { *failed = 1; atomicExch(a.err, 1); return false; }
+    }
+    return true;
+  };
+  auto wait_warp = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait(bar, parity)) != 0; };
+
+  if (warp == 4) {
+    // ---- copies: K and V blocks into the ring in turn, Q ahead of its first block ----
+    int slot = 0, n_tile = 0;                  // halves of blocks, and tiles with blocks, of this CTA
+    for (int u = u_begin; u < u_end;) {
+      const Part p = part_at(u);
+      u = p.u0 + p.j1 + 1;
+      if (p.j1 <= p.j0) continue;
+      const int qb = n_tile & 1;
+      if (n_tile >= 2 && !wait_warp(&sh.q_free[qb], (uint32_t)(n_tile / 2 - 1) & 1u)) break;
+      if (elect_one()) {
+        mbar_expect_tx(&sh.q_full[qb], (uint32_t)(a.rpt * a.G) * 128);
+        un_box(&q_map, p.kvh * a.G, p.row0, Qs + qb * kTlHalf, &sh.q_full[qb]);
+      }
+      __syncwarp();
+      ++n_tile;
+      bool fine = true;
+      for (int j = p.j0; j < p.j1 && fine; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h, ++slot) {
+          const int s = slot % kTlRing;
+          fine = fine && (slot < kTlRing || wait_warp(&sh.empty[s], (uint32_t)(slot / kTlRing - 1) & 1u));
+          if (!fine) break;
+          if (elect_one()) {
+            mbar_expect_tx(&sh.full[s], kTlHalf);
+            const int row = p.key0 + j * kTlKeys, tf = h ? a.v_tokens_first : a.k_tokens_first;
+            un_box(h ? &v_map : &k_map, tf ? row : p.kvh, tf ? p.kvh : row, ring + s * kTlHalf, &sh.full[s]);
+          }
+          __syncwarp();
+        }
+      if (!fine) break;
+    }
+  } else if (warp == 5) {
+    // ---- products: Q K^T of block i as soon as the softmax has read S of the block before, P V of block i - 1 behind it ----
+    const uint32_t kind = F16 ? ~((1u << 7) | (1u << 10)) : ~0u;
+    const uint32_t idesc_qk = tc_instr_desc(kTlRows, kTlKeys) & kind, idesc_pv = (tc_instr_desc(kTlRows, kHeadDim) & kind) | (1u << 16);   // V is MN-major
+    int i = 0, n_tile = 0;                     // blocks, and tiles with blocks, of this CTA
+    bool fine = true;
+    auto pv = [&](int blk, bool begins) {
+      const int s = (2 * blk + 1) % kTlRing;
+      fine = fine && wait_warp(&sh.full[s], (uint32_t)((2 * blk + 1) / kTlRing) & 1u) && wait_warp(&sh.p_full, (uint32_t)blk & 1u);
+      if (!fine) return;
+      tc_fence_after_sync();
+      const uint64_t dv = tc_smem_desc(ring + s * kTlHalf);
+      if (elect_one()) {
+#pragma unroll
+        for (int q = 0; q < kTlKeys / 16; ++q)   // 16 keys an instruction: 8 columns of P, two groups of 8 rows of V
+          tc_mma_ts(tmem + 192u, tmem + 128u + 8u * q, dv + 128 * q, idesc_pv, begins && q == 0 ? 0u : 1u);
+        tc_commit(&sh.pv_done);
+        tc_commit(&sh.empty[s]);
+      }
+      __syncwarp();
+    };
+    for (int u = u_begin; u < u_end && fine;) {
+      const Part p = part_at(u);
+      u = p.u0 + p.j1 + 1;
+      if (p.j1 <= p.j0) continue;
+      const int qb = n_tile & 1;
+      fine = wait_warp(&sh.q_full[qb], (uint32_t)(n_tile / 2) & 1u);
+      ++n_tile;
+      for (int j = p.j0; j < p.j1 && fine; ++j, ++i) {
+        const int s = (2 * i) % kTlRing;
+        fine = wait_warp(&sh.full[s], (uint32_t)((2 * i) / kTlRing) & 1u) && (i == 0 || wait_warp(&sh.s_free, (uint32_t)(i - 1) & 1u));
+        if (!fine) break;
+        tc_fence_after_sync();
+        const uint64_t dq = tc_smem_desc(Qs + qb * kTlHalf), dk = tc_smem_desc(ring + s * kTlHalf);
+        if (elect_one()) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) tc_mma(tmem, dq + 2 * q, dk + 2 * q, idesc_qk, q == 0 ? 0u : 1u);
+          tc_commit(&sh.s_full);
+          tc_commit(&sh.empty[s]);
+          if (j + 1 == p.j1) tc_commit(&sh.q_free[qb]);
+        }
+        __syncwarp();
+        if (j > p.j0) pv(i - 1, j - 1 == p.j0);
+      }
+      if (fine) pv(i - 1, p.j1 - 1 == p.j0);   // the tile's last, ahead of the next tile's first S: O is read in between
+    }
+  } else {
+    // ---- softmax ----
+    const uint32_t t_lane = tmem + ((uint32_t)(32 * warp) << 16);
+    int i = 0;
+    bool fine = true;
+    for (int u = u_begin; u < u_end && fine;) {
+      const Part p = part_at(u);
+      u = p.u0 + p.j1 + 1;
+      const bool live = 32 * warp < p.n_i, mine = tid < p.n_i;   // some row of the warp exists, the thread's own does
+      float m = -INFINITY, l = 0.f;
+      for (int j = p.j0; j < p.j1; ++j, ++i) {
+        fine = wait_warp(&sh.s_full, (uint32_t)i & 1u);
+        if (!fine) break;
+        tc_fence_after_sync();
+        const int n = min(kTlKeys, p.keys - j * kTlKeys);
+        float sc = 1.f;
+        if (live) {
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < kTlKeys; c += 32) {
+            float s[32];
+            tmem_ld32(t_lane + (uint32_t)c, s);
+            if (n < kTlKeys) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) s[e] = c + e < n ? s[e] : -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], s[e]);
+          }
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale;
+          if (m == -INFINITY) { sc = 0.f; m = top; }   // nothing seen yet; O, where there is one, is zero
+          else if (top > m + kTlSlack) { sc = pt_exp2(m - top); m = top; }
+          if (!mine) { sc = 1.f; m = 0.f; }            // a row that does not exist holds anything
+        }
+        // P and O belong to the tensor core until P V of the block before has completed
+        if (j > p.j0) {
+          fine = wait_warp(&sh.pv_done, (uint32_t)(i - 1) & 1u);
+          if (!fine) break;
+          tc_fence_after_sync();
+          if (__any_sync(0xFFFFFFFFu, sc != 1.f)) {
+#pragma unroll
+            for (int c = 0; c < kHeadDim; c += 32) {
+              float o[32];
+              tmem_ld32(t_lane + 192u + (uint32_t)c, o);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] *= sc;
+              tmem_st32(t_lane + 192u + (uint32_t)c, o);
+            }
+          }
+        }
+        if (live) {
+          const float ref = m == -INFINITY ? 0.f : m;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < kTlKeys; c += 32) {
+            float s[32];
+            tmem_ld32(t_lane + (uint32_t)c, s);
+            if (n < kTlKeys) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) s[e] = c + e < n ? s[e] : -INFINITY;
+            }
+            uint32_t pk[16];
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float x = pt_exp2(fmaf(s[e], a.scale, -ref)), y = pt_exp2(fmaf(s[e + 1], a.scale, -ref));
+              sum[(e >> 1) & 3] += x + y;
+              pk[e >> 1] = un_pack<F16>(x, y);
+            }
+            tmem_st16_async(t_lane + 128u + (uint32_t)(c / 2), pk);
+          }
+          l = fmaf(l, sc, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+          tmem_wait_st();
+        }
+        tc_fence_before_sync();
+        mbar_arrive(&sh.s_free);
+        if (n < kTlKeys) {                     // the sequence's last block: V rows behind its keys may hold NaN, and 0 * NaN must not reach O
+          const int s = (2 * i + 1) % kTlRing;
+          fine = wait_warp(&sh.full[s], (uint32_t)((2 * i + 1) / kTlRing) & 1u);
+          if (!fine) break;
+          for (int x = n * 8 + tid; x < kTlKeys * 8; x += kTlRows) *reinterpret_cast<uint4 *>(ring + s * kTlHalf + x * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
+        }
+        mbar_arrive(&sh.p_full);
+      }
+      if (!fine) break;
+      // ---- the tile's rows leave ----
+      float o[kHeadDim];
+#pragma unroll
+      for (int c = 0; c < kHeadDim; ++c) o[c] = 0.f;
+      if (p.j1 > p.j0) {
+        fine = wait_warp(&sh.pv_done, (uint32_t)(i - 1) & 1u);
+        if (!fine) break;
+        tc_fence_after_sync();
+        if (live) {
+#pragma unroll
+          for (int c = 0; c < kHeadDim; c += 32) tmem_ld32(t_lane + 192u + (uint32_t)c, *reinterpret_cast<float (*)[32]>(o + c));
+        }
+        tc_fence_before_sync();                // O may be overwritten once this thread's next P is announced
+      }
+      const int c0 = size.of(p.u0), c1 = size.of(p.u0 + p.nu - 1);
+      const int r = a.by_G.of(tid);
+      uint16_t *dst = a.out + ((size_t)(p.row0 + r) * a.H + (p.kvh - r) * a.G + tid) * kHeadDim;
+      bool write = c0 == c1;
+      if (!write) {
+        auto place = [&](int c) { return a.part + ((size_t)(2 * c + (c == c0)) * kTlRows + tid) * kUnPitch; };
+        if (mine) {
+          float *x = place(blockIdx.x);
+#pragma unroll
+          for (int c = 0; c < kHeadDim; c += 4) *reinterpret_cast<float4 *>(x + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+          *reinterpret_cast<float2 *>(x + kHeadDim) = make_float2(m, l);
+        }
+        // a ticket for each warp's 32 rows
+        __threadfence();
+        __syncwarp();
+        int last = 0;
+        if (lane == 0) {
+          unsigned *tk = a.tickets + 4 * c0 + warp;
+          last = atomicAdd(tk, 1u) + 1u == (unsigned)(c1 - c0 + 1);
+          if (last) *tk = 0u;
+        }
+        write = __shfl_sync(0xFFFFFFFFu, last, 0) != 0;
+        if (write && mine) {                   // all parts, this CTA's own among them, in the order of their keys
+          __threadfence();
+          m = -INFINITY; l = 0.f;
+#pragma unroll
+          for (int c = 0; c < kHeadDim; ++c) o[c] = 0.f;
+#pragma unroll 1
+          for (int c = c0; c <= c1; ++c) {
+            const float *x = place(c);
+            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(x + kHeadDim));
+            if (ml.y == 0.f) continue;         // no key in it
+            const float mn = fmaxf(m, ml.x), fo = m == mn ? 1.f : pt_exp2(m - mn), fn = pt_exp2(ml.x - mn);
+            m = mn;
+            l = fmaf(l, fo, ml.y * fn);
+#pragma unroll
+            for (int e = 0; e < kHeadDim; e += 4) {
+              const float4 v = __ldcg(reinterpret_cast<const float4 *>(x + e));
+              o[e] = fmaf(o[e], fo, v.x * fn); o[e + 1] = fmaf(o[e + 1], fo, v.y * fn);
+              o[e + 2] = fmaf(o[e + 2], fo, v.z * fn); o[e + 3] = fmaf(o[e + 3], fo, v.w * fn);
+            }
+          }
+        }
+      }
+      if (write && mine && !*failed && __ldcg(a.err) == 0) {
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+        for (int c = 0; c < kHeadDim; c += 8)
+          *reinterpret_cast<uint4 *>(dst + c) = make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
+                                                           un_pack<F16>(o[c + 4] * inv, o[c + 5] * inv), un_pack<F16>(o[c + 6] * inv, o[c + 7] * inv));
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (*failed) {   // copies and products may still be in flight
+    const unsigned long long t0 = global_timer_ns();
+    while (global_timer_ns() - t0 <= 10000000ull) {}
+  }
+  if (warp == 5) tmem_dealloc(tmem, 256);
+}
+
+inline long long tiles_part_rows() { return 2ll * kTlMaxCtas * kTlRows; }
+
+template <bool F16>
+inline cudaError_t launch_tiles_as(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUtensorMap &v_map, const UnitArgs &a, int n_sm, cudaStream_t st) {
+  static SmemOptIn opt_in;
+  if (const cudaError_t e = opt_in(attention_tiles_kernel<F16>, tiles_smem_bytes(kTlMaxSeq))) return e;
+  return launch_kernel(attention_tiles_kernel<F16>, dim3(std::min(2 * n_sm, kTlMaxCtas)), dim3(kTlThreads), tiles_smem_bytes(a.n_seq), st, false, q_map, k_map, v_map, a);
+}
+
+// Query rows: G heads of one group and rpt rows a copy.
+inline cudaError_t tiles_q_map(CUtensorMap *map, bool f16, const void *q, size_t heads, size_t rows, size_t row, int G, int rpt) {
+  const cuuint64_t dims[3] = {kHeadDim, heads, rows}, strides[2] = {kHeadDim * 2, rows == 1 ? heads * kHeadDim * 2 : row};
+  const cuuint32_t box[3] = {kHeadDim, (cuuint32_t)G, (cuuint32_t)rpt};
+  return tensor_map_encode(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, q, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+}  // namespace ttsgpt

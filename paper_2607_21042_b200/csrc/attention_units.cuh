@@ -9,10 +9,13 @@
 // with M, the sums and o in fp32; zero where no key is left.
 //
 // Work split.  The units of all tiles are laid end to end and cut into one range a warp, equal to within a unit whatever the
-// lengths are.  A tile inside one range, whose rows read no other keys, is finished by its warp.  The others' parts go to
-// scratch, and a second kernel, launched behind the first's start, adds a row's parts in the order of their keys: no warp waits for
-// another, and results do not depend on timing.  (Tickets, with the merge by the warp that comes last, took 5 us a tile in a
-// chain of fence, atomic and reads: a warp with twenty short rows ended 100 us behind the others.)
+// lengths are; a tile counts one unit more than its keys have, about what it costs besides them.  A tile inside one range, whose
+// rows read no other keys, is finished by its warp.  The others' parts go to scratch and are added in the order of their keys, so
+// that results do not depend on timing and no warp waits for another:
+//   - by the CTA that comes last, at its end (cross attention, where only the tiles at a CTA's two ends reach another; few rows over
+//     a shared prefix): a barrier, a fence and an atomic per tile, once a CTA;
+//   - by a second kernel (many rows over a shared prefix, each of which reads two tiles).  The same tickets there took a warp with
+//     twenty short rows 100 us: fence, atomic and reads at each of them.
 //
 // Instructions.  Queries are the 16-row operand of m16n8k16, keys the 8-wide one, so the scores come out in the layout in which
 // P enters P V.  Queries in fp32 enter as two bf16 parts (16 bits), P is rounded to the cache's type (half a step of it: as
@@ -33,17 +36,50 @@ constexpr int kUnTile = 16;                 // query rows of a tile
 constexpr int kUnMaxSeq = 4096;             // rows (shared) or sequences (cross) of a call
 constexpr int kUnMaxCtas = 160;
 constexpr int kUnMaxWarps = kUnMaxCtas * kUnWarps;
+constexpr int kUnMaxTiles = 64;             // tiles that a CTA can merge
+constexpr int kUnTickets = 16384;
 constexpr int kUnPitch = 68;                // floats of a partial row: o[64], m, l, and two to keep 16-byte rows
 constexpr unsigned long long kUnWaitNs = 2000000000ull;
 
 enum { KV_BF16 = 0, KV_F16 = 1, KV_E4M3 = 2 };   // what the keys and values are stored as
+
+// Division by a number that is the same throughout a launch, in three instructions and not in the thirty of a general one: code is
+// fetched cold in every launch, and these kernels divide in many places.  For 0 <= n < 2^31: with l = ceil(log2 d) and
+// m = ceil(2^(31 + l) / d), n / d = floor(n m / 2^(31 + l)) (m d exceeds 2^(31 + l) by less than d <= 2^l).
+struct Div {
+  uint32_t d, m, s;
+  __host__ __device__ void set(uint32_t by) {
+    d = by; m = 0; s = 0;
+    if (by > 1) {
+      uint32_t q = 0x80000000u / by, r = 0x80000000u - q * by, l = 0;   // 2^31 = q d + r, doubled l times
+      while ((1u << l) < by) {
+        ++l;
+        q <<= 1; r <<= 1;
+        if (r >= by) { r -= by; ++q; }
+      }
+      m = q + (r != 0);
+      s = l - 1;
+    }
+  }
+  __device__ __forceinline__ int of(int n) const {
+#ifdef __CUDA_ARCH__
+    return d == 1 ? n : (int)(__umulhi((uint32_t)n, m) >> s);
+#else
+    return n / (int)d;
+#endif
+  }
+};
 
 struct UnitArgs {
   const void *q;
   uint16_t *out;                // [rows][H * 64]
   long long q_stride;           // elements between query rows
   int q_rows, H, Hkv, G;        // G = H / Hkv query heads share a head of keys
-  int rpt;                      // query rows of a tile: 16 / G
+  int rpt;                      // query rows of a tile: 16 / G (128 / G)
+  Div by_G, by_rpt, by_H, by_Hkv;
+  // shared prefix: its tiles of a head of keys (0 without one), and the units of each of them
+  int tiles_head, prefix_nu;
+  Div by_tiles_head, by_prefix_nu;
   float scale;                  // of the scores, in log2 units
   // shared prefix: pages
   const int *page_table, *row_stream, *row_pos;
@@ -55,9 +91,22 @@ struct UnitArgs {
   int k_tokens_first, v_tokens_first;   // the map's middle dimension is the token, not the head
   // scratch
   int *err;                     // [0]: set when a wait ran out
-  int *plan;                    // shared: {units of a range, ranges with one more, running sums of units}; cross: an int4 a range
+  unsigned *tickets;            // zero between calls; null: the second kernel merges
+  int *plan;                    // ... which finds here {units of a range (a Div), running sums of units}
   float *part;
   int suffix_part0;             // partial row at which those of the rows' own tiles begin
+
+  void set_heads(int n_head, int n_kv_head, int tile = kUnTile) {
+    H = n_head; Hkv = n_kv_head; G = H / Hkv; rpt = tile / G;
+    by_G.set(G); by_rpt.set(rpt); by_H.set(H); by_Hkv.set(Hkv);
+    by_tiles_head.set(1); by_prefix_nu.set(1);
+  }
+  void set_shared(int pages) {
+    n_shared = pages;
+    tiles_head = pages > 0 ? (q_rows + rpt - 1) / rpt : 0;
+    prefix_nu = 2 * pages + 1;
+    by_tiles_head.set(tiles_head > 0 ? tiles_head : 1); by_prefix_nu.set(prefix_nu);
+  }
 };
 
 template <int KV> struct UnitLayout {
@@ -94,16 +143,77 @@ __device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t x) {
   return r;
 }
 
-// the range that unit u lies in: the first `rem` ranges have size + 1 units, the others size
-__device__ __forceinline__ int unit_range(int u, int size, int rem) {
-  const int t = rem * (size + 1);
-  return u < t ? u / (size + 1) : rem + (u - t) / size;
-}
 // First partial row of a part.  A tile's parts are numbered tile + range, which never repeats along the units; sequences, whose
 // tiles only meet where a range ends, have two places a range: for the tile that goes on behind it, and the one that began before.
 __device__ __forceinline__ size_t prefix_part(int tile, int range) { return (size_t)(tile + range) * kUnTile; }
 __device__ __forceinline__ size_t own_part(const UnitArgs &a, int row, int kvh, int range) { return (size_t)a.suffix_part0 + (size_t)(row * a.Hkv + kvh + range) * a.G; }
 __device__ __forceinline__ size_t seq_part(int range, bool begins) { return (size_t)(2 * range + (begins ? 1 : 0)) * kUnTile; }
+
+// The parts of a query row, added in the order of their keys by 8 PG lanes: lane group pg takes every PG-th part, a lane eight
+// dimensions.  part(p): the p-th of n partial rows.
+template <int PG, bool F16, typename Part>
+__device__ __forceinline__ void merge_parts(int n, Part part, uint16_t *out, bool store) {
+  const int sub = threadIdx.x & 7, pg = (threadIdx.x >> 3) & (PG - 1);
+  float M = -INFINITY, l = 0.f, acc[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) acc[c] = 0.f;
+  auto add = [&](float m, float pl, const float (&v)[8]) {
+    if (pl == 0.f) return;                     // no key in it; a sum that is NaN goes in
+    const float Mn = fmaxf(M, m), fo = M == Mn ? 1.f : pt_exp2(M - Mn), fn = pt_exp2(m - Mn);
+    M = Mn;
+    l = fmaf(l, fo, pl * fn);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[c] = fmaf(acc[c], fo, v[c] * fn);
+  };
+#pragma unroll 2
+  for (int p = pg; p < n; p += PG) {
+    const float *x = part(p);
+    const float2 ml = __ldcg(reinterpret_cast<const float2 *>(x + kHeadDim));
+    const float4 a = __ldcg(reinterpret_cast<const float4 *>(x + 8 * sub)), b = __ldcg(reinterpret_cast<const float4 *>(x + 8 * sub + 4));
+    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    add(ml.x, ml.y, v);
+  }
+#pragma unroll
+  for (int o = 8; o < 8 * PG; o <<= 1) {       // the groups' sums, the lower group's first
+    const float m2 = __shfl_down_sync(0xFFFFFFFFu, M, o), l2 = __shfl_down_sync(0xFFFFFFFFu, l, o);
+    float v[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] = __shfl_down_sync(0xFFFFFFFFu, acc[c], o);
+    add(m2, l2, v);
+  }
+  if (store && pg == 0) {
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    *reinterpret_cast<uint4 *>(out + 8 * sub) = make_uint4(un_pack<F16>(acc[0] * inv, acc[1] * inv), un_pack<F16>(acc[2] * inv, acc[3] * inv),
+                                                           un_pack<F16>(acc[4] * inv, acc[5] * inv), un_pack<F16>(acc[6] * inv, acc[7] * inv));
+  }
+}
+
+// Where the parts of a query row over a shared prefix are: those of its prefix tile, then those of its own keys.
+struct RowParts {
+  int p_n, o_n;
+  size_t pp, op;
+  __device__ __forceinline__ const float *at(const UnitArgs &a, int k) const {
+    return a.part + (k < p_n ? pp + (size_t)k * kUnTile : op + (size_t)(k - p_n) * a.G) * kUnPitch;
+  }
+};
+// size: units of a range; f0, f1: running sums of units of the row and of the next
+__device__ __forceinline__ RowParts row_parts(const UnitArgs &a, int r, int kvh, int gi, const Div &size, int f0, int f1) {
+  const int nu = f1 - f0;
+  RowParts x = {0, 0, 0, 0};
+  if (a.tiles_head > 0) {
+    const int row_tile = a.by_rpt.of(r), tile = kvh * a.tiles_head + row_tile, u0 = tile * a.prefix_nu, w0 = size.of(u0);
+    x.p_n = size.of(u0 + a.prefix_nu - 1) - w0 + 1;
+    x.pp = prefix_part(tile, w0) + (r - row_tile * a.rpt) * a.G + gi;
+  }
+  if (nu > 0) {
+    const int u0 = a.Hkv * (a.tiles_head * a.prefix_nu + f0) + kvh * nu, w0 = size.of(u0);
+    x.o_n = size.of(u0 + nu - 1) - w0 + 1;
+    x.op = own_part(a, r, kvh, w0) + gi;
+  }
+  return x;
+}
+
+template <int N> struct IntC { static constexpr int value = N; };
 
 // what a unit is; one per lane, 32 units at a time
 struct UnitDesc {
@@ -128,13 +238,16 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   int *first = reinterpret_cast<int *>(bars + kUnWarps * L::kStages);   // running sums of units: of a head of each row, or of all tiles of each sequence
   int *stream_s = first + (SHARED ? a.q_rows : a.n_seq) + 1;             // shared: the rows' streams
   __shared__ int warp_tot[kUnWarps];
+  __shared__ int4 tile_s[kUnMaxTiles];         // tiles whose parts this CTA may have to add: {first unit | own << 31, units, first row, heads and rows}
+  __shared__ int n_tile_s, n_item_s;
+  __shared__ Div size_s, aw_s;
   __shared__ unsigned long long lead_s;   // keys of the longest row, and that row: its list names the shared pages
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int n_items = SHARED ? a.q_rows : a.n_seq;
 
   if (lane < L::kStages) mbar_init(&bars[warp * L::kStages + lane], 1);
   if (tid == 0) {
-    lead_s = 0;
+    lead_s = 0; n_tile_s = 0; n_item_s = 0;
     if constexpr (KV != KV_E4M3) {
       asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
       if (!SHARED) asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
@@ -166,7 +279,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         int qb, qe, kb, ke;
         q_span(i, qb, qe);
         k_span(i, kb, ke);
-        u = a.Hkv * ((qe - qb + a.rpt - 1) / a.rpt) * (1 + (ke - kb + kUnKeys - 1) / kUnKeys);
+        u = a.Hkv * a.by_rpt.of(qe - qb + a.rpt - 1) * (1 + (ke - kb + kUnKeys - 1) / kUnKeys);
       }
     }
     int incl = u;
@@ -187,20 +300,24 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   if (tid == 0) first[n_items] = carry;
   __syncthreads();
   const int lead = (int)(lead_s & 0xFFFFFFFFu), lead_keys = (int)(lead_s >> 32);
-  const int tiles_head = SHARED && a.n_shared > 0 ? (a.q_rows + a.rpt - 1) / a.rpt : 0;   // prefix tiles of a head
-  const int prefix_nu = SHARED ? 2 * a.n_shared + 1 : 0;                                     // units of each of them
-  const int U_prefix = a.Hkv * tiles_head * prefix_nu;
+  const int tiles_head = SHARED ? a.tiles_head : 0, prefix_nu = a.prefix_nu;
+  const int U_prefix = SHARED ? a.Hkv * tiles_head * prefix_nu : 0;
   const int T = U_prefix + carry * (SHARED ? a.Hkv : 1);
-  // W ranges of at least two units; range j goes to CTA j % grid, so that few units reach every CTA
-  const int W = min((T + 1) / 2, (int)gridDim.x * kUnWarps), size = T / max(1, W), rem = T - size * W;
-  const int w = warp * gridDim.x + blockIdx.x;
-  const int u_begin = w * size + min(w, rem), n_mine = w < W ? size + (w < rem ? 1 : 0) : 0;
-  auto warp_of = [&](int u) { return unit_range(u, size, rem); };
-  if (SHARED && blockIdx.x == 0) {
-    for (int i = tid; i <= n_items; i += kUnWarps * 32) a.plan[2 + i] = first[i];
-    if (tid == 0) { a.plan[0] = size; a.plan[1] = rem; }
+  // ranges of `size` units, at least two; a CTA's are neighbours, `aw` of them, so that all CTAs have some
+  if (tid == 0) {
+    const int n = (int)gridDim.x * kUnWarps, units = max(2, (T + n - 1) / n), ranges = (T + units - 1) / units;
+    size_s.set(units);
+    aw_s.set(max(1, (ranges + (int)gridDim.x - 1) / (int)gridDim.x));
   }
-  if (!SHARED && lane == 0) reinterpret_cast<int4 *>(a.plan)[w] = make_int4(0, 0, 0, 0);
+  __syncthreads();
+  const Div size = size_s;
+  const int aw = aw_s.d, w_cta = blockIdx.x * aw, w = w_cta + warp;
+  const int u_begin = w * (int)size.d, n_mine = warp < aw ? min(max(T - u_begin, 0), (int)size.d) : 0;
+  auto warp_of = [&](int u) { return size.of(u); };
+  if (SHARED && !a.tickets && blockIdx.x == 0) {
+    for (int i = tid; i <= n_items; i += kUnWarps * 32) a.plan[sizeof(Div) / 4 + i] = first[i];
+    if (tid == 0) *reinterpret_cast<Div *>(a.plan) = size;
+  }
   pdl_launch_dependents();
 
   auto find = [&](int x) {   // last item that begins at or before x
@@ -214,8 +331,8 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
     if constexpr (SHARED) {
       int r, kvh, page, n, list, kk;            // unit 0 of a tile has no keys: it stands for what a tile costs besides them
       if (u < U_prefix) {
-        const int tile = u / prefix_nu, k = u - tile * prefix_nu;
-        kvh = tile / tiles_head;
+        const int tile = a.by_prefix_nu.of(u), k = u - tile * prefix_nu;
+        kvh = a.by_tiles_head.of(tile);
         r = (tile - kvh * tiles_head) * a.rpt;
         d.u0 = u - k; d.nu = prefix_nu;
         d.hn = kvh | (min(a.rpt, a.q_rows - r) * a.G << 16);
@@ -224,9 +341,9 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         n = min(kUnKeys, lead_keys - kk * kUnKeys);   // a page of the shared ones holds 64 keys, unless no row is that long
       } else {
         const int v = u - U_prefix;
-        r = find(v / a.Hkv);
+        r = find(a.by_Hkv.of(v));
         const int nu = first[r + 1] - first[r], x = v - first[r] * a.Hkv;
-        kvh = x / nu;
+        kvh = (int)((unsigned)x / (unsigned)nu);
         const int k = x - kvh * nu;
         d.u0 = u - k; d.nu = nu; d.own = 1;
         d.hn = kvh | (a.G << 16);
@@ -245,8 +362,8 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
       int qb, qe, kb, ke;
       q_span(s, qb, qe);
       k_span(s, kb, ke);
-      const int nu = 1 + (ke - kb + kUnKeys - 1) / kUnKeys, tile = x / nu, k = x - tile * nu;
-      const int blocks = (qe - qb + a.rpt - 1) / a.rpt, kvh = tile / blocks;
+      const int nu = 1 + (ke - kb + kUnKeys - 1) / kUnKeys, tile = (int)((unsigned)x / (unsigned)nu), k = x - tile * nu;
+      const int blocks = a.by_rpt.of(qe - qb + a.rpt - 1), kvh = (int)((unsigned)tile / (unsigned)blocks);
       d.row0 = qb + (tile - kvh * blocks) * a.rpt;
       d.u0 = u - k; d.nu = nu;
       d.hn = kvh | (min(a.rpt, qe - d.row0) * a.G << 16);
@@ -301,7 +418,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   int tile_u0 = -1, tile_nu = 0, row0 = 0, kvh = 0, n_i = 0, own = 0, vis0 = 0, vis1 = 0;
   bool whole = true, dead = false;
 
-  auto q_ptr = [&](int i) { return (size_t)(row0 + i / a.G) * a.q_stride + (size_t)(kvh * a.G + i % a.G) * kHeadDim; };
+  auto q_ptr = [&](int i) { const int r = a.by_G.of(i); return (size_t)(row0 + r) * a.q_stride + (size_t)((kvh - r) * a.G + i) * kHeadDim; };
   auto load_q = [&]() {
     const bool h0 = g < n_i, h1 = g + 8 < n_i;
     const size_t p0 = h0 ? q_ptr(g) : 0, p1 = h1 ? q_ptr(g + 8) : 0;
@@ -322,7 +439,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         }
       }
   };
-  auto out_ptr = [&](int i) { return a.out + ((size_t)(row0 + i / a.G) * a.H + kvh * a.G + i % a.G) * kHeadDim; };
+  auto out_ptr = [&](int i) { const int r = a.by_G.of(i); return a.out + ((size_t)(row0 + r) * a.H + (kvh - r) * a.G + i) * kHeadDim; };
 
   auto finish = [&]() {                       // the warp leaves its tile
     l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 1); l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 2);
@@ -355,7 +472,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
       return;
     }
     // this part into scratch
-    float *dst = a.part + (SHARED ? (own ? own_part(a, row0, kvh, w) : prefix_part(tile_u0 / max(1, prefix_nu), w)) : seq_part(w, w == w0)) * kUnPitch;
+    float *dst = a.part + (SHARED ? (own ? own_part(a, row0, kvh, w) : prefix_part(a.by_prefix_nu.of(tile_u0), w)) : seq_part(w, w == w0)) * kUnPitch;
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       if (g + 8 * e < n_i) {
@@ -371,252 +488,247 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         }
         if (t == 0) { p[64] = e ? m1 : m0; p[65] = e ? l1 : l0; }
       }
-    // the merge finds a cut tile at the range that begins it
-    if (!SHARED && w == w0 && lane == 0) reinterpret_cast<int4 *>(a.plan)[w] = make_int4(row0, kvh | (n_i << 16), w1 - w0 + 1, 0);
+    // the tile's first range of this CTA enters it
+    if (a.tickets && w == max(w0, w_cta) && lane == 0) {
+      const int i = atomicAdd(&n_tile_s, 1);
+      if (i < kUnMaxTiles) tile_s[i] = make_int4(tile_u0 | (own << 31), tile_nu, row0, kvh | (n_i << 16));
+    }
   };
 
   // turn i copies unit i and computes unit i - kStages, whose stage it frees; one place for each in the code, which is fetched cold
 #pragma unroll 1
   for (int turn = 0;; ++turn) {
     const int idx = turn - L::kStages;
-    if (idx < 0) {
-      if (turn < n_mine) issue(turn);
-      continue;
-    }
-    if ((idx & 31) == 0) cur = nxt;            // copies run a few units ahead: `nxt` still describes these
-    const bool end = idx >= n_mine;
-    const int u0 = end ? -2 : __shfl_sync(0xFFFFFFFFu, cur.u0, idx & 31), n = __shfl_sync(0xFFFFFFFFu, cur.n, idx & 31);
-    if (u0 != tile_u0) {
-      if (tile_u0 >= 0) finish();
-      if (end) break;
-      tile_u0 = u0;
-      tile_nu = __shfl_sync(0xFFFFFFFFu, cur.nu, idx & 31);
-      row0 = __shfl_sync(0xFFFFFFFFu, cur.row0, idx & 31);
-      const int hn = __shfl_sync(0xFFFFFFFFu, cur.hn, idx & 31);
-      own = __shfl_sync(0xFFFFFFFFu, cur.own, idx & 31);
-      kvh = hn & 0xffff; n_i = hn >> 16;
-      load_q();
-      whole = true;
-      if constexpr (SHARED) {
-        if (!own) {                            // a row may end inside the shared pages
-          vis0 = g < n_i ? a.row_pos[row0 + g / a.G] + 1 : prefix_keys;
-          vis1 = g + 8 < n_i ? a.row_pos[row0 + (g + 8) / a.G] + 1 : prefix_keys;
-          whole = __all_sync(0xFFFFFFFFu, vis0 >= prefix_keys && vis1 >= prefix_keys);
-        }
-      }
-      m0 = m1 = -INFINITY; l0 = l1 = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-    }
-    const int s = idx % L::kStages;
-    unsigned char *st = stage0 + (size_t)s * L::kStage;
-    if (!dead && !mbar_wait_bounded(&bar[s], (uint32_t)(idx / L::kStages) & 1u, kUnWaitNs)) {
-      atomicExch(a.err, 1);
-      dead = true;
-    }
-    dead = __any_sync(0xFFFFFFFFu, dead);
-    if (n > 0 && !dead) {
-      const uint32_t k_base = smem_u32(st), v_base = k_base + L::kHalf;
-      float sc[4][4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
-      if constexpr (KV == KV_E4M3) {
-        const float *ks = reinterpret_cast<const float *>(st + 2 * L::kHalf);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {          // eight keys: lane (g, t) holds dimensions 16 t .. 16 t + 15 of key g
-          const uint4 c = *reinterpret_cast<const uint4 *>(st + (8 * j + g) * kHeadDim + 16 * t);
-          const uint32_t cw[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-          for (int k4 = 0; k4 < 4; ++k4) {
-            const uint32_t b0 = e4m3x2_to_bf16x2(__byte_perm(cw[k4], 0u, 0x1404)), b1 = e4m3x2_to_bf16x2(__byte_perm(cw[k4], 0u, 0x3424));
-            un_mma<false>(sc[j], qa[k4], b0, b1);
-            if constexpr (QF32) un_mma<false>(sc[j], qlo[k4], b0, b1);
+    if (idx >= 0) {
+      if ((idx & 31) == 0) cur = nxt;            // copies run a few units ahead: `nxt` still describes these
+      const bool end = idx >= n_mine;
+      const int u0 = end ? -2 : __shfl_sync(0xFFFFFFFFu, cur.u0, idx & 31), n = __shfl_sync(0xFFFFFFFFu, cur.n, idx & 31);
+      if (u0 != tile_u0) {
+        if (tile_u0 >= 0) finish();
+        if (end) break;
+        tile_u0 = u0;
+        tile_nu = __shfl_sync(0xFFFFFFFFu, cur.nu, idx & 31);
+        row0 = __shfl_sync(0xFFFFFFFFu, cur.row0, idx & 31);
+        const int hn = __shfl_sync(0xFFFFFFFFu, cur.hn, idx & 31);
+        own = __shfl_sync(0xFFFFFFFFu, cur.own, idx & 31);
+        kvh = hn & 0xffff; n_i = hn >> 16;
+        load_q();
+        whole = true;
+        if constexpr (SHARED) {
+          if (!own) {                            // a row may end inside the shared pages
+            vis0 = g < n_i ? a.row_pos[row0 + a.by_G.of(g)] + 1 : prefix_keys;
+            vis1 = g + 8 < n_i ? a.row_pos[row0 + a.by_G.of(g + 8)] + 1 : prefix_keys;
+            whole = __all_sync(0xFFFFFFFFu, vis0 >= prefix_keys && vis1 >= prefix_keys);
           }
-          const float2 f = *reinterpret_cast<const float2 *>(ks + 8 * j + 2 * t);
-          sc[j][0] *= f.x; sc[j][1] *= f.y; sc[j][2] *= f.x; sc[j][3] *= f.y;
         }
-      } else {
-        // V rows without a key may hold NaN, and 0 * NaN must not reach O
-        if (n < kUnKeys) {
-          const int zero_to = min(kUnKeys, (n + kUnBox - 1) / kUnBox * kUnBox);
-          for (int i = n * 8 + lane; i < zero_to * 8; i += 32) *reinterpret_cast<uint4 *>(st + L::kHalf + i * 16) = make_uint4(0, 0, 0, 0);
-          __syncwarp();
+        m0 = m1 = -INFINITY; l0 = l1 = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+      }
+      const int s = idx % L::kStages;
+      unsigned char *st = stage0 + (size_t)s * L::kStage;
+      if (!dead && !mbar_wait_bounded(&bar[s], (uint32_t)(idx / L::kStages) & 1u, kUnWaitNs)) {
+        atomicExch(a.err, 1);
+        dead = true;
+      }
+      dead = __any_sync(0xFFFFFFFFu, dead);
+      if (n > 0 && !dead) {
+        const uint32_t k_base = smem_u32(st), v_base = k_base + L::kHalf;
+        float sc[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
+        if constexpr (KV == KV_E4M3) {
+          const float *ks = reinterpret_cast<const float *>(st + 2 * L::kHalf);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {          // eight keys: lane (g, t) holds dimensions 16 t .. 16 t + 15 of key g
+            const uint4 c = *reinterpret_cast<const uint4 *>(st + (8 * j + g) * kHeadDim + 16 * t);
+            const uint32_t cw[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int k4 = 0; k4 < 4; ++k4) {
+              const uint32_t b0 = e4m3x2_to_bf16x2(__byte_perm(cw[k4], 0u, 0x1404)), b1 = e4m3x2_to_bf16x2(__byte_perm(cw[k4], 0u, 0x3424));
+              un_mma<false>(sc[j], qa[k4], b0, b1);
+              if constexpr (QF32) un_mma<false>(sc[j], qlo[k4], b0, b1);
+            }
+            const float2 f = *reinterpret_cast<const float2 *>(ks + 8 * j + 2 * t);
+            sc[j][0] *= f.x; sc[j][1] *= f.y; sc[j][2] *= f.x; sc[j][3] *= f.y;
+          }
+        } else {
+          // V rows without a key may hold NaN, and 0 * NaN must not reach O
+          if (n < kUnKeys) {
+            const int zero_to = min(kUnKeys, (n + kUnBox - 1) / kUnBox * kUnBox);
+            for (int i = n * 8 + lane; i < zero_to * 8; i += 32) *reinterpret_cast<uint4 *>(st + L::kHalf + i * 16) = make_uint4(0, 0, 0, 0);
+            __syncwarp();
+          }
+#pragma unroll
+          for (int np = 0; np < 2; ++np) {
+            if (np * kUnBox >= n) break;
+            const int key = 16 * np + 8 * (lane >> 4) + (lane & 7);
+#pragma unroll
+            for (int k4 = 0; k4 < 4; ++k4) {
+              uint32_t f[4];
+              ldmatrix_x4(f, k_base + key * 128 + (((2 * k4 + ((lane >> 3) & 1)) ^ (key & 7)) << 4));
+              un_mma<F16>(sc[2 * np], qa[k4], f[0], f[1]);
+              un_mma<F16>(sc[2 * np + 1], qa[k4], f[2], f[3]);
+              if constexpr (QF32) {
+                un_mma<F16>(sc[2 * np], qlo[k4], f[0], f[1]);
+                un_mma<F16>(sc[2 * np + 1], qlo[k4], f[2], f[3]);
+              }
+            }
+          }
+        }
+        if (n < kUnKeys || !whole) {
+          const int k0 = (u_begin + idx - tile_u0 - 1) * kUnKeys;
+          const int lim0 = whole ? n : min(n, vis0 - k0), lim1 = whole ? n : min(n, vis1 - k0);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int c = 8 * j + 2 * t;
+            if (c >= lim0) sc[j][0] = -INFINITY;
+            if (c + 1 >= lim0) sc[j][1] = -INFINITY;
+            if (c >= lim1) sc[j][2] = -INFINITY;
+            if (c + 1 >= lim1) sc[j][3] = -INFINITY;
+          }
+        }
+        float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { x0 = fmaxf(x0, fmaxf(sc[j][0], sc[j][1])); x1 = fmaxf(x1, fmaxf(sc[j][2], sc[j][3])); }
+        x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 1)); x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2));
+        x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1)); x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
+        const float n0 = fmaxf(m0, x0 * a.scale), n1 = fmaxf(m1, x1 * a.scale);
+        const float r0 = n0 == -INFINITY ? 0.f : n0, r1 = n1 == -INFINITY ? 0.f : n1;   // a row that has seen nothing keeps -inf
+        const float f0 = pt_exp2(m0 - r0), f1 = pt_exp2(m1 - r1);
+        m0 = n0; m1 = n1;
+        float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          sc[j][0] = pt_exp2(fmaf(sc[j][0], a.scale, -r0)); sc[j][1] = pt_exp2(fmaf(sc[j][1], a.scale, -r0));
+          sc[j][2] = pt_exp2(fmaf(sc[j][2], a.scale, -r1)); sc[j][3] = pt_exp2(fmaf(sc[j][3], a.scale, -r1));
+          s0 += sc[j][0] + sc[j][1];
+          s1 += sc[j][2] + sc[j][3];
+        }
+        l0 = fmaf(l0, f0, s0); l1 = fmaf(l1, f1, s1);
+        if (__any_sync(0xFFFFFFFFu, f0 != 1.0f || f1 != 1.0f)) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
+        }
+        if constexpr (KV == KV_E4M3) {
+          const float *vs = reinterpret_cast<const float *>(st + 2 * L::kHalf + kUnKeys * 4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {          // the values' scales belong to P; a key that is none may have any
+            const float2 f = *reinterpret_cast<const float2 *>(vs + 8 * j + 2 * t);
+            const float fx = 8 * j + 2 * t < n ? f.x : 0.f, fy = 8 * j + 2 * t + 1 < n ? f.y : 0.f;
+            sc[j][0] *= fx; sc[j][1] *= fy; sc[j][2] *= fx; sc[j][3] *= fy;
+          }
         }
 #pragma unroll
         for (int np = 0; np < 2; ++np) {
           if (np * kUnBox >= n) break;
-          const int key = 16 * np + 8 * (lane >> 4) + (lane & 7);
+          const uint32_t pa[4] = {un_pack<F16>(sc[2 * np][0], sc[2 * np][1]), un_pack<F16>(sc[2 * np][2], sc[2 * np][3]),
+                                  un_pack<F16>(sc[2 * np + 1][0], sc[2 * np + 1][1]), un_pack<F16>(sc[2 * np + 1][2], sc[2 * np + 1][3])};
+          if constexpr (KV == KV_E4M3) {
+            const unsigned char *vp = st + L::kHalf + (16 * np + 2 * t) * kHeadDim + 8 * g;   // dimensions 8 g .. 8 g + 7 of four keys
+            const uint2 v0 = *reinterpret_cast<const uint2 *>(vp), v1 = *reinterpret_cast<const uint2 *>(vp + kHeadDim);
+            const uint2 v8 = *reinterpret_cast<const uint2 *>(vp + 8 * kHeadDim), v9 = *reinterpret_cast<const uint2 *>(vp + 9 * kHeadDim);
 #pragma unroll
-          for (int k4 = 0; k4 < 4; ++k4) {
-            uint32_t f[4];
-            ldmatrix_x4(f, k_base + key * 128 + (((2 * k4 + ((lane >> 3) & 1)) ^ (key & 7)) << 4));
-            un_mma<F16>(sc[2 * np], qa[k4], f[0], f[1]);
-            un_mma<F16>(sc[2 * np + 1], qa[k4], f[2], f[3]);
-            if constexpr (QF32) {
-              un_mma<F16>(sc[2 * np], qlo[k4], f[0], f[1]);
-              un_mma<F16>(sc[2 * np + 1], qlo[k4], f[2], f[3]);
+            for (int j = 0; j < 8; ++j) {        // byte j of the first key below, of the second above
+              constexpr uint32_t sel[4] = {0x4000, 0x5010, 0x6020, 0x7030};
+              const uint32_t b0 = e4m3x2_to_bf16x2(__byte_perm(j < 4 ? v0.x : v0.y, j < 4 ? v1.x : v1.y, sel[j & 3]));
+              const uint32_t b1 = e4m3x2_to_bf16x2(__byte_perm(j < 4 ? v8.x : v8.y, j < 4 ? v9.x : v9.y, sel[j & 3]));
+              un_mma<false>(o[j], pa, b0, b1);
+            }
+          } else {
+            const int key = 16 * np + 8 * ((lane >> 3) & 1) + (lane & 7);
+#pragma unroll
+            for (int dp = 0; dp < 4; ++dp) {
+              uint32_t f[4];
+              ldmatrix_x4_trans(f, v_base + key * 128 + (((2 * dp + (lane >> 4)) ^ (key & 7)) << 4));
+              un_mma<F16>(o[2 * dp], pa, f[0], f[1]);
+              un_mma<F16>(o[2 * dp + 1], pa, f[2], f[3]);
             }
           }
         }
       }
-      if (n < kUnKeys || !whole) {
-        const int k0 = (u_begin + idx - tile_u0 - 1) * kUnKeys;
-        const int lim0 = whole ? n : min(n, vis0 - k0), lim1 = whole ? n : min(n, vis1 - k0);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int c = 8 * j + 2 * t;
-          if (c >= lim0) sc[j][0] = -INFINITY;
-          if (c + 1 >= lim0) sc[j][1] = -INFINITY;
-          if (c >= lim1) sc[j][2] = -INFINITY;
-          if (c + 1 >= lim1) sc[j][3] = -INFINITY;
-        }
-      }
-      float x0 = -INFINITY, x1 = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) { x0 = fmaxf(x0, fmaxf(sc[j][0], sc[j][1])); x1 = fmaxf(x1, fmaxf(sc[j][2], sc[j][3])); }
-      x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 1)); x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2));
-      x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1)); x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
-      const float n0 = fmaxf(m0, x0 * a.scale), n1 = fmaxf(m1, x1 * a.scale);
-      const float r0 = n0 == -INFINITY ? 0.f : n0, r1 = n1 == -INFINITY ? 0.f : n1;   // a row that has seen nothing keeps -inf
-      const float f0 = pt_exp2(m0 - r0), f1 = pt_exp2(m1 - r1);
-      m0 = n0; m1 = n1;
-      float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        sc[j][0] = pt_exp2(fmaf(sc[j][0], a.scale, -r0)); sc[j][1] = pt_exp2(fmaf(sc[j][1], a.scale, -r0));
-        sc[j][2] = pt_exp2(fmaf(sc[j][2], a.scale, -r1)); sc[j][3] = pt_exp2(fmaf(sc[j][3], a.scale, -r1));
-        s0 += sc[j][0] + sc[j][1];
-        s1 += sc[j][2] + sc[j][3];
-      }
-      l0 = fmaf(l0, f0, s0); l1 = fmaf(l1, f1, s1);
-      if (__any_sync(0xFFFFFFFFu, f0 != 1.0f || f1 != 1.0f)) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
-      }
-      if constexpr (KV == KV_E4M3) {
-        const float *vs = reinterpret_cast<const float *>(st + 2 * L::kHalf + kUnKeys * 4);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {          // the values' scales belong to P; a key that is none may have any
-          const float2 f = *reinterpret_cast<const float2 *>(vs + 8 * j + 2 * t);
-          const float fx = 8 * j + 2 * t < n ? f.x : 0.f, fy = 8 * j + 2 * t + 1 < n ? f.y : 0.f;
-          sc[j][0] *= fx; sc[j][1] *= fy; sc[j][2] *= fx; sc[j][3] *= fy;
-        }
-      }
-#pragma unroll
-      for (int np = 0; np < 2; ++np) {
-        if (np * kUnBox >= n) break;
-        const uint32_t pa[4] = {un_pack<F16>(sc[2 * np][0], sc[2 * np][1]), un_pack<F16>(sc[2 * np][2], sc[2 * np][3]),
-                                un_pack<F16>(sc[2 * np + 1][0], sc[2 * np + 1][1]), un_pack<F16>(sc[2 * np + 1][2], sc[2 * np + 1][3])};
-        if constexpr (KV == KV_E4M3) {
-          const unsigned char *vp = st + L::kHalf + (16 * np + 2 * t) * kHeadDim + 8 * g;   // dimensions 8 g .. 8 g + 7 of four keys
-          const uint2 v0 = *reinterpret_cast<const uint2 *>(vp), v1 = *reinterpret_cast<const uint2 *>(vp + kHeadDim);
-          const uint2 v8 = *reinterpret_cast<const uint2 *>(vp + 8 * kHeadDim), v9 = *reinterpret_cast<const uint2 *>(vp + 9 * kHeadDim);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {        // byte j of the first key below, of the second above
-            constexpr uint32_t sel[4] = {0x4000, 0x5010, 0x6020, 0x7030};
-            const uint32_t b0 = e4m3x2_to_bf16x2(__byte_perm(j < 4 ? v0.x : v0.y, j < 4 ? v1.x : v1.y, sel[j & 3]));
-            const uint32_t b1 = e4m3x2_to_bf16x2(__byte_perm(j < 4 ? v8.x : v8.y, j < 4 ? v9.x : v9.y, sel[j & 3]));
-            un_mma<false>(o[j], pa, b0, b1);
-          }
-        } else {
-          const int key = 16 * np + 8 * ((lane >> 3) & 1) + (lane & 7);
-#pragma unroll
-          for (int dp = 0; dp < 4; ++dp) {
-            uint32_t f[4];
-            ldmatrix_x4_trans(f, v_base + key * 128 + (((2 * dp + (lane >> 4)) ^ (key & 7)) << 4));
-            un_mma<F16>(o[2 * dp], pa, f[0], f[1]);
-            un_mma<F16>(o[2 * dp + 1], pa, f[2], f[3]);
-          }
-        }
-      }
+      // every lane has read the stage: refill it
+      fence_proxy_async_smem();
+      __syncwarp();
     }
-    // every lane has read the stage: refill it
-    fence_proxy_async_smem();
-    __syncwarp();
     if (turn < n_mine && !dead) issue(turn);
   }
   if (dead) {   // copies of the warp may still be in flight, and none may land in a CTA that has left
     const unsigned long long t0 = global_timer_ns();
     while (global_timer_ns() - t0 <= 10000000ull) {}
   }
-}
-
-// The parts of a query row, added in the order of their keys by 8 PG lanes: lane group pg takes every PG-th part, a lane eight
-// dimensions.  part(p): the p-th of n partial rows.
-template <int PG, bool F16, typename Part>
-__device__ __forceinline__ void merge_parts(int n, Part part, uint16_t *out, bool store) {
-  const int sub = threadIdx.x & 7, pg = (threadIdx.x >> 3) & (PG - 1);
-  float M = -INFINITY, l = 0.f, acc[8];
-#pragma unroll
-  for (int c = 0; c < 8; ++c) acc[c] = 0.f;
-  auto add = [&](float m, float pl, const float (&v)[8]) {
-    if (pl == 0.f) return;                     // no key in it; a sum that is NaN goes in
-    const float Mn = fmaxf(M, m), fo = M == Mn ? 1.f : pt_exp2(M - Mn), fn = pt_exp2(m - Mn);
-    M = Mn;
-    l = fmaf(l, fo, pl * fn);
-#pragma unroll
-    for (int c = 0; c < 8; ++c) acc[c] = fmaf(acc[c], fo, v[c] * fn);
-  };
-#pragma unroll 2
-  for (int p = pg; p < n; p += PG) {
-    const float *x = part(p);
-    const float2 ml = __ldcg(reinterpret_cast<const float2 *>(x + kHeadDim));
-    const float4 a = __ldcg(reinterpret_cast<const float4 *>(x + 8 * sub)), b = __ldcg(reinterpret_cast<const float4 *>(x + 8 * sub + 4));
-    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    add(ml.x, ml.y, v);
-  }
-#pragma unroll
-  for (int o = 8; o < 8 * PG; o <<= 1) {       // the groups' sums, the lower group's first
-    const float m2 = __shfl_down_sync(0xFFFFFFFFu, M, o), l2 = __shfl_down_sync(0xFFFFFFFFu, l, o);
-    float v[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) v[c] = __shfl_down_sync(0xFFFFFFFFu, acc[c], o);
-    add(m2, l2, v);
-  }
-  if (store && pg == 0) {
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    *reinterpret_cast<uint4 *>(out + 8 * sub) = make_uint4(un_pack<F16>(acc[0] * inv, acc[1] * inv), un_pack<F16>(acc[2] * inv, acc[3] * inv),
-                                                           un_pack<F16>(acc[4] * inv, acc[5] * inv), un_pack<F16>(acc[6] * inv, acc[7] * inv));
+  if (a.tickets) {
+    __threadfence();
+    __syncthreads();
+    const int n_tile = min(n_tile_s, kUnMaxTiles);
+    int *item_s = reinterpret_cast<int *>(stages);   // query rows to be merged here: tile * 16 + row of the tile
+    static_assert(kUnMaxTiles * kUnTile * 4 <= kUnWarps * L::kStages * L::kStage, "over the stages, which nothing is copied into any more");
+    // ---- which rows are complete with this CTA's parts ----
+    auto ctas = [&](int u0, int nu) { return aw_s.of(warp_of(u0 + nu - 1)) - aw_s.of(warp_of(u0)) + 1; };   // that have units of a tile
+    for (int j = tid; j < n_tile * (SHARED ? kUnTile : 1); j += kUnWarps * 32) {
+      const int4 d = tile_s[SHARED ? j / kUnTile : j];
+      const int u0 = d.x & 0x7FFFFFFF, h = d.w & 0xffff, n = d.w >> 16;
+      int want = ctas(u0, d.y), i0 = 0, cnt = n;
+      unsigned *tk = a.tickets + warp_of(u0);   // a tile that reaches another CTA is the last one of its first range
+      bool there = true;
+      if constexpr (SHARED) {                   // a ticket for each row and group: its prefix tile's CTAs and its own
+        const int li = j & (kUnTile - 1), r = d.z + li;
+        there = li * a.G < n;
+        if (there) {
+          i0 = li * a.G; cnt = a.G;
+          const int nu = first[r + 1] - first[r];
+          if (d.x < 0) { if (tiles_head > 0) want += ctas((h * tiles_head + a.by_rpt.of(r)) * prefix_nu, prefix_nu); }
+          else if (nu > 0) want += ctas(U_prefix + first[r] * a.Hkv + h * nu, nu);
+          tk = a.tickets + (size_t)r * a.Hkv + h;
+        }
+      }
+      if (there) {
+        bool ready = want == 1;
+        if (!ready && atomicAdd(tk, 1u) + 1u == (unsigned)want) { ready = true; *tk = 0u; }
+        if (ready) {
+          const int at = atomicAdd(&n_item_s, cnt);
+          for (int i = 0; i < cnt; ++i) item_s[at + i] = (SHARED ? j / kUnTile : j) * kUnTile + i0 + i;
+        }
+      }
+    }
+    __threadfence();
+    __syncthreads();
+    // ---- and those are merged, by as many lanes each as there are ----
+    const int n_item = n_item_s;
+    const bool store = n_item > 0 && __ldcg(a.err) == 0;
+    auto merge = [&](auto pg_c, int item) {
+      constexpr int PG = decltype(pg_c)::value;
+      const bool real = item < n_item;
+      const int x = real ? item_s[item] : item_s[0], i = x & (kUnTile - 1);
+      const int4 d = tile_s[x / kUnTile];
+      const int h = d.w & 0xffff, li = a.by_G.of(i), r = d.z + li, gi = i - li * a.G;
+      uint16_t *dst = a.out + ((size_t)r * a.H + h * a.G + gi) * kHeadDim;
+      if constexpr (SHARED) {
+        const RowParts p = row_parts(a, r, h, gi, size, first[r], first[r + 1]);
+        merge_parts<PG, F16>(p.p_n + p.o_n, [&](int k) { return p.at(a, k); }, dst, real && store);
+      } else {
+        const int f = warp_of(d.x);
+        merge_parts<PG, F16>(warp_of(d.x + d.y - 1) - f + 1, [&](int k) { return a.part + (seq_part(f + k, k == 0) + i) * kUnPitch; }, dst, real && store);
+      }
+    };
+    if (n_item <= kUnWarps) { if (warp < n_item) merge(IntC<4>(), warp); }
+    else for (int it = warp * 4; it < n_item; it += kUnWarps * 4) merge(IntC<1>(), it + ((lane >> 3) & 3));
   }
 }
 
 constexpr int kMergeWarps = 8;
-// a warp per query row and head: the parts of the prefix tile, then those of the row's own keys
+// a warp per query row and head
 __global__ void __launch_bounds__(kMergeWarps * 32) merge_shared_kernel(const UnitArgs a) {
   pdl_wait();
   const int item = blockIdx.x * kMergeWarps + (threadIdx.x >> 5);
   if (item >= a.q_rows * a.H) return;          // whole warps
-  const int r = item / a.H, h = item - r * a.H, kvh = h / a.G, gi = h - kvh * a.G;
-  const int size = a.plan[0], rem = a.plan[1], f0 = a.plan[2 + r], nu = a.plan[3 + r] - f0;
-  const int tiles_head = a.n_shared > 0 ? (a.q_rows + a.rpt - 1) / a.rpt : 0, prefix_nu = 2 * a.n_shared + 1;
-  int p_n = 0, o_n = 0;
-  const float *pp = a.part, *op = a.part;
-  if (tiles_head > 0) {
-    const int tile = kvh * tiles_head + r / a.rpt, w0 = unit_range(tile * prefix_nu, size, rem);
-    p_n = unit_range(tile * prefix_nu + prefix_nu - 1, size, rem) - w0 + 1;
-    pp += (prefix_part(tile, w0) + (r % a.rpt) * a.G + gi) * kUnPitch;
-  }
-  if (nu > 0) {
-    const int u0 = a.Hkv * tiles_head * prefix_nu + f0 * a.Hkv + kvh * nu, w0 = unit_range(u0, size, rem);
-    o_n = unit_range(u0 + nu - 1, size, rem) - w0 + 1;
-    op += (own_part(a, r, kvh, w0) + gi) * kUnPitch;
-  }
-  if (p_n == 0 && o_n == 1) return;            // finished by its warp
-  merge_parts<4, false>(p_n + o_n, [&](int p) { return p < p_n ? pp + (size_t)p * kUnTile * kUnPitch : op + (size_t)(p - p_n) * a.G * kUnPitch; },
-                        a.out + ((size_t)r * a.H + h) * kHeadDim, *a.err == 0);
-}
-
-// four warps per range: the rows of the tile that begins in it and goes on behind it, four a warp
-template <bool F16>
-__global__ void __launch_bounds__(kMergeWarps * 32) merge_ranges_kernel(const UnitArgs a, int ranges) {
-  pdl_wait();
-  const int w = blockIdx.x * (kMergeWarps / 4) + (threadIdx.x >> 7);
-  if (w >= ranges) return;
-  const int4 c = __ldcg(reinterpret_cast<const int4 *>(a.plan) + w);
-  const int kvh = c.y & 0xffff, n_i = c.y >> 16, i = (threadIdx.x >> 3) & 15, ic = min(i, n_i - 1);
-  if (c.z == 0 || (i & ~3) >= n_i) return;     // whole warps
-  merge_parts<1, F16>(c.z, [&](int p) { return a.part + (seq_part(w + p, p == 0) + ic) * kUnPitch; },
-                      a.out + ((size_t)(c.x + ic / a.G) * a.H + kvh * a.G + ic % a.G) * kHeadDim, i < n_i && *a.err == 0);
+  const int r = a.by_H.of(item), h = item - r * a.H, kvh = a.by_G.of(h);
+  const int4 size4 = __ldcg(reinterpret_cast<const int4 *>(a.plan));   // the Div, and the first sum
+  const int f0 = __ldcg(a.plan + 3 + r), f1 = __ldcg(a.plan + 4 + r);
+  const Div size = {(uint32_t)size4.x, (uint32_t)size4.y, (uint32_t)size4.z};
+  const RowParts x = row_parts(a, r, kvh, h - kvh * a.G, size, f0, f1);
+  if (x.p_n == 0 && x.o_n == 1) return;        // finished by its warp
+  merge_parts<4, false>(x.p_n + x.o_n, [&](int p) { return x.at(a, p); }, a.out + ((size_t)r * a.H + h) * kHeadDim, __ldcg(a.err) == 0);
 }
 
 // partial rows of the shared form: prefix tiles (their number + ranges places of 16), then the rows' own (rows x heads + ranges
@@ -635,9 +747,8 @@ inline cudaError_t launch_units_as(const CUtensorMap &k_map, const CUtensorMap &
   const int grid = std::min(n_sm, kUnMaxCtas);
   if (const cudaError_t e = launch_kernel(attention_units_kernel<SHARED, KV, QF32>, dim3(grid), dim3(kUnWarps * 32),
                                           units_smem_bytes<KV>(SHARED ? a.q_rows : a.n_seq), st, false, k_map, v_map, a)) return e;
-  if (SHARED) return launch_kernel(merge_shared_kernel, dim3((a.q_rows * a.H + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), 0, st, true, a);
-  const int ranges = grid * kUnWarps;
-  return launch_kernel(merge_ranges_kernel<KV == KV_F16>, dim3((ranges + kMergeWarps / 4 - 1) / (kMergeWarps / 4)), dim3(kMergeWarps * 32), 0, st, true, a, ranges);
+  if (a.tickets) return cudaSuccess;
+  return launch_kernel(merge_shared_kernel, dim3((a.q_rows * a.H + kMergeWarps - 1) / kMergeWarps), dim3(kMergeWarps * 32), 0, st, true, a);
 }
 
 // The maps of K and V: 16 keys of one head a copy, with the 128-byte swizzle.  A pool of 16-bit pages: [64, 64 tokens, blocks].

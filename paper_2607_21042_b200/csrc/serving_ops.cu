@@ -6,7 +6,7 @@
 
 #include "host.cuh"
 #include "page_tables.cuh"
-#include "attention_units.cuh"
+#include "attention_tiles.cuh"
 
 using namespace ttsgpt;
 
@@ -18,9 +18,11 @@ namespace {
     if (e_ != cudaSuccess) return fail_op(TTS_GPT_E_CUDA, "%s: %s", #expr, cudaGetErrorString(e_));   \
   } while (0)
 
-// Scratch of the two attentions: [error word][plan][partial rows]; only the error word outlives a call.
-constexpr size_t kOpPlanBytes = align256(kUnMaxWarps * sizeof(int4) + (kUnMaxSeq + 3) * sizeof(int));
-constexpr size_t kOpHeaderBytes = 256 + kOpPlanBytes;
+// Scratch of the two attentions: [error word][tickets][plan][partial rows], the first three of the same size in every call, so
+// that calls of other sizes, of either kind, find the tickets at zero where the call before left them.
+constexpr size_t kOpTicketBytes = kUnTickets * sizeof(unsigned), kOpPlanBytes = align256((kUnMaxSeq + 4) * sizeof(int));
+constexpr size_t kOpHeaderBytes = 256 + kOpTicketBytes + kOpPlanBytes;
+static_assert(kUnTickets >= kUnMaxWarps && kUnTickets >= 4 * kTlMaxCtas && kUnTickets >= kUnMaxTiles * kUnMaxCtas, "a ticket per range, or per row and group of a call that merges itself");
 size_t scratch_bytes(long long part_rows) { return kOpHeaderBytes + (size_t)part_rows * kUnPitch * sizeof(float); }
 
 bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
@@ -106,22 +108,27 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
   // units of 32 keys are numbered in 31 bits, blocks of the pool too
   const int G = n_head / n_kv_head;
   const long long tiles = (long long)n_kv_head * ((R + kUnTile / G - 1) / (kUnTile / G));
-  if (pages_per_stream > (1 << 24) || tiles * (2ll * n_shared + 1) + (long long)R * n_kv_head * (2ll * (pages_per_stream - n_shared) + 1) >= (1ll << 31) ||
+  const long long units = tiles * (2ll * n_shared + 1) + (long long)R * n_kv_head * (2ll * (pages_per_stream - n_shared) + 1);
+  if (pages_per_stream > (1 << 24) || units >= (1ll << 31) ||
       2ll * n_pages * n_kv_head >= (1ll << 31))
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_shared: too many pages");
   if (scratch_size < scratch_bytes(shared_part_rows(R, n_kv_head, G)))
     return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_shared: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(shared_part_rows(R, n_kv_head, G)));
   UnitArgs a = {};
-  a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = R; a.H = n_head; a.Hkv = n_kv_head; a.G = G; a.rpt = kUnTile / G;
+  a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = R;
+  a.set_heads(n_head, n_kv_head);
+  a.set_shared(n_shared);
   a.scale = 0.125f * 1.4426950408889634f;
   a.page_table = page_table; a.row_stream = row_stream; a.row_pos = row_pos; a.pool = (const unsigned char *)kv_layer; a.pps = pages_per_stream;
-  a.n_shared = n_shared; a.n_pages = n_pages;
+  a.n_pages = n_pages;
   a.err = (int *)scratch;
-  a.plan = (int *)((char *)scratch + 256);
+  a.plan = (int *)((char *)scratch + 256 + kOpTicketBytes);
   a.part = (float *)((char *)scratch + kOpHeaderBytes);
   a.suffix_part0 = (int)shared_prefix_part_rows(R, n_kv_head, G);
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const int n_sm = device_sms();
+  // One kernel where no CTA can have more tiles than it has room to merge (at most a unit a range more than its share).
+  a.tickets = units <= (long long)(kUnMaxTiles - kUnWarps) * std::min(n_sm, kUnMaxCtas) ? (unsigned *)((char *)scratch + 256) : nullptr;
   CUtensorMap map = {};
   if (kv_fmt == TTS_GPT_KV_BF16) {
     OP_TRY(units_pool_map(&map, kv_layer, (size_t)n_pages * 2 * n_kv_head));
@@ -134,7 +141,7 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
 
 int32_t tts_gpt_op_attention_cross_scratch_bytes(size_t *bytes) {
   if (!bytes) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: null argument");
-  *bytes = scratch_bytes(cross_part_rows());
+  *bytes = scratch_bytes(std::max(cross_part_rows(), tiles_part_rows()));
   return TTS_GPT_OK;
 }
 
@@ -154,26 +161,37 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   if (n_kv_head > 1 && k_rows > 0 && (k_head_stride < kHeadDim || v_head_stride < kHeadDim)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: heads of K or V overlap");
   if (n > kUnMaxSeq) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: at most %d sequences", kUnMaxSeq);
   if (q_max > q_rows) q_max = q_rows;
-  const int G = n_head / n_kv_head, rpt = kUnTile / G;
+  const int G = n_head / n_kv_head;
+  const bool tiles = q_max * G > kUnTile && n <= kTlMaxSeq;
+  // units and blocks of keys are numbered in 31 bits
+  const int rpt = (tiles ? kTlRows : kUnTile) / G, keys = tiles ? kTlKeys : kUnKeys;
   const long long blocks = std::min((long long)n * ((q_max + rpt - 1) / rpt), (long long)q_rows / rpt + n);
-  if ((long long)n_kv_head * blocks * ((long long)k_rows / kUnKeys + 2) >= (1ll << 31) &&
-      (long long)n_kv_head * ((q_max + rpt - 1) / rpt) * ((long long)k_rows / kUnKeys + 2 * n) >= (1ll << 31))
+  if ((long long)n_kv_head * blocks * ((long long)k_rows / keys + 2) >= (1ll << 31) &&
+      (long long)n_kv_head * ((q_max + rpt - 1) / rpt) * ((long long)k_rows / keys + 2 * n) >= (1ll << 31))
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: too many queries times keys");
-  if (scratch_size < scratch_bytes(cross_part_rows()))
-    return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_cross: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(cross_part_rows()));
+  if (scratch_size < scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())))
+    return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_cross: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())));
   UnitArgs a = {};
-  a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = q_rows; a.H = n_head; a.Hkv = n_kv_head; a.G = G; a.rpt = rpt;
+  a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = q_rows;
+  a.set_heads(n_head, n_kv_head, tiles ? kTlRows : kUnTile);
   a.scale = scale * 1.4426950408889634f;
   a.q_start = q_start; a.k_start = k_start; a.n_seq = n; a.q_max = q_max; a.k_rows = k_rows;
   a.err = (int *)scratch;
-  a.plan = (int *)((char *)scratch + 256);
+  a.tickets = (unsigned *)((char *)scratch + 256);
   a.part = (float *)((char *)scratch + kOpHeaderBytes);
   CUtensorMap k_map = {}, v_map = {};
   const bool f16 = type == TTS_GPT_T_F16;
   if (k_rows > 0) {
-    OP_TRY(units_rows_map(&k_map, &a.k_tokens_first, f16, k, n_kv_head, k_rows, k_head_stride * 2, k_stride * 2, kUnBox));
-    OP_TRY(units_rows_map(&v_map, &a.v_tokens_first, f16, v, n_kv_head, k_rows, v_head_stride * 2, v_stride * 2, kUnBox));
+    OP_TRY(units_rows_map(&k_map, &a.k_tokens_first, f16, k, n_kv_head, k_rows, k_head_stride * 2, k_stride * 2, tiles ? kTlKeys : kUnBox));
+    OP_TRY(units_rows_map(&v_map, &a.v_tokens_first, f16, v, n_kv_head, k_rows, v_head_stride * 2, v_stride * 2, tiles ? kTlKeys : kUnBox));
   }
+  if (tiles && k_rows > 0) {
+    CUtensorMap q_map;
+    OP_TRY(tiles_q_map(&q_map, f16, q, n_head, q_rows, q_stride * 2, G, rpt));
+    OP_TRY((f16 ? launch_tiles_as<true> : launch_tiles_as<false>)(q_map, k_map, v_map, a, device_sms(), (cudaStream_t)cuda_stream));
+    return TTS_GPT_OK;
+  }
+  if (tiles) a.set_heads(n_head, n_kv_head);   // no keys at all: rows of zeros, from the kernel that needs no maps
   OP_TRY((f16 ? launch_units_as<false, KV_F16, false> : launch_units_as<false, KV_BF16, false>)(k_map, v_map, a, device_sms(), (cudaStream_t)cuda_stream));
   return TTS_GPT_OK;
 }
