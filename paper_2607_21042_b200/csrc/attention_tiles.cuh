@@ -20,14 +20,26 @@
 namespace ttsgpt {
 
 constexpr int kTlRows = 128, kTlKeys = 128;
-constexpr int kTlThreads = 192;             // warps 0-3: softmax, 4: copies, 5: products
+constexpr int kTlThreads = 256;             // warps 0-3: softmax, 4: copies, 5: products; 6 and 7 only give up their registers
+// Registers of a thread: 128 at launch (two CTAs of 256), of which the second four warps hand 88 each to the first four, whose rows'
+// 128 scores then stay in registers: 216 + 40 = 2 x 128.
+constexpr int kTlRegsSoftmax = 216, kTlRegsOthers = 40;
 constexpr int kTlHalf = kTlKeys * 128;      // K or V of a block: 16 KB
 constexpr int kTlRing = 4;                  // places for K and V blocks in turn
 constexpr int kTlMaxSeq = 2048;
 constexpr int kTlMaxCtas = 2 * kUnMaxCtas;
 constexpr float kTlSlack = 8.0f;            // log2 by which a score may exceed the reference
 
+// The part of a tile that lies in a CTA's range.
+struct TilePart {
+  int row0, n_i, kvh, u0, nu;     // first query row, rows times heads, head of keys; the tile's units
+  int j0, j1, key0, keys;         // its blocks here; first key row and number of keys of the sequence
+};
+constexpr int kTlParts = 4;       // that the copying warp is ahead at most
+
 struct TileShared {
+  TilePart part[kTlParts];
+  uint64_t part_full[kTlParts], part_free[kTlParts];
   uint64_t full[kTlRing], empty[kTlRing];   // K and V blocks
   uint64_t q_full[2], q_free[2];
   uint64_t s_full, s_free, p_full, pv_done;
@@ -38,11 +50,29 @@ struct TileShared {
 };
 inline size_t tiles_smem_bytes(int n) { return 1024 + (size_t)(kTlRing + 2) * kTlHalf + sizeof(TileShared) + (size_t)(n + 1) * sizeof(int); }
 
-// 32 lanes x 16 or 32 columns of 32 bits into tensor memory, of which the caller waits for all at once
-__device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const uint32_t (&v)[16]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
-                 "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+// 32 lanes x 32 columns of 32 bits out of and into tensor memory, several of which are waited for at once
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]),
+        "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]),
+        "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// no use of the registers moves ahead of this, which stands behind the wait
+__device__ __forceinline__ void tmem_landed32(float *v) {
+  asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]),
+               "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+               "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]));
+  asm volatile("" : "+f"(v[30]), "+f"(v[31]));
+}
+__device__ __forceinline__ void tmem_st32_async(uint32_t taddr, const float *v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]),
+        "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]),
+        "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31]) : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // A in tensor memory (row = lane, two 16-bit values of consecutive k a column), B in shared memory
@@ -66,8 +96,9 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
 
   if (tid == 0) {
     for (int i = 0; i < kTlRing; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_free[i], 1); }
-    mbar_init(&sh.s_full, 1); mbar_init(&sh.s_free, kTlRows); mbar_init(&sh.p_full, kTlRows); mbar_init(&sh.pv_done, 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_free[i], kTlRows / 32); }
+    for (int i = 0; i < kTlParts; ++i) { mbar_init(&sh.part_full[i], 1); mbar_init(&sh.part_free[i], 1 + kTlRows / 32); }
+    mbar_init(&sh.s_full, 1); mbar_init(&sh.s_free, kTlRows / 32); mbar_init(&sh.p_full, kTlRows / 32); mbar_init(&sh.pv_done, 1);
     sh.failed = 0;
   }
   if (warp == 4) {
@@ -121,13 +152,9 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
   const Div size = sh.size;
   const int u_begin = blockIdx.x * (int)size.d, u_end = min(T, u_begin + (int)size.d);
 
-  // the part of a tile that lies in this CTA's range, from unit u on
-  struct Part {
-    int row0, n_i, kvh, u0, nu;     // first query row, rows times heads, head of keys; the tile's units
-    int j0, j1, key0, keys;         // its blocks here; first key row and number of keys of the sequence
-  };
+  // from unit u on
   auto part_at = [&](int u) {
-    Part p;
+    TilePart p;
     int lo = 0, hi = a.n_seq - 1;
     while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (first[m] <= u) lo = m; else hi = m - 1; }
     int qb, qe, kb, ke;
@@ -145,7 +172,8 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
     return p;
   };
   auto wait = [&](uint64_t *bar, uint32_t parity) {   // the whole warp; false: some wait of the CTA has run out
-    if (mbar_try_wait(bar, parity)) return true;
+    for (int polls = 0; polls < 8; ++polls)    // the timer is read only where the wait is long
+      if (mbar_try_wait(bar, parity)) return true;
     const unsigned long long t0 = global_timer_ns();
     while (!mbar_try_wait(bar, parity)) {
       if (*failed) return false;
@@ -154,91 +182,112 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
     return true;
   };
   auto wait_warp = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait(bar, parity)) != 0; };
+  // part number n as the copying warp has described it; the reader's warp has it in registers when it gives the place back
+  auto take_part = [&](int n, TilePart &p) {
+    const int k = n % kTlParts;
+    if (!wait_warp(&sh.part_full[k], (uint32_t)(n / kTlParts) & 1u)) return false;
+    p = sh.part[k];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.part_free[k]);
+    return true;
+  };
 
-  if (warp == 4) {
-    // ---- copies: K and V blocks into the ring in turn, Q ahead of its first block ----
-    int slot = 0, n_tile = 0;                  // halves of blocks, and tiles with blocks, of this CTA
-    for (int u = u_begin; u < u_end;) {
-      const Part p = part_at(u);
-      u = p.u0 + p.j1 + 1;
-      if (p.j1 <= p.j0) continue;
-      const int qb = n_tile & 1;
-      if (n_tile >= 2 && !wait_warp(&sh.q_free[qb], (uint32_t)(n_tile / 2 - 1) & 1u)) break;
-      if (elect_one()) {
-        mbar_expect_tx(&sh.q_full[qb], (uint32_t)(a.rpt * a.G) * 128);
-        un_box(&q_map, p.kvh * a.G, p.row0, Qs + qb * kTlHalf, &sh.q_full[qb]);
-      }
-      __syncwarp();
-      ++n_tile;
-      bool fine = true;
-      for (int j = p.j0; j < p.j1 && fine; ++j)
-#pragma unroll
-        for (int h = 0; h < 2; ++h, ++slot) {
-          const int s = slot % kTlRing;
-          fine = fine && (slot < kTlRing || wait_warp(&sh.empty[s], (uint32_t)(slot / kTlRing - 1) & 1u));
-          if (!fine) break;
-          if (elect_one()) {
-            mbar_expect_tx(&sh.full[s], kTlHalf);
-            const int row = p.key0 + j * kTlKeys, tf = h ? a.v_tokens_first : a.k_tokens_first;
-            un_box(h ? &v_map : &k_map, tf ? row : p.kvh, tf ? p.kvh : row, ring + s * kTlHalf, &sh.full[s]);
-          }
-          __syncwarp();
-        }
-      if (!fine) break;
-    }
-  } else if (warp == 5) {
-    // ---- products: Q K^T of block i as soon as the softmax has read S of the block before, P V of block i - 1 behind it ----
-    const uint32_t kind = F16 ? ~((1u << 7) | (1u << 10)) : ~0u;
-    const uint32_t idesc_qk = tc_instr_desc(kTlRows, kTlKeys) & kind, idesc_pv = (tc_instr_desc(kTlRows, kHeadDim) & kind) | (1u << 16);   // V is MN-major
-    int i = 0, n_tile = 0;                     // blocks, and tiles with blocks, of this CTA
-    bool fine = true;
-    auto pv = [&](int blk, bool begins) {
-      const int s = (2 * blk + 1) % kTlRing;
-      fine = fine && wait_warp(&sh.full[s], (uint32_t)((2 * blk + 1) / kTlRing) & 1u) && wait_warp(&sh.p_full, (uint32_t)blk & 1u);
-      if (!fine) return;
-      tc_fence_after_sync();
-      const uint64_t dv = tc_smem_desc(ring + s * kTlHalf);
-      if (elect_one()) {
-#pragma unroll
-        for (int q = 0; q < kTlKeys / 16; ++q)   // 16 keys an instruction: 8 columns of P, two groups of 8 rows of V
-          tc_mma_ts(tmem + 192u, tmem + 128u + 8u * q, dv + 128 * q, idesc_pv, begins && q == 0 ? 0u : 1u);
-        tc_commit(&sh.pv_done);
-        tc_commit(&sh.empty[s]);
-      }
-      __syncwarp();
-    };
-    for (int u = u_begin; u < u_end && fine;) {
-      const Part p = part_at(u);
-      u = p.u0 + p.j1 + 1;
-      if (p.j1 <= p.j0) continue;
-      const int qb = n_tile & 1;
-      fine = wait_warp(&sh.q_full[qb], (uint32_t)(n_tile / 2) & 1u);
-      ++n_tile;
-      for (int j = p.j0; j < p.j1 && fine; ++j, ++i) {
-        const int s = (2 * i) % kTlRing;
-        fine = wait_warp(&sh.full[s], (uint32_t)((2 * i) / kTlRing) & 1u) && (i == 0 || wait_warp(&sh.s_free, (uint32_t)(i - 1) & 1u));
-        if (!fine) break;
-        tc_fence_after_sync();
-        const uint64_t dq = tc_smem_desc(Qs + qb * kTlHalf), dk = tc_smem_desc(ring + s * kTlHalf);
+  if (warp >= 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTlRegsOthers));
+    if (warp == 4) {
+      // ---- copies: K and V blocks into the ring in turn, Q ahead of its first block ----
+      int slot = 0, n_tile = 0, n_part = 0;      // halves of blocks, tiles with blocks, and parts of this CTA
+      for (int u = u_begin; u < u_end;) {
+        const TilePart p = part_at(u);
+        const int k = n_part % kTlParts;
+        if (n_part >= kTlParts && !wait_warp(&sh.part_free[k], (uint32_t)(n_part / kTlParts - 1) & 1u)) break;
+        if (lane == 0) { sh.part[k] = p; mbar_arrive(&sh.part_full[k]); }
+        __syncwarp();
+        ++n_part;
+        u = p.u0 + p.j1 + 1;
+        if (p.j1 <= p.j0) continue;
+        const int qb = n_tile & 1;
+        if (n_tile >= 2 && !wait_warp(&sh.q_free[qb], (uint32_t)(n_tile / 2 - 1) & 1u)) break;
         if (elect_one()) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) tc_mma(tmem, dq + 2 * q, dk + 2 * q, idesc_qk, q == 0 ? 0u : 1u);
-          tc_commit(&sh.s_full);
-          tc_commit(&sh.empty[s]);
-          if (j + 1 == p.j1) tc_commit(&sh.q_free[qb]);
+          mbar_expect_tx(&sh.q_full[qb], (uint32_t)(a.rpt * a.G) * 128);
+          un_box(&q_map, p.kvh * a.G, p.row0, Qs + qb * kTlHalf, &sh.q_full[qb]);
         }
         __syncwarp();
-        if (j > p.j0) pv(i - 1, j - 1 == p.j0);
+        ++n_tile;
+        bool fine = true;
+        for (int j = p.j0; j < p.j1 && fine; ++j)
+#pragma unroll
+          for (int h = 0; h < 2; ++h, ++slot) {
+            const int s = slot % kTlRing;
+            fine = fine && (slot < kTlRing || wait_warp(&sh.empty[s], (uint32_t)(slot / kTlRing - 1) & 1u));
+            if (!fine) break;
+            if (elect_one()) {
+              mbar_expect_tx(&sh.full[s], kTlHalf);
+              const int row = p.key0 + j * kTlKeys, tf = h ? a.v_tokens_first : a.k_tokens_first;
+              un_box(h ? &v_map : &k_map, tf ? row : p.kvh, tf ? p.kvh : row, ring + s * kTlHalf, &sh.full[s]);
+            }
+            __syncwarp();
+          }
+        if (!fine) break;
       }
-      if (fine) pv(i - 1, p.j1 - 1 == p.j0);   // the tile's last, ahead of the next tile's first S: O is read in between
+    } else if (warp == 5) {
+      // ---- products: Q K^T of block i as soon as the softmax has read S of the block before, P V of block i - 1 behind it ----
+      const uint32_t kind = F16 ? ~((1u << 7) | (1u << 10)) : ~0u;
+      const uint32_t idesc_qk = tc_instr_desc(kTlRows, kTlKeys) & kind, idesc_pv = (tc_instr_desc(kTlRows, kHeadDim) & kind) | (1u << 16);   // V is MN-major
+      int i = 0, n_tile = 0, n_part = 0;         // blocks, tiles with blocks, and parts of this CTA
+      bool fine = true;
+      auto pv = [&](int blk, bool begins) {
+        const int s = (2 * blk + 1) % kTlRing;
+        fine = fine && wait_warp(&sh.full[s], (uint32_t)((2 * blk + 1) / kTlRing) & 1u) && wait_warp(&sh.p_full, (uint32_t)blk & 1u);
+        if (!fine) return;
+        tc_fence_after_sync();
+        const uint64_t dv = tc_smem_desc(ring + s * kTlHalf);
+        if (elect_one()) {
+#pragma unroll
+          for (int q = 0; q < kTlKeys / 16; ++q)   // 16 keys an instruction: 8 columns of P, two groups of 8 rows of V
+            tc_mma_ts(tmem + 192u, tmem + 128u + 8u * q, dv + 128 * q, idesc_pv, begins && q == 0 ? 0u : 1u);
+          tc_commit(&sh.pv_done);
+          tc_commit(&sh.empty[s]);
+        }
+        __syncwarp();
+      };
+      for (int u = u_begin; u < u_end && fine;) {
+        TilePart p;
+        fine = take_part(n_part++, p);
+        if (!fine) break;
+        u = p.u0 + p.j1 + 1;
+        if (p.j1 <= p.j0) continue;
+        const int qb = n_tile & 1;
+        fine = wait_warp(&sh.q_full[qb], (uint32_t)(n_tile / 2) & 1u);
+        ++n_tile;
+        for (int j = p.j0; j < p.j1 && fine; ++j, ++i) {
+          const int s = (2 * i) % kTlRing;
+          fine = wait_warp(&sh.full[s], (uint32_t)((2 * i) / kTlRing) & 1u) && (i == 0 || wait_warp(&sh.s_free, (uint32_t)(i - 1) & 1u));
+          if (!fine) break;
+          tc_fence_after_sync();
+          const uint64_t dq = tc_smem_desc(Qs + qb * kTlHalf), dk = tc_smem_desc(ring + s * kTlHalf);
+          if (elect_one()) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) tc_mma(tmem, dq + 2 * q, dk + 2 * q, idesc_qk, q == 0 ? 0u : 1u);
+            tc_commit(&sh.s_full);
+            tc_commit(&sh.empty[s]);
+          }
+          __syncwarp();
+          if (j > p.j0) pv(i - 1, j - 1 == p.j0);
+        }
+        if (fine) pv(i - 1, p.j1 - 1 == p.j0);   // the tile's last, ahead of the next tile's first S: O is read in between
+      }
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTlRegsSoftmax));
     // ---- softmax ----
     const uint32_t t_lane = tmem + ((uint32_t)(32 * warp) << 16);
-    int i = 0;
+    int i = 0, n_tile = 0, n_part = 0;
     bool fine = true;
     for (int u = u_begin; u < u_end && fine;) {
-      const Part p = part_at(u);
+      TilePart p;
+      fine = take_part(n_part++, p);
+      if (!fine) break;
       u = p.u0 + p.j1 + 1;
       const bool live = 32 * warp < p.n_i, mine = tid < p.n_i;   // some row of the warp exists, the thread's own does
       float m = -INFINITY, l = 0.f;
@@ -247,24 +296,42 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
         if (!fine) break;
         tc_fence_after_sync();
         const int n = min(kTlKeys, p.keys - j * kTlKeys);
-        float sc = 1.f;
+        // all scores of the row into registers, so that the next block's may be computed behind the exponentials
+        float s[kTlKeys], sc = 1.f;
         if (live) {
+#pragma unroll
+          for (int c = 0; c < kTlKeys; c += 32) tmem_ld32_async(t_lane + (uint32_t)c, s + c);
+          tmem_wait_ld();
+#pragma unroll
+          for (int c = 0; c < kTlKeys; c += 32) tmem_landed32(s + c);
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.s_free);
+        if (live) {
+          if (n < kTlKeys) {
+#pragma unroll
+            for (int e = 0; e < kTlKeys; ++e) s[e] = e < n ? s[e] : -INFINITY;
+          }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int c = 0; c < kTlKeys; c += 32) {
-            float s[32];
-            tmem_ld32(t_lane + (uint32_t)c, s);
-            if (n < kTlKeys) {
+          for (int e = 0; e < kTlKeys; e += 8) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) s[e] = c + e < n ? s[e] : -INFINITY;
-            }
-#pragma unroll
-            for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], s[e]);
+            for (int q = 0; q < 4; ++q) mx[q] = fmaxf(mx[q], fmaxf(s[e + 2 * q], s[e + 2 * q + 1]));
           }
           const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale;
           if (m == -INFINITY) { sc = 0.f; m = top; }   // nothing seen yet; O, where there is one, is zero
           else if (top > m + kTlSlack) { sc = pt_exp2(m - top); m = top; }
           if (!mine) { sc = 1.f; m = 0.f; }            // a row that does not exist holds anything
+          const float ref = m == -INFINITY ? 0.f : m;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int e = 0; e < kTlKeys; e += 2) {
+            const float x = pt_exp2(fmaf(s[e], a.scale, -ref)), y = pt_exp2(fmaf(s[e + 1], a.scale, -ref));
+            sum[(e >> 1) & 3] += x + y;
+            s[e >> 1] = __uint_as_float(un_pack<F16>(x, y));
+          }
+          l = fmaf(l, sc, (sum[0] + sum[1]) + (sum[2] + sum[3]));
         }
         // P and O belong to the tensor core until P V of the block before has completed
         if (j > p.j0) {
@@ -283,38 +350,20 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
           }
         }
         if (live) {
-          const float ref = m == -INFINITY ? 0.f : m;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int c = 0; c < kTlKeys; c += 32) {
-            float s[32];
-            tmem_ld32(t_lane + (uint32_t)c, s);
-            if (n < kTlKeys) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) s[e] = c + e < n ? s[e] : -INFINITY;
-            }
-            uint32_t pk[16];
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float x = pt_exp2(fmaf(s[e], a.scale, -ref)), y = pt_exp2(fmaf(s[e + 1], a.scale, -ref));
-              sum[(e >> 1) & 3] += x + y;
-              pk[e >> 1] = un_pack<F16>(x, y);
-            }
-            tmem_st16_async(t_lane + 128u + (uint32_t)(c / 2), pk);
-          }
-          l = fmaf(l, sc, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+          for (int c = 0; c < kTlKeys / 2; c += 32) tmem_st32_async(t_lane + 128u + (uint32_t)c, s + c);
           tmem_wait_st();
         }
-        tc_fence_before_sync();
-        mbar_arrive(&sh.s_free);
         if (n < kTlKeys) {                     // the sequence's last block: V rows behind its keys may hold NaN, and 0 * NaN must not reach O
-          const int s = (2 * i + 1) % kTlRing;
-          fine = wait_warp(&sh.full[s], (uint32_t)((2 * i + 1) / kTlRing) & 1u);
+          const int sl = (2 * i + 1) % kTlRing;
+          fine = wait_warp(&sh.full[sl], (uint32_t)((2 * i + 1) / kTlRing) & 1u);
           if (!fine) break;
-          for (int x = n * 8 + tid; x < kTlKeys * 8; x += kTlRows) *reinterpret_cast<uint4 *>(ring + s * kTlHalf + x * 16) = make_uint4(0, 0, 0, 0);
+          for (int x = n * 8 + tid; x < kTlKeys * 8; x += kTlRows) *reinterpret_cast<uint4 *>(ring + sl * kTlHalf + x * 16) = make_uint4(0, 0, 0, 0);
           fence_proxy_async_smem();
         }
-        mbar_arrive(&sh.p_full);
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_full);
       }
       if (!fine) break;
       // ---- the tile's rows leave ----
@@ -332,16 +381,16 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
         tc_fence_before_sync();                // O may be overwritten once this thread's next P is announced
       }
       const int c0 = size.of(p.u0), c1 = size.of(p.u0 + p.nu - 1);
-      const int r = a.by_G.of(tid);
-      uint16_t *dst = a.out + ((size_t)(p.row0 + r) * a.H + (p.kvh - r) * a.G + tid) * kHeadDim;
       bool write = c0 == c1;
       if (!write) {
-        auto place = [&](int c) { return a.part + ((size_t)(2 * c + (c == c0)) * kTlRows + tid) * kUnPitch; };
+        // a place of 128 rows: 16 columns of four dimensions, then reference and sum; for the tile that goes on behind a CTA's range, and
+        // the one that began before
+        auto place = [&](int c) { return a.part + (size_t)(2 * c + (c == c0)) * kTlRows * kUnPitch; };
         if (mine) {
           float *x = place(blockIdx.x);
 #pragma unroll
-          for (int c = 0; c < kHeadDim; c += 4) *reinterpret_cast<float4 *>(x + c) = make_float4(o[c], o[c + 1], o[c + 2], o[c + 3]);
-          *reinterpret_cast<float2 *>(x + kHeadDim) = make_float2(m, l);
+          for (int c = 0; c < kHeadDim / 4; ++c) *reinterpret_cast<float4 *>(x + (c * kTlRows + tid) * 4) = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+          *reinterpret_cast<float2 *>(x + kTlRows * kHeadDim + 2 * tid) = make_float2(m, l);
         }
         // a ticket for each warp's 32 rows
         __threadfence();
@@ -361,26 +410,47 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
 #pragma unroll 1
           for (int c = c0; c <= c1; ++c) {
             const float *x = place(c);
-            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(x + kHeadDim));
-            if (ml.y == 0.f) continue;         // no key in it
-            const float mn = fmaxf(m, ml.x), fo = m == mn ? 1.f : pt_exp2(m - mn), fn = pt_exp2(ml.x - mn);
-            m = mn;
-            l = fmaf(l, fo, ml.y * fn);
+            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(x + kTlRows * kHeadDim + 2 * tid));
+            const float mn = fmaxf(m, ml.x), fo = m == mn ? 1.f : pt_exp2(m - mn), fn = ml.y == 0.f ? 0.f : pt_exp2(ml.x - mn);   // 0: no key in it
+            if (ml.y != 0.f) m = mn;
+            const float fk = ml.y != 0.f ? fo : 1.f;
+            l = fmaf(l, fk, ml.y * fn);
 #pragma unroll
-            for (int e = 0; e < kHeadDim; e += 4) {
-              const float4 v = __ldcg(reinterpret_cast<const float4 *>(x + e));
-              o[e] = fmaf(o[e], fo, v.x * fn); o[e + 1] = fmaf(o[e + 1], fo, v.y * fn);
-              o[e + 2] = fmaf(o[e + 2], fo, v.z * fn); o[e + 3] = fmaf(o[e + 3], fo, v.w * fn);
+            for (int e = 0; e < kHeadDim / 4; ++e) {
+              const float4 v = __ldcg(reinterpret_cast<const float4 *>(x + (e * kTlRows + tid) * 4));
+              o[4 * e] = fmaf(o[4 * e], fk, v.x * fn); o[4 * e + 1] = fmaf(o[4 * e + 1], fk, v.y * fn);
+              o[4 * e + 2] = fmaf(o[4 * e + 2], fk, v.z * fn); o[4 * e + 3] = fmaf(o[4 * e + 3], fk, v.w * fn);
             }
           }
         }
       }
-      if (write && mine && !*failed && __ldcg(a.err) == 0) {
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
+      write = write && !*failed && __ldcg(a.err) == 0;
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      auto row_ptr = [&](int i2) { const int r = a.by_G.of(i2); return a.out + ((size_t)(p.row0 + r) * a.H + (p.kvh - r) * a.G + i2) * kHeadDim; };
+      if (p.j1 > p.j0) {                       // through the tile's Q, which no product reads any more: whole 128-byte rows leave
+        const int qb = n_tile++ & 1;
+        unsigned char *stage = Qs + qb * kTlHalf;
+        if (write && live) {
+#pragma unroll
+          for (int c = 0; c < kHeadDim; c += 8)
+            *reinterpret_cast<uint4 *>(stage + tid * 128 + (((c >> 3) ^ (tid & 7)) << 4)) =
+                make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
+                           un_pack<F16>(o[c + 4] * inv, o[c + 5] * inv), un_pack<F16>(o[c + 6] * inv, o[c + 7] * inv));
+          __syncwarp();
+#pragma unroll
+          for (int it = 0; it < 8; ++it) {
+            const int r = 32 * warp + 4 * it + (lane >> 3), c8 = lane & 7;
+            if (r < p.n_i) *reinterpret_cast<uint4 *>(row_ptr(r) + 8 * c8) = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((c8 ^ (r & 7)) << 4));
+          }
+        }
+        fence_proxy_async_smem();              // Q of the tile after next is copied over it
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.q_free[qb]);
+      } else if (write && mine) {              // no block here, and no Q: zeros, or the sum of other CTAs' parts
 #pragma unroll
         for (int c = 0; c < kHeadDim; c += 8)
-          *reinterpret_cast<uint4 *>(dst + c) = make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
-                                                           un_pack<F16>(o[c + 4] * inv, o[c + 5] * inv), un_pack<F16>(o[c + 6] * inv, o[c + 7] * inv));
+          *reinterpret_cast<uint4 *>(row_ptr(tid) + c) = make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
+                                                                    un_pack<F16>(o[c + 4] * inv, o[c + 5] * inv), un_pack<F16>(o[c + 6] * inv, o[c + 7] * inv));
       }
     }
   }
