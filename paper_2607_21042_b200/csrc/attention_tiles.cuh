@@ -1,15 +1,16 @@
-// Attention of query tiles of 128 rows over blocks of 128 keys on the 5th-generation tensor cores: cross attention where a
+// Attention of query tiles of 256 rows over blocks of 128 keys on the 5th-generation tensor cores: cross attention where a
 // sequence has more queries than a tile of the warp-level kernel (Section I: the decode engine's attention kernels).
 //
-// A tile is 128 (row, head of the group) pairs of one sequence and one head of keys; thread t of the softmax warps owns row t =
-// accumulator lane t.  For each block of 128 keys
+// A tile is two halves of 128 (row, head of the group) pairs of one sequence and one head of keys; thread t of a half's four softmax
+// warps owns its row t = accumulator lane t.  For each block of 128 keys, which both halves read from one copy in shared memory,
 //     S = Q K^T     tcgen05.mma M=128 x N=128 x K=64, S (fp32) in tensor memory
 //     softmax       S out of tensor memory, running reference m and sum l in fp32, P = 2^(S scale - m) rounded to the inputs' type
 //                   back into tensor memory.  The reference moves, and O with it, only where a score exceeds it by 2^8: weights
 //                   stay below 256 and the rounding of a weight is relative, so nothing is lost
 //     O += P V      M=128 x N=64 x K=128, P as the operand in tensor memory, V as stored
-// S takes 128 columns, P 64 and O 64: half of an SM's tensor memory, so that two CTAs share an SM and one's softmax runs while
-// the other's products do.  What bounds it is the softmax's exponentials: 16384 of them a block, 16 a cycle and SM.
+// S takes 128 columns, P 64 and O 64 of each half: all of an SM's tensor memory.  One half's softmax runs while the other's products
+// do.  With 128 rows a CTA, two or four CTAs an SM, a block's copies alone took 1460 cycles of an SM (K and V came out of L2 for
+// every 128 rows, 6.2 TB/s); for 256 rows they are half of that, and the exponentials, 16 a cycle and SM, bound the kernel.
 //
 // Work split.  The blocks of all tiles are laid end to end and cut into one range a CTA, equal to within a block; a tile counts
 // one block more than its keys have.  The parts of a tile that several CTAs share meet as in the warp-level kernel: in scratch,
@@ -19,15 +20,18 @@
 
 namespace ttsgpt {
 
-constexpr int kTlRows = 128, kTlKeys = 128;
-constexpr int kTlThreads = 256;             // warps 0-3: softmax, 4: copies, 5: products; 6 and 7 only give up their registers
-// Registers of a thread: 128 at launch (two CTAs of 256), of which the second four warps hand 88 each to the first four, whose rows'
-// 128 scores then stay in registers: 216 + 40 = 2 x 128.
-constexpr int kTlRegsSoftmax = 216, kTlRegsOthers = 40;
+constexpr int kTlRows = 128, kTlKeys = 128;   // rows of a half tile, keys of a block
+constexpr int kTlTile = 2 * kTlRows;
+constexpr int kTlThreads = 384;             // warps 0-3 and 4-7: softmax of a half, 8: copies, 9: products; 10 and 11 only give up their registers
+// Registers of a thread: 168 at launch, of which the last four warps hand 96 each to the first eight, whose rows' 128 scores then
+// stay in registers: 256 x 216 + 128 x 72 = 384 x 168.
+constexpr int kTlRegsSoftmax = 216, kTlRegsOthers = 72;
 constexpr int kTlHalf = kTlKeys * 128;      // K or V of a block: 16 KB
-constexpr int kTlRing = 4;                  // places for K and V blocks in turn
+constexpr int kTlBlock = 2 * kTlHalf;       // both
+constexpr int kTlRing = 4;                  // places for blocks
+constexpr int kTlQ = kTlTile * 128;         // Q of a tile: 32 KB
 constexpr int kTlMaxSeq = 2048;
-constexpr int kTlMaxCtas = 2 * kUnMaxCtas;
+constexpr int kTlMaxCtas = kUnMaxCtas;
 constexpr float kTlSlack = 8.0f;            // log2 by which a score may exceed the reference
 
 // The part of a tile that lies in a CTA's range.
@@ -40,15 +44,15 @@ constexpr int kTlParts = 4;       // that the copying warp is ahead at most
 struct TileShared {
   TilePart part[kTlParts];
   uint64_t part_full[kTlParts], part_free[kTlParts];
-  uint64_t full[kTlRing], empty[kTlRing];   // K and V blocks
+  uint64_t full[kTlRing], empty[kTlRing];   // blocks
   uint64_t q_full[2], q_free[2];
-  uint64_t s_full, s_free, p_full, pv_done;
+  uint64_t s_full[2], s_free[2], p_full[2], pv_done[2];   // by half
   uint32_t tmem;
   int failed;
   Div size;
   int warp_tot[kTlThreads / 32];
 };
-inline size_t tiles_smem_bytes(int n) { return 1024 + (size_t)(kTlRing + 2) * kTlHalf + sizeof(TileShared) + (size_t)(n + 1) * sizeof(int); }
+inline size_t tiles_smem_bytes(int n) { return 1024 + (size_t)kTlRing * kTlBlock + 2 * kTlQ + sizeof(TileShared) + (size_t)(n + 1) * sizeof(int); }
 
 // 32 lanes x 32 columns of 32 bits out of and into tensor memory, several of which are waited for at once
 __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float *v) {
@@ -74,6 +78,11 @@ __device__ __forceinline__ void tmem_st32_async(uint32_t taddr, const float *v) 
         "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]),
         "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31]) : "memory");
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // A in tensor memory (row = lane, two 16-bit values of consecutive k a column), B in shared memory
 __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -84,28 +93,28 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint
 }
 
 template <bool F16>
-__global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+__global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                                                                         const __grid_constant__ CUtensorMap v_map, const UnitArgs a) {
   extern __shared__ __align__(16) unsigned char tl_smem_raw[];
   unsigned char *base = tl_smem_raw + ((1024u - (smem_u32(tl_smem_raw) & 1023u)) & 1023u);
-  unsigned char *ring = base, *Qs = base + kTlRing * kTlHalf;      // [2] 128 rows x 64 values, K-major, 128-byte swizzle
-  TileShared &sh = *reinterpret_cast<TileShared *>(Qs + 2 * kTlHalf);
+  unsigned char *ring = base, *Qs = base + kTlRing * kTlBlock;      // [2] 256 rows x 64 values, K-major, 128-byte swizzle
+  TileShared &sh = *reinterpret_cast<TileShared *>(Qs + 2 * kTlQ);
   int *first = reinterpret_cast<int *>(&sh + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int *failed = &sh.failed;
 
   if (tid == 0) {
     for (int i = 0; i < kTlRing; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_free[i], kTlRows / 32); }
-    for (int i = 0; i < kTlParts; ++i) { mbar_init(&sh.part_full[i], 1); mbar_init(&sh.part_free[i], 1 + kTlRows / 32); }
-    mbar_init(&sh.s_full, 1); mbar_init(&sh.s_free, kTlRows / 32); mbar_init(&sh.p_full, kTlRows / 32); mbar_init(&sh.pv_done, 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_free[i], kTlTile / 32); }
+    for (int i = 0; i < kTlParts; ++i) { mbar_init(&sh.part_full[i], 1); mbar_init(&sh.part_free[i], 1 + kTlTile / 32); }
+    for (int h = 0; h < 2; ++h) { mbar_init(&sh.s_full[h], 1); mbar_init(&sh.s_free[h], kTlRows / 32); mbar_init(&sh.p_full[h], kTlRows / 32); mbar_init(&sh.pv_done[h], 1); }
     sh.failed = 0;
   }
-  if (warp == 4) {
+  if (warp == 8) {
     if (lane < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &q_map : lane == 1 ? &k_map : &v_map) : "memory");
     __syncwarp();
   }
-  if (warp == 5) tmem_alloc(&sh.tmem, 256);   // S: columns 0 .. 127, P: 128 .. 191, O: 192 .. 255
+  if (warp == 9) tmem_alloc(&sh.tmem, 512);   // half h, from column 256 h on: S 128 columns, P 64, O 64
   // ---- running sums of blocks over the sequences ----
   auto q_span = [&](int i, int &b, int &e) {
     b = min(max(a.q_start[i], 0), a.q_rows);
@@ -172,12 +181,15 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
     return p;
   };
   auto wait = [&](uint64_t *bar, uint32_t parity) {   // the whole warp; false: some wait of the CTA has run out
-    for (int polls = 0; polls < 8; ++polls)    // the timer is read only where the wait is long
-      if (mbar_try_wait(bar, parity)) return true;
-    const unsigned long long t0 = global_timer_ns();
-    while (!mbar_try_wait(bar, parity)) {
+    if (mbar_try_wait(bar, parity)) return true;
+    unsigned long long t0 = 0;
+#pragma unroll 1
+    for (int polls = 1; !mbar_try_wait(bar, parity); ++polls) {
+      if (polls & 15) continue;                // the timer is read only where the wait is long
       if (*failed) return false;
-      if (global_timer_ns() - t0 > kUnWaitNs) { *failed = 1; atomicExch(a.err, 1); return false; }
+      const unsigned long long t1 = global_timer_ns();
+      if (t0 == 0) t0 = t1;
+      if (t1 - t0 > kUnWaitNs) { *failed = 1; atomicExch(a.err, 1); return false; }
     }
     return true;
   };
@@ -192,11 +204,11 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
     return true;
   };
 
-  if (warp >= 4) {
+  if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTlRegsOthers));
-    if (warp == 4) {
+    if (warp == 8) {
       // ---- copies: K and V blocks into the ring in turn, Q ahead of its first block ----
-      int slot = 0, n_tile = 0, n_part = 0;      // halves of blocks, tiles with blocks, and parts of this CTA
+      int slot = 0, n_tile = 0, n_part = 0;      // blocks, tiles with blocks, and parts of this CTA
       for (int u = u_begin; u < u_end;) {
         const TilePart p = part_at(u);
         const int k = n_part % kTlParts;
@@ -209,47 +221,53 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
         const int qb = n_tile & 1;
         if (n_tile >= 2 && !wait_warp(&sh.q_free[qb], (uint32_t)(n_tile / 2 - 1) & 1u)) break;
         if (elect_one()) {
-          mbar_expect_tx(&sh.q_full[qb], (uint32_t)(a.rpt * a.G) * 128);
-          un_box(&q_map, p.kvh * a.G, p.row0, Qs + qb * kTlHalf, &sh.q_full[qb]);
+          const int rows = a.rpt >> 1;         // of a half
+          mbar_expect_tx(&sh.q_full[qb], (uint32_t)(rows * a.G) * (p.n_i > rows * a.G ? 256 : 128));
+          un_box(&q_map, p.kvh * a.G, p.row0, Qs + qb * kTlQ, &sh.q_full[qb]);
+          if (p.n_i > rows * a.G) un_box(&q_map, p.kvh * a.G, p.row0 + rows, Qs + qb * kTlQ + kTlHalf, &sh.q_full[qb]);
         }
         __syncwarp();
         ++n_tile;
         bool fine = true;
-        for (int j = p.j0; j < p.j1 && fine; ++j)
-#pragma unroll
-          for (int h = 0; h < 2; ++h, ++slot) {
-            const int s = slot % kTlRing;
-            fine = fine && (slot < kTlRing || wait_warp(&sh.empty[s], (uint32_t)(slot / kTlRing - 1) & 1u));
-            if (!fine) break;
-            if (elect_one()) {
-              mbar_expect_tx(&sh.full[s], kTlHalf);
-              const int row = p.key0 + j * kTlKeys, tf = h ? a.v_tokens_first : a.k_tokens_first;
-              un_box(h ? &v_map : &k_map, tf ? row : p.kvh, tf ? p.kvh : row, ring + s * kTlHalf, &sh.full[s]);
-            }
-            __syncwarp();
+        for (int j = p.j0; j < p.j1 && fine; ++j, ++slot) {
+          const int s = slot % kTlRing;
+          fine = slot < kTlRing || wait_warp(&sh.empty[s], (uint32_t)(slot / kTlRing - 1) & 1u);
+          if (!fine) break;
+          if (elect_one()) {
+            mbar_expect_tx(&sh.full[s], kTlBlock);
+            un_box(&k_map, p.key0 + j * kTlKeys, p.kvh, ring + s * kTlBlock, &sh.full[s]);
+            un_box(&v_map, p.key0 + j * kTlKeys, p.kvh, ring + s * kTlBlock + kTlHalf, &sh.full[s]);
           }
+          __syncwarp();
+        }
         if (!fine) break;
       }
-    } else if (warp == 5) {
-      // ---- products: Q K^T of block i as soon as the softmax has read S of the block before, P V of block i - 1 behind it ----
+    } else if (warp == 9) {
+      // ---- products: of either half in turn Q K^T of block i, as soon as its softmax has read S of the block before, and P V of
+      //      block i - 1 behind it ----
       const uint32_t kind = F16 ? ~((1u << 7) | (1u << 10)) : ~0u;
       const uint32_t idesc_qk = tc_instr_desc(kTlRows, kTlKeys) & kind, idesc_pv = (tc_instr_desc(kTlRows, kHeadDim) & kind) | (1u << 16);   // V is MN-major
-      int i = 0, n_tile = 0, n_part = 0;         // blocks, tiles with blocks, and parts of this CTA
+      int n_tile = 0, n_part = 0;                // tiles with blocks, and parts of this CTA
       bool fine = true;
-      auto pv = [&](int blk, bool begins) {
-        const int s = (2 * blk + 1) % kTlRing;
-        fine = fine && wait_warp(&sh.full[s], (uint32_t)((2 * blk + 1) / kTlRing) & 1u) && wait_warp(&sh.p_full, (uint32_t)blk & 1u);
+      const uint64_t dring = tc_smem_desc(ring);
+      int done[2] = {0, 0}, n_block = 0;       // blocks of either half that have had their P V, blocks of the CTA
+      // P V of the block that half h has come to, block b of the CTA; last: no other half reads that block any more
+      auto pv = [&](int h, int b, bool begins, bool last) {
+        fine = fine && wait_warp(&sh.p_full[h], (uint32_t)done[h] & 1u);
         if (!fine) return;
         tc_fence_after_sync();
-        const uint64_t dv = tc_smem_desc(ring + s * kTlHalf);
+        const int s = b % kTlRing;
+        const uint64_t dv = dring + (uint64_t)((s * kTlBlock + kTlHalf) >> 4);
+        const uint32_t t = tmem + 256u * h;
         if (elect_one()) {
 #pragma unroll
           for (int q = 0; q < kTlKeys / 16; ++q)   // 16 keys an instruction: 8 columns of P, two groups of 8 rows of V
-            tc_mma_ts(tmem + 192u, tmem + 128u + 8u * q, dv + 128 * q, idesc_pv, begins && q == 0 ? 0u : 1u);
-          tc_commit(&sh.pv_done);
-          tc_commit(&sh.empty[s]);
+            tc_mma_ts(t + 192u, t + 128u + 8u * q, dv + 128 * q, idesc_pv, begins && q == 0 ? 0u : 1u);
+          tc_commit(&sh.pv_done[h]);
+          if (last) tc_commit(&sh.empty[s]);
         }
         __syncwarp();
+        ++done[h];
       };
       for (int u = u_begin; u < u_end && fine;) {
         TilePart p;
@@ -257,42 +275,54 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
         if (!fine) break;
         u = p.u0 + p.j1 + 1;
         if (p.j1 <= p.j0) continue;
-        const int qb = n_tile & 1;
+        const int qb = n_tile & 1, halves = p.n_i > (a.rpt >> 1) * a.G ? 2 : 1;
         fine = wait_warp(&sh.q_full[qb], (uint32_t)(n_tile / 2) & 1u);
         ++n_tile;
-        for (int j = p.j0; j < p.j1 && fine; ++j, ++i) {
-          const int s = (2 * i) % kTlRing;
-          fine = wait_warp(&sh.full[s], (uint32_t)((2 * i) / kTlRing) & 1u) && (i == 0 || wait_warp(&sh.s_free, (uint32_t)(i - 1) & 1u));
-          if (!fine) break;
-          tc_fence_after_sync();
-          const uint64_t dq = tc_smem_desc(Qs + qb * kTlHalf), dk = tc_smem_desc(ring + s * kTlHalf);
-          if (elect_one()) {
+        const uint64_t dq = tc_smem_desc(Qs + qb * kTlQ);
+        for (int j = p.j0; j < p.j1 && fine; ++j, ++n_block) {
+          fine = wait_warp(&sh.full[n_block % kTlRing], (uint32_t)(n_block / kTlRing) & 1u);
+          const uint64_t dk = dring + (uint64_t)((n_block % kTlRing * kTlBlock) >> 4);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) tc_mma(tmem, dq + 2 * q, dk + 2 * q, idesc_qk, q == 0 ? 0u : 1u);
-            tc_commit(&sh.s_full);
-            tc_commit(&sh.empty[s]);
+          for (int h = 0; h < 2; ++h) {
+            if (h == halves || !fine) break;
+            const int before = done[h] + (j > p.j0);   // blocks of this half whose S has been computed
+            fine = before == 0 || wait_warp(&sh.s_free[h], (uint32_t)(before - 1) & 1u);
+            if (!fine) break;
+            tc_fence_after_sync();
+            if (elect_one()) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) tc_mma(tmem + 256u * h, dq + (uint64_t)(h * (kTlHalf >> 4) + 2 * q), dk + 2 * q, idesc_qk, q == 0 ? 0u : 1u);
+              tc_commit(&sh.s_full[h]);
+            }
+            __syncwarp();
+            if (j > p.j0) pv(h, n_block - 1, j - 1 == p.j0, h + 1 == halves);
           }
-          __syncwarp();
-          if (j > p.j0) pv(i - 1, j - 1 == p.j0);
         }
-        if (fine) pv(i - 1, p.j1 - 1 == p.j0);   // the tile's last, ahead of the next tile's first S: O is read in between
+        for (int h = 0; h < halves && fine; ++h) pv(h, n_block - 1, p.j1 - 1 == p.j0, h + 1 == halves);   // the tile's last
       }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTlRegsSoftmax));
     // ---- softmax ----
-    const uint32_t t_lane = tmem + ((uint32_t)(32 * warp) << 16);
-    int i = 0, n_tile = 0, n_part = 0;
+    const int half = warp >> 2, quarter = warp & 3, t = tid & (kTlRows - 1);   // the thread's row of the half
+    const uint32_t t_lane = tmem + ((uint32_t)(32 * quarter) << 16) + 256u * half;
+    int i = 0, n_block = 0, n_tile = 0, n_part = 0;   // blocks of this half and of the CTA, tiles with blocks, parts
     bool fine = true;
     for (int u = u_begin; u < u_end && fine;) {
       TilePart p;
       fine = take_part(n_part++, p);
       if (!fine) break;
       u = p.u0 + p.j1 + 1;
-      const bool live = 32 * warp < p.n_i, mine = tid < p.n_i;   // some row of the warp exists, the thread's own does
+      const int n_half = (a.rpt >> 1) * a.G, n_i = min(p.n_i - half * n_half, n_half);   // rows of this half, none where not positive
+      const bool live = 32 * quarter < n_i, mine = t < n_i;   // some row of the warp exists, the thread's own does
+      const int blocks = n_i > 0 ? p.j1 : p.j0;
+      if (n_i <= 0 && p.j1 > p.j0) {           // no such half here: no block holds it back, but it gives Q back below, once for each Q
+        fine = wait_warp(&sh.q_full[n_tile & 1], (uint32_t)(n_tile / 2) & 1u);
+        if (!fine) break;
+      }
       float m = -INFINITY, l = 0.f;
-      for (int j = p.j0; j < p.j1; ++j, ++i) {
-        fine = wait_warp(&sh.s_full, (uint32_t)i & 1u);
+      for (int j = p.j0; j < blocks; ++j, ++i) {
+        fine = wait_warp(&sh.s_full[half], (uint32_t)i & 1u);
         if (!fine) break;
         tc_fence_after_sync();
         const int n = min(kTlKeys, p.keys - j * kTlKeys);
@@ -307,9 +337,9 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.s_free);
+        if (lane == 0) mbar_arrive(&sh.s_free[half]);
         if (live) {
-          if (n < kTlKeys) {
+          if (n < kTlKeys) {                   // scores of keys that do not exist
 #pragma unroll
             for (int e = 0; e < kTlKeys; ++e) s[e] = e < n ? s[e] : -INFINITY;
           }
@@ -317,25 +347,30 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
 #pragma unroll
           for (int e = 0; e < kTlKeys; e += 8) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) mx[q] = fmaxf(mx[q], fmaxf(s[e + 2 * q], s[e + 2 * q + 1]));
+            for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], s[e + 2 * q], s[e + 2 * q + 1]);
           }
           const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale;
           if (m == -INFINITY) { sc = 0.f; m = top; }   // nothing seen yet; O, where there is one, is zero
           else if (top > m + kTlSlack) { sc = pt_exp2(m - top); m = top; }
           if (!mine) { sc = 1.f; m = 0.f; }            // a row that does not exist holds anything
           const float ref = m == -INFINITY ? 0.f : m;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          const unsigned long long scale2 = pack_f32x2(a.scale, a.scale), ref2 = pack_f32x2(-ref, -ref);
+          unsigned long long sum2[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
           for (int e = 0; e < kTlKeys; e += 2) {
-            const float x = pt_exp2(fmaf(s[e], a.scale, -ref)), y = pt_exp2(fmaf(s[e + 1], a.scale, -ref));
-            sum[(e >> 1) & 3] += x + y;
+            float x, y;
+            unpack_f32x2(fma_f32x2(pack_f32x2(s[e], s[e + 1]), scale2, ref2), x, y);
+            x = pt_exp2(x); y = pt_exp2(y);
+            sum2[(e >> 1) & 3] = add_f32x2(sum2[(e >> 1) & 3], pack_f32x2(x, y));
             s[e >> 1] = __uint_as_float(un_pack<F16>(x, y));
           }
-          l = fmaf(l, sc, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+          float s0, s1;
+          unpack_f32x2(add_f32x2(add_f32x2(sum2[0], sum2[1]), add_f32x2(sum2[2], sum2[3])), s0, s1);
+          l = fmaf(l, sc, s0 + s1);
         }
         // P and O belong to the tensor core until P V of the block before has completed
         if (j > p.j0) {
-          fine = wait_warp(&sh.pv_done, (uint32_t)(i - 1) & 1u);
+          fine = wait_warp(&sh.pv_done[half], (uint32_t)(i - 1) & 1u);
           if (!fine) break;
           tc_fence_after_sync();
           if (__any_sync(0xFFFFFFFFu, sc != 1.f)) {
@@ -355,23 +390,23 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
           tmem_wait_st();
         }
         if (n < kTlKeys) {                     // the sequence's last block: V rows behind its keys may hold NaN, and 0 * NaN must not reach O
-          const int sl = (2 * i + 1) % kTlRing;
-          fine = wait_warp(&sh.full[sl], (uint32_t)((2 * i + 1) / kTlRing) & 1u);
-          if (!fine) break;
-          for (int x = n * 8 + tid; x < kTlKeys * 8; x += kTlRows) *reinterpret_cast<uint4 *>(ring + sl * kTlHalf + x * 16) = make_uint4(0, 0, 0, 0);
+          // (both halves write the same zeros, each ahead of its own P V; S of the block is there, so its K and V are)
+          unsigned char *v = ring + (n_block + j - p.j0) % kTlRing * kTlBlock + kTlHalf;
+          for (int x = n * 8 + t; x < kTlKeys * 8; x += kTlRows) *reinterpret_cast<uint4 *>(v + x * 16) = make_uint4(0, 0, 0, 0);
           fence_proxy_async_smem();
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_full);
+        if (lane == 0) mbar_arrive(&sh.p_full[half]);
       }
       if (!fine) break;
       // ---- the tile's rows leave ----
       float o[kHeadDim];
 #pragma unroll
       for (int c = 0; c < kHeadDim; ++c) o[c] = 0.f;
-      if (p.j1 > p.j0) {
-        fine = wait_warp(&sh.pv_done, (uint32_t)(i - 1) & 1u);
+      n_block += p.j1 - p.j0;
+      if (blocks > p.j0) {
+        fine = wait_warp(&sh.pv_done[half], (uint32_t)(i - 1) & 1u);
         if (!fine) break;
         tc_fence_after_sync();
         if (live) {
@@ -383,21 +418,21 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
       const int c0 = size.of(p.u0), c1 = size.of(p.u0 + p.nu - 1);
       bool write = c0 == c1;
       if (!write) {
-        // a place of 128 rows: 16 columns of four dimensions, then reference and sum; for the tile that goes on behind a CTA's range, and
+        // a place of 256 rows: 16 columns of four dimensions, then reference and sum; for the tile that goes on behind a CTA's range, and
         // the one that began before
-        auto place = [&](int c) { return a.part + (size_t)(2 * c + (c == c0)) * kTlRows * kUnPitch; };
+        auto place = [&](int c) { return a.part + (size_t)(2 * c + (c == c0)) * kTlTile * kUnPitch; };
         if (mine) {
           float *x = place(blockIdx.x);
 #pragma unroll
-          for (int c = 0; c < kHeadDim / 4; ++c) *reinterpret_cast<float4 *>(x + (c * kTlRows + tid) * 4) = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
-          *reinterpret_cast<float2 *>(x + kTlRows * kHeadDim + 2 * tid) = make_float2(m, l);
+          for (int c = 0; c < kHeadDim / 4; ++c) *reinterpret_cast<float4 *>(x + (c * kTlTile + tid) * 4) = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+          *reinterpret_cast<float2 *>(x + kTlTile * kHeadDim + 2 * tid) = make_float2(m, l);
         }
         // a ticket for each warp's 32 rows
         __threadfence();
         __syncwarp();
         int last = 0;
         if (lane == 0) {
-          unsigned *tk = a.tickets + 4 * c0 + warp;
+          unsigned *tk = a.tickets + (kTlTile / 32) * c0 + warp;
           last = atomicAdd(tk, 1u) + 1u == (unsigned)(c1 - c0 + 1);
           if (last) *tk = 0u;
         }
@@ -410,14 +445,14 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
 #pragma unroll 1
           for (int c = c0; c <= c1; ++c) {
             const float *x = place(c);
-            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(x + kTlRows * kHeadDim + 2 * tid));
+            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(x + kTlTile * kHeadDim + 2 * tid));
             const float mn = fmaxf(m, ml.x), fo = m == mn ? 1.f : pt_exp2(m - mn), fn = ml.y == 0.f ? 0.f : pt_exp2(ml.x - mn);   // 0: no key in it
             if (ml.y != 0.f) m = mn;
             const float fk = ml.y != 0.f ? fo : 1.f;
             l = fmaf(l, fk, ml.y * fn);
 #pragma unroll
             for (int e = 0; e < kHeadDim / 4; ++e) {
-              const float4 v = __ldcg(reinterpret_cast<const float4 *>(x + (e * kTlRows + tid) * 4));
+              const float4 v = __ldcg(reinterpret_cast<const float4 *>(x + (e * kTlTile + tid) * 4));
               o[4 * e] = fmaf(o[4 * e], fk, v.x * fn); o[4 * e + 1] = fmaf(o[4 * e + 1], fk, v.y * fn);
               o[4 * e + 2] = fmaf(o[4 * e + 2], fk, v.z * fn); o[4 * e + 3] = fmaf(o[4 * e + 3], fk, v.w * fn);
             }
@@ -426,21 +461,21 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
       }
       write = write && !*failed && __ldcg(a.err) == 0;
       const float inv = l == 0.f ? 0.f : 1.0f / l;
-      auto row_ptr = [&](int i2) { const int r = a.by_G.of(i2); return a.out + ((size_t)(p.row0 + r) * a.H + (p.kvh - r) * a.G + i2) * kHeadDim; };
+      auto row_ptr = [&](int i2) { const int r = a.by_G.of(i2); return a.out + ((size_t)(p.row0 + half * (a.rpt >> 1) + r) * a.H + (p.kvh - r) * a.G + i2) * kHeadDim; };
       if (p.j1 > p.j0) {                       // through the tile's Q, which no product reads any more: whole 128-byte rows leave
         const int qb = n_tile++ & 1;
-        unsigned char *stage = Qs + qb * kTlHalf;
+        unsigned char *stage = Qs + qb * kTlQ + half * kTlHalf;
         if (write && live) {
 #pragma unroll
           for (int c = 0; c < kHeadDim; c += 8)
-            *reinterpret_cast<uint4 *>(stage + tid * 128 + (((c >> 3) ^ (tid & 7)) << 4)) =
+            *reinterpret_cast<uint4 *>(stage + t * 128 + (((c >> 3) ^ (t & 7)) << 4)) =
                 make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
                            un_pack<F16>(o[c + 4] * inv, o[c + 5] * inv), un_pack<F16>(o[c + 6] * inv, o[c + 7] * inv));
           __syncwarp();
 #pragma unroll
           for (int it = 0; it < 8; ++it) {
-            const int r = 32 * warp + 4 * it + (lane >> 3), c8 = lane & 7;
-            if (r < p.n_i) *reinterpret_cast<uint4 *>(row_ptr(r) + 8 * c8) = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((c8 ^ (r & 7)) << 4));
+            const int r = 32 * quarter + 4 * it + (lane >> 3), c8 = lane & 7;
+            if (r < n_i) *reinterpret_cast<uint4 *>(row_ptr(r) + 8 * c8) = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((c8 ^ (r & 7)) << 4));
           }
         }
         fence_proxy_async_smem();              // Q of the tile after next is copied over it
@@ -449,7 +484,7 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
       } else if (write && mine) {              // no block here, and no Q: zeros, or the sum of other CTAs' parts
 #pragma unroll
         for (int c = 0; c < kHeadDim; c += 8)
-          *reinterpret_cast<uint4 *>(row_ptr(tid) + c) = make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
+          *reinterpret_cast<uint4 *>(row_ptr(t) + c) = make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
                                                                     un_pack<F16>(o[c + 4] * inv, o[c + 5] * inv), un_pack<F16>(o[c + 6] * inv, o[c + 7] * inv));
       }
     }
@@ -461,22 +496,22 @@ __global__ void __launch_bounds__(kTlThreads, 2) attention_tiles_kernel(const __
     const unsigned long long t0 = global_timer_ns();
     while (global_timer_ns() - t0 <= 10000000ull) {}
   }
-  if (warp == 5) tmem_dealloc(tmem, 256);
+  if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-inline long long tiles_part_rows() { return 2ll * kTlMaxCtas * kTlRows; }
+inline long long tiles_part_rows() { return 2ll * kTlMaxCtas * kTlTile; }
 
 template <bool F16>
 inline cudaError_t launch_tiles_as(const CUtensorMap &q_map, const CUtensorMap &k_map, const CUtensorMap &v_map, const UnitArgs &a, int n_sm, cudaStream_t st) {
   static SmemOptIn opt_in;
   if (const cudaError_t e = opt_in(attention_tiles_kernel<F16>, tiles_smem_bytes(kTlMaxSeq))) return e;
-  return launch_kernel(attention_tiles_kernel<F16>, dim3(std::min(2 * n_sm, kTlMaxCtas)), dim3(kTlThreads), tiles_smem_bytes(a.n_seq), st, false, q_map, k_map, v_map, a);
+  return launch_kernel(attention_tiles_kernel<F16>, dim3(std::min(n_sm, kTlMaxCtas)), dim3(kTlThreads), tiles_smem_bytes(a.n_seq), st, false, q_map, k_map, v_map, a);
 }
 
-// Query rows: G heads of one group and rpt rows a copy.
-inline cudaError_t tiles_q_map(CUtensorMap *map, bool f16, const void *q, size_t heads, size_t rows, size_t row, int G, int rpt) {
+// Query rows: G heads of one group and `rows` rows a copy.
+inline cudaError_t tiles_q_map(CUtensorMap *map, bool f16, const void *q, size_t heads, size_t rows, size_t row, int G, int n) {
   const cuuint64_t dims[3] = {kHeadDim, heads, rows}, strides[2] = {kHeadDim * 2, rows == 1 ? heads * kHeadDim * 2 : row};
-  const cuuint32_t box[3] = {kHeadDim, (cuuint32_t)G, (cuuint32_t)rpt};
+  const cuuint32_t box[3] = {kHeadDim, (cuuint32_t)G, (cuuint32_t)n};
   return tensor_map_encode(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, q, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 

@@ -75,7 +75,7 @@ struct UnitArgs {
   uint16_t *out;                // [rows][H * 64]
   long long q_stride;           // elements between query rows
   int q_rows, H, Hkv, G;        // G = H / Hkv query heads share a head of keys
-  int rpt;                      // query rows of a tile: 16 / G (128 / G)
+  int rpt;                      // query rows of a tile: 16 / G, or two halves of 128 / G
   Div by_G, by_rpt, by_H, by_Hkv;
   // shared prefix: its tiles of a head of keys (0 without one), and the units of each of them
   int tiles_head, prefix_nu;
@@ -88,7 +88,6 @@ struct UnitArgs {
   // cross: sequences
   const int *q_start, *k_start;
   int n_seq, q_max, k_rows;
-  int k_tokens_first, v_tokens_first;   // the map's middle dimension is the token, not the head
   // scratch
   int *err;                     // [0]: set when a wait ran out
   unsigned *tickets;            // zero between calls; null: the second kernel merges
@@ -96,8 +95,8 @@ struct UnitArgs {
   float *part;
   int suffix_part0;             // partial row at which those of the rows' own tiles begin
 
-  void set_heads(int n_head, int n_kv_head, int tile = kUnTile) {
-    H = n_head; Hkv = n_kv_head; G = H / Hkv; rpt = tile / G;
+  void set_heads(int n_head, int n_kv_head, int rows) {
+    H = n_head; Hkv = n_kv_head; G = H / Hkv; rpt = rows;
     by_G.set(G); by_rpt.set(rpt); by_H.set(H); by_Hkv.set(Hkv);
     by_tiles_head.set(1); by_prefix_nu.set(1);
   }
@@ -403,8 +402,8 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
               un_box(&k_map, c1 + o, c2, st + o * 128, b);
               un_box(&v_map, c1 + o, c2 + a.Hkv, st + L::kHalf + o * 128, b);
             } else {
-              un_box(&k_map, a.k_tokens_first ? c2 + o : c1, a.k_tokens_first ? c1 : c2 + o, st + o * 128, b);
-              un_box(&v_map, a.v_tokens_first ? c2 + o : c1, a.v_tokens_first ? c1 : c2 + o, st + L::kHalf + o * 128, b);
+              un_box(&k_map, c2 + o, c1, st + o * 128, b);
+              un_box(&v_map, c2 + o, c1, st + L::kHalf + o * 128, b);
             }
           }
       }
@@ -757,15 +756,12 @@ inline cudaError_t units_pool_map(CUtensorMap *map, const void *pool, size_t blo
   const cuuint32_t box[3] = {kHeadDim, kUnBox, 1};
   return tensor_map_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, pool, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-// Rows of 64 values: heads and tokens `head` and `row` bytes apart, in whichever order; `box_rows` tokens of one head a copy.  The
-// dimension with the smaller stride comes first: *tokens_first says whether that is the token.
-inline cudaError_t units_rows_map(CUtensorMap *map, int *tokens_first, bool f16, const void *base, size_t heads, size_t rows, size_t head, size_t row, int box_rows) {
-  if (heads == 1) head = std::max(row, (size_t)(kHeadDim * 2)) * rows;   // strides that nothing is addressed with
-  if (rows == 1) row = head * heads;
-  const bool tf = row < head;
-  *tokens_first = tf;
-  const cuuint64_t dims[3] = {kHeadDim, tf ? rows : heads, tf ? heads : rows}, strides[2] = {tf ? row : head, tf ? head : row};
-  const cuuint32_t box[3] = {kHeadDim, tf ? (cuuint32_t)box_rows : 1u, tf ? 1u : (cuuint32_t)box_rows};
+// Rows of 64 values [64, tokens, heads], tokens and heads `row` and `head` bytes apart; `box_rows` tokens of one head a copy.  The token is
+// the second dimension even where heads lie closer together: a box of 128 tokens along the third dimension was copied at 16 bytes a
+// cycle and SM.
+inline cudaError_t units_rows_map(CUtensorMap *map, bool f16, const void *base, size_t heads, size_t rows, size_t head, size_t row, int box_rows) {
+  const cuuint64_t dims[3] = {kHeadDim, rows, heads}, strides[2] = {row, head};
+  const cuuint32_t box[3] = {kHeadDim, (cuuint32_t)box_rows, 1};
   return tensor_map_encode(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 

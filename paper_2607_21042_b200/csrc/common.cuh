@@ -60,6 +60,12 @@ __device__ __forceinline__ unsigned long long mul_f32x2(unsigned long long a, un
   return r;
 }
 
+__device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // Streaming 128-bit load that does not pollute L1 (weights and KV pages are read once per step).
 __device__ __forceinline__ uint4 ld_stream_u4(const void *p) {
   uint4 r;

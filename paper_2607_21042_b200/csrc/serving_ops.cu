@@ -22,7 +22,7 @@ namespace {
 // that calls of other sizes, of either kind, find the tickets at zero where the call before left them.
 constexpr size_t kOpTicketBytes = kUnTickets * sizeof(unsigned), kOpPlanBytes = align256((kUnMaxSeq + 4) * sizeof(int));
 constexpr size_t kOpHeaderBytes = 256 + kOpTicketBytes + kOpPlanBytes;
-static_assert(kUnTickets >= kUnMaxWarps && kUnTickets >= 4 * kTlMaxCtas && kUnTickets >= kUnMaxTiles * kUnMaxCtas, "a ticket per range, or per row and group of a call that merges itself");
+static_assert(kUnTickets >= kUnMaxWarps && kUnTickets >= kTlTile / 32 * kTlMaxCtas && kUnTickets >= kUnMaxTiles * kUnMaxCtas, "a ticket per range, or per row and group of a call that merges itself");
 size_t scratch_bytes(long long part_rows) { return kOpHeaderBytes + (size_t)part_rows * kUnPitch * sizeof(float); }
 
 bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
@@ -116,7 +116,7 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
     return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_shared: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(shared_part_rows(R, n_kv_head, G)));
   UnitArgs a = {};
   a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = R;
-  a.set_heads(n_head, n_kv_head);
+  a.set_heads(n_head, n_kv_head, kUnTile / G);
   a.set_shared(n_shared);
   a.scale = 0.125f * 1.4426950408889634f;
   a.page_table = page_table; a.row_stream = row_stream; a.row_pos = row_pos; a.pool = (const unsigned char *)kv_layer; a.pps = pages_per_stream;
@@ -164,7 +164,7 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   const int G = n_head / n_kv_head;
   const bool tiles = q_max * G > kUnTile && n <= kTlMaxSeq;
   // units and blocks of keys are numbered in 31 bits
-  const int rpt = (tiles ? kTlRows : kUnTile) / G, keys = tiles ? kTlKeys : kUnKeys;
+  const int rpt = tiles ? 2 * (kTlRows / G) : kUnTile / G, keys = tiles ? kTlKeys : kUnKeys;
   const long long blocks = std::min((long long)n * ((q_max + rpt - 1) / rpt), (long long)q_rows / rpt + n);
   if ((long long)n_kv_head * blocks * ((long long)k_rows / keys + 2) >= (1ll << 31) &&
       (long long)n_kv_head * ((q_max + rpt - 1) / rpt) * ((long long)k_rows / keys + 2 * n) >= (1ll << 31))
@@ -173,7 +173,7 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
     return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_cross: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())));
   UnitArgs a = {};
   a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = q_rows;
-  a.set_heads(n_head, n_kv_head, tiles ? kTlRows : kUnTile);
+  a.set_heads(n_head, n_kv_head, rpt);
   a.scale = scale * 1.4426950408889634f;
   a.q_start = q_start; a.k_start = k_start; a.n_seq = n; a.q_max = q_max; a.k_rows = k_rows;
   a.err = (int *)scratch;
@@ -182,16 +182,16 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   CUtensorMap k_map = {}, v_map = {};
   const bool f16 = type == TTS_GPT_T_F16;
   if (k_rows > 0) {
-    OP_TRY(units_rows_map(&k_map, &a.k_tokens_first, f16, k, n_kv_head, k_rows, k_head_stride * 2, k_stride * 2, tiles ? kTlKeys : kUnBox));
-    OP_TRY(units_rows_map(&v_map, &a.v_tokens_first, f16, v, n_kv_head, k_rows, v_head_stride * 2, v_stride * 2, tiles ? kTlKeys : kUnBox));
+    OP_TRY(units_rows_map(&k_map, f16, k, n_kv_head, k_rows, k_head_stride * 2, k_stride * 2, tiles ? kTlKeys : kUnBox));
+    OP_TRY(units_rows_map(&v_map, f16, v, n_kv_head, k_rows, v_head_stride * 2, v_stride * 2, tiles ? kTlKeys : kUnBox));
   }
   if (tiles && k_rows > 0) {
     CUtensorMap q_map;
-    OP_TRY(tiles_q_map(&q_map, f16, q, n_head, q_rows, q_stride * 2, G, rpt));
+    OP_TRY(tiles_q_map(&q_map, f16, q, n_head, q_rows, q_stride * 2, G, rpt / 2));
     OP_TRY((f16 ? launch_tiles_as<true> : launch_tiles_as<false>)(q_map, k_map, v_map, a, device_sms(), (cudaStream_t)cuda_stream));
     return TTS_GPT_OK;
   }
-  if (tiles) a.set_heads(n_head, n_kv_head);   // no keys at all: rows of zeros, from the kernel that needs no maps
+  if (tiles) a.set_heads(n_head, n_kv_head, kUnTile / G);   // no keys at all: rows of zeros, from the kernel that needs no maps
   OP_TRY((f16 ? launch_units_as<false, KV_F16, false> : launch_units_as<false, KV_BF16, false>)(k_map, v_map, a, device_sms(), (cudaStream_t)cuda_stream));
   return TTS_GPT_OK;
 }
