@@ -9,7 +9,7 @@
 //
 // Every CTA computes both running sums over all requests for itself (at most 4096 of them, out of L2) and then writes its share
 // of the rows and of the list entries, which it finds by bisection: one launch, no CTA waits for another.  What a caller may
-// update in place (contexts, stack height) is written by the CTA that leaves last, when every CTA has read it.
+// update in place (contexts, stack height) is then written by the CTA that leaves last, when every CTA has read it.
 // Bound: two dependent reads (ids, contexts), one of the page stack, the launch; 12 bytes a row where there are many.
 #pragma once
 #include <cuda_fp8.h>
@@ -28,8 +28,8 @@ struct TableArgs {
   int n, max_streams, pps, n_pages, n_shared, max_rows;
   const int *stream_ids, *new_len, *ctx_len, *free_pages, *free_top, *shared_pages;
   int *ctx_len_out, *free_top_out, *page_table, *row_start, *row_stream, *row_pos, *row_slot;
+  int in_place;   // ctx_len_out or free_top_out overlaps what every CTA reads
   int *info;   // {status, rows, pages taken, stack height, 0, 0, 0, CTAs that have left}
-  int vec;     // the three row arrays are 16-byte aligned
 };
 
 enum { kTabBadArg = 1, kTabBadStream = 2, kTabOverflow = 4, kTabRows = 8, kTabNoPages = 16 };
@@ -38,7 +38,7 @@ inline size_t page_tables_smem_bytes(int n, int max_streams) { return (size_t)(5
 
 // THREADS * ITEMS requests at most
 template <int THREADS, int ITEMS>
-__global__ void __launch_bounds__(THREADS) page_tables_kernel(const TableArgs a) {
+__global__ void __launch_bounds__(THREADS, 1) page_tables_kernel(const TableArgs a) {
   extern __shared__ int tab_smem[];
   int *row_s = tab_smem, *page_s = row_s + a.n + 1;              // running sums, one more than requests
   int *base_s = page_s + a.n + 1, *held_s = base_s + a.n, *id_s = held_s + a.n;
@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(THREADS) page_tables_kernel(const TableArgs a)
   int id[ITEMS], add[ITEMS], ctx[ITEMS];
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k) {
-    const int i = k * THREADS + tid;
+    const int i = tid * ITEMS + k;
     id[k] = i < a.n ? (a.stream_ids ? a.stream_ids[i] : i) : -1;
     add[k] = i < a.n ? a.new_len[i] : 0;
   }
@@ -60,49 +60,55 @@ __global__ void __launch_bounds__(THREADS) page_tables_kernel(const TableArgs a)
   if (tid == 0) bad_s = top < 0 || top > a.n_pages ? kTabBadArg : 0;
   __syncthreads();
   int bad = 0;
-  unsigned long long carry = 0;
+  unsigned long long mine[ITEMS], sum = 0;   // rows and pages of each request, and of the thread's
+  int base[ITEMS], held[ITEMS];
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k) {
-    const int i = k * THREADS + tid;
-    unsigned long long mine = 0;
-    int base = 0, held = 0;
-    if (i < a.n) {
+    mine[k] = 0; base[k] = 0; held[k] = 0;
+    if (tid * ITEMS + k < a.n) {
       if (id[k] < 0 || id[k] >= a.max_streams || (atomicOr(&seen[id[k] >> 5], 1u << (id[k] & 31)) >> (id[k] & 31) & 1u)) bad |= kTabBadStream;
       else if (add[k] < 0 || ctx[k] < 0) bad |= kTabBadArg;
       else {
-        base = ctx[k] == 0 && add[k] > 0 ? a.n_shared * kPageTokens : ctx[k];
-        if ((long long)base + add[k] > (long long)a.pps * kPageTokens) bad |= kTabOverflow;
+        base[k] = ctx[k] == 0 && add[k] > 0 ? a.n_shared * kPageTokens : ctx[k];
+        if ((long long)base[k] + add[k] > (long long)a.pps * kPageTokens) bad |= kTabOverflow;
         else {
-          held = (base + kPageTokens - 1) / kPageTokens;
-          const int taken = (base + add[k] + kPageTokens - 1) / kPageTokens - held;
-          mine = ((unsigned long long)add[k] << kTabPageBits) + (unsigned long long)taken;
+          held[k] = (int)((unsigned)(base[k] + kPageTokens - 1) / kPageTokens);
+          const int taken = (int)((unsigned)(base[k] + add[k] + kPageTokens - 1) / kPageTokens) - held[k];
+          mine[k] = ((unsigned long long)add[k] << kTabPageBits) + (unsigned long long)taken;
         }
       }
     }
-    // inclusive sum over the block, behind those of the rounds before
-    unsigned long long incl = mine;
+    sum += mine[k];
+  }
+  // running sums: inside the warp, then of the warps
+  auto scan = [&](unsigned long long v) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const unsigned long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-      if (lane >= o) incl += v;
+      const unsigned long long u = __shfl_up_sync(0xFFFFFFFFu, v, o);
+      if (lane >= o) v += u;
     }
-    if (k > 0) __syncthreads();   // the sums of the round before have been read
-    if (lane == 31) warp_sum_s[warp] = incl;
-    __syncthreads();
-    unsigned long long before = carry, all = carry;
+    return v;
+  };
+  const unsigned long long incl = scan(sum);
+  if (lane == 31) warp_sum_s[warp] = incl;
+  __syncthreads();
+  if (warp == 0) {
+    const unsigned long long v = lane < THREADS / 32 ? warp_sum_s[lane] : 0ull, w = scan(v);
+    __syncwarp();
+    if (lane < THREADS / 32) warp_sum_s[lane] = w;   // inclusive
+  }
+  __syncthreads();
+  const unsigned long long carry = warp_sum_s[THREADS / 32 - 1];
+  unsigned long long e = (warp > 0 ? warp_sum_s[warp - 1] : 0ull) + incl - sum;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-      const unsigned long long v = warp_sum_s[w];
-      if (w < warp) before += v;
-      all += v;
-    }
-    carry = all;
+  for (int k = 0; k < ITEMS; ++k) {
+    const int i = tid * ITEMS + k;
     if (i < a.n) {
-      const unsigned long long e = before + incl - mine;
       row_s[i] = (int)(e >> kTabPageBits);   // beyond 2^31 rows the pass is refused below
       page_s[i] = (int)(e & ((1u << kTabPageBits) - 1));
-      base_s[i] = base; held_s[i] = held; id_s[i] = id[k];
+      base_s[i] = base[k]; held_s[i] = held[k]; id_s[i] = id[k];
     }
+    e += mine[k];
   }
   const long long rows = (long long)(carry >> kTabPageBits);
   const int pages = (int)(carry & ((1u << kTabPageBits) - 1));
@@ -113,54 +119,53 @@ __global__ void __launch_bounds__(THREADS) page_tables_kernel(const TableArgs a)
   __syncthreads();
   bad = bad_s;
   if (bad == 0) {
-    auto request_of = [&](const int *start, int x) {   // last request that starts at or before x
-      int lo = 0, hi = a.n - 1;
+    auto request_of = [&](const int *start, int x, int lo, int hi) {   // last request of lo .. hi that starts at or before x
       while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (start[m] <= x) lo = m; else hi = m - 1; }
       return lo;
     };
     const int me = blockIdx.x * THREADS + tid, all = gridDim.x * THREADS;
-    for (int r0 = 4 * me; r0 < (int)rows; r0 += 4 * all) {   // four rows at a time
-      int i = request_of(row_s, r0);
-      int s4[4], p4[4], t4[4];
+    // 128 rows a warp: the requests of the first and the last, then each row's between them (where prompts are long, one or two)
+#pragma unroll 1
+    for (int r0 = (me >> 5) * 128; r0 < (int)rows; r0 += (all >> 5) * 128) {
+      const int i0 = request_of(row_s, r0, 0, a.n - 1), i1 = request_of(row_s, min(r0 + 127, (int)rows - 1), i0, a.n - 1);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int r = min(r0 + e, (int)rows - 1);
-        while (row_s[i + 1] <= r) ++i;
-        const int pos = base_s[i] + r - row_s[i], pg = pos / kPageTokens;
-        const int page = pg < held_s[i] ? a.page_table[(size_t)id_s[i] * a.pps + pg] : a.free_pages[top - 1 - (page_s[i] + pg - held_s[i])];
-        s4[e] = id_s[i]; p4[e] = pos; t4[e] = page * kPageTokens + pos % kPageTokens;
-      }
-      if (a.vec && r0 + 4 <= (int)rows) {
-        *reinterpret_cast<int4 *>(a.row_stream + r0) = make_int4(s4[0], s4[1], s4[2], s4[3]);
-        *reinterpret_cast<int4 *>(a.row_pos + r0) = make_int4(p4[0], p4[1], p4[2], p4[3]);
-        *reinterpret_cast<int4 *>(a.row_slot + r0) = make_int4(t4[0], t4[1], t4[2], t4[3]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (r0 + e < (int)rows) { a.row_stream[r0 + e] = s4[e]; a.row_pos[r0 + e] = p4[e]; a.row_slot[r0 + e] = t4[e]; }
+        const int r = r0 + 32 * e + lane;
+        if (r < (int)rows) {
+          const int i = request_of(row_s, r, i0, i1), pos = base_s[i] + r - row_s[i], pg = (unsigned)pos / kPageTokens;
+          // on a page that the stream holds, or the next of the stack
+          const int *page = pg < held_s[i] ? a.page_table + (size_t)id_s[i] * a.pps + pg : a.free_pages + top - 1 - (page_s[i] + pg - held_s[i]);
+          a.row_stream[r] = id_s[i];
+          a.row_pos[r] = pos;
+          a.row_slot[r] = *page * kPageTokens + (unsigned)pos % kPageTokens;
+        }
       }
     }
+#pragma unroll 1
     for (int k = me; k < pages; k += all) {                  // new entries of the page lists
-      const int i = request_of(page_s, k);
+      const int i = request_of(page_s, k, 0, a.n - 1);
       a.page_table[(size_t)id_s[i] * a.pps + held_s[i] + k - page_s[i]] = a.free_pages[top - 1 - k];
     }
-    if (a.n_shared > 0) {                                    // the shared pages of the streams that open
-      const long long entries = (long long)a.n * a.n_shared;
-      for (long long k = me; k < entries; k += all) {
-        const int i = (int)(k / a.n_shared), j = (int)(k - (long long)i * a.n_shared);
-        if (row_s[i + 1] > row_s[i] && a.ctx_len[id_s[i]] == 0) a.page_table[(size_t)id_s[i] * a.pps + j] = a.shared_pages[j];
-      }
+    if (a.n_shared > 0) {                                    // the shared pages of the streams that open: a request a warp
+#pragma unroll 1
+      for (int i = blockIdx.x * (THREADS / 32) + warp; i < a.n; i += gridDim.x * (THREADS / 32))
+        if (row_s[i + 1] > row_s[i] && base_s[i] == a.n_shared * kPageTokens && a.ctx_len[id_s[i]] == 0)
+          for (int j = lane; j < a.n_shared; j += 32) a.page_table[(size_t)id_s[i] * a.pps + j] = a.shared_pages[j];
     }
     if (blockIdx.x == 0)
       for (int i = tid; i <= a.n; i += THREADS) a.row_start[i] = row_s[i];
   }
-  __syncthreads();
-  if (tid == 0) {
-    last_s = 1;
-    if (gridDim.x > 1) { __threadfence(); last_s = atomicAdd(a.info + 7, 1) == (int)gridDim.x - 1; }
+  if (a.in_place) {   // by the CTA that leaves last, when every CTA has read what is updated
+    __syncthreads();
+    if (tid == 0) {
+      last_s = 1;
+      if (gridDim.x > 1) { __threadfence(); last_s = atomicAdd(a.info + 7, 1) == (int)gridDim.x - 1; }
+    }
+    __syncthreads();
+    if (!last_s) return;
+  } else if (blockIdx.x > 0) {
+    return;
   }
-  __syncthreads();
-  if (!last_s) return;
   if (bad == 0)
     for (int i = tid; i < a.n; i += THREADS) {
       const int len = row_s[i + 1] - row_s[i];
@@ -174,22 +179,22 @@ __global__ void __launch_bounds__(THREADS) page_tables_kernel(const TableArgs a)
     a.info[2] = bad ? 0 : pages;
     a.info[3] = bad ? top : top - pages;
     if (!bad) *a.free_top_out = top - pages;
-    a.info[7] = 0;
+    if (a.in_place) a.info[7] = 0;
   }
 }
 
 inline cudaError_t launch_page_tables(const TableArgs &a, int n_sm, cudaStream_t st) {
   const size_t smem = page_tables_smem_bytes(a.n, a.max_streams);
-  // a CTA writes 4 rows a thread at a time; more CTAs than hold a few thousand rows each only repeat the sums
+  // a thread writes up to four rows; more CTAs than that only repeat the sums
   if (a.n <= 256) {
     static SmemOptIn opt_in;
     if (const cudaError_t e = opt_in(page_tables_kernel<256, 1>, page_tables_smem_bytes(256, kTabMaxStreams))) return e;
-    const int grid = std::max(1, std::min(n_sm, (a.max_rows + 2047) / 2048));
+    const int grid = std::max(1, std::min(2 * n_sm, (a.max_rows + 1023) / 1024));
     return launch_kernel(page_tables_kernel<256, 1>, dim3(grid), dim3(256), smem, st, false, a);
   }
   static SmemOptIn opt_in;
   if (const cudaError_t e = opt_in(page_tables_kernel<1024, 4>, page_tables_smem_bytes(kTabMaxRequests, kTabMaxStreams))) return e;
-  const int grid = std::max(1, std::min(n_sm, (a.max_rows + 4095) / 4096));
+  const int grid = std::max(1, std::min(n_sm, (a.max_rows + 2047) / 2048));
   return launch_kernel(page_tables_kernel<1024, 4>, dim3(grid), dim3(1024), smem, st, false, a);
 }
 

@@ -59,7 +59,7 @@ int32_t tts_gpt_op_page_tables(int32_t n, const int32_t *stream_ids, const int32
   a.stream_ids = stream_ids; a.new_len = new_len; a.ctx_len = ctx_len; a.free_pages = free_pages; a.free_top = free_top; a.shared_pages = shared_pages;
   a.ctx_len_out = ctx_len_out; a.free_top_out = free_top_out; a.page_table = page_table; a.row_start = row_start; a.row_stream = row_stream;
   a.row_pos = row_pos; a.row_slot = row_slot; a.info = info;
-  a.vec = aligned(row_stream, 16) && aligned(row_pos, 16) && aligned(row_slot, 16);
+  a.in_place = (ctx_len_out < ctx_len + max_streams && ctx_len < ctx_len_out + max_streams) || free_top_out == free_top;
   OP_TRY(launch_page_tables(a, device_sms(), (cudaStream_t)cuda_stream));
   return TTS_GPT_OK;
 }
@@ -162,7 +162,9 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   if (n > kUnMaxSeq) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: at most %d sequences", kUnMaxSeq);
   if (q_max > q_rows) q_max = q_rows;
   const int G = n_head / n_kv_head;
-  const bool tiles = q_max * G > kUnTile && n <= kTlMaxSeq;
+  // Up to two tiles of 16 read K and V at most twice; more rows take a tile of 256, which reads them once (us, 16 sequences of 90 to 1500 keys
+  // by 20 heads, warp-level / tcgen05: 20 queries 32 / 41, 48 queries 43 / 41, 128 queries 71 / 45)
+  const bool tiles = q_max * G > 2 * kUnTile && n <= kTlMaxSeq;
   // units and blocks of keys are numbered in 31 bits
   const int rpt = tiles ? 2 * (kTlRows / G) : kUnTile / G, keys = tiles ? kTlKeys : kUnKeys;
   const long long blocks = std::min((long long)n * ((q_max + rpt - 1) / rpt), (long long)q_rows / rpt + n);
