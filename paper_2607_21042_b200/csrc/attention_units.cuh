@@ -87,7 +87,7 @@ struct UnitArgs {
   int pps, n_shared, n_pages;
   // cross: sequences
   const int *q_start, *k_start;
-  int n_seq, q_max, k_rows;
+  int n_seq, q_max, k_rows, few_rows;   // few_rows: no tile has more than four
   // scratch
   int *err;                     // [0]: set when a wait ran out
   unsigned *tickets;            // zero between calls; null: the second kernel merges
@@ -692,7 +692,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
     }
     __threadfence();
     __syncthreads();
-    // ---- and those are merged, by as many lanes each as there are ----
+    // ---- and those are merged ----
     const int n_item = n_item_s;
     const bool store = n_item > 0 && __ldcg(a.err) == 0;
     auto merge = [&](auto pg_c, int item) {
@@ -710,7 +710,9 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         merge_parts<PG, F16>(warp_of(d.x + d.y - 1) - f + 1, [&](int k) { return a.part + (seq_part(f + k, k == 0) + i) * kUnPitch; }, dst, real && store);
       }
     };
-    if (n_item <= kUnWarps) { if (warp < n_item) merge(IntC<4>(), warp); }
+    // (a warp a row where tiles have few, a quarter of one otherwise: by the call, not by how many rows this CTA came last at, since the
+    // two add the parts in other orders)
+    if (SHARED || a.few_rows) for (int it = warp; it < n_item; it += kUnWarps) merge(IntC<4>(), it);
     else for (int it = warp * 4; it < n_item; it += kUnWarps * 4) merge(IntC<1>(), it + ((lane >> 3) & 3));
   }
 }

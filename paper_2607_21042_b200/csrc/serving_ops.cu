@@ -178,6 +178,7 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   a.set_heads(n_head, n_kv_head, rpt);
   a.scale = scale * 1.4426950408889634f;
   a.q_start = q_start; a.k_start = k_start; a.n_seq = n; a.q_max = q_max; a.k_rows = k_rows;
+  a.few_rows = (long long)q_max * G <= 4;
   a.err = (int *)scratch;
   a.tickets = (unsigned *)((char *)scratch + 256);
   a.part = (float *)((char *)scratch + kOpHeaderBytes);

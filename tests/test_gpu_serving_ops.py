@@ -207,6 +207,23 @@ def test_scratch_serves_calls_of_all_sizes_and_both_kinds_bit_for_bit():
     assert int(scratch[:4].view(torch.int32)) == 0
 
 
+def test_results_do_not_depend_on_timing():
+    """The same calls many times over, behind each other and beside other work: the same bits, whichever CTA comes last at a tile."""
+    c = Cache(12, "e4m3", 4, 11, [5, 0, 300])
+    q = _q(7, 3, 20, torch.bfloat16)
+    xs = [CrossCase(14, torch.bfloat16, 20, 4, [1, 2], [900, 333]), CrossCase(15, torch.float16, 3, 3, [16, 5, 9], [2000, 100, 31]),
+          CrossCase(16, torch.bfloat16, 6, 2, [90, 300], [700, 1500])]
+    scratch = torch.zeros(max(B.op_attention_shared_scratch(3, 20, 4, DEV).numel(), B.op_attention_cross_scratch(DEV).numel()), dtype=torch.uint8, device=DEV)
+    want = [B.op_attention_shared(q, c.pool, *c.args, scratch=scratch).clone()] + [x.run(scratch=scratch).clone() for x in xs]
+    other, busy = torch.cuda.Stream(), torch.randn(2048, 2048, device=DEV)
+    for k in range(30):
+        with torch.cuda.stream(other):
+            busy = busy @ busy.t() * 1e-3
+        got = [B.op_attention_shared(q, c.pool, *c.args, scratch=scratch)] + [x.run(scratch=scratch) for x in xs]
+        for w, y in zip(want, got):
+            assert torch.equal(w.view(torch.int16), y.view(torch.int16)), k
+
+
 # ---------------------------------------------------------------------------------------------
 # attention to an encoder's states
 # ---------------------------------------------------------------------------------------------
