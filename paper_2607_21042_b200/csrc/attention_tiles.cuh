@@ -46,7 +46,7 @@ struct TileShared {
   uint64_t part_full[kTlParts], part_free[kTlParts];
   uint64_t full[kTlRing], empty[kTlRing];   // blocks
   uint64_t q_full[2], q_free[2];
-  uint64_t s_full[2], s_free[2], p_full[2], pv_done[2];   // by half
+  uint64_t s_full[2], p_full[2], pv_done[2];   // by half
   uint32_t tmem;
   int failed;
   Div size;
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
     for (int i = 0; i < kTlRing; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_free[i], kTlTile / 32); }
     for (int i = 0; i < kTlParts; ++i) { mbar_init(&sh.part_full[i], 1); mbar_init(&sh.part_free[i], 1 + kTlTile / 32); }
-    for (int h = 0; h < 2; ++h) { mbar_init(&sh.s_full[h], 1); mbar_init(&sh.s_free[h], kTlRows / 32); mbar_init(&sh.p_full[h], kTlRows / 32); mbar_init(&sh.pv_done[h], 1); }
+    for (int h = 0; h < 2; ++h) { mbar_init(&sh.s_full[h], 1); mbar_init(&sh.p_full[h], kTlRows / 32); mbar_init(&sh.pv_done[h], 1); }
     sh.failed = 0;
   }
   if (warp == 8) {
@@ -243,8 +243,9 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
         if (!fine) break;
       }
     } else if (warp == 9) {
-      // ---- products: of either half in turn Q K^T of block i, as soon as its softmax has read S of the block before, and P V of
-      //      block i - 1 behind it ----
+      // ---- products: of either half in turn, when P of block j - 1 is there (and S has been read), Q K^T of block j, which its softmax
+      //      waits for, and P V of block j - 1 behind it.  (Q K^T ahead of P, with a barrier of its own, made seven waits of this warp a
+      //      block where there are three: 106 -> 165 us.) ----
       const uint32_t kind = F16 ? ~((1u << 7) | (1u << 10)) : ~0u;
       const uint32_t idesc_qk = tc_instr_desc(kTlRows, kTlKeys) & kind, idesc_pv = (tc_instr_desc(kTlRows, kHeadDim) & kind) | (1u << 16);   // V is MN-major
       int n_tile = 0, n_part = 0;                // tiles with blocks, and parts of this CTA
@@ -253,9 +254,6 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
       int done[2] = {0, 0}, n_block = 0;       // blocks of either half that have had their P V, blocks of the CTA
       // P V of the block that half h has come to, block b of the CTA; last: no other half reads that block any more
       auto pv = [&](int h, int b, bool begins, bool last) {
-        fine = fine && wait_warp(&sh.p_full[h], (uint32_t)done[h] & 1u);
-        if (!fine) return;
-        tc_fence_after_sync();
         const int s = b % kTlRing;
         const uint64_t dv = dring + (uint64_t)((s * kTlBlock + kTlHalf) >> 4);
         const uint32_t t = tmem + 256u * h;
@@ -285,8 +283,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (h == halves || !fine) break;
-            const int before = done[h] + (j > p.j0);   // blocks of this half whose S has been computed
-            fine = before == 0 || wait_warp(&sh.s_free[h], (uint32_t)(before - 1) & 1u);
+            if (j > p.j0) fine = wait_warp(&sh.p_full[h], (uint32_t)done[h] & 1u);
             if (!fine) break;
             tc_fence_after_sync();
             if (elect_one()) {
@@ -298,7 +295,12 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
             if (j > p.j0) pv(h, n_block - 1, j - 1 == p.j0, h + 1 == halves);
           }
         }
-        for (int h = 0; h < halves && fine; ++h) pv(h, n_block - 1, p.j1 - 1 == p.j0, h + 1 == halves);   // the tile's last
+        for (int h = 0; h < halves && fine; ++h) {   // the tile's last
+          fine = wait_warp(&sh.p_full[h], (uint32_t)done[h] & 1u);
+          if (!fine) break;
+          tc_fence_after_sync();
+          pv(h, n_block - 1, p.j1 - 1 == p.j0, h + 1 == halves);
+        }
       }
     }
   } else {
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
         if (!fine) break;
         tc_fence_after_sync();
         const int n = min(kTlKeys, p.keys - j * kTlKeys);
-        // all scores of the row into registers, so that the next block's may be computed behind the exponentials
+        // all scores of the row into registers
         float s[kTlKeys], sc = 1.f;
         if (live) {
 #pragma unroll
@@ -335,9 +337,6 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
 #pragma unroll
           for (int c = 0; c < kTlKeys; c += 32) tmem_landed32(s + c);
         }
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.s_free[half]);
         if (live) {
           if (n < kTlKeys) {                   // scores of keys that do not exist
 #pragma unroll
