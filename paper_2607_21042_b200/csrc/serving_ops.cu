@@ -72,11 +72,11 @@ int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void
   const int per16 = type == TTS_GPT_T_F32 ? 4 : 8;
   if (!aligned(k, 16) || !aligned(v, 16) || k_stride % per16 || v_stride % per16 || !aligned(kv_layer, 16) || !aligned(row_slot, 4))
     return fail_op(TTS_GPT_E_ARG, "op_kv_append: K and V rows and the pool must be 16-byte aligned, slots 4-byte");
-  if ((long long)R * n_head > (1ll << 31)) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_kv_append: R * n_head must be at most 2^31");
+  if ((long long)R * n_head >= (1ll << 29)) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_kv_append: R * n_head must be below 2^29");
   AppendArgs a;
   a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride; a.row_slot = row_slot; a.pool = (unsigned char *)kv_layer;
   a.R = R; a.H = n_head; a.n_slots = n_pages * kPageTokens;
-  OP_TRY(launch_kv_append(a, type == TTS_GPT_T_F32, kv_fmt == TTS_GPT_KV_FP8_E4M3, (cudaStream_t)cuda_stream));
+  OP_TRY(launch_kv_append(a, type == TTS_GPT_T_F32, kv_fmt == TTS_GPT_KV_FP8_E4M3, device_sms(), (cudaStream_t)cuda_stream));
   return TTS_GPT_OK;
 }
 
