@@ -6,6 +6,7 @@ there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -533,6 +534,11 @@ def op_kv_append(k, v, kv_layer, row_slot, stream=None):
          kv_layer.data_ptr())
 
 
+def _on(stream):
+    """Where memory that a call makes for itself belongs: the stream that the call runs on."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _scratch(scratch, d):
     if scratch.dtype is not _U8 or scratch.get_device() != d or not scratch.is_contiguous():
         _refuse("scratch must be a contiguous uint8 tensor on the same device")
@@ -564,11 +570,13 @@ def op_attention_shared(q, kv_layer, page_table, row_stream, row_pos, n_shared, 
         _refuse_index(d, page_table=page_table, row_stream=row_stream, row_pos=row_pos)
         _refuse("page_table must be [streams, pages of a stream], row_stream and row_pos at least R long")
     if out is None:
-        out = torch.empty(shape, dtype=_I16, device=q.device)
+        with _on(stream):
+            out = torch.empty(shape, dtype=_I16, device=q.device)
     elif out.shape != shape or (out.dtype is not _BF16 and out.dtype is not _I16) or out.get_device() != d or not out.is_contiguous():
         _refuse("out must be a contiguous bf16 tensor of q's shape on the same device")
     if scratch is None:
-        scratch = op_attention_shared_scratch(R, heads, kv_heads, q.device)
+        with _on(stream):
+            scratch = op_attention_shared_scratch(R, heads, kv_heads, q.device)
     sp, sn = _scratch(scratch, d)
     _run((_lib or load()).tts_gpt_op_attention_shared, d, stream, R, heads, kv_heads, _TYPES[t], q.data_ptr(), qs, fmt, pages, kv_layer.data_ptr(), n_shared,
          page_table.data_ptr(), lists[1], row_stream.data_ptr(), row_pos.data_ptr(), out.data_ptr(), sp, sn)
@@ -608,11 +616,13 @@ def op_attention_cross(q, k, v, q_start, k_start, q_max, scale=0.125, scratch=No
         _refuse_index(d, q_start=q_start, k_start=k_start)
         _refuse("q_start and k_start must have one value more than there are sequences")
     if out is None:
-        out = torch.empty(shape, dtype=t, device=q.device)
+        with _on(stream):
+            out = torch.empty(shape, dtype=t, device=q.device)
     elif out.shape != shape or out.dtype is not t or out.get_device() != d or not out.is_contiguous():
         _refuse("out must be a contiguous tensor of q's shape and type on the same device")
     if scratch is None:
-        scratch = op_attention_cross_scratch(q.device)
+        with _on(stream):
+            scratch = op_attention_cross_scratch(q.device)
     sp, sn = _scratch(scratch, d)
     _run((_lib or load()).tts_gpt_op_attention_cross, d, stream, n, heads, kv_heads, _TYPES[t], rows, q.data_ptr(), qs, k_rows, k.data_ptr(), kr, kh,
          v.data_ptr(), vr, vh, q_start.data_ptr(), k_start.data_ptr(), q_max, scale, out.data_ptr(), sp, sn)

@@ -6,7 +6,9 @@ kernels round is: each weight to the 16-bit type (relative half step h: 2^-8 bf1
 the output, by at most h (|o| + h A); fp32 queries to 16 bits (two bf16 parts; the second is rounded, 2^-8 of 2^-8) and the
 sums to fp32, which move a score by at most d = scale (2^-16 + 64 2^-24) sum |q| |k|, a weight by the factor e^(2 d), so
 o by at most (e^(2 d) - 1) A.  The exponential is good to 2^-22.  Together, with 1 % for the products of two of these and the
-fp32 sums over the keys:  |error| <= 1.01 (h (A + |o|) + (e^(2 d) - 1) A) + 2^-20 A.
+fp32 sums over the keys:  |error| <= 1.01 (h (A + |o|) + (e^(2 d) - 1) A) + 2^-20 A.  Below 2^-14 fp16 has steps of 2^-24, so that there
+a rounding is off by up to 2^-25 whatever the value: of the output, and of weights whose sum is at least 1 (the largest of a row is),
+which adds 2^-25 (1 + sum |v_j|).
 """
 import numpy as np
 import pytest
@@ -29,7 +31,8 @@ def _bound(q, k, v, scale, h):
     p = np.exp(s - s.max(-1, keepdims=True))
     p /= p.sum(-1, keepdims=True)
     o, A = p @ v, p @ np.abs(v)
-    return o, 1.01 * (h * (A + np.abs(o)) + np.expm1(2 * d) * A) + 2.0 ** -20 * A
+    small = 2.0 ** -25 * (1 + np.abs(v).sum(0)) if h == HALF[torch.float16] else 0.0
+    return o, 1.01 * (h * (A + np.abs(o)) + np.expm1(2 * d) * A) + 2.0 ** -20 * A + small
 
 
 def _check(got, ref, tol, what):
@@ -310,6 +313,8 @@ def test_cross_attention_with_no_keys_at_all_and_no_queries():
     k = torch.empty(0, 4, 64, dtype=torch.bfloat16, device=DEV)
     out = B.op_attention_cross(q, k, k, _i32([0, 3]), _i32([0, 0]), 3)
     assert torch.all(out == 0)
+    q = torch.ones(90, 4, 64, dtype=torch.bfloat16, device=DEV)
+    assert torch.all(B.op_attention_cross(q, k, k, _i32([0, 40, 90]), _i32([0, 0, 0]), 50) == 0)
     out = torch.full_like(q, 5.0)
     k = torch.ones(8, 4, 64, dtype=torch.bfloat16, device=DEV)
     B.op_attention_cross(q, k, k, _i32([0, 0, 0]), _i32([0, 8, 8]), 1, out=out)
@@ -551,6 +556,35 @@ def test_captured_steps_on_a_stream_of_their_own():
     for _ in range(5):
         step(out, None)
     assert torch.equal(out, got) and torch.equal(pool, replayed)
+
+
+def test_calls_on_a_stream_that_is_not_the_current_one():
+    """Memory that a call makes for itself belongs to the stream it runs on."""
+    st, c, x = torch.cuda.Stream(), Cache(41, "bf16", 4, 2, [70, 3, 200]), CrossCase(42, torch.float16, 4, 2, [3, 80], [600, 90])
+    q = _q(43, 3, 4, torch.float32)
+    want, wx = B.op_attention_shared(q, c.pool, *c.args).clone(), B.op_attention_cross(*x.args, scale=x.scale).clone()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        st.wait_stream(torch.cuda.current_stream())
+        got = [B.op_attention_shared(q, c.pool, *c.args, stream=st), B.op_attention_cross(*x.args, scale=x.scale, stream=st)]
+        junk = [torch.full((1 << 22,), 3.0, device=DEV) for _ in range(4)]      # what the current stream allocates meanwhile
+        st.synchronize()
+        assert torch.equal(got[0], want) and torch.equal(got[1][:x.qs[-1]], wx[:x.qs[-1]])
+        del junk
+
+
+def test_many_sequences_and_a_large_batch():
+    """The largest numbers of sequences and of rows, with small work for each."""
+    g = _gen(50)
+    for n in (2049, 4096):
+        ql, kl = torch.randint(0, 4, (n,), generator=g).tolist(), torch.randint(0, 40, (n,), generator=g).tolist()
+        ql[7] = 45                             # more than two tiles of the warp-level kernel
+        x = CrossCase(51, torch.bfloat16, 2, 1, ql, kl)
+        x.check(x.run(), "%d sequences" % n)
+    own = torch.randint(0, 70, (4096,), generator=g).tolist()
+    c = Cache(52, "bf16", 1, 1, own)
+    q = _q(53, 4096, 2, torch.bfloat16)
+    c.check(B.op_attention_shared(q, c.pool, *c.args), q, "4096 rows")
 
 
 def test_cross_attention_captured_and_on_two_streams_at_once():
