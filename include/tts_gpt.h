@@ -384,8 +384,8 @@ int32_t tts_gpt_op_sample(int32_t R, int32_t V, const float *logits, int32_t top
  *   row_stream[r] = stream, row_pos[r] = first position + k, row_slot[r] = page * 64 + position % 64,
  * row_start[i] (n + 1 of them) is the number of request i's first row; places behind the last row are left as they were.
  * page_table [max_streams][pages_per_stream] receives the new entries, ctx_len_out[stream] the new lengths of the call's
- * streams, *free_top_out the new height; ctx_len_out and free_top_out may be ctx_len and free_top.  info: int32 [8], zero before
- * its first use: {status, rows, pages taken, height of the stack, ...}.  The lengths live on the device, so their
+ * streams, *free_top_out the new height; ctx_len_out and free_top_out may be ctx_len and free_top, no other arrays may
+ * overlap (E_ARG).  info: int32 [8], zero before its first use: {status, rows, pages taken, height of the stack, ...}.  The lengths live on the device, so their
  * errors do too: info[0] is TTS_GPT_OK, or E_ARG (a negative length, a height outside 0..n_pages), E_STREAM (an id outside
  * 0..max_streams-1, or one that comes twice), E_CTX_OVERFLOW, E_WORKSPACE (more than max_rows rows) or E_NO_PAGES, and then
  * nothing but info is written.  Limits: n <= 4096, max_streams <= 32768, pages_per_stream <= 32768 (E_UNSUPPORTED).  Two
@@ -409,7 +409,7 @@ int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void
  * 0..row_pos[r] of stream row_stream[r], o = softmax(q.K^T / 8) V per head), where the first n_shared entries of the page lists of
  * all R rows are the same pages, which are read once for all rows and not once for each.  n_shared may be 0.  Query head
  * h reads the keys of head h / (n_head / n_kv_head), at most 16 to one.  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements
- * apart; out bf16 [R][n_head*64].  A row with row_pos -1 has no keys: its output is zero.  Several rows may belong to one stream.
+ * apart; out bf16 [R][n_head*64], which may not overlap q.  A row with row_pos -1 has no keys: its output is zero.  Several rows may belong to one stream.
  * Keys on a page outside 0..n_pages-1 are left out, as are those behind the list's pages_per_stream pages.  K and V of the shared
  * pages must be finite.  fp32 queries enter with 16 bits, the softmax weights are rounded to bf16, sums are fp32; results do
  * not depend on timing.  R <= 4096.
@@ -427,7 +427,8 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
  * independent; a sequence without keys has zero outputs, rows outside every sequence are left as they were.  q_start, k_start:
  * ascending, n + 1 each, at most q_rows and k_rows; q_max: at least the longest sequence of queries (rows beyond it are not
  * computed).  q, k, v, out of one type, TTS_GPT_T_BF16 or TTS_GPT_T_F16; q rows q_stride elements apart with contiguous heads, k and v with
- * strides of rows and of heads (so both [rows][heads][64], parts of one array, and [heads][rows][64]); out [q_rows][n_head*64].
+ * strides of rows and of heads (so both [rows][heads][64], parts of one array, and [heads][rows][64]); out [q_rows][n_head*64], which
+ * may overlap none of them.
  * Heads, roundings and scratch as for op_attention_shared (scratch size independent of the call).  n <= 4096. */
 int32_t tts_gpt_op_attention_cross_scratch_bytes(size_t *bytes);
 int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head, int32_t type, int32_t q_rows, const void *q,

@@ -27,6 +27,15 @@ size_t scratch_bytes(long long part_rows) { return kOpHeaderBytes + (size_t)part
 
 bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
 
+struct Bytes { const void *p; size_t n; };
+bool overlap(const Bytes &a, const Bytes &b) {
+  return a.p && b.p && a.n && b.n && (uintptr_t)a.p < (uintptr_t)b.p + b.n && (uintptr_t)b.p < (uintptr_t)a.p + a.n;
+}
+// rows of `width` elements, `stride` apart
+Bytes rows_of(const void *p, long long rows, long long stride, long long width, size_t size) {
+  return {p, rows > 0 ? (size_t)((rows - 1) * stride + width) * size : 0};
+}
+
 int check_heads(const char *op, int32_t n_head, int32_t n_kv_head) {
   if (n_head < 1 || n_kv_head < 1 || n_head % n_kv_head) return fail_op(TTS_GPT_E_ARG, "%s: n_head must be a multiple of n_kv_head", op);
   if (n_head / n_kv_head > kUnTile || n_head > 1024)
@@ -54,12 +63,24 @@ int32_t tts_gpt_op_page_tables(int32_t n, const int32_t *stream_ids, const int32
     return fail_op(TTS_GPT_E_ARG, "op_page_tables: bad argument");
   if (n > kTabMaxRequests || max_streams > kTabMaxStreams || pages_per_stream > kTabMaxListPages)
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_page_tables: at most %d requests, %d streams, %d pages to a stream", kTabMaxRequests, kTabMaxStreams, kTabMaxListPages);
+  // CTAs read the inputs while others already write: only ctx_len and free_top may be updated in place
+  const size_t streams = (size_t)max_streams * 4, rows = (size_t)max_rows * 4;
+  const Bytes in[] = {{ctx_len, streams}, {free_top, 4}, {stream_ids, (size_t)n * 4}, {new_len, (size_t)n * 4}, {free_pages, (size_t)n_pages * 4},
+                      {shared_pages, (size_t)n_shared * 4}};
+  const Bytes out[] = {{ctx_len_out, streams}, {free_top_out, 4}, {page_table, streams * pages_per_stream}, {row_start, (size_t)(n + 1) * 4}, {row_stream, rows},
+                       {row_pos, rows}, {row_slot, rows}, {info, 32}};
+  for (int o = 0; o < 8; ++o) {
+    for (int i = 0; i < 6; ++i)
+      if (overlap(out[o], in[i]) && !(o < 2 && o == i && out[o].p == in[i].p)) return fail_op(TTS_GPT_E_ARG, "op_page_tables: an output overlaps an input");
+    for (int i = 0; i < o; ++i)
+      if (overlap(out[o], out[i])) return fail_op(TTS_GPT_E_ARG, "op_page_tables: two outputs overlap");
+  }
   TableArgs a;
   a.n = n; a.max_streams = max_streams; a.pps = pages_per_stream; a.n_pages = n_pages; a.n_shared = n_shared; a.max_rows = max_rows;
   a.stream_ids = stream_ids; a.new_len = new_len; a.ctx_len = ctx_len; a.free_pages = free_pages; a.free_top = free_top; a.shared_pages = shared_pages;
   a.ctx_len_out = ctx_len_out; a.free_top_out = free_top_out; a.page_table = page_table; a.row_start = row_start; a.row_stream = row_stream;
   a.row_pos = row_pos; a.row_slot = row_slot; a.info = info;
-  a.in_place = (ctx_len_out < ctx_len + max_streams && ctx_len < ctx_len_out + max_streams) || free_top_out == free_top;
+  a.in_place = ctx_len_out == ctx_len || free_top_out == free_top;
   OP_TRY(launch_page_tables(a, device_sms(), (cudaStream_t)cuda_stream));
   return TTS_GPT_OK;
 }
@@ -114,6 +135,8 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_shared: too many pages");
   if (scratch_size < scratch_bytes(shared_part_rows(R, n_kv_head, G)))
     return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_shared: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(shared_part_rows(R, n_kv_head, G)));
+  if (overlap({out, (size_t)R * n_head * kHeadDim * 2}, rows_of(q, R, q_stride, (long long)n_head * kHeadDim, type == TTS_GPT_T_F32 ? 4 : 2)))
+    return fail_op(TTS_GPT_E_ARG, "op_attention_shared: out overlaps q");
   UnitArgs a = {};
   a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = R;
   a.set_heads(n_head, n_kv_head, kUnTile / G);
@@ -173,6 +196,11 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: too many queries times keys");
   if (scratch_size < scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())))
     return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_cross: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())));
+  const Bytes to = {out, (size_t)q_rows * n_head * kHeadDim * 2};
+  if (overlap(to, rows_of(q, q_rows, q_stride, (long long)n_head * kHeadDim, 2)) ||
+      overlap(to, rows_of(k, k_rows, k_stride, (n_kv_head - 1) * k_head_stride + kHeadDim, 2)) ||
+      overlap(to, rows_of(v, k_rows, v_stride, (n_kv_head - 1) * v_head_stride + kHeadDim, 2)))
+    return fail_op(TTS_GPT_E_ARG, "op_attention_cross: out overlaps q, K or V");
   UnitArgs a = {};
   a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = q_rows;
   a.set_heads(n_head, n_kv_head, rpt);

@@ -90,6 +90,27 @@ def test_attention_cross(lib, code, kw):
     assert b"op_attention_cross" in lib.tts_gpt_last_error(None)
 
 
+def test_outputs_that_overlap_what_is_read(lib):
+    """Addresses 1 MB apart are refused for nothing but an overlap, and with one only for that."""
+    def refused(fn, args):
+        return fn(*args) == B.E_ARG and b"overlap" in lib.tts_gpt_last_error(None)
+
+    apart = {name: (i + 1) << 20 for i, name in enumerate(["ids", "new", "ctx", "ctx_out", "free", "top", "top_out", "shared", "table", "start", "rs", "rp", "sl", "info"])}
+    for a, b in [("rs", "ids"), ("start", "new"), ("ctx_out", "new"), ("info", "top"), ("table", "free"), ("rp", "rs"), ("sl", "shared"), ("top_out", "ctx"), ("info", "start")]:
+        assert refused(lib.tts_gpt_op_page_tables, _tables(**{**apart, a: apart[b]})), (a, b)
+    assert refused(lib.tts_gpt_op_page_tables, _tables(**{**apart, "top": apart["info"] + 12}))            # the height that a call reports, as the next call's
+    assert refused(lib.tts_gpt_op_page_tables, _tables(**{**apart, "ctx_out": apart["ctx"] + 4}))
+    assert refused(lib.tts_gpt_op_page_tables, _tables(**{**apart, "rs": apart["rp"] - 60}))                # the last of 16 rows
+    Q = P + (1 << 24)
+    assert refused(lib.tts_gpt_op_attention_shared, _shared(q=Q, out=Q))
+    assert refused(lib.tts_gpt_op_attention_shared, _shared(q=Q, out=Q + 4 * 1024 - 16))
+    assert refused(lib.tts_gpt_op_attention_shared, _shared(q=Q, out=Q - 4 * 512 + 16))
+    for name in ("q", "k", "v"):
+        far = dict(q=P + (1 << 24), k=P + (2 << 24), v=P + (3 << 24))
+        assert refused(lib.tts_gpt_op_attention_cross, _cross(**far, out=far[name])), name
+        assert refused(lib.tts_gpt_op_attention_cross, _cross(**far, out=far[name] - 9 * 512 + 16)), name
+
+
 def test_scratch_sizes(lib):
     n, m = C.c_size_t(0), C.c_size_t(0)
     assert lib.tts_gpt_op_attention_shared_scratch_bytes(C.c_int32(1), C.c_int32(4), C.c_int32(4), C.byref(n)) == B.OK
