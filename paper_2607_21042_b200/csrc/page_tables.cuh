@@ -126,13 +126,13 @@ __global__ void __launch_bounds__(THREADS, 1) page_tables_kernel(const TableArgs
     const int me = blockIdx.x * THREADS + tid, all = gridDim.x * THREADS;
     // 128 rows a warp: the requests of the first and the last, then each row's between them (where prompts are long, one or two)
 #pragma unroll 1
-    for (int r0 = (me >> 5) * 128; r0 < (int)rows; r0 += (all >> 5) * 128) {
-      const int i0 = request_of(row_s, r0, 0, a.n - 1), i1 = request_of(row_s, min(r0 + 127, (int)rows - 1), i0, a.n - 1);
+    for (unsigned r0 = (me >> 5) * 128; r0 < (unsigned)rows; r0 += (all >> 5) * 128) {   // unsigned: the last turn may step past 2^31
+      const int i0 = request_of(row_s, (int)r0, 0, a.n - 1), i1 = request_of(row_s, (int)min(r0 + 127, (unsigned)rows - 1), i0, a.n - 1);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int r = r0 + 32 * e + lane;
-        if (r < (int)rows) {
-          const int i = request_of(row_s, r, i0, i1), pos = base_s[i] + r - row_s[i], pg = (unsigned)pos / kPageTokens;
+        const unsigned r = r0 + 32 * e + lane;
+        if (r < (unsigned)rows) {
+          const int i = request_of(row_s, (int)r, i0, i1), pos = base_s[i] + (int)r - row_s[i], pg = (unsigned)pos / kPageTokens;
           // on a page that the stream holds, or the next of the stack
           const int *page = pg < held_s[i] ? a.page_table + (size_t)id_s[i] * a.pps + pg : a.free_pages + top - 1 - (page_s[i] + pg - held_s[i]);
           a.row_stream[r] = id_s[i];
