@@ -409,9 +409,9 @@ int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void
  * 0..row_pos[r] of stream row_stream[r], o = softmax(q.K^T / 8) V per head), where the first n_shared entries of the page lists of
  * all R rows are the same pages, which are read once for all rows and not once for each.  n_shared may be 0.  Query head
  * h reads the keys of head h / (n_head / n_kv_head), at most 16 to one.  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements
- * apart; out bf16 [R][n_head*64], which may not overlap q.  A row with row_pos -1 has no keys: its output is zero.  Several rows may belong to one stream.
- * Keys on a page outside 0..n_pages-1 are left out, as are those behind the list's pages_per_stream pages.  K and V of the shared
- * pages must be finite.  fp32 queries enter with 16 bits, the softmax weights are rounded to bf16, sums are fp32; results do
+ * apart; out bf16 [R][n_head*64], which may not overlap q.  A row with row_pos -1 or a negative row_stream has no keys: its output
+ * is zero.  Several rows may belong to one stream.  Keys on a page outside 0..n_pages-1 are left out, as are those behind the
+ * list's pages_per_stream pages.  K and V of the shared pages must be finite.  fp32 queries enter with 16 bits, the softmax weights are rounded to bf16, sums are fp32; results do
  * not depend on timing.  R <= 4096.
  * scratch (256-byte aligned, >= scratch_bytes; zero before its first use, by this call or op_attention_cross, in any size)
  * belongs to one call at a time: calls that may overlap, replays of captured graphs among them, need one each.  Its first

@@ -263,15 +263,17 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
     e = min(max(a.k_start[i + 1], b), a.k_rows);
   };
   const int prefix_keys = SHARED ? a.n_shared * kPageTokens : 0;
-  auto own_keys = [&](int r) { return min(max(a.row_pos[r] + 1, 0), a.pps * kPageTokens) - prefix_keys; };   // may be negative
+  // keys of a row: none where it is padding, of no stream
+  auto row_keys = [&](int r) { return stream_s[r] < 0 ? 0 : min(max(a.row_pos[r], -1), a.pps * kPageTokens - 1) + 1; };
+  auto own_keys = [&](int r) { return row_keys(r) - prefix_keys; };   // may be negative
   int carry = 0;
   for (int base = 0; base < n_items; base += kUnWarps * 32) {
     const int i = base + tid;
     int u = 0;
     if (i < n_items) {
       if (SHARED) {
-        const int n = own_keys(i);
         stream_s[i] = a.row_stream[i];
+        const int n = own_keys(i);
         atomicMax(&lead_s, ((unsigned long long)(unsigned)(n + prefix_keys) << 32) | (unsigned)i);
         u = n > 0 ? 1 + (n + kUnKeys - 1) / kUnKeys : (a.n_shared == 0 ? 1 : 0);   // a row without any key still gets its zeros
       } else {
@@ -515,8 +517,8 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         whole = true;
         if constexpr (SHARED) {
           if (!own) {                            // a row may end inside the shared pages
-            vis0 = g < n_i ? a.row_pos[row0 + a.by_G.of(g)] + 1 : prefix_keys;
-            vis1 = g + 8 < n_i ? a.row_pos[row0 + a.by_G.of(g + 8)] + 1 : prefix_keys;
+            vis0 = g < n_i ? row_keys(row0 + a.by_G.of(g)) : prefix_keys;
+            vis1 = g + 8 < n_i ? row_keys(row0 + a.by_G.of(g + 8)) : prefix_keys;
             whole = __all_sync(0xFFFFFFFFu, vis0 >= prefix_keys && vis1 >= prefix_keys);
           }
         }

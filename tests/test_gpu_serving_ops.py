@@ -156,6 +156,18 @@ def test_shared_prefix_padding_short_rows_and_rows_of_one_stream(fmt):
     assert torch.all(out[7:] == 0)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_shared_prefix_padding_rows_whose_positions_were_left(fmt):
+    # a row of no stream is padding whatever its position says: it has no keys, and its length, the longest, says nothing about the others
+    c = Cache(7, fmt, 2, 2, [40, 0, 9], pad=3, same_stream=[(1, 1, 70)])
+    pos = c.args[2].clone()
+    pos[3:] = torch.tensor([500, 0, 2 ** 31 - 1], dtype=torch.int32)
+    q = _q(5, 6, 4, torch.float32)
+    got = B.op_attention_shared(q, c.pool, c.args[0], c.args[1], pos, 2)
+    c.check(got, q, "left positions")
+    assert torch.all(got[3:].view(torch.bfloat16) == 0)
+
+
 def test_shared_prefix_of_padding_rows_alone():
     c = Cache(6, "bf16", 2, 3, [], pad=5)
     c.args = (torch.zeros(1, 4, dtype=torch.int32, device=DEV),) + c.args[1:]
