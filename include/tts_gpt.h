@@ -425,7 +425,7 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
 /* Attention to an encoder's states: n sequences, queries q_start[i] .. q_start[i+1]-1 (rows of q) over keys
  * k_start[i] .. k_start[i+1]-1 (rows of k and v), all of them, o = softmax(scale q.K^T) V per head.  Lengths are ragged and
  * independent; a sequence without keys has zero outputs, rows outside every sequence are left as they were.  q_start, k_start:
- * ascending, n + 1 each, at most q_rows and k_rows; q_max: at least the longest sequence of queries (rows beyond it are not
+ * ascending (where one does not, nothing is written), n + 1 each, at most q_rows and k_rows; q_max: at least the longest sequence of queries (rows beyond it are not
  * computed).  q, k, v, out of one type, TTS_GPT_T_BF16 or TTS_GPT_T_F16; q rows q_stride elements apart with contiguous heads, k and v with
  * strides of rows and of heads (so both [rows][heads][64], parts of one array, and [heads][rows][64]); out [q_rows][n_head*64], which
  * may overlap none of them.

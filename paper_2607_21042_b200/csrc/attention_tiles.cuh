@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
     b = min(max(a.k_start[i], 0), a.k_rows);
     e = min(max(a.k_start[i + 1], b), a.k_rows);
   };
-  int carry = 0;
+  int carry = 0, bad = 0;                      // bad: starts that do not ascend, whose blocks nothing bounds
   for (int i0 = 0; i0 < a.n_seq; i0 += kTlThreads) {
     const int i = i0 + tid;
     int u = 0;
@@ -132,6 +132,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
       int qb, qe, kb, ke;
       q_span(i, qb, qe);
       k_span(i, kb, ke);
+      bad |= a.q_start[i + 1] < a.q_start[i] || a.k_start[i + 1] < a.k_start[i];
       u = a.Hkv * a.by_rpt.of(qe - qb + a.rpt - 1) * (1 + (ke - kb + kTlKeys - 1) / kTlKeys);
     }
     int incl = u;
@@ -142,14 +143,14 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
     }
     __syncthreads();
     if (lane == 31) sh.warp_tot[warp] = incl;
-    __syncthreads();
+    bad = __syncthreads_or(bad);
     int before = carry, all = carry;
 #pragma unroll
     for (int w = 0; w < kTlThreads / 32; ++w) { if (w < warp) before += sh.warp_tot[w]; all += sh.warp_tot[w]; }
     if (i < a.n_seq) first[i] = before + incl - u;
     carry = all;
   }
-  const int T = carry;
+  const int T = bad ? 0 : carry;
   if (tid == 0) {
     first[a.n_seq] = T;
     sh.size.set(max(2, (T + (int)gridDim.x - 1) / (int)gridDim.x));

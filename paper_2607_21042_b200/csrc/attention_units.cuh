@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   // keys of a row: none where it is padding, of no stream
   auto row_keys = [&](int r) { return stream_s[r] < 0 ? 0 : min(max(a.row_pos[r], -1), a.pps * kPageTokens - 1) + 1; };
   auto own_keys = [&](int r) { return row_keys(r) - prefix_keys; };   // may be negative
-  int carry = 0;
+  int carry = 0, bad = 0;                      // bad: starts that do not ascend, whose units nothing bounds
   for (int base = 0; base < n_items; base += kUnWarps * 32) {
     const int i = base + tid;
     int u = 0;
@@ -280,6 +280,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         int qb, qe, kb, ke;
         q_span(i, qb, qe);
         k_span(i, kb, ke);
+        bad |= a.q_start[i + 1] < a.q_start[i] || a.k_start[i + 1] < a.k_start[i];
         u = a.Hkv * a.by_rpt.of(qe - qb + a.rpt - 1) * (1 + (ke - kb + kUnKeys - 1) / kUnKeys);
       }
     }
@@ -291,13 +292,15 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
     }
     __syncthreads();
     if (lane == 31) warp_tot[warp] = incl;
-    __syncthreads();
+    if constexpr (SHARED) __syncthreads();
+    else bad = __syncthreads_or(bad);
     int before = carry, all = carry;
 #pragma unroll
     for (int w = 0; w < kUnWarps; ++w) { if (w < warp) before += warp_tot[w]; all += warp_tot[w]; }
     if (i < n_items) first[i] = before + incl - u;
     carry = all;
   }
+  if (bad) carry = 0;
   if (tid == 0) first[n_items] = carry;
   __syncthreads();
   const int lead = (int)(lead_s & 0xFFFFFFFFu), lead_keys = (int)(lead_s >> 32);

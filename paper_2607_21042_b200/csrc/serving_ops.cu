@@ -126,11 +126,11 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
   if (!aligned(q, 16) || q_stride % (type == TTS_GPT_T_F32 ? 4 : 8) || !aligned(kv_layer, 16) || !aligned(out, 16) || !aligned(scratch, 256) ||
       !aligned(page_table, 4) || !aligned(row_stream, 4) || !aligned(row_pos, 4))
     return fail_op(TTS_GPT_E_ARG, "op_attention_shared: q rows, out and the KV pool must be 16-byte aligned, scratch 256-byte, index arrays 4-byte");
-  // units of 32 keys are numbered in 31 bits, blocks of the pool too
+  // units of 32 keys are numbered in 31 bits, one of them for what a division rounds up; blocks of the pool too
   const int G = n_head / n_kv_head;
   const long long tiles = (long long)n_kv_head * ((R + kUnTile / G - 1) / (kUnTile / G));
   const long long units = tiles * (2ll * n_shared + 1) + (long long)R * n_kv_head * (2ll * (pages_per_stream - n_shared) + 1);
-  if (pages_per_stream > (1 << 24) || units >= (1ll << 31) ||
+  if (pages_per_stream > (1 << 24) || units >= (1ll << 30) ||
       2ll * n_pages * n_kv_head >= (1ll << 31))
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_shared: too many pages");
   if (scratch_size < scratch_bytes(shared_part_rows(R, n_kv_head, G)))
@@ -183,16 +183,17 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   if (k_rows > 1 && (k_stride < kHeadDim || v_stride < kHeadDim)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: rows of K or V overlap");
   if (n_kv_head > 1 && k_rows > 0 && (k_head_stride < kHeadDim || v_head_stride < kHeadDim)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: heads of K or V overlap");
   if (n > kUnMaxSeq) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: at most %d sequences", kUnMaxSeq);
+  if (q_rows > (1 << 30) || k_rows > (1 << 30)) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: at most 2^30 rows");
   if (q_max > q_rows) q_max = q_rows;
   const int G = n_head / n_kv_head;
   // Up to two tiles of 16 read K and V at most twice; more rows take a tile of 256, which reads them once (us, 16 sequences of 90 to 1500 keys
   // by 20 heads, warp-level / tcgen05: 20 queries 32 / 41, 48 queries 43 / 41, 128 queries 71 / 45)
   const bool tiles = q_max * G > 2 * kUnTile && n <= kTlMaxSeq;
-  // units and blocks of keys are numbered in 31 bits
+  // units and blocks of keys are numbered in 31 bits, one of them for what a division rounds up
   const int rpt = tiles ? 2 * (kTlRows / G) : kUnTile / G, keys = tiles ? kTlKeys : kUnKeys;
   const long long blocks = std::min((long long)n * ((q_max + rpt - 1) / rpt), (long long)q_rows / rpt + n);
-  if ((long long)n_kv_head * blocks * ((long long)k_rows / keys + 2) >= (1ll << 31) &&
-      (long long)n_kv_head * ((q_max + rpt - 1) / rpt) * ((long long)k_rows / keys + 2 * n) >= (1ll << 31))
+  if ((long long)n_kv_head * blocks * ((long long)k_rows / keys + 2) >= (1ll << 30) &&
+      (long long)n_kv_head * ((q_max + rpt - 1) / rpt) * ((long long)k_rows / keys + 2 * n) >= (1ll << 30))
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: too many queries times keys");
   if (scratch_size < scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())))
     return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_cross: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())));

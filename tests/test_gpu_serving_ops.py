@@ -320,6 +320,19 @@ def test_cross_attention_neighbours_infinities_and_peaked_scores(ql):
     c.check(got, "neighbours")
 
 
+@pytest.mark.parametrize("ql", [[2, 2, 2], [150, 200, 150]])
+def test_cross_attention_writes_nothing_where_starts_do_not_ascend(ql):
+    c = CrossCase(24, torch.bfloat16, 2, 2, ql, [37, 50, 41])
+    scratch = B.op_attention_cross_scratch(DEV)
+    for at in (3, 4):
+        args = list(c.args)
+        args[at] = args[at][[0, 2, 1, 3]].contiguous()
+        out = torch.full(c.q.shape, 9.0, dtype=c.dtype, device=DEV)
+        B.op_attention_cross(*args, out=out, scratch=scratch)
+        assert torch.all(out == 9.0)
+    c.check(c.run(scratch=scratch), "after them")
+
+
 def test_cross_attention_with_no_keys_at_all_and_no_queries():
     q = torch.ones(3, 4, 64, dtype=torch.bfloat16, device=DEV)
     k = torch.empty(0, 4, 64, dtype=torch.bfloat16, device=DEV)
