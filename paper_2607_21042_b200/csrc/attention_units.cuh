@@ -263,18 +263,16 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
     e = min(max(a.k_start[i + 1], b), a.k_rows);
   };
   const int prefix_keys = SHARED ? a.n_shared * kPageTokens : 0;
-  // keys of a row: none where it is padding, of no stream
-  auto row_keys = [&](int r) { return stream_s[r] < 0 ? 0 : min(max(a.row_pos[r], -1), a.pps * kPageTokens - 1) + 1; };
-  auto own_keys = [&](int r) { return row_keys(r) - prefix_keys; };   // may be negative
+  auto row_keys = [&](int r) { return min(max(a.row_pos[r], -1), a.pps * kPageTokens - 1) + 1; };   // of a row of no stream: none, whatever this says
   int carry = 0, bad = 0;                      // bad: starts that do not ascend, whose units nothing bounds
   for (int base = 0; base < n_items; base += kUnWarps * 32) {
     const int i = base + tid;
     int u = 0;
     if (i < n_items) {
       if (SHARED) {
-        stream_s[i] = a.row_stream[i];
-        const int n = own_keys(i);
-        atomicMax(&lead_s, ((unsigned long long)(unsigned)(n + prefix_keys) << 32) | (unsigned)i);
+        const int s = a.row_stream[i], all = row_keys(i), keys = s < 0 ? 0 : all, n = keys - prefix_keys;   // n may be negative
+        stream_s[i] = s;
+        atomicMax(&lead_s, ((unsigned long long)(unsigned)keys << 32) | (unsigned)i);
         u = n > 0 ? 1 + (n + kUnKeys - 1) / kUnKeys : (a.n_shared == 0 ? 1 : 0);   // a row without any key still gets its zeros
       } else {
         int qb, qe, kb, ke;
@@ -353,7 +351,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         d.hn = kvh | (a.G << 16);
         kk = k - 1;
         page = a.n_shared + (kk >> 1); list = r;
-        n = kk < 0 ? 0 : min(kUnKeys, own_keys(r) - kk * kUnKeys);
+        n = kk < 0 ? 0 : min(kUnKeys, row_keys(r) - prefix_keys - kk * kUnKeys);
       }
       d.row0 = r;
       d.c1 = (kk & 1) * kUnKeys;
@@ -520,8 +518,9 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         whole = true;
         if constexpr (SHARED) {
           if (!own) {                            // a row may end inside the shared pages
-            vis0 = g < n_i ? row_keys(row0 + a.by_G.of(g)) : prefix_keys;
-            vis1 = g + 8 < n_i ? row_keys(row0 + a.by_G.of(g + 8)) : prefix_keys;
+            const int r0 = row0 + a.by_G.of(min(g, n_i - 1)), r1 = row0 + a.by_G.of(min(g + 8, n_i - 1)), k0 = row_keys(r0), k1 = row_keys(r1);
+            vis0 = stream_s[r0] < 0 ? 0 : k0;
+            vis1 = stream_s[r1] < 0 ? 0 : k1;
             whole = __all_sync(0xFFFFFFFFu, vis0 >= prefix_keys && vis1 >= prefix_keys);
           }
         }
