@@ -8,13 +8,20 @@
 //                   back into tensor memory.  The reference moves, and O with it, only where a score exceeds it by 2^8: weights
 //                   stay below 256 and the rounding of a weight is relative, so nothing is lost
 //     O += P V      M=128 x N=64 x K=128, P as the operand in tensor memory, V as stored
-// S takes 128 columns, P 64 and O 64 of each half: all of an SM's tensor memory.  One half's softmax runs while the other's products
-// do.  With 128 rows a CTA, two or four CTAs an SM, a block's copies alone took 1460 cycles of an SM (K and V came out of L2 for
-// every 128 rows, 6.2 TB/s); for 256 rows they are half of that, and the exponentials, 16 a cycle and SM, bound the kernel.
+// S takes 128 columns, P 64 and O 64 of each half: all of an SM's tensor memory.  S of block j + 1 is computed while the softmax works on
+// S of block j, which by then is in registers; one half's softmax runs beside the other's.
 //
-// Work split.  The blocks of all tiles are laid end to end and cut into one range a CTA, equal to within a block; a tile counts
-// one block more than its keys have.  The parts of a tile that several CTAs share meet as in the warp-level kernel: in scratch,
-// added in the order of their keys by the CTA that arrives last at the tile's ticket.  Every wait on a copy or a product is bounded.
+// Bound and measurements.  A block of 256 rows by 128 keys is 1024 tensor cycles, and 2048 cycles of exponentials at 16 a cycle and
+// SM; a quarter of them goes through a polynomial on the FMA pipes (every 8th, 4th, 3rd, 2nd pair: 99, 94, 95, 107 us for 8 sequences
+// of 517 to 1500 queries by 700 to 1500 keys, 20 heads, fp16; none: 99).  With the loads and stores of tensor memory and the maximum a
+// block takes some 2500 cycles, a change of tile 4500.  Those sequences take 94 us, 0.52 PFLOP/s; 1536 by 1536 take 145 us, 0.67 PFLOP/s.
+// What came before: S only once P of the block before was there 102 us (3000 cycles a block, though no pipe had more than 2048 to do);
+// 128 rows a CTA, two or four CTAs an SM, K and V out of L2 twice as often 131 us; two threads a row 134 us.
+//
+// Work split.  Tiles are laid end to end by what they cost (blocks of one half or two, a tile besides its blocks) and cut into equal
+// ranges, one a CTA.  A part of a tile that several CTAs share goes to scratch with a ticket; the CTA that comes last adds the
+// parts in the order of their keys, so that results do not depend on timing.  As a rule that is the CTA in which the tile begins, at
+// the end of its range, with its own part, the first, still in registers.  Every wait on a copy or a product is bounded.
 #pragma once
 #include "attention_units.cuh"
 
@@ -33,10 +40,12 @@ constexpr int kTlQ = kTlTile * 128;         // Q of a tile: 32 KB
 constexpr int kTlMaxSeq = 2048;
 constexpr int kTlMaxCtas = kUnMaxCtas;
 constexpr float kTlSlack = 8.0f;            // log2 by which a score may exceed the reference
+// What a range is measured in, about 700 cycles each: a block of both halves, of one half alone, and a tile besides its blocks.
+constexpr int kTlCost2 = 4, kTlCost1 = 3, kTlCostTile = 6;
 
 // The part of a tile that lies in a CTA's range.
 struct TilePart {
-  int row0, n_i, kvh, u0, nu;     // first query row, rows times heads, head of keys; the tile's units
+  int row0, n_i, kvh, u0, nu;     // first query row, rows times heads, head of keys; where the tile's cost begins, its cost
   int j0, j1, key0, keys;         // its blocks here; first key row and number of keys of the sequence
 };
 constexpr int kTlParts = 4;       // that the copying warp is ahead at most
@@ -49,6 +58,7 @@ struct TileShared {
   uint64_t s_full[2], p_full[2], pv_done[2];   // by half
   uint32_t tmem;
   int failed;
+  TilePart meets;                 // the tile that began before the CTA's range
   Div size;
   int warp_tot[kTlThreads / 32];
 };
@@ -82,6 +92,29 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// 2^x of two values by additions and products: x = n + f with n the nearest integer and |f| <= 1/2, 2^f by the polynomial of degree 5 with
+// the least relative error there (found by iterated least squares; 2.1e-07 with all roundings), times 2^n put together from its bits.  Zero below 2^-126;
+// x <= 127; NaN stays NaN.
+__device__ __forceinline__ unsigned long long poly_exp2(unsigned long long x2) {
+  constexpr float kMagic = 12582912.0f;        // 1.5 * 2^23: the sum's last bits are n
+  auto both = [](float v) { return pack_f32x2(v, v); };
+  float x, y;
+  unpack_f32x2(x2, x, y);
+  x2 = pack_f32x2(max_nan(x, -127.0f), max_nan(y, -127.0f));
+  const unsigned long long z2 = add_f32x2(x2, both(kMagic)), f2 = add_f32x2(x2, fma_f32x2(z2, both(-1.0f), both(kMagic)));
+  unsigned long long p2 = fma_f32x2(f2, both(0.00132764608f), both(0.00967554096f));
+  p2 = fma_f32x2(p2, f2, both(0.0555071346f));
+  p2 = fma_f32x2(p2, f2, both(0.240221202f));
+  p2 = fma_f32x2(p2, f2, both(0.693146944f));
+  p2 = fma_f32x2(p2, f2, both(1.00000012f));
+  unpack_f32x2(z2, x, y);
+  return mul_f32x2(p2, pack_f32x2(__int_as_float((__float_as_int(x) << 23) + 0x3F800000), __int_as_float((__float_as_int(y) << 23) + 0x3F800000)));
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // A in tensor memory (row = lane, two 16-bit values of consecutive k a column), B in shared memory
@@ -124,6 +157,17 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
     b = min(max(a.k_start[i], 0), a.k_rows);
     e = min(max(a.k_start[i + 1], b), a.k_rows);
   };
+  // a head of a sequence: tiles, of which the last may have one half; cost of a tile, a block of the last one, and all of them
+  struct SeqCost { int tiles, blocks, full, last_block, head; };
+  auto seq_cost = [&](int q, int k) {
+    SeqCost c;
+    c.tiles = a.by_rpt.of(q + a.rpt - 1);
+    c.blocks = (k + kTlKeys - 1) / kTlKeys;
+    c.full = kTlCostTile + kTlCost2 * c.blocks;
+    c.last_block = q - (c.tiles - 1) * a.rpt > (a.rpt >> 1) ? kTlCost2 : kTlCost1;
+    c.head = c.tiles > 0 ? (c.tiles - 1) * c.full + kTlCostTile + c.last_block * c.blocks : 0;
+    return c;
+  };
   int carry = 0, bad = 0;                      // bad: starts that do not ascend, whose blocks nothing bounds
   for (int i0 = 0; i0 < a.n_seq; i0 += kTlThreads) {
     const int i = i0 + tid;
@@ -133,7 +177,8 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
       q_span(i, qb, qe);
       k_span(i, kb, ke);
       bad |= a.q_start[i + 1] < a.q_start[i] || a.k_start[i + 1] < a.k_start[i];
-      u = a.Hkv * a.by_rpt.of(qe - qb + a.rpt - 1) * (1 + (ke - kb + kTlKeys - 1) / kTlKeys);
+      const SeqCost c = seq_cost(qe - qb, ke - kb);
+      u = a.Hkv * c.head;
     }
     int incl = u;
 #pragma unroll
@@ -153,7 +198,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
   const int T = bad ? 0 : carry;
   if (tid == 0) {
     first[a.n_seq] = T;
-    sh.size.set(max(2, (T + (int)gridDim.x - 1) / (int)gridDim.x));
+    sh.size.set(max(2 * kTlCost2, (T + (int)gridDim.x - 1) / (int)gridDim.x));
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -170,15 +215,18 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
     int qb, qe, kb, ke;
     q_span(lo, qb, qe);
     k_span(lo, kb, ke);
+    const SeqCost c = seq_cost(qe - qb, ke - kb);
     p.key0 = kb; p.keys = ke - kb;
-    p.nu = 1 + (p.keys + kTlKeys - 1) / kTlKeys;
-    const int x = u - first[lo], tile = (int)((unsigned)x / (unsigned)p.nu), blocks = a.by_rpt.of(qe - qb + a.rpt - 1);
-    p.u0 = first[lo] + tile * p.nu;
-    p.kvh = (int)((unsigned)tile / (unsigned)blocks);
-    p.row0 = qb + (tile - p.kvh * blocks) * a.rpt;
+    p.kvh = (int)((unsigned)(u - first[lo]) / (unsigned)c.head);
+    p.u0 = first[lo] + p.kvh * c.head;
+    const int tile = min((int)((unsigned)(u - p.u0) / (unsigned)c.full), c.tiles - 1), block = tile + 1 < c.tiles ? kTlCost2 : c.last_block;
+    p.u0 += tile * c.full;
+    p.nu = kTlCostTile + block * c.blocks;
+    p.row0 = qb + tile * a.rpt;
     p.n_i = min(a.rpt, qe - p.row0) * a.G;
-    p.j0 = max(u - p.u0 - 1, 0);
-    p.j1 = min(u_end - p.u0, p.nu) - 1;
+    auto blocks_before = [&](int x) { return min((int)((unsigned)(max(x - p.u0 - kTlCostTile, 0) + block - 1) / (unsigned)block), c.blocks); };   // that begin before x
+    p.j0 = blocks_before(u);
+    p.j1 = blocks_before(u_end);
     return p;
   };
   auto wait = [&](uint64_t *bar, uint32_t parity) {   // the whole warp; false: some wait of the CTA has run out
@@ -217,7 +265,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
         if (lane == 0) { sh.part[k] = p; mbar_arrive(&sh.part_full[k]); }
         __syncwarp();
         ++n_part;
-        u = p.u0 + p.j1 + 1;
+        u = p.u0 + p.nu;
         if (p.j1 <= p.j0) continue;
         const int qb = n_tile & 1;
         if (n_tile >= 2 && !wait_warp(&sh.q_free[qb], (uint32_t)(n_tile / 2 - 1) & 1u)) break;
@@ -244,64 +292,57 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
         if (!fine) break;
       }
     } else if (warp == 9) {
-      // ---- products: of either half in turn, when P of block j - 1 is there (and S has been read), Q K^T of block j, which its softmax
-      //      waits for, and P V of block j - 1 behind it.  (Q K^T ahead of P, with a barrier of its own, made seven waits of this warp a
-      //      block where there are three: 106 -> 165 us.) ----
+      // ---- products: of either half in turn.  A half's turn k comes when its softmax has taken S of block k into registers and
+      //      left P of block k - 1: then P V of block k - 1 and Q K^T of block k + 1 are issued, one wait and one commit for both (a wait
+      //      and a commit for each product made seven waits of this warp a block: 106 us where 102 were) ----
       const uint32_t kind = F16 ? ~((1u << 7) | (1u << 10)) : ~0u;
       const uint32_t idesc_qk = tc_instr_desc(kTlRows, kTlKeys) & kind, idesc_pv = (tc_instr_desc(kTlRows, kHeadDim) & kind) | (1u << 16);   // V is MN-major
       int n_tile = 0, n_part = 0;                // tiles with blocks, and parts of this CTA
       bool fine = true;
       const uint64_t dring = tc_smem_desc(ring);
-      int done[2] = {0, 0}, n_block = 0;       // blocks of either half that have had their P V, blocks of the CTA
-      // P V of the block that half h has come to, block b of the CTA; last: no other half reads that block any more
-      auto pv = [&](int h, int b, bool begins, bool last) {
-        const int s = b % kTlRing;
-        const uint64_t dv = dring + (uint64_t)((s * kTlBlock + kTlHalf) >> 4);
-        const uint32_t t = tmem + 256u * h;
-        if (elect_one()) {
-#pragma unroll
-          for (int q = 0; q < kTlKeys / 16; ++q)   // 16 keys an instruction: 8 columns of P, two groups of 8 rows of V
-            tc_mma_ts(t + 192u, t + 128u + 8u * q, dv + 128 * q, idesc_pv, begins && q == 0 ? 0u : 1u);
-          tc_commit(&sh.pv_done[h]);
-          if (last) tc_commit(&sh.empty[s]);
-        }
-        __syncwarp();
-        ++done[h];
-      };
+      uint32_t odd = 0, n_block = 0;             // bit h: half h has had an odd number of turns; blocks of the CTA
       for (int u = u_begin; u < u_end && fine;) {
         TilePart p;
         fine = take_part(n_part++, p);
         if (!fine) break;
-        u = p.u0 + p.j1 + 1;
+        u = p.u0 + p.nu;
         if (p.j1 <= p.j0) continue;
         const int qb = n_tile & 1, halves = p.n_i > (a.rpt >> 1) * a.G ? 2 : 1;
         fine = wait_warp(&sh.q_full[qb], (uint32_t)(n_tile / 2) & 1u);
         ++n_tile;
         const uint64_t dq = tc_smem_desc(Qs + qb * kTlQ);
-        for (int j = p.j0; j < p.j1 && fine; ++j, ++n_block) {
-          fine = wait_warp(&sh.full[n_block % kTlRing], (uint32_t)(n_block / kTlRing) & 1u);
-          const uint64_t dk = dring + (uint64_t)((n_block % kTlRing * kTlBlock) >> 4);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (h == halves || !fine) break;
-            if (j > p.j0) fine = wait_warp(&sh.p_full[h], (uint32_t)done[h] & 1u);
-            if (!fine) break;
-            tc_fence_after_sync();
+        const int nb = p.j1 - p.j0;
+#pragma unroll 1
+        for (int k = -1; k <= nb && fine; ++k) {   // turn k: P V of block k - 1 and Q K^T of block k + 1
+          const uint32_t s_qk = (n_block + k + 1) % kTlRing, s_pv = (n_block + k - 1) % kTlRing;
+          if (k + 1 < nb) fine = wait_warp(&sh.full[s_qk], (n_block + k + 1) / kTlRing & 1u);
+          const uint64_t dk = dring + (uint64_t)((s_qk * kTlBlock) >> 4), dv = dring + (uint64_t)((s_pv * kTlBlock + kTlHalf) >> 4);
+#pragma unroll 1
+          for (int h = 0; h < halves && fine; ++h) {
+            if (k >= 0) {
+              fine = wait_warp(&sh.p_full[h], odd >> h & 1u);
+              odd ^= 1u << h;
+              if (!fine) break;
+              tc_fence_after_sync();
+            }
+            const uint32_t t = tmem + 256u * h;
             if (elect_one()) {
+              if (k >= 1) {
 #pragma unroll
-              for (int q = 0; q < 4; ++q) tc_mma(tmem + 256u * h, dq + (uint64_t)(h * (kTlHalf >> 4) + 2 * q), dk + 2 * q, idesc_qk, q == 0 ? 0u : 1u);
-              tc_commit(&sh.s_full[h]);
+                for (int q = 0; q < kTlKeys / 16; ++q)   // 16 keys an instruction: 8 columns of P, two groups of 8 rows of V
+                  tc_mma_ts(t + 192u, t + 128u + 8u * q, dv + 128 * q, idesc_pv, k == 1 && q == 0 ? 0u : 1u);
+                if (h + 1 == halves) tc_commit(&sh.empty[s_pv]);   // no other half reads that block any more
+              }
+              if (k + 1 < nb) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tc_mma(t, dq + (uint64_t)(h * (kTlHalf >> 4) + 2 * q), dk + 2 * q, idesc_qk, q == 0 ? 0u : 1u);
+              }
+              tc_commit(k < nb ? &sh.s_full[h] : &sh.pv_done[h]);
             }
             __syncwarp();
-            if (j > p.j0) pv(h, n_block - 1, j - 1 == p.j0, h + 1 == halves);
           }
         }
-        for (int h = 0; h < halves && fine; ++h) {   // the tile's last
-          fine = wait_warp(&sh.p_full[h], (uint32_t)done[h] & 1u);
-          if (!fine) break;
-          tc_fence_after_sync();
-          pv(h, n_block - 1, p.j1 - 1 == p.j0, h + 1 == halves);
-        }
+        n_block += nb;
       }
     }
   } else {
@@ -309,36 +350,102 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
     // ---- softmax ----
     const int half = warp >> 2, quarter = warp & 3, t = tid & (kTlRows - 1);   // the thread's row of the half
     const uint32_t t_lane = tmem + ((uint32_t)(32 * quarter) << 16) + 256u * half;
-    int i = 0, n_block = 0, n_tile = 0, n_part = 0;   // blocks of this half and of the CTA, tiles with blocks, parts
+    int i = 0, n_o = 0, n_block = 0, n_tile = 0, n_part = 0;   // waits of this half for s_full and for pv_done, blocks of the CTA, tiles with blocks, parts
     bool fine = true;
+    int came_first = 0;                        // how many had a ticket of the tile that began before the CTA's range, this CTA among them
+    const bool sound = __ldcg(a.err) == 0;   // the scratch
+    // A tile that several CTAs share has a place in each: 256 rows, 16 columns of four dimensions, then reference and sum.  A CTA has two
+    // places: for the tile that began before its range, and the one that goes on behind it.
+    auto part_at_place = [&](int c, int c0) { return a.part + (size_t)(2 * c + (c == c0)) * kTlTile * kUnPitch; };
+    auto add_parts = [&](int c0, int c, int c1, float (&o)[kHeadDim], float &m, float &l) {   // those of CTAs c .. c1, in the order of their keys
+#pragma unroll 1
+      for (; c <= c1; ++c) {
+        const float *x = part_at_place(c, c0);
+        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(x + kTlTile * kHeadDim + 2 * tid));
+        float4 v[kHeadDim / 4];
+#pragma unroll
+        for (int e = 0; e < kHeadDim / 4; ++e) v[e] = __ldcg(reinterpret_cast<const float4 *>(x + (e * kTlTile + tid) * 4));
+        const bool has = ml.y != 0.f;          // a key in it
+        const float mn = fmaxf(m, ml.x), fk = !has || m == mn ? 1.f : pt_exp2(m - mn), fn = has ? pt_exp2(ml.x - mn) : 0.f;
+        if (has) m = mn;
+        l = fmaf(l, fk, ml.y * fn);
+#pragma unroll
+        for (int e = 0; e < kHeadDim / 4; ++e) {
+          o[4 * e] = fmaf(o[4 * e], fk, v[e].x * fn); o[4 * e + 1] = fmaf(o[4 * e + 1], fk, v[e].y * fn);
+          o[4 * e + 2] = fmaf(o[4 * e + 2], fk, v[e].z * fn); o[4 * e + 3] = fmaf(o[4 * e + 3], fk, v[e].w * fn);
+        }
+      }
+    };
+    auto row_ptr = [&](const TilePart &p, int i2) {
+      const int r = a.by_G.of(i2);
+      return a.out + ((size_t)(p.row0 + half * (a.rpt >> 1) + r) * a.H + (p.kvh - r) * a.G + i2) * kHeadDim;
+    };
+    // the warp's rows, by way of shared memory: whole 128-byte rows
+    auto leave = [&](const TilePart &p, int n_i, const float (&o)[kHeadDim], float l, unsigned char *stage) {
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+      for (int c = 0; c < kHeadDim; c += 8)
+        *reinterpret_cast<uint4 *>(stage + t * 128 + (((c >> 3) ^ (t & 7)) << 4)) =
+            make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
+                       un_pack<F16>(o[c + 4] * inv, o[c + 5] * inv), un_pack<F16>(o[c + 6] * inv, o[c + 7] * inv));
+      __syncwarp();
+#pragma unroll
+      for (int it = 0; it < 8; ++it) {
+        const int r = 32 * quarter + 4 * it + (lane >> 3), c8 = lane & 7;
+        if (r < n_i && sound && !*failed) *reinterpret_cast<uint4 *>(row_ptr(p, r) + 8 * c8) = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((c8 ^ (r & 7)) << 4));
+      }
+    };
     for (int u = u_begin; u < u_end && fine;) {
-      TilePart p;
-      fine = take_part(n_part++, p);
+      const int place_p = n_part % kTlParts;
+      fine = wait_warp(&sh.part_full[place_p], (uint32_t)(n_part / kTlParts) & 1u);
       if (!fine) break;
-      u = p.u0 + p.j1 + 1;
+      ++n_part;
+      const TilePart &p = sh.part[place_p];
+      u = p.u0 + p.nu;
       const int n_half = (a.rpt >> 1) * a.G, n_i = min(p.n_i - half * n_half, n_half);   // rows of this half, none where not positive
       const bool live = 32 * quarter < n_i, mine = t < n_i;   // some row of the warp exists, the thread's own does
-      const int blocks = n_i > 0 ? p.j1 : p.j0;
-      if (n_i <= 0 && p.j1 > p.j0) {           // no such half here: no block holds it back, but it gives Q back below, once for each Q
+      const int j0 = p.j0, j1 = p.j1, keys = p.keys, blocks = n_i > 0 ? j1 : j0;
+      if (n_i <= 0 && j1 > j0) {           // no such half here: no block holds it back, but it gives Q back below, once for each Q
         fine = wait_warp(&sh.q_full[n_tile & 1], (uint32_t)(n_tile / 2) & 1u);
         if (!fine) break;
       }
       float m = -INFINITY, l = 0.f;
-      for (int j = p.j0; j < blocks; ++j, ++i) {
-        fine = wait_warp(&sh.s_full[half], (uint32_t)i & 1u);
+      auto pass_turn = [&]() {                       // to the products
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_full[half]);
+      };
+      if (blocks > j0) {
+        fine = wait_warp(&sh.s_full[half], (uint32_t)i++ & 1u);
         if (!fine) break;
         tc_fence_after_sync();
-        const int n = min(kTlKeys, p.keys - j * kTlKeys);
-        // all scores of the row into registers
-        float s[kTlKeys], sc = 1.f;
-        if (live) {
+      }
+      auto clear_v = [&](int j, int n) {       // the sequence's last block: V rows behind its keys may hold NaN, and 0 * NaN must not reach O
+        // (both halves write the same zeros, each ahead of its own P V; S of the block is there, so its K and V are)
+        unsigned char *v = ring + (n_block + j - j0) % kTlRing * kTlBlock + kTlHalf;
+        for (int x = n * 8 + t; x < kTlKeys * 8; x += kTlRows) *reinterpret_cast<uint4 *>(v + x * 16) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+      };
+      if (!live) {                             // no row of this warp exists: it takes its turns
+#pragma unroll 1
+        for (int j = j0; j < blocks; ++j) {
+          pass_turn();
+          fine = wait_warp(&sh.s_full[half], (uint32_t)i++ & 1u);
+          if (!fine) break;
+          if (keys - j * kTlKeys < kTlKeys) clear_v(j, keys - j * kTlKeys);
+        }
+      } else {
+#pragma unroll 1
+        for (int j = j0; j < blocks; ++j) {
+          const int n = min(kTlKeys, keys - j * kTlKeys);
+          // all scores of the row into registers; the next block's may then come in their place
+          float s[kTlKeys], sc = 1.f;
 #pragma unroll
           for (int c = 0; c < kTlKeys; c += 32) tmem_ld32_async(t_lane + (uint32_t)c, s + c);
           tmem_wait_ld();
 #pragma unroll
           for (int c = 0; c < kTlKeys; c += 32) tmem_landed32(s + c);
-        }
-        if (live) {
+          pass_turn();
           if (n < kTlKeys) {                   // scores of keys that do not exist
 #pragma unroll
             for (int e = 0; e < kTlKeys; ++e) s[e] = e < n ? s[e] : -INFINITY;
@@ -356,24 +463,30 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
           const float ref = m == -INFINITY ? 0.f : m;
           const unsigned long long scale2 = pack_f32x2(a.scale, a.scale), ref2 = pack_f32x2(-ref, -ref);
           unsigned long long sum2[4] = {0ull, 0ull, 0ull, 0ull};
+          auto weights = [&](int e0, int e1) {
 #pragma unroll
-          for (int e = 0; e < kTlKeys; e += 2) {
-            float x, y;
-            unpack_f32x2(fma_f32x2(pack_f32x2(s[e], s[e + 1]), scale2, ref2), x, y);
-            x = pt_exp2(x); y = pt_exp2(y);
-            sum2[(e >> 1) & 3] = add_f32x2(sum2[(e >> 1) & 3], pack_f32x2(x, y));
-            s[e >> 1] = __uint_as_float(un_pack<F16>(x, y));
-          }
+            for (int e = e0; e < e1; e += 2) {
+              float x, y;
+              const unsigned long long d2 = fma_f32x2(pack_f32x2(s[e], s[e + 1]), scale2, ref2);
+              if ((e >> 1) % 4 == 3) {
+                unpack_f32x2(poly_exp2(d2), x, y);
+              } else {
+                unpack_f32x2(d2, x, y);
+                x = pt_exp2(x); y = pt_exp2(y);
+              }
+              sum2[(e >> 1) & 3] = add_f32x2(sum2[(e >> 1) & 3], pack_f32x2(x, y));
+              s[e >> 1] = __uint_as_float(un_pack<F16>(x, y));
+            }
+          };
+          weights(0, kTlKeys);
           float s0, s1;
           unpack_f32x2(add_f32x2(add_f32x2(sum2[0], sum2[1]), add_f32x2(sum2[2], sum2[3])), s0, s1);
           l = fmaf(l, sc, s0 + s1);
-        }
-        // P and O belong to the tensor core until P V of the block before has completed
-        if (j > p.j0) {
-          fine = wait_warp(&sh.pv_done[half], (uint32_t)(i - 1) & 1u);
+          // P V of the block before, to which P and O belong, and the scores of the next block, both under way since its turn began
+          fine = wait_warp(&sh.s_full[half], (uint32_t)i++ & 1u);
           if (!fine) break;
           tc_fence_after_sync();
-          if (__any_sync(0xFFFFFFFFu, sc != 1.f)) {
+          if (j > j0 && __any_sync(0xFFFFFFFFu, sc != 1.f)) {
 #pragma unroll
             for (int c = 0; c < kHeadDim; c += 32) {
               float o[32];
@@ -383,30 +496,21 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
               tmem_st32(t_lane + 192u + (uint32_t)c, o);
             }
           }
-        }
-        if (live) {
-#pragma unroll
-          for (int c = 0; c < kTlKeys / 2; c += 32) tmem_st32_async(t_lane + 128u + (uint32_t)c, s + c);
+          tmem_st32_async(t_lane + 128u, s);
+          tmem_st32_async(t_lane + 160u, s + 32);
           tmem_wait_st();
+          if (n < kTlKeys) clear_v(j, n);
         }
-        if (n < kTlKeys) {                     // the sequence's last block: V rows behind its keys may hold NaN, and 0 * NaN must not reach O
-          // (both halves write the same zeros, each ahead of its own P V; S of the block is there, so its K and V are)
-          unsigned char *v = ring + (n_block + j - p.j0) % kTlRing * kTlBlock + kTlHalf;
-          for (int x = n * 8 + t; x < kTlKeys * 8; x += kTlRows) *reinterpret_cast<uint4 *>(v + x * 16) = make_uint4(0, 0, 0, 0);
-          fence_proxy_async_smem();
-        }
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_full[half]);
       }
       if (!fine) break;
       // ---- the tile's rows leave ----
       float o[kHeadDim];
 #pragma unroll
       for (int c = 0; c < kHeadDim; ++c) o[c] = 0.f;
-      n_block += p.j1 - p.j0;
-      if (blocks > p.j0) {
-        fine = wait_warp(&sh.pv_done[half], (uint32_t)(i - 1) & 1u);
+      n_block += j1 - j0;
+      if (blocks > j0) {
+        pass_turn();
+        fine = wait_warp(&sh.pv_done[half], (uint32_t)n_o++ & 1u);
         if (!fine) break;
         tc_fence_after_sync();
         if (live) {
@@ -416,76 +520,60 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
         tc_fence_before_sync();                // O may be overwritten once this thread's next P is announced
       }
       const int c0 = size.of(p.u0), c1 = size.of(p.u0 + p.nu - 1);
-      bool write = c0 == c1;
-      if (!write) {
-        // a place of 256 rows: 16 columns of four dimensions, then reference and sum; for the tile that goes on behind a CTA's range, and
-        // the one that began before
-        auto place = [&](int c) { return a.part + (size_t)(2 * c + (c == c0)) * kTlTile * kUnPitch; };
+      bool whole = c0 == c1;
+      if (!whole) {                            // this part into scratch, and a ticket for the warp's 32 rows
+        const bool begins = c0 == (int)blockIdx.x;
         if (mine) {
-          float *x = place(blockIdx.x);
+          float *x = part_at_place(blockIdx.x, c0);
 #pragma unroll
           for (int c = 0; c < kHeadDim / 4; ++c) *reinterpret_cast<float4 *>(x + (c * kTlTile + tid) * 4) = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
           *reinterpret_cast<float2 *>(x + kTlTile * kHeadDim + 2 * tid) = make_float2(m, l);
         }
-        // a ticket for each warp's 32 rows
         __threadfence();
         __syncwarp();
-        int last = 0;
-        if (lane == 0) {
-          unsigned *tk = a.tickets + (kTlTile / 32) * c0 + warp;
-          last = atomicAdd(tk, 1u) + 1u == (unsigned)(c1 - c0 + 1);
-          if (last) *tk = 0u;
-        }
-        write = __shfl_sync(0xFFFFFFFFu, last, 0) != 0;
-        if (write && mine) {                   // all parts, this CTA's own among them, in the order of their keys
-          __threadfence();
-          m = -INFINITY; l = 0.f;
-#pragma unroll
-          for (int c = 0; c < kHeadDim; ++c) o[c] = 0.f;
-#pragma unroll 1
-          for (int c = c0; c <= c1; ++c) {
-            const float *x = place(c);
-            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(x + kTlTile * kHeadDim + 2 * tid));
-            const float mn = fmaxf(m, ml.x), fo = m == mn ? 1.f : pt_exp2(m - mn), fn = ml.y == 0.f ? 0.f : pt_exp2(ml.x - mn);   // 0: no key in it
-            if (ml.y != 0.f) m = mn;
-            const float fk = ml.y != 0.f ? fo : 1.f;
-            l = fmaf(l, fk, ml.y * fn);
-#pragma unroll
-            for (int e = 0; e < kHeadDim / 4; ++e) {
-              const float4 v = __ldcg(reinterpret_cast<const float4 *>(x + (e * kTlTile + tid) * 4));
-              o[4 * e] = fmaf(o[4 * e], fk, v.x * fn); o[4 * e + 1] = fmaf(o[4 * e + 1], fk, v.y * fn);
-              o[4 * e + 2] = fmaf(o[4 * e + 2], fk, v.z * fn); o[4 * e + 3] = fmaf(o[4 * e + 3], fk, v.w * fn);
-            }
+        int came = 0;
+        if (lane == 0) came = (int)atomicAdd(a.tickets + (kTlTile / 32) * c0 + warp, 1u) + 1;
+        if (begins) {                          // the CTA's last tile; as a rule the others have long had theirs
+          whole = __shfl_sync(0xFFFFFFFFu, came, 0) == c1 - c0 + 1;
+          if (whole) {
+            if (lane == 0) a.tickets[(kTlTile / 32) * c0 + warp] = 0u;
+            __threadfence();
+            if (mine) add_parts(c0, c0 + 1, c1, o, m, l);
           }
+        } else {                               // the CTA's first: the answer is looked at when its range is done
+          came_first = came;
+          if (lane == 0) sh.meets = p;         // (every warp writes the same)
         }
       }
-      write = write && !*failed && __ldcg(a.err) == 0;
-      const float inv = l == 0.f ? 0.f : 1.0f / l;
-      auto row_ptr = [&](int i2) { const int r = a.by_G.of(i2); return a.out + ((size_t)(p.row0 + half * (a.rpt >> 1) + r) * a.H + (p.kvh - r) * a.G + i2) * kHeadDim; };
-      if (p.j1 > p.j0) {                       // through the tile's Q, which no product reads any more: whole 128-byte rows leave
+      if (j1 > j0) {                           // through the tile's Q, which no product reads any more
         const int qb = n_tile++ & 1;
-        unsigned char *stage = Qs + qb * kTlQ + half * kTlHalf;
-        if (write && live) {
-#pragma unroll
-          for (int c = 0; c < kHeadDim; c += 8)
-            *reinterpret_cast<uint4 *>(stage + t * 128 + (((c >> 3) ^ (t & 7)) << 4)) =
-                make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
-                           un_pack<F16>(o[c + 4] * inv, o[c + 5] * inv), un_pack<F16>(o[c + 6] * inv, o[c + 7] * inv));
-          __syncwarp();
-#pragma unroll
-          for (int it = 0; it < 8; ++it) {
-            const int r = 32 * quarter + 4 * it + (lane >> 3), c8 = lane & 7;
-            if (r < n_i) *reinterpret_cast<uint4 *>(row_ptr(r) + 8 * c8) = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((c8 ^ (r & 7)) << 4));
-          }
-        }
+        if (whole && live) leave(p, n_i, o, l, Qs + qb * kTlQ + half * kTlHalf);
         fence_proxy_async_smem();              // Q of the tile after next is copied over it
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.q_free[qb]);
-      } else if (write && mine) {              // no block here, and no Q: zeros, or the sum of other CTAs' parts
+      } else if (whole && mine && sound && !*failed) {   // no block here, and no Q: zeros, or the sum of other CTAs' parts
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
         for (int c = 0; c < kHeadDim; c += 8)
-          *reinterpret_cast<uint4 *>(row_ptr(t) + c) = make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
-                                                                    un_pack<F16>(o[c + 4] * inv, o[c + 5] * inv), un_pack<F16>(o[c + 6] * inv, o[c + 7] * inv));
+          *reinterpret_cast<uint4 *>(row_ptr(p, t) + c) = make_uint4(un_pack<F16>(o[c] * inv, o[c + 1] * inv), un_pack<F16>(o[c + 2] * inv, o[c + 3] * inv),
+                                                                     un_pack<F16>(o[c + 4] * inv, o[c + 5] * inv), un_pack<F16>(o[c + 6] * inv, o[c + 7] * inv));
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.part_free[place_p]);
+    }
+    // ---- the tile that began before this CTA's range, where this CTA came to it last ----
+    if (fine && (came_first = __shfl_sync(0xFFFFFFFFu, came_first, 0)) > 0) {
+      const TilePart &p = sh.meets;
+      const int c0 = size.of(p.u0), c1 = size.of(p.u0 + p.nu - 1), n_half = (a.rpt >> 1) * a.G, n_i = min(p.n_i - half * n_half, n_half);
+      if (came_first == c1 - c0 + 1) {
+        if (lane == 0) a.tickets[(kTlTile / 32) * c0 + warp] = 0u;
+        __threadfence();
+        float m = -INFINITY, l = 0.f, o[kHeadDim];
+#pragma unroll
+        for (int c = 0; c < kHeadDim; ++c) o[c] = 0.f;
+        if (t < n_i) add_parts(c0, c0, c1, o, m, l);
+        // (through the first Q: the products of this half are done, and its other warps keep to their own rows)
+        if (32 * quarter < n_i) leave(p, n_i, o, l, Qs + half * kTlHalf);
       }
     }
   }

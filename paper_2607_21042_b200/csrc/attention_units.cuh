@@ -8,8 +8,8 @@
 //     O = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p,   M = max m_p,
 // with M, the sums and o in fp32; zero where no key is left.
 //
-// Work split.  The units of all tiles are laid end to end and cut into one range a warp, equal to within a unit whatever the
-// lengths are; a tile counts one unit more than its keys have, about what it costs besides them.  A tile inside one range, whose
+// Work split.  The units of all tiles are laid end to end and cut into ranges of equal size, one a warp, whatever the lengths
+// are; a tile counts one unit more than its keys have, about what it costs besides them.  A tile inside one range, whose
 // rows read no other keys, is finished by its warp.  The others' parts go to scratch and are added in the order of their keys, so
 // that results do not depend on timing and no warp waits for another:
 //   - by the CTA that comes last, at its end (cross attention, where only the tiles at a CTA's two ends reach another; few rows over
@@ -19,8 +19,16 @@
 //
 // Instructions.  Queries are the 16-row operand of m16n8k16, keys the 8-wide one, so the scores come out in the layout in which
 // P enters P V.  Queries in fp32 enter as two bf16 parts (16 bits), P is rounded to the cache's type (half a step of it: as
-// much again as the rounding of the output).  A unit is copied two or four ahead per warp, as 16-key boxes of K and of V with the
-// 128-byte swizzle; of the 8-bit cache as plain rows, whose codes become bf16 in registers (exact).
+// much again as the rounding of the output).  A warp copies two units ahead (three of the 8-bit cache), as 16-key boxes of K and of V
+// with the 128-byte swizzle; of the 8-bit cache as plain rows, whose codes become bf16 in registers (exact).
+//
+// Bound and measurements.  Where each row has keys of its own, the bytes: 128 rows behind 1024 shared tokens, 3 to 900 of their own,
+// 20 heads, bf16, 302 MB: 64 us, 4.7 TB/s, of which the start and the second kernel take 8; 16 queries of one token by 100 to 1500
+// keys, 20 heads, 65 MB: 20 us, half of them the start, the tickets and the merge.  Where many rows share keys, m16n8k16, which runs at about
+// 1/16 of the tcgen05 rate, and the code around it: 300 rows of 20 heads by 4, 1536 shared tokens, 8 bits: 44 us, 60 TFLOP/s; 16 by 32
+// queries by 90 to 1500 keys: 30 us.  Five rows behind 448 tokens: 10.6 us, latency from end to end.
+// Measured and not kept (us for 128 rows / 300 rows above): tiles of 32 rows 83 / 51; queries as the 8-wide operand 65 and 12.3 for five
+// rows; tickets instead of the second kernel 79 / 56.
 #pragma once
 #include <cuda_fp16.h>
 #include "page_tables.cuh"
@@ -762,9 +770,8 @@ inline cudaError_t units_pool_map(CUtensorMap *map, const void *pool, size_t blo
   const cuuint32_t box[3] = {kHeadDim, kUnBox, 1};
   return tensor_map_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, pool, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-// Rows of 64 values [64, tokens, heads], tokens and heads `row` and `head` bytes apart; `box_rows` tokens of one head a copy.  The token is
-// the second dimension even where heads lie closer together: a box of 128 tokens along the third dimension was copied at 16 bytes a
-// cycle and SM.
+// Rows of 64 values [64, tokens, heads], tokens and heads `row` and `head` bytes apart; `box_rows` tokens of one head a copy.  The order
+// of the two outer dimensions makes no difference in time.
 inline cudaError_t units_rows_map(CUtensorMap *map, bool f16, const void *base, size_t heads, size_t rows, size_t head, size_t row, int box_rows) {
   const cuuint64_t dims[3] = {kHeadDim, rows, heads}, strides[2] = {row, head};
   const cuuint32_t box[3] = {kHeadDim, (cuuint32_t)box_rows, 1};

@@ -10,7 +10,8 @@
 // Every CTA computes both running sums over all requests for itself (at most 4096 of them, out of L2) and then writes its share
 // of the rows and of the list entries, which it finds by bisection: one launch, no CTA waits for another.  What a caller may
 // update in place (contexts, stack height) is then written by the CTA that leaves last, when every CTA has read it.
-// Bound: two dependent reads (ids, contexts), one of the page stack, the launch; 12 bytes a row where there are many.
+// Bound: two dependent reads (ids, contexts), one of the page stack, the launch; 12 bytes a row where there are many.  16 requests of a
+// token 3.5 us, 128 requests 5.3 us, 1000 requests with half a million rows 6.8 us.
 #pragma once
 #include <cuda_fp8.h>
 #include <algorithm>
@@ -224,7 +225,7 @@ __device__ __forceinline__ void load8(const uint16_t *p, float (&x)[8]) {
 
 // Eight lanes take the 64 values of one (row, K|V, head), eight values each.  16-bit cache: each value rounded once.  8-bit cache:
 // s = max|x| / 448 over the 64 (1 if all are zero), codes e4m3(x / s).  Bound: bytes in and out; a thread has PER such pieces under
-// way, of rows far apart (3584 fp32 rows of 20 heads: one 11.8 us, 4.7 TB/s).
+// way, of rows far apart (3584 fp32 rows of 20 heads, 55 MB: four 10.4 us, 5.3 TB/s; one 11.8 us; 16 rows 1.8 us).
 constexpr int kAppendThreads = 256;
 template <typename Src, bool E4M3, int PER>
 __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const AppendArgs a) {

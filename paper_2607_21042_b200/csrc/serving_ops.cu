@@ -189,11 +189,12 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   // Up to two tiles of 16 read K and V at most twice; more rows take a tile of 256, which reads them once (us, 16 sequences of 90 to 1500 keys
   // by 20 heads, warp-level / tcgen05: 20 queries 32 / 41, 48 queries 43 / 41, 128 queries 71 / 45)
   const bool tiles = q_max * G > 2 * kUnTile && n <= kTlMaxSeq;
-  // units and blocks of keys are numbered in 31 bits, one of them for what a division rounds up
+  // units of keys are numbered in 31 bits, one of them for what a division rounds up; blocks by their cost
   const int rpt = tiles ? 2 * (kTlRows / G) : kUnTile / G, keys = tiles ? kTlKeys : kUnKeys;
+  const long long limit = (1ll << 30) / (tiles ? kTlCost2 : 1);
   const long long blocks = std::min((long long)n * ((q_max + rpt - 1) / rpt), (long long)q_rows / rpt + n);
-  if ((long long)n_kv_head * blocks * ((long long)k_rows / keys + 2) >= (1ll << 30) &&
-      (long long)n_kv_head * ((q_max + rpt - 1) / rpt) * ((long long)k_rows / keys + 2 * n) >= (1ll << 30))
+  if ((long long)n_kv_head * blocks * ((long long)k_rows / keys + 2) >= limit &&
+      (long long)n_kv_head * ((q_max + rpt - 1) / rpt) * ((long long)k_rows / keys + 2 * n) >= limit)
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: too many queries times keys");
   if (scratch_size < scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())))
     return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_cross: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())));

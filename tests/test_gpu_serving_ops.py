@@ -333,6 +333,17 @@ def test_cross_attention_writes_nothing_where_starts_do_not_ascend(ql):
     c.check(c.run(scratch=scratch), "after them")
 
 
+@pytest.mark.parametrize("ql", [[5, 5], [60, 70]])
+@pytest.mark.parametrize("key", [0, 5, 6, 7, 37, 130])
+def test_cross_attention_keeps_nan(ql, key):
+    # wherever the key lies that has it
+    c = CrossCase(25, torch.bfloat16, 2, 2, ql, [140, 33])
+    c.k[key] = float("nan")
+    got = c.run()
+    assert torch.isnan(got[:c.qs[1]]).all()
+    assert torch.isfinite(got[c.qs[1]:c.qs[2]]).all()
+
+
 def test_cross_attention_with_no_keys_at_all_and_no_queries():
     q = torch.ones(3, 4, 64, dtype=torch.bfloat16, device=DEV)
     k = torch.empty(0, 4, 64, dtype=torch.bfloat16, device=DEV)
