@@ -187,7 +187,8 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   if (q_max > q_rows) q_max = q_rows;
   const int G = n_head / n_kv_head;
   // Up to two tiles of 16 read K and V at most twice; more rows take a tile of 256, which reads them once (us, 16 sequences of 90 to 1500 keys
-  // by 20 heads, warp-level / tcgen05: 20 queries 32 / 41, 48 queries 43 / 41, 128 queries 71 / 45)
+  // by 20 heads, warp-level / tcgen05: 20 queries 27 / 32, 32 queries 30 / 33, 48 queries 35 / 33, 128 queries 63 / 35; four heads of
+  // keys, 7 queries of 5 heads each 18 / 16)
   const bool tiles = q_max * G > 2 * kUnTile && n <= kTlMaxSeq;
   // units of keys are numbered in 31 bits, one of them for what a division rounds up; blocks by their cost
   const int rpt = tiles ? 2 * (kTlRows / G) : kUnTile / G, keys = tiles ? kTlKeys : kUnKeys;
