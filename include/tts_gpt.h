@@ -429,7 +429,7 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
  * computed).  q, k, v, out of one type, TTS_GPT_T_BF16 or TTS_GPT_T_F16; q rows q_stride elements apart with contiguous heads, k and v with
  * strides of rows and of heads (so both [rows][heads][64], parts of one array, and [heads][rows][64]); out [q_rows][n_head*64], which
  * may overlap none of them.
- * Heads, roundings and scratch as for op_attention_shared (scratch size independent of the call).  n <= 4096. */
+ * Heads, roundings and scratch as for op_attention_shared (scratch size independent of the call).  n <= 4096, rows below 2^30. */
 int32_t tts_gpt_op_attention_cross_scratch_bytes(size_t *bytes);
 int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head, int32_t type, int32_t q_rows, const void *q,
                                    int64_t q_stride, int32_t k_rows, const void *k, int64_t k_stride, int64_t k_head_stride,

@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
       fine = wait_warp(&sh.part_full[place_p], (uint32_t)(n_part / kTlParts) & 1u);
       if (!fine) break;
       ++n_part;
-      const TilePart &p = sh.part[place_p];
+      const TilePart &p = sh.part[place_p];    // stays there until the tile's rows have left: its registers would be spilled
       u = p.u0 + p.nu;
       const int n_half = (a.rpt >> 1) * a.G, n_i = min(p.n_i - half * n_half, n_half);   // rows of this half, none where not positive
       const bool live = 32 * quarter < n_i, mine = t < n_i;   // some row of the warp exists, the thread's own does

@@ -183,7 +183,7 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   if (k_rows > 1 && (k_stride < kHeadDim || v_stride < kHeadDim)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: rows of K or V overlap");
   if (n_kv_head > 1 && k_rows > 0 && (k_head_stride < kHeadDim || v_head_stride < kHeadDim)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: heads of K or V overlap");
   if (n > kUnMaxSeq) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: at most %d sequences", kUnMaxSeq);
-  if (q_rows > (1 << 30) || k_rows > (1 << 30)) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: at most 2^30 rows");
+  if (q_rows >= (1 << 30) || k_rows >= (1 << 30)) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: rows must be below 2^30");
   if (q_max > q_rows) q_max = q_rows;
   const int G = n_head / n_kv_head;
   // Up to two tiles of 16 read K and V at most twice; more rows take a tile of 256, which reads them once (us, 16 sequences of 90 to 1500 keys

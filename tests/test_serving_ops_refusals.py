@@ -84,7 +84,7 @@ def _cross(**kw):
     (B.E_ARG, dict(scale=0.0)), (B.E_ARG, dict(scale=-1.0)), (B.E_ARG, dict(scale=float("nan"))), (B.E_ARG, dict(scale=float("inf"))), (B.E_ARG, dict(qs=248)),
     (B.E_ARG, dict(qs=260)), (B.E_ARG, dict(ks=132)), (B.E_ARG, dict(kh=32)), (B.E_ARG, dict(vh=68)), (B.E_ARG, dict(vs=8)), (B.E_ARG, dict(k=P + 8)),
     (B.E_ARG, dict(scratch=P + 16)), (B.E_ARG, dict(scratch=0)), (B.E_UNSUPPORTED, dict(n=4097)), (B.E_WORKSPACE, dict(size=1 << 20)),
-    (B.E_UNSUPPORTED, dict(qr=2 ** 24, q_max=2 ** 24, kr=2 ** 20)), (B.E_UNSUPPORTED, dict(qr=2 ** 30 + 1)), (B.E_UNSUPPORTED, dict(kr=2 ** 30 + 1)), (B.E_UNSUPPORTED, dict(n=1, heads=1, kv=1, qr=2 ** 22, q_max=2 ** 22, kr=2 ** 23)),
+    (B.E_UNSUPPORTED, dict(qr=2 ** 24, q_max=2 ** 24, kr=2 ** 20)), (B.E_UNSUPPORTED, dict(qr=2 ** 30)), (B.E_UNSUPPORTED, dict(kr=2 ** 30)), (B.E_UNSUPPORTED, dict(n=1, heads=1, kv=1, qr=2 ** 22, q_max=2 ** 22, kr=2 ** 23)),
 ])
 def test_attention_cross(lib, code, kw):
     assert lib.tts_gpt_op_attention_cross(*_cross(**kw)) == code
