@@ -95,7 +95,7 @@ struct UnitArgs {
   int pps, n_shared, n_pages;
   // cross: sequences
   const int *q_start, *k_start;
-  int n_seq, q_max, k_rows, few_rows;   // few_rows: no tile has more than four
+  int n_seq, q_max, k_rows, few_rows;   // few_rows: a warp a row merges
   // scratch
   int *err;                     // [0]: set when a wait ran out
   unsigned *tickets;            // zero between calls; null: the second kernel merges
@@ -722,7 +722,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
         merge_parts<PG, F16>(warp_of(d.x + d.y - 1) - f + 1, [&](int k) { return a.part + (seq_part(f + k, k == 0) + i) * kUnPitch; }, dst, real && store);
       }
     };
-    // (a warp a row where tiles have few, a quarter of one otherwise: by the call, not by how many rows this CTA came last at, since the
+    // (a warp a row or a quarter of one: by the call, not by how many rows this CTA came last at, since the
     // two add the parts in other orders)
     if (SHARED || a.few_rows) for (int it = warp; it < n_item; it += kUnWarps) merge(IntC<4>(), it);
     else for (int it = warp * 4; it < n_item; it += kUnWarps * 4) merge(IntC<1>(), it + ((lane >> 3) & 3));

@@ -188,8 +188,9 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   const int G = n_head / n_kv_head;
   // Up to two tiles of 16 read K and V at most twice; more rows take a tile of 256, which reads them once (us, 16 sequences of 90 to 1500 keys
   // by 20 heads, warp-level / tcgen05: 20 queries 27 / 32, 32 queries 30 / 33, 48 queries 35 / 33, 128 queries 63 / 35; four heads of
-  // keys, 7 queries of 5 heads each 18 / 16)
-  const bool tiles = q_max * G > 2 * kUnTile && n <= kTlMaxSeq;
+  // keys, 7 queries of 5 heads each 18 / 16), where there are keys to read: a block has 128 (30 sequences by 20 heads: 100 to 400 queries
+  // by 100 to 120 keys 50 / 40, by 60 to 70 keys 39 / 39; 40 to 100 queries by 60 to 70 keys 23 / 27, by 10 to 20 keys 10 / 27).
+  const bool tiles = (long long)q_max * G > 2 * kUnTile && k_rows > 64ll * n && n <= kTlMaxSeq;
   // units of keys are numbered in 31 bits, one of them for what a division rounds up; blocks by their cost
   const int rpt = tiles ? 2 * (kTlRows / G) : kUnTile / G, keys = tiles ? kTlKeys : kUnKeys;
   const long long limit = (1ll << 30) / (tiles ? kTlCost2 : 1);
@@ -209,7 +210,10 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   a.set_heads(n_head, n_kv_head, rpt);
   a.scale = scale * 1.4426950408889634f;
   a.q_start = q_start; a.k_start = k_start; a.n_seq = n; a.q_max = q_max; a.k_rows = k_rows;
-  a.few_rows = (long long)q_max * G <= 4;
+  // a warp a row merges where tiles have few rows, or many parts since there are few tiles (us: 20 tiles of 47 units 15, a quarter of a
+  // warp a row 19; 64 tiles 17.6 and 18.7; 160 tiles 24.6 and 23.3)
+  const int n_sm = device_sms();
+  a.few_rows = (long long)q_max * G <= 4 || n_kv_head * blocks * 16 <= (long long)std::min(n_sm, kUnMaxCtas) * kUnWarps;
   a.err = (int *)scratch;
   a.tickets = (unsigned *)((char *)scratch + 256);
   a.part = (float *)((char *)scratch + kOpHeaderBytes);
@@ -219,14 +223,13 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
     OP_TRY(units_rows_map(&k_map, f16, k, n_kv_head, k_rows, k_head_stride * 2, k_stride * 2, tiles ? kTlKeys : kUnBox));
     OP_TRY(units_rows_map(&v_map, f16, v, n_kv_head, k_rows, v_head_stride * 2, v_stride * 2, tiles ? kTlKeys : kUnBox));
   }
-  if (tiles && k_rows > 0) {
+  if (tiles) {
     CUtensorMap q_map;
     OP_TRY(tiles_q_map(&q_map, f16, q, n_head, q_rows, q_stride * 2, G, rpt / 2));
-    OP_TRY((f16 ? launch_tiles_as<true> : launch_tiles_as<false>)(q_map, k_map, v_map, a, device_sms(), (cudaStream_t)cuda_stream));
+    OP_TRY((f16 ? launch_tiles_as<true> : launch_tiles_as<false>)(q_map, k_map, v_map, a, n_sm, (cudaStream_t)cuda_stream));
     return TTS_GPT_OK;
   }
-  if (tiles) a.set_heads(n_head, n_kv_head, kUnTile / G);   // no keys at all: rows of zeros, from the kernel that needs no maps
-  OP_TRY((f16 ? launch_units_as<false, KV_F16, false> : launch_units_as<false, KV_BF16, false>)(k_map, v_map, a, device_sms(), (cudaStream_t)cuda_stream));
+  OP_TRY((f16 ? launch_units_as<false, KV_F16, false> : launch_units_as<false, KV_BF16, false>)(k_map, v_map, a, n_sm, (cudaStream_t)cuda_stream));
   return TTS_GPT_OK;
 }
 

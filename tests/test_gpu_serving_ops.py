@@ -333,6 +333,50 @@ def test_cross_attention_writes_nothing_where_starts_do_not_ascend(ql):
     c.check(c.run(scratch=scratch), "after them")
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("layout", ["rows", "fused", "heads", "odd"])
+@pytest.mark.parametrize("heads,kv", [(2, 2), (10, 2), (16, 1), (3, 1)])
+def test_cross_attention_of_long_and_short_sequences(heads, kv, layout, dtype):
+    # many keys on average, and sequences with none, one, a block, a block and one
+    ql, kl = [300, 64, 129, 40, 0, 257, 2, 513], [40, 0, 77, 1, 9, 128, 700, 129]
+    c = CrossCase(26, dtype, heads, kv, ql, kl, layout=layout, gap_q=3, scale=0.2)
+    c.check(c.run(), layout)
+    short = CrossCase(27, dtype, heads, kv, [130, 90, 40], [0, 400, 0], layout=layout, q_max=129)
+    short.ql[0] = 129                       # the row beyond q_max is not computed
+    qs = short.qs
+    got = short.run()
+    assert torch.all(got[129] == 9.0) and torch.all(got[:129] == 0) and torch.all(got[qs[2]:qs[3]] == 0) and torch.all(got[qs[3]:] == 9.0)
+
+
+def test_cross_attention_of_many_keys_neighbours_infinities_and_peaked_scores():
+    c = CrossCase(28, torch.bfloat16, 2, 2, [150, 200, 150], [137, 150, 141], std=40.0)
+    c.check(c.run(), "peaked")
+    c.k[140:160] = float("inf")
+    c.v[137:287] = float("nan")
+    got = c.run()
+    a, b = c.qs[1], c.qs[2]
+    assert torch.isnan(got[a:b]).all()
+    c.vd[137:287] = c.kd[137:287] = 0
+    got[a:b] = 0
+    c.check(got, "neighbours")
+    # starts that do not ascend
+    for at in (3, 4):
+        args = list(c.args)
+        args[at] = args[at][[0, 2, 1, 3]].contiguous()
+        out = torch.full(c.q.shape, 9.0, dtype=c.dtype, device=DEV)
+        B.op_attention_cross(*args, out=out)
+        assert torch.all(out == 9.0)
+
+
+@pytest.mark.parametrize("heads,kv,n,q", [(16, 1, 6, 1), (20, 4, 16, 3), (20, 20, 1, 16), (8, 8, 13, 9), (20, 20, 8, 16)])
+def test_cross_attention_tiles_of_many_parts(heads, kv, n, q):
+    c = CrossCase(29, torch.bfloat16, heads, kv, [q] * n, [700 + 37 * i for i in range(n)])
+    got = c.run()
+    c.check(got, "many parts")
+    for _ in range(5):
+        assert torch.equal(got.view(torch.int16), c.run().view(torch.int16))
+
+
 @pytest.mark.parametrize("ql", [[5, 5], [60, 70]])
 @pytest.mark.parametrize("key", [0, 5, 6, 7, 37, 130])
 def test_cross_attention_keeps_nan(ql, key):
