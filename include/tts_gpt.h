@@ -398,8 +398,8 @@ int32_t tts_gpt_op_page_tables(int32_t n, const int32_t *stream_ids, const int32
 
 /* K and V rows of a pass into their slots: k, v TTS_GPT_T_F32 or TTS_GPT_T_BF16, n_head heads of 64 contiguous values a row, rows
  * k_stride / v_stride elements apart (so that both may be parts of one QKV array); rows and pool 16-byte aligned.  The bf16 cache
- * takes each value rounded once, the 8-bit cache codes e4m3(x / s) with s = max|x| / 448 over a head's 64 values (1 if all are
- * zero).  A row whose row_slot lies outside 0 .. 64 n_pages - 1 is left out.  Slots must be distinct: of two rows with the same
+ * takes each value rounded once, the 8-bit cache codes e4m3(x / s) with s = max|x| / 448 over a head's 64 values (1 where that is
+ * zero in fp32).  A row whose row_slot lies outside 0 .. 64 n_pages - 1 is left out.  Slots must be distinct: of two rows with the same
  * slot either may be kept, for each 16 bytes anew.  Values must be finite in the 8-bit format. */
 int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void *k, int64_t k_stride, const void *v,
                              int64_t v_stride, const int32_t *row_slot, int32_t kv_fmt, int32_t n_pages, void *kv_layer,

@@ -224,7 +224,7 @@ __device__ __forceinline__ void load8(const uint16_t *p, float (&x)[8]) {
 }
 
 // Eight lanes take the 64 values of one (row, K|V, head), eight values each.  16-bit cache: each value rounded once.  8-bit cache:
-// s = max|x| / 448 over the 64 (1 if all are zero), codes e4m3(x / s).  Bound: bytes in and out; a thread has PER such pieces under
+// s = max|x| / 448 over the 64 (1 where that is zero in fp32), codes e4m3(x / s).  Bound: bytes in and out; a thread has PER such pieces under
 // way, of rows far apart (3584 fp32 rows of 20 heads, 55 MB: four 10.4 us, 5.3 TB/s; one 11.8 us; 16 rows 1.8 us).
 constexpr int kAppendThreads = 256;
 template <typename Src, bool E4M3, int PER>
@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const AppendA
       for (int i = 1; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-      const float s = m > 0.f ? m / 448.0f : 1.0f;
+      const float quotient = m / 448.0f, s = quotient > 0.f ? quotient : 1.0f;   // below 448 2^-150 it is zero though m is not
       uint32_t w[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
