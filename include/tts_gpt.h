@@ -400,7 +400,8 @@ int32_t tts_gpt_op_page_tables(int32_t n, const int32_t *stream_ids, const int32
  * k_stride / v_stride elements apart (so that both may be parts of one QKV array); rows and pool 16-byte aligned.  The bf16 cache
  * takes each value rounded once, the 8-bit cache codes e4m3(x / s) with s = max|x| / 448 over a head's 64 values (1 where that is
  * zero in fp32).  A row whose row_slot lies outside 0 .. 64 n_pages - 1 is left out.  Slots must be distinct: of two rows with the same
- * slot either may be kept, for each 16 bytes anew.  Values must be finite in the 8-bit format. */
+ * slot either may be kept, for each 16 bytes anew.  Values must be finite in the 8-bit format.  The
+ * pool may overlap neither K and V nor the slots (E_ARG). */
 int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void *k, int64_t k_stride, const void *v,
                              int64_t v_stride, const int32_t *row_slot, int32_t kv_fmt, int32_t n_pages, void *kv_layer,
                              void *cuda_stream);
@@ -409,7 +410,7 @@ int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void
  * 0..row_pos[r] of stream row_stream[r], o = softmax(q.K^T / 8) V per head), where the first n_shared entries of the page lists of
  * all R rows are the same pages, which are read once for all rows and not once for each.  n_shared may be 0.  Query head
  * h reads the keys of head h / (n_head / n_kv_head), at most 16 to one.  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements
- * apart; out bf16 [R][n_head*64], which may not overlap q.  A row with row_pos -1 or a negative row_stream has no keys: its output
+ * apart; out bf16 [R][n_head*64]; neither it nor scratch may overlap anything else that the call is given (E_ARG).  A row with row_pos -1 or a negative row_stream has no keys: its output
  * is zero.  Several rows may belong to one stream.  Keys on a page outside 0..n_pages-1 are left out, as are those behind the
  * list's pages_per_stream pages.  K and V of the shared pages must be finite.  fp32 queries enter with 16 bits, the softmax weights are rounded to bf16, sums are fp32; results do
  * not depend on timing.  R <= 4096.
@@ -427,8 +428,8 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
  * independent; a sequence without keys has zero outputs, rows outside every sequence are left as they were.  q_start, k_start:
  * ascending (where one does not, nothing is written), n + 1 each, at most q_rows and k_rows; q_max: at least the longest sequence of queries (rows beyond it are not
  * computed).  q, k, v, out of one type, TTS_GPT_T_BF16 or TTS_GPT_T_F16; q rows q_stride elements apart with contiguous heads, k and v with
- * strides of rows and of heads (so both [rows][heads][64], parts of one array, and [heads][rows][64]); out [q_rows][n_head*64], which
- * may overlap none of them.
+ * strides of rows and of heads (so both [rows][heads][64], parts of one array, and [heads][rows][64]); out [q_rows][n_head*64]; neither
+ * it nor scratch may overlap anything else that the call is given (E_ARG).
  * Heads, roundings and scratch as for op_attention_shared (scratch size independent of the call).  n <= 4096, rows below 2^30. */
 int32_t tts_gpt_op_attention_cross_scratch_bytes(size_t *bytes);
 int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head, int32_t type, int32_t q_rows, const void *q,

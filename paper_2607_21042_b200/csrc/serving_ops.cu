@@ -36,6 +36,10 @@ Bytes rows_of(const void *p, long long rows, long long stride, long long width, 
   return {p, rows > 0 ? (size_t)((rows - 1) * stride + width) * size : 0};
 }
 
+Bytes pool_of(const void *kv_layer, int32_t kv_fmt, int32_t n_pages, int32_t heads) {
+  return {kv_layer, (size_t)n_pages * 2 * heads * (kv_fmt == TTS_GPT_KV_BF16 ? (size_t)kPageElems * 2 : (size_t)kE4m3BlockBytes)};
+}
+
 int check_heads(const char *op, int32_t n_head, int32_t n_kv_head) {
   if (n_head < 1 || n_kv_head < 1 || n_head % n_kv_head) return fail_op(TTS_GPT_E_ARG, "%s: n_head must be a multiple of n_kv_head", op);
   if (n_head / n_kv_head > kUnTile || n_head > 1024)
@@ -94,6 +98,11 @@ int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void
   if (!aligned(k, 16) || !aligned(v, 16) || k_stride % per16 || v_stride % per16 || !aligned(kv_layer, 16) || !aligned(row_slot, 4))
     return fail_op(TTS_GPT_E_ARG, "op_kv_append: K and V rows and the pool must be 16-byte aligned, slots 4-byte");
   if ((long long)R * n_head >= (1ll << 29)) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_kv_append: R * n_head must be below 2^29");
+  const size_t size = type == TTS_GPT_T_F32 ? 4 : 2;
+  const Bytes pool = pool_of(kv_layer, kv_fmt, n_pages, n_head);
+  if (overlap(pool, rows_of(k, R, k_stride, (long long)n_head * kHeadDim, size)) || overlap(pool, rows_of(v, R, v_stride, (long long)n_head * kHeadDim, size)) ||
+      overlap(pool, {row_slot, (size_t)R * 4}))
+    return fail_op(TTS_GPT_E_ARG, "op_kv_append: K, V or the slots overlap the pool");
   AppendArgs a;
   a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride; a.row_slot = row_slot; a.pool = (unsigned char *)kv_layer;
   a.R = R; a.H = n_head; a.n_slots = n_pages * kPageTokens;
@@ -135,8 +144,14 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_shared: too many pages");
   if (scratch_size < scratch_bytes(shared_part_rows(R, n_kv_head, G)))
     return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_shared: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(shared_part_rows(R, n_kv_head, G)));
-  if (overlap({out, (size_t)R * n_head * kHeadDim * 2}, rows_of(q, R, q_stride, (long long)n_head * kHeadDim, type == TTS_GPT_T_F32 ? 4 : 2)))
-    return fail_op(TTS_GPT_E_ARG, "op_attention_shared: out overlaps q");
+  const Bytes to = {out, (size_t)R * n_head * kHeadDim * 2}, own = {scratch, scratch_bytes(shared_part_rows(R, n_kv_head, G))};
+  // (of the page lists, whose number the call does not know, the first)
+  const Bytes read[] = {rows_of(q, R, q_stride, (long long)n_head * kHeadDim, type == TTS_GPT_T_F32 ? 4 : 2), pool_of(kv_layer, kv_fmt, n_pages, n_kv_head),
+                        {page_table, (size_t)pages_per_stream * 4}, {row_stream, (size_t)R * 4}, {row_pos, (size_t)R * 4}};
+  for (const Bytes &x : read)
+    if (overlap(to, x) || overlap(own, x))
+      return fail_op(TTS_GPT_E_ARG, "op_attention_shared: out or scratch overlaps q, the pool, the page lists or the rows' streams and positions");
+  if (overlap(to, own)) return fail_op(TTS_GPT_E_ARG, "op_attention_shared: out and scratch overlap");
   UnitArgs a = {};
   a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = R;
   a.set_heads(n_head, n_kv_head, kUnTile / G);
@@ -200,11 +215,12 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: too many queries times keys");
   if (scratch_size < scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())))
     return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_cross: scratch of %zu bytes, %zu needed", scratch_size, scratch_bytes(std::max(cross_part_rows(), tiles_part_rows())));
-  const Bytes to = {out, (size_t)q_rows * n_head * kHeadDim * 2};
-  if (overlap(to, rows_of(q, q_rows, q_stride, (long long)n_head * kHeadDim, 2)) ||
-      overlap(to, rows_of(k, k_rows, k_stride, (n_kv_head - 1) * k_head_stride + kHeadDim, 2)) ||
-      overlap(to, rows_of(v, k_rows, v_stride, (n_kv_head - 1) * v_head_stride + kHeadDim, 2)))
-    return fail_op(TTS_GPT_E_ARG, "op_attention_cross: out overlaps q, K or V");
+  const Bytes to = {out, (size_t)q_rows * n_head * kHeadDim * 2}, own = {scratch, scratch_bytes(std::max(cross_part_rows(), tiles_part_rows()))};
+  const Bytes read[] = {rows_of(q, q_rows, q_stride, (long long)n_head * kHeadDim, 2), rows_of(k, k_rows, k_stride, (n_kv_head - 1) * k_head_stride + kHeadDim, 2),
+                        rows_of(v, k_rows, v_stride, (n_kv_head - 1) * v_head_stride + kHeadDim, 2), {q_start, (size_t)(n + 1) * 4}, {k_start, (size_t)(n + 1) * 4}};
+  for (const Bytes &x : read)
+    if (overlap(to, x) || overlap(own, x)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: out or scratch overlaps q, K, V or the starts");
+  if (overlap(to, own)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: out and scratch overlap");
   UnitArgs a = {};
   a.q = q; a.out = (uint16_t *)out; a.q_stride = q_stride; a.q_rows = q_rows;
   a.set_heads(n_head, n_kv_head, rpt);
