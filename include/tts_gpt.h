@@ -373,7 +373,8 @@ int32_t tts_gpt_op_sample(int32_t R, int32_t V, const float *logits, int32_t top
  * requests begin with read once (op_attention_shared); op_attention_cross reads an encoder's states instead.  The layer's
  * pool is that of the engine: bf16 [n_pages][2 (K,V)][heads][64 tokens][64], or with TTS_GPT_KV_FP8_E4M3 blocks of 4352 bytes
  * [n_pages][2][heads]: 64 tokens x 64 codes, then the 64 fp32 scales.  All index arrays DEVICE int32.  A call
- * allocates nothing, does not wait for the GPU and can be captured into a CUDA graph.
+ * allocates nothing, does not wait for the GPU and can be captured into a CUDA graph.  The stride of a single row or head is not
+ * looked at.
  * ------------------------------------------------------------------------------------------- */
 
 /* Page lists and slot maps of a pass.  Request i (of n) adds new_len[i] >= 0 tokens to stream stream_ids[i] (NULL: i), which

@@ -91,6 +91,7 @@ int32_t tts_gpt_op_page_tables(int32_t n, const int32_t *stream_ids, const int32
 
 int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                              const int32_t *row_slot, int32_t kv_fmt, int32_t n_pages, void *kv_layer, void *cuda_stream) {
+  if (R == 1) k_stride = v_stride = (int64_t)n_head * kHeadDim;   // the stride of a single row addresses nothing
   if (R < 1 || n_head < 1 || !k || !v || !row_slot || !kv_layer || n_pages < 1 || n_pages > INT32_MAX / kPageTokens || (type != TTS_GPT_T_F32 && type != TTS_GPT_T_BF16) ||
       (kv_fmt != TTS_GPT_KV_BF16 && kv_fmt != TTS_GPT_KV_FP8_E4M3) || k_stride < (int64_t)n_head * kHeadDim || v_stride < (int64_t)n_head * kHeadDim)
     return fail_op(TTS_GPT_E_ARG, "op_kv_append: bad argument");
@@ -128,6 +129,7 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
                                     int32_t n_pages, const void *kv_layer, int32_t n_shared, const int32_t *page_table, int32_t pages_per_stream,
                                     const int32_t *row_stream, const int32_t *row_pos, void *out, void *scratch, size_t scratch_size, void *cuda_stream) {
   if (const int rc = check_shared(R, n_head, n_kv_head)) return rc;
+  if (R == 1) q_stride = (int64_t)n_head * kHeadDim;
   if (!q || !kv_layer || !page_table || !row_stream || !row_pos || !out || !scratch || (type != TTS_GPT_T_F32 && type != TTS_GPT_T_BF16) ||
       (kv_fmt != TTS_GPT_KV_BF16 && kv_fmt != TTS_GPT_KV_FP8_E4M3) || n_pages < 1 || pages_per_stream < 1 || n_shared < 0 || n_shared > pages_per_stream ||
       q_stride < (int64_t)n_head * kHeadDim)
@@ -188,6 +190,9 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
                                    int64_t v_head_stride, const int32_t *q_start, const int32_t *k_start, int32_t q_max, float scale, void *out,
                                    void *scratch, size_t scratch_size, void *cuda_stream) {
   if (const int rc = check_heads("op_attention_cross", n_head, n_kv_head)) return rc;
+  if (q_rows == 1) q_stride = (int64_t)n_head * kHeadDim;
+  if (k_rows <= 1) k_stride = v_stride = kHeadDim;
+  if (n_kv_head == 1) k_head_stride = v_head_stride = kHeadDim;
   if (n < 1 || q_rows < 1 || k_rows < 0 || q_max < 1 || !q || (k_rows > 0 && (!k || !v)) || !q_start || !k_start || !out || !scratch ||
       (type != TTS_GPT_T_BF16 && type != TTS_GPT_T_F16) || q_stride < (int64_t)n_head * kHeadDim || !std::isfinite(scale))
     return fail_op(TTS_GPT_E_ARG, "op_attention_cross: bad argument");
@@ -195,8 +200,8 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(scratch, 256) || !aligned(q_start, 4) || !aligned(k_start, 4) || q_stride % 8 ||
       k_stride % 8 || v_stride % 8 || k_head_stride % 8 || v_head_stride % 8)
     return fail_op(TTS_GPT_E_ARG, "op_attention_cross: rows of q, K, V and out must be 16-byte aligned, scratch 256-byte, index arrays 4-byte");
-  if (k_rows > 1 && (k_stride < kHeadDim || v_stride < kHeadDim)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: rows of K or V overlap");
-  if (n_kv_head > 1 && k_rows > 0 && (k_head_stride < kHeadDim || v_head_stride < kHeadDim)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: heads of K or V overlap");
+  if (k_stride < kHeadDim || v_stride < kHeadDim) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: rows of K or V overlap");
+  if (k_rows > 0 && (k_head_stride < kHeadDim || v_head_stride < kHeadDim)) return fail_op(TTS_GPT_E_ARG, "op_attention_cross: heads of K or V overlap");
   if (n > kUnMaxSeq) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: at most %d sequences", kUnMaxSeq);
   if (q_rows >= (1 << 30) || k_rows >= (1 << 30)) return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_cross: rows must be below 2^30");
   if (q_max > q_rows) q_max = q_rows;

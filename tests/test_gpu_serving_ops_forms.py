@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2607_21042_b200 import binding as B
-from test_gpu_serving_ops import DEV, E4M3_BLOCK
+from test_gpu_serving_ops import DEV, E4M3_BLOCK, Cache, CrossCase, _gen, _q
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,60 @@ def test_kv_append_of_values_whose_scale_vanishes():
         assert torch.equal(scales[part].cpu(), want_scales.t())
         assert torch.equal(codes[part].cpu(), want_codes.transpose(0, 1))
     assert not bool(((codes & 0x7F) == 0x7F).any()) and bool((scales > 0).all())
+
+
+# ---------------------------------------------------------------------------------------------
+# strides that address nothing
+# ---------------------------------------------------------------------------------------------
+def _cross_c(x, scratch, out, **kw):
+    """The C entry point on a CrossCase's arrays, with some arguments replaced."""
+    a = dict(n=len(x.ql), heads=x.heads, kv=x.kv, type=B.T_BF16, qr=x.q.shape[0], q=x.q.data_ptr(), qs=x.q.stride(0), kr=x.k.shape[0], k=x.k.data_ptr(), ks=x.k.stride(0),
+             kh=x.k.stride(1), v=x.v.data_ptr(), vs=x.v.stride(0), vh=x.v.stride(1), q0=x.args[3].data_ptr(), k0=x.args[4].data_ptr(), q_max=max(x.ql), scale=x.scale,
+             out=out.data_ptr(), scratch=scratch.data_ptr(), size=scratch.numel(), stream=0)
+    assert set(kw) <= set(a)
+    return B.load().tts_gpt_op_attention_cross(*{**a, **kw}.values())
+
+
+@pytest.mark.parametrize("ql", [[1, 3], [70, 40]])
+@pytest.mark.parametrize("stride", [0, 8, -64, 3])
+def test_the_stride_of_a_single_head_or_row_is_not_looked_at(ql, stride):
+    scratch = B.op_attention_cross_scratch(DEV)
+    x = CrossCase(61, torch.bfloat16, 4, 1, ql, [150, 90])                       # one head of keys
+    out = torch.full(x.q.shape, 9.0, dtype=x.dtype, device=DEV)
+    torch.cuda.synchronize()
+    assert _cross_c(x, scratch, out, kh=stride, vh=stride) == B.OK, B.load().tts_gpt_last_error(None)
+    torch.cuda.synchronize()
+    x.check(out, "one head")
+    x = CrossCase(62, torch.bfloat16, 4, 2, [3], [1])                            # one row of keys, one of queries: its first row alone
+    out = torch.full(x.q.shape, 9.0, dtype=x.dtype, device=DEV)
+    torch.cuda.synchronize()
+    assert _cross_c(x, scratch, out, kr=1, ks=stride, vs=stride) == B.OK, B.load().tts_gpt_last_error(None)
+    torch.cuda.synchronize()
+    x.check(out, "one row of keys")
+    one = torch.full(x.q.shape, 9.0, dtype=x.dtype, device=DEV)
+    torch.cuda.synchronize()
+    assert _cross_c(x, scratch, one, qr=1, qs=stride) == B.OK, B.load().tts_gpt_last_error(None)
+    torch.cuda.synchronize()
+    assert torch.equal(one[:1], out[:1]) and torch.all(one[1:] == 9.0)
+
+
+@pytest.mark.parametrize("stride", [0, 8, -64, 3])
+def test_the_stride_of_a_single_row_is_not_looked_at(stride):
+    c = Cache(63, "bf16", 2, 1, [40])
+    q = _q(64, 1, 4, torch.float32)
+    want = B.op_attention_shared(q, c.pool, *c.args)
+    out, scratch = torch.empty_like(want), B.op_attention_shared_scratch(1, 4, 2, DEV)
+    torch.cuda.synchronize()
+    lib = B.load()
+    assert lib.tts_gpt_op_attention_shared(1, 4, 2, B.T_F32, q.data_ptr(), stride, 0, c.n_pages, c.pool.data_ptr(), 1, c.args[0].data_ptr(), c.args[0].shape[1], c.args[1].data_ptr(),
+                                           c.args[2].data_ptr(), out.data_ptr(), scratch.data_ptr(), scratch.numel(), 0) == B.OK, lib.tts_gpt_last_error(None)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    kv = torch.randn(2, 128, generator=_gen(65)).to(DEV)
+    slot, pool = torch.tensor([70], dtype=torch.int32, device=DEV), torch.zeros(2, 2, 2, 64, 64, dtype=torch.bfloat16, device=DEV)
+    want = pool.clone()
+    B.op_kv_append(kv[:1], kv[1:], want, slot)
+    torch.cuda.synchronize()
+    assert lib.tts_gpt_op_kv_append(1, 2, B.T_F32, kv.data_ptr(), stride, kv.data_ptr() + 512, stride, slot.data_ptr(), 0, 2, pool.data_ptr(), 0) == B.OK, lib.tts_gpt_last_error(None)
+    torch.cuda.synchronize()
+    assert torch.equal(pool, want) and bool(pool.any())
