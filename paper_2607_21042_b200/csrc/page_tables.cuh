@@ -184,18 +184,21 @@ __global__ void __launch_bounds__(THREADS, 1) page_tables_kernel(const TableArgs
   }
 }
 
+// A thread writes up to four rows; more CTAs than that only repeat the sums.
+inline int page_tables_grid(int n, int max_rows, int n_sm) {
+  return n <= 256 ? std::min(2 * n_sm, (max_rows - 1) / 1024 + 1) : std::min(n_sm, (max_rows - 1) / 2048 + 1);   // max_rows is 1 at least
+}
+
 inline cudaError_t launch_page_tables(const TableArgs &a, int n_sm, cudaStream_t st) {
   const size_t smem = page_tables_smem_bytes(a.n, a.max_streams);
-  // a thread writes up to four rows; more CTAs than that only repeat the sums
+  const int grid = page_tables_grid(a.n, a.max_rows, n_sm);
   if (a.n <= 256) {
     static SmemOptIn opt_in;
     if (const cudaError_t e = opt_in(page_tables_kernel<256, 1>, page_tables_smem_bytes(256, kTabMaxStreams))) return e;
-    const int grid = std::max(1, std::min(2 * n_sm, (a.max_rows + 1023) / 1024));
     return launch_kernel(page_tables_kernel<256, 1>, dim3(grid), dim3(256), smem, st, false, a);
   }
   static SmemOptIn opt_in;
   if (const cudaError_t e = opt_in(page_tables_kernel<1024, 4>, page_tables_smem_bytes(kTabMaxRequests, kTabMaxStreams))) return e;
-  const int grid = std::max(1, std::min(n_sm, (a.max_rows + 2047) / 2048));
   return launch_kernel(page_tables_kernel<1024, 4>, dim3(grid), dim3(1024), smem, st, false, a);
 }
 
