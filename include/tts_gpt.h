@@ -268,6 +268,12 @@ int32_t tts_gpt_debug_expire_wait(tts_gpt_t *h, uint32_t limit_us);
  * after the 2 s that every wait has, and its cluster stores nothing.  Nothing hangs or faults. */
 int32_t tts_gpt_debug_expire_linear(tts_gpt_t *h, int32_t kernel, int32_t rows, int32_t tile, uint32_t limit_us, float *out);
 
+/* Test aid for the same path inside op_attention_shared and op_attention_cross: in the calls that this thread makes from now
+ * on, the copies of CTA number `cta` (0 on) never count as complete, and waits give up after limit_us microseconds (1..100000; in
+ * op_attention_cross, where its tiles have 256 rows, after the 2 s that every wait has).  cta -1: as usual again, limit_us is
+ * ignored.  Nothing hangs or faults. */
+int32_t tts_gpt_debug_expire_op(int32_t cta, uint32_t limit_us);
+
 /* ---------------------------------------------------------------------------------------------
  * Single-kernel entry points: the building blocks of the step, callable on their own (unit parity
  * tests, micro-benchmarks).  All pointers DEVICE unless marked HOST; `cuda_stream` as above; each
@@ -417,7 +423,8 @@ int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void
  * not depend on timing.  R <= 4096.
  * scratch (256-byte aligned, >= scratch_bytes; zero before its first use, by this call or op_attention_cross, in any size)
  * belongs to one call at a time: calls that may overlap, replays of captured graphs among them, need one each.  Its first
- * word is set to 1 if a bounded wait inside a kernel ran out; outputs are then incomplete and the scratch must be zeroed. */
+ * word is set to 1 if a bounded wait inside a kernel ran out.  Rows that were then not computed are NaN, others may be, and all rows
+ * of later calls with this scratch are until it has been zeroed. */
 int32_t tts_gpt_op_attention_shared_scratch_bytes(int32_t R, int32_t n_head, int32_t n_kv_head, size_t *bytes);
 int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head, int32_t type, const void *q, int64_t q_stride,
                                     int32_t kv_fmt, int32_t n_pages, const void *kv_layer, int32_t n_shared,

@@ -25,7 +25,7 @@ EXPORTS = [
     "tts_gpt_query_workspace", "tts_gpt_create", "tts_gpt_prefill", "tts_gpt_prefill_tokens", "tts_gpt_decode_step", "tts_gpt_decode_step_host", "tts_gpt_decode_steps",
     "tts_gpt_release_stream", "tts_gpt_sync", "tts_gpt_destroy", "tts_gpt_last_error",
     "tts_gpt_stats", "tts_gpt_stream_context", "tts_gpt_debug_shuffle_free_pages",
-    "tts_gpt_debug_kernel_launches", "tts_gpt_debug_set_trace", "tts_gpt_debug_expire_wait", "tts_gpt_debug_expire_linear", "tts_gpt_debug_set_option", "tts_gpt_debug_check_canaries",
+    "tts_gpt_debug_kernel_launches", "tts_gpt_debug_set_trace", "tts_gpt_debug_expire_wait", "tts_gpt_debug_expire_linear", "tts_gpt_debug_expire_op", "tts_gpt_debug_set_option", "tts_gpt_debug_check_canaries",
     "tts_gpt_op_linear_packed_bytes", "tts_gpt_op_linear_pack", "tts_gpt_op_linear",
     "tts_gpt_op_linear_tc_scratch_bytes", "tts_gpt_op_linear_tc", "tts_gpt_op_attention_scratch_bytes", "tts_gpt_op_attention", "tts_gpt_op_attention_static", "tts_gpt_op_attention_cluster",
     "tts_gpt_op_layernorm",
@@ -545,6 +545,11 @@ def _scratch(scratch, d):
     return scratch.data_ptr(), scratch.numel()
 
 
+def debug_expire_op(cta, limit_us=1000):
+    """Test aid: copies of CTA `cta` never count as complete in this thread's next attention calls; -1: as usual again."""
+    _check(load().tts_gpt_debug_expire_op(C.c_int32(cta), C.c_uint32(limit_us)))
+
+
 def op_attention_shared_scratch(R, n_head, n_kv_head, device):
     n = C.c_size_t(0)
     _check(load().tts_gpt_op_attention_shared_scratch_bytes(C.c_int32(R), C.c_int32(n_head), C.c_int32(n_kv_head), C.byref(n)))
@@ -553,7 +558,8 @@ def op_attention_shared_scratch(R, n_head, n_kv_head, device):
 
 def op_attention_shared(q, kv_layer, page_table, row_stream, row_pos, n_shared, scratch=None, out=None, stream=None):
     """Attention of rows q [R, heads * 64] (fp32 or bf16) over a paged cache whose page lists all begin with the same n_shared
-    pages.  The pool may have fewer heads than q.  Returns bf16 bits [R, heads * 64], or `out`."""
+    pages.  The pool may have fewer heads than q.  Returns bf16 bits [R, heads * 64], or `out`.  Rows that are not computed since a
+    wait inside a kernel ran out are NaN (others may be); the first int32 of `scratch` is then 1, and it must be zeroed before its next use."""
     d, t, shape = q.get_device(), q.dtype, q.shape
     fmt, pages, kv_heads = _pool(kv_layer, d)
     if len(shape) != 2 or shape[1] % 64 or t is _F16 or t not in _TYPES:
@@ -593,7 +599,7 @@ def op_attention_cross(q, k, v, q_start, k_start, q_max, scale=0.125, scratch=No
     """Attention of ragged sequences of queries q [rows, heads, 64] to keys and values k, v [rows, kv heads, 64] of other lengths, bf16
     or fp16; sequence i has rows q_start[i] .. q_start[i+1]-1 of q and k_start[i] .. k_start[i+1]-1 of k and v, whose rows and heads
     may be strided.  q_max: at least the longest sequence of queries.  Returns [rows, heads, 64] (rows of no sequence undefined), or `out`
-    (in which they are left as they were)."""
+    (in which they are left as they were).  NaN rows and scratch as for op_attention_shared."""
     d, t, shape, kshape = q.get_device(), q.dtype, q.shape, k.shape
     if (t is not _BF16 and t is not _F16) or not (k.dtype is v.dtype is t) or len(shape) != 3 or len(kshape) != 3 or v.shape != kshape or shape[2] != 64 \
             or kshape[2] != 64 or k.get_device() != d or v.get_device() != d:

@@ -21,7 +21,7 @@
 // Work split.  Tiles are laid end to end by what they cost (blocks of one half or two, a tile besides its blocks) and cut into equal
 // ranges, one a CTA.  A part of a tile that several CTAs share goes to scratch with a ticket; the CTA that comes last adds the
 // parts in the order of their keys, so that results do not depend on timing.  As a rule that is the CTA in which the tile begins, at
-// the end of its range, with its own part, the first, still in registers.  Every wait on a copy or a product is bounded.
+// the end of its range, with its own part, the first, still in registers.  Every wait on a copy or a product is bounded: two seconds.
 #pragma once
 #include "attention_units.cuh"
 
@@ -58,7 +58,7 @@ struct TileShared {
   uint64_t q_full[2], q_free[2];
   uint64_t s_full[2], p_full[2], pv_done[2];   // by half
   uint32_t tmem;
-  int failed;
+  int failed;                     // 1: a wait of the CTA has run out; 2: one of an earlier call with the same scratch had
   TilePart meets;                 // the tile that began before the CTA's range
   Div size;
   int warp_tot[kTlThreads / 32];
@@ -138,11 +138,11 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
   volatile int *failed = &sh.failed;
 
   if (tid == 0) {
-    for (int i = 0; i < kTlRing; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+    for (int i = 0; i < kTlRing; ++i) { mbar_init(&sh.full[i], (int)blockIdx.x == a.starve ? 2 : 1); mbar_init(&sh.empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_free[i], kTlTile / 32); }
     for (int i = 0; i < kTlParts; ++i) { mbar_init(&sh.part_full[i], 1); mbar_init(&sh.part_free[i], 1 + kTlTile / 32); }
     for (int h = 0; h < 2; ++h) { mbar_init(&sh.s_full[h], 1); mbar_init(&sh.p_full[h], kTlRows / 32); mbar_init(&sh.pv_done[h], 1); }
-    sh.failed = 0;
+    sh.failed = __ldcg(a.err) ? 2 : 0;
   }
   if (warp == 8) {
     if (lane < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &q_map : lane == 1 ? &k_map : &v_map) : "memory");
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
   tc_fence_after_sync();
   const uint32_t tmem = sh.tmem;
   const Div size = sh.size;
-  const int u_begin = blockIdx.x * (int)size.d, u_end = min(T, u_begin + (int)size.d);
+  const int u_begin = blockIdx.x * (int)size.d, u_end = *failed ? u_begin : min(T, u_begin + (int)size.d);
 
   // from unit u on
   auto part_at = [&](int u) {
@@ -354,7 +354,6 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
     int i = 0, n_o = 0, n_block = 0, n_tile = 0, n_part = 0;   // waits of this half for s_full and for pv_done, blocks of the CTA, tiles with blocks, parts
     bool fine = true;
     int came_first = 0;                        // how many had a ticket of the tile that began before the CTA's range, this CTA among them
-    const bool sound = __ldcg(a.err) == 0;   // the scratch
     // A tile that several CTAs share has a place in each: 256 rows, 16 columns of four dimensions, then reference and sum.  A CTA has two
     // places: for the tile that began before its range, and the one that goes on behind it.
     auto part_at_place = [&](int c, int c0) { return a.part + (size_t)(2 * c + (c == c0)) * kTlTile * kUnPitch; };
@@ -393,7 +392,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
 #pragma unroll
       for (int it = 0; it < 8; ++it) {
         const int r = 32 * quarter + 4 * it + (lane >> 3), c8 = lane & 7;
-        if (r < n_i && sound && !*failed) *reinterpret_cast<uint4 *>(row_ptr(p, r) + 8 * c8) = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((c8 ^ (r & 7)) << 4));
+        if (r < n_i) *reinterpret_cast<uint4 *>(row_ptr(p, r) + 8 * c8) = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((c8 ^ (r & 7)) << 4));
       }
     };
     for (int u = u_begin; u < u_end && fine;) {
@@ -552,7 +551,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
         fence_proxy_async_smem();              // Q of the tile after next is copied over it
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.q_free[qb]);
-      } else if (whole && mine && sound && !*failed) {   // no block here, and no Q: zeros, or the sum of other CTAs' parts
+      } else if (whole && mine) {   // no block here, and no Q: zeros, or the sum of other CTAs' parts
         const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
         for (int c = 0; c < kHeadDim; c += 8)
@@ -577,11 +576,25 @@ __global__ void __launch_bounds__(kTlThreads, 1) attention_tiles_kernel(const __
         if (32 * quarter < n_i) leave(p, n_i, o, l, Qs + half * kTlHalf);
       }
     }
+    // ---- behind a wait that ran out: NaN into all rows of the call, among which are those that are not computed (a warp that has found the
+    //      error covers them alone: others may have left before; one of an earlier call is found by all) ----
+    if (*failed && first[a.n_seq] > 0) {
+      const int x0 = *failed == 2 ? t : lane, step = *failed == 2 ? kTlRows : 32;
+#pragma unroll 1
+      for (int i = 0; i < a.n_seq; ++i) {
+        int qb, qe;
+        q_span(i, qb, qe);
+        uint4 *rows = reinterpret_cast<uint4 *>(a.out) + (size_t)qb * a.H * (kHeadDim / 8);
+        const size_t n = (size_t)(qe - qb) * a.H * (kHeadDim / 8);
+#pragma unroll 1
+        for (size_t x = x0; x < n; x += step) rows[x] = make_uint4(0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu);
+      }
+    }
   }
   __syncwarp();
   tc_fence_before_sync();
   __syncthreads();
-  if (*failed) {   // copies and products may still be in flight
+  if (*failed == 1) {   // copies and products may still be in flight
     const unsigned long long t0 = global_timer_ns();
     while (global_timer_ns() - t0 <= 10000000ull) {}
   }

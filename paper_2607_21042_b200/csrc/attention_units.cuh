@@ -97,7 +97,9 @@ struct UnitArgs {
   const int *q_start, *k_start;
   int n_seq, q_max, k_rows, few_rows;   // few_rows: a warp a row merges
   // scratch
-  int *err;                     // [0]: set when a wait ran out
+  int *err;                     // [0]: set when a wait ran out; rows that are then not computed become NaN
+  unsigned long long wait_ns;   // that a wait may take (in the tiles kernel always kUnWaitNs: as an argument it cost 1 % there)
+  int starve;                   // test aid: the CTA whose copies never count as complete; -1: none
   unsigned *tickets;            // zero between calls; null: the second kernel merges
   int *plan;                    // ... which finds here {units of a range (a Div), running sums of units}
   float *part;
@@ -157,9 +159,9 @@ __device__ __forceinline__ size_t own_part(const UnitArgs &a, int row, int kvh, 
 __device__ __forceinline__ size_t seq_part(int range, bool begins) { return (size_t)(2 * range + (begins ? 1 : 0)) * kUnTile; }
 
 // The parts of a query row, added in the order of their keys by 8 PG lanes: lane group pg takes every PG-th part, a lane eight
-// dimensions.  part(p): the p-th of n partial rows.
+// dimensions.  part(p): the p-th of n partial rows.  sound: no wait has run out; otherwise the row is NaN.
 template <int PG, bool F16, typename Part>
-__device__ __forceinline__ void merge_parts(int n, Part part, uint16_t *out, bool store) {
+__device__ __forceinline__ void merge_parts(int n, Part part, uint16_t *out, bool store, bool sound) {
   const int sub = threadIdx.x & 7, pg = (threadIdx.x >> 3) & (PG - 1);
   float M = -INFINITY, l = 0.f, acc[8];
 #pragma unroll
@@ -189,7 +191,7 @@ __device__ __forceinline__ void merge_parts(int n, Part part, uint16_t *out, boo
     add(m2, l2, v);
   }
   if (store && pg == 0) {
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const float inv = !sound ? __int_as_float(0x7FFFFFFF) : l == 0.f ? 0.f : 1.0f / l;
     *reinterpret_cast<uint4 *>(out + 8 * sub) = make_uint4(un_pack<F16>(acc[0] * inv, acc[1] * inv), un_pack<F16>(acc[2] * inv, acc[3] * inv),
                                                            un_pack<F16>(acc[4] * inv, acc[5] * inv), un_pack<F16>(acc[6] * inv, acc[7] * inv));
   }
@@ -252,7 +254,8 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int n_items = SHARED ? a.q_rows : a.n_seq;
 
-  if (lane < L::kStages) mbar_init(&bars[warp * L::kStages + lane], 1);
+  const int failed = __ldcg(a.err);            // by an earlier call, unless the scratch has been zeroed since
+  if (lane < L::kStages) mbar_init(&bars[warp * L::kStages + lane], (int)blockIdx.x == a.starve ? 2 : 1);
   if (tid == 0) {
     lead_s = 0; n_tile_s = 0; n_item_s = 0;
     if constexpr (KV != KV_E4M3) {
@@ -386,12 +389,13 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   unsigned char *stage0 = stages + (size_t)warp * L::kStages * L::kStage;
   uint64_t *bar = bars + warp * L::kStages;
   UnitDesc nxt = {}, cur = {};                          // descriptions of the units being copied, and of those being computed
+  bool whole = true, dead = __any_sync(0xFFFFFFFFu, failed != 0);   // dead: nothing is copied or computed any more, rows become NaN
   auto issue = [&](int i) {                   // unit u_begin + i into stage i % kStages
     if ((i & 31) == 0) nxt = describe(u_begin + i + lane);
     const int c1 = __shfl_sync(0xFFFFFFFFu, nxt.c1, i & 31), c2 = __shfl_sync(0xFFFFFFFFu, nxt.c2, i & 31), n = __shfl_sync(0xFFFFFFFFu, nxt.n, i & 31);
     unsigned char *st = stage0 + (size_t)(i % L::kStages) * L::kStage;
     uint64_t *b = &bar[i % L::kStages];
-    if (elect_one()) {
+    if (!dead && elect_one()) {
       if constexpr (KV == KV_E4M3) {
         const uint32_t codes = (uint32_t)n * kHeadDim, scales = (uint32_t)(n + 3) / 4 * 16;
         mbar_expect_tx(b, 2 * (codes + scales));
@@ -426,7 +430,6 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
   uint32_t qa[4][4], qlo[QF32 ? 4 : 1][4];    // query fragments by 16 dimensions; fp32: what the first part leaves
   float o[8][4], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;   // rows g and g + 8
   int tile_u0 = -1, tile_nu = 0, row0 = 0, kvh = 0, n_i = 0, own = 0, vis0 = 0, vis1 = 0;
-  bool whole = true, dead = false;
 
   auto q_ptr = [&](int i) { const int r = a.by_G.of(i); return (size_t)(row0 + r) * a.q_stride + (size_t)((kvh - r) * a.G + i) * kHeadDim; };
   auto load_q = [&]() {
@@ -458,28 +461,27 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
     const int w0 = warp_of(tile_u0), w1 = warp_of(last);
     // does nothing else feed this tile's rows?
     const bool alone = w0 == w1 && (!SHARED || (own && tiles_head == 0));
-    if (alone) {
-      const float i0 = l0 > 0.f || l0 != l0 ? 1.0f / l0 : 0.f, i1 = l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
-      if (!dead) {
+    if (alone || dead) {                       // (dead: NaN, whoever merges the tile's parts finds the error too)
+      const float nan = __int_as_float(0x7FFFFFFF);
+      const float i0 = dead ? nan : l0 > 0.f || l0 != l0 ? 1.0f / l0 : 0.f, i1 = dead ? nan : l1 > 0.f || l1 != l1 ? 1.0f / l1 : 0.f;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (g + 8 * e < n_i) {
-            uint16_t *dst = out_ptr(g + 8 * e);
-            const float inv = e ? i1 : i0;
-            if constexpr (KV == KV_E4M3) {
+      for (int e = 0; e < 2; ++e) {
+        if (g + 8 * e < n_i) {
+          uint16_t *dst = out_ptr(g + 8 * e);
+          const float inv = e ? i1 : i0;
+          if constexpr (KV == KV_E4M3) {
 #pragma unroll
-              for (int hf = 0; hf < 2; ++hf)
-                *reinterpret_cast<uint4 *>(dst + 16 * t + 8 * hf) =
-                    make_uint4(un_pack<F16>(o[0][2 * e + hf] * inv, o[1][2 * e + hf] * inv), un_pack<F16>(o[2][2 * e + hf] * inv, o[3][2 * e + hf] * inv),
-                               un_pack<F16>(o[4][2 * e + hf] * inv, o[5][2 * e + hf] * inv), un_pack<F16>(o[6][2 * e + hf] * inv, o[7][2 * e + hf] * inv));
-            } else {
+            for (int hf = 0; hf < 2; ++hf)
+              *reinterpret_cast<uint4 *>(dst + 16 * t + 8 * hf) =
+                  make_uint4(un_pack<F16>(o[0][2 * e + hf] * inv, o[1][2 * e + hf] * inv), un_pack<F16>(o[2][2 * e + hf] * inv, o[3][2 * e + hf] * inv),
+                             un_pack<F16>(o[4][2 * e + hf] * inv, o[5][2 * e + hf] * inv), un_pack<F16>(o[6][2 * e + hf] * inv, o[7][2 * e + hf] * inv));
+          } else {
 #pragma unroll
-              for (int j = 0; j < 8; ++j) *reinterpret_cast<uint32_t *>(dst + 8 * j + 2 * t) = un_pack<F16>(o[j][2 * e] * inv, o[j][2 * e + 1] * inv);
-            }
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint32_t *>(dst + 8 * j + 2 * t) = un_pack<F16>(o[j][2 * e] * inv, o[j][2 * e + 1] * inv);
           }
         }
       }
-      return;
+      if (alone) return;
     }
     // this part into scratch
     float *dst = a.part + (SHARED ? (own ? own_part(a, row0, kvh, w) : prefix_part(a.by_prefix_nu.of(tile_u0), w)) : seq_part(w, w == w0)) * kUnPitch;
@@ -538,9 +540,11 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
       }
       const int s = idx % L::kStages;
       unsigned char *st = stage0 + (size_t)s * L::kStage;
-      if (!dead && !mbar_wait_bounded(&bar[s], (uint32_t)(idx / L::kStages) & 1u, kUnWaitNs)) {
+      if (!dead && !mbar_wait_bounded(&bar[s], (uint32_t)(idx / L::kStages) & 1u, a.wait_ns)) {
         atomicExch(a.err, 1);
         dead = true;
+        const unsigned long long t0 = global_timer_ns();   // copies of the warp may still be in flight, and none may land in a CTA that has left
+        while (global_timer_ns() - t0 <= 10000000ull) {}
       }
       dead = __any_sync(0xFFFFFFFFu, dead);
       if (n > 0 && !dead) {
@@ -662,11 +666,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
       fence_proxy_async_smem();
       __syncwarp();
     }
-    if (turn < n_mine && !dead) issue(turn);
-  }
-  if (dead) {   // copies of the warp may still be in flight, and none may land in a CTA that has left
-    const unsigned long long t0 = global_timer_ns();
-    while (global_timer_ns() - t0 <= 10000000ull) {}
+    if (turn < n_mine) issue(turn);
   }
   if (a.tickets) {
     __threadfence();
@@ -706,7 +706,7 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
     __syncthreads();
     // ---- and those are merged ----
     const int n_item = n_item_s;
-    const bool store = n_item > 0 && __ldcg(a.err) == 0;
+    const bool sound = n_item == 0 || __ldcg(a.err) == 0;
     auto merge = [&](auto pg_c, int item) {
       constexpr int PG = decltype(pg_c)::value;
       const bool real = item < n_item;
@@ -716,10 +716,10 @@ __global__ void __launch_bounds__(kUnWarps * 32, 1) attention_units_kernel(const
       uint16_t *dst = a.out + ((size_t)r * a.H + h * a.G + gi) * kHeadDim;
       if constexpr (SHARED) {
         const RowParts p = row_parts(a, r, h, gi, size, first[r], first[r + 1]);
-        merge_parts<PG, F16>(p.p_n + p.o_n, [&](int k) { return p.at(a, k); }, dst, real && store);
+        merge_parts<PG, F16>(p.p_n + p.o_n, [&](int k) { return p.at(a, k); }, dst, real, sound);
       } else {
         const int f = warp_of(d.x);
-        merge_parts<PG, F16>(warp_of(d.x + d.y - 1) - f + 1, [&](int k) { return a.part + (seq_part(f + k, k == 0) + i) * kUnPitch; }, dst, real && store);
+        merge_parts<PG, F16>(warp_of(d.x + d.y - 1) - f + 1, [&](int k) { return a.part + (seq_part(f + k, k == 0) + i) * kUnPitch; }, dst, real, sound);
       }
     };
     // (a warp a row or a quarter of one: by the call, not by how many rows this CTA came last at, since the
@@ -740,8 +740,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_shared_kernel(const Un
   const int f0 = __ldcg(a.plan + 3 + r), f1 = __ldcg(a.plan + 4 + r);
   const Div size = {(uint32_t)size4.x, (uint32_t)size4.y, (uint32_t)size4.z};
   const RowParts x = row_parts(a, r, kvh, h - kvh * a.G, size, f0, f1);
-  if (x.p_n == 0 && x.o_n == 1) return;        // finished by its warp
-  merge_parts<4, false>(x.p_n + x.o_n, [&](int p) { return x.at(a, p); }, a.out + ((size_t)r * a.H + h) * kHeadDim, __ldcg(a.err) == 0);
+  if (x.p_n == 0 && x.o_n == 1) return;        // finished by its warp, as NaN where that gave up
+  merge_parts<4, false>(x.p_n + x.o_n, [&](int p) { return x.at(a, p); }, a.out + ((size_t)r * a.H + h) * kHeadDim, true, __ldcg(a.err) == 0);
 }
 
 // partial rows of the shared form: prefix tiles (their number + ranges places of 16), then the rows' own (rows x heads + ranges

@@ -27,6 +27,10 @@ size_t scratch_bytes(long long part_rows) { return kOpHeaderBytes + (size_t)part
 
 bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
 
+// test aid: the CTA of this thread's calls whose copies never count as complete, and how long it waits for them
+struct Expire { int cta = -1; unsigned long long wait_ns = kUnWaitNs; };
+thread_local Expire g_expire;
+
 struct Bytes { const void *p; size_t n; };
 bool overlap(const Bytes &a, const Bytes &b) {
   return a.p && b.p && a.n && b.n && (uintptr_t)a.p < (uintptr_t)b.p + b.n && (uintptr_t)b.p < (uintptr_t)a.p + a.n;
@@ -50,6 +54,13 @@ int check_heads(const char *op, int32_t n_head, int32_t n_kv_head) {
 }  // namespace
 
 extern "C" {
+
+int32_t tts_gpt_debug_expire_op(int32_t cta, uint32_t limit_us) {
+  if (cta < -1 || (cta >= 0 && (limit_us < 1 || limit_us > 100000))) return fail_op(TTS_GPT_E_ARG, "expire_op: cta must be -1 or more, limit_us in 1..100000");
+  g_expire = Expire();
+  if (cta >= 0) { g_expire.cta = cta; g_expire.wait_ns = (unsigned long long)limit_us * 1000ull; }
+  return TTS_GPT_OK;
+}
 
 int32_t tts_gpt_op_page_tables(int32_t n, const int32_t *stream_ids, const int32_t *new_len, int32_t max_streams, const int32_t *ctx_len,
                                int32_t *ctx_len_out, int32_t n_pages, const int32_t *free_pages, const int32_t *free_top, int32_t *free_top_out,
@@ -162,6 +173,7 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
   a.page_table = page_table; a.row_stream = row_stream; a.row_pos = row_pos; a.pool = (const unsigned char *)kv_layer; a.pps = pages_per_stream;
   a.n_pages = n_pages;
   a.err = (int *)scratch;
+  a.wait_ns = g_expire.wait_ns; a.starve = g_expire.cta;
   a.plan = (int *)((char *)scratch + 256 + kOpTicketBytes);
   a.part = (float *)((char *)scratch + kOpHeaderBytes);
   a.suffix_part0 = (int)shared_prefix_part_rows(R, n_kv_head, G);
@@ -236,6 +248,7 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   const int n_sm = device_sms();
   a.few_rows = (long long)q_max * G <= 4 || n_kv_head * blocks * 16 <= (long long)std::min(n_sm, kUnMaxCtas) * kUnWarps;
   a.err = (int *)scratch;
+  a.wait_ns = g_expire.wait_ns; a.starve = g_expire.cta;
   a.tickets = (unsigned *)((char *)scratch + 256);
   a.part = (float *)((char *)scratch + kOpHeaderBytes);
   CUtensorMap k_map = {}, v_map = {};

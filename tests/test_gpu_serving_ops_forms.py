@@ -94,3 +94,76 @@ def test_the_stride_of_a_single_row_is_not_looked_at(stride):
     assert lib.tts_gpt_op_kv_append(1, 2, B.T_F32, kv.data_ptr(), stride, kv.data_ptr() + 512, stride, slot.data_ptr(), 0, 2, pool.data_ptr(), 0) == B.OK, lib.tts_gpt_last_error(None)
     torch.cuda.synchronize()
     assert torch.equal(pool, want) and bool(pool.any())
+
+
+# ---------------------------------------------------------------------------------------------
+# waits that run out
+# ---------------------------------------------------------------------------------------------
+def _shared_call(seed, fmt, H, kv, n_shared, own, qt, pad=0):
+    c = Cache(seed, fmt, kv, n_shared, own, pad=pad)
+    q = _q(seed + 1, len(own) + pad, H, qt)
+    scratch = B.op_attention_shared_scratch(len(own) + pad, H, kv, DEV)
+    rows = torch.ones(q.shape[0], dtype=torch.bool, device=DEV)
+    return lambda **kw: B.op_attention_shared(q, c.pool, *c.args, **kw).view(torch.bfloat16).view(-1, H, 64), scratch, rows
+
+
+def _cross_call(seed, dtype, heads, kv, ql, kl):
+    x = CrossCase(seed, dtype, heads, kv, ql, kl, gap_q=2)
+    rows = torch.zeros(x.q.shape[0], dtype=torch.bool, device=DEV)
+    rows[x.qs[0]:x.qs[-1]] = True
+    return x.run, B.op_attention_cross_scratch(DEV), rows
+
+
+CALLS = {
+    "five rows": lambda: _shared_call(71, "bf16", 20, 20, 7, [1, 40, 130, 0, 64], torch.float32),
+    "8-bit, grouped, padding": lambda: _shared_call(72, "e4m3", 20, 4, 2, [300, 9, 64], torch.bfloat16, pad=2),
+    "no prefix": lambda: _shared_call(73, "bf16", 4, 4, 0, [530, 2, 1000, 1], torch.float32),
+    "second kernel": lambda: _shared_call(74, "bf16", 20, 20, 3, [1 + 7 * i % 90 for i in range(130)], torch.float32),
+    "second kernel, no prefix, 8-bit": lambda: _shared_call(75, "e4m3", 20, 20, 0, [1 + 7 * i % 150 for i in range(130)], torch.bfloat16),
+    "one token each": lambda: _cross_call(76, torch.bfloat16, 20, 20, [1] * 9, [900 - 70 * i for i in range(9)]),
+    "latents": lambda: _cross_call(77, torch.float16, 6, 2, [32, 5, 0, 17], [90, 0, 50, 700]),
+    "tiles": lambda: _cross_call(78, torch.bfloat16, 3, 3, [300, 64, 0, 129], [700, 0, 100, 257]),
+    "tiles, one sequence, grouped": lambda: _cross_call(79, torch.float16, 10, 2, [700], [1500]),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_a_scratch_of_a_failed_call_gives_nan_until_it_is_zeroed(name):
+    call, scratch, rows = CALLS[name]()
+    want = call(scratch=scratch).clone()
+    scratch[:4].view(torch.int32).fill_(1)
+    got = call(scratch=scratch)
+    assert bool(torch.isnan(got[rows]).all()) and torch.equal(got[~rows], want[~rows])
+    assert int(scratch[:4].view(torch.int32)) == 1
+    scratch.zero_()
+    assert torch.equal(call(scratch=scratch), want)
+
+
+@pytest.mark.parametrize("cta", [1, 5])       # both copy something in each of the calls; CTA 0's range may end before a tile's first block
+@pytest.mark.parametrize("name", CALLS)
+def test_rows_behind_an_expired_wait_are_nan(name, cta):
+    """The copies of one CTA never count as complete: the call ends, says so in its scratch, and every head of a row is whole or NaN, also
+    where the caller gave no scratch to look into.  (Calls on tiles of 256 rows take the two seconds of an ordinary wait.)"""
+    call, scratch, rows = CALLS[name]()
+    want = call(scratch=scratch).clone()
+    try:
+        B.debug_expire_op(cta, 20000)
+        got = [call(scratch=scratch).clone()] + ([call().clone()] if cta == 1 else [])
+    finally:
+        B.debug_expire_op(-1)
+    assert int(scratch[:4].view(torch.int32)) == 1
+    for y in got:
+        lost = torch.isnan(y).all(-1)
+        assert bool(lost[rows].any()) and not bool(lost[~rows].any())
+        assert torch.equal(y[~lost], want[~lost])
+    after = call(scratch=scratch)
+    assert bool(torch.isnan(after[rows]).all())
+    scratch.zero_()
+    assert torch.equal(call(scratch=scratch), want) and torch.equal(call()[rows], want[rows])
+
+
+def test_expire_op_refuses():
+    for bad in ((-2, 10), (0, 0), (0, 100001)):
+        with pytest.raises(B.TtsGptError) as e:
+            B.debug_expire_op(*bad)
+        assert e.value.code == B.E_ARG
