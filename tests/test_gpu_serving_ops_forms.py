@@ -39,6 +39,75 @@ def test_kv_append_of_values_whose_scale_vanishes():
     assert not bool(((codes & 0x7F) == 0x7F).any()) and bool((scales > 0).all())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("R,heads,strided", [(6315, 3, True), (1001, 20, False), (3584, 20, True)])
+def test_kv_append_of_large_passes(R, heads, strided, fmt, dtype):
+    """From 8 * 256 * SMs lanes on a thread writes four pieces, of rows a quarter of the pass apart.  6315 rows of 3 heads are 37 890 pieces, not a
+    multiple of four; rows without a slot lie in all four quarters, at their ends too."""
+    assert R * 2 * heads * 8 >= 8 * 256 * torch.cuda.get_device_properties(DEV).multi_processor_count
+    g = _gen(R + heads)
+    n_pages = (R + 63) // 64 + 2
+    if strided:
+        x = (torch.randn(R, 3, heads * 64, generator=g) * 3).to(dtype).to(DEV)
+        k, v = x[:, 1], x[:, 2]
+    else:
+        k, v = torch.randn(R, heads * 64, generator=g).to(dtype).to(DEV), (torch.randn(R, heads * 64, generator=g) * 1e-3).to(dtype).to(DEV)
+    k[R // 2, :64] = 0                              # a head whose values are all zero
+    slot = torch.randperm(n_pages * 64, generator=g)[:R].int()
+    for i in range(4):
+        a, b = i * R // 4, (i + 1) * R // 4
+        for at, bad in zip((a, a + 1, (a + b) // 2, b - 2, b - 1), (-1, n_pages * 64, 2 ** 31 - 1, -2 ** 31, -64)):
+            slot[at] = bad
+    pool = torch.randint(0, 100, (n_pages, 2, heads, 8192 if fmt == "bf16" else E4M3_BLOCK), generator=g, dtype=torch.uint8).to(DEV)
+    want = pool.clone()
+    B.op_kv_append(k, v, pool.view(torch.bfloat16).view(n_pages, 2, heads, 64, 64) if fmt == "bf16" else pool, slot.to(DEV))
+    ok = (slot >= 0) & (slot < n_pages * 64)
+    assert int(ok.sum()) == R - 20
+    rows, slots = torch.nonzero(ok)[:, 0].to(DEV), slot[ok].long().to(DEV)
+    page, off = slots // 64, slots % 64
+    for part, src in enumerate((k, v)):
+        y = src[rows].float().view(-1, heads, 64)
+        if fmt == "bf16":
+            want.view(torch.bfloat16).view(n_pages, 2, heads, 64, 64)[page, part, :, off] = y.bfloat16()
+        else:
+            codes, scales = _encoded(y)
+            want[..., :4096].unflatten(-1, (64, 64))[page, part, :, off] = codes
+            want[..., 4096:].view(torch.float32)[page, part, :, off] = scales
+    assert torch.equal(pool, want)
+
+
+# ---------------------------------------------------------------------------------------------
+# attention whose parts a second kernel adds
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("qt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("R,H,kv,n_shared", [(130, 20, 20, 0), (130, 20, 20, 3), (300, 20, 4, 0), (300, 20, 4, 5), (520, 12, 4, 1), (1300, 16, 1, 2), (2600, 3, 3, 0)])
+def test_shared_prefix_attention_of_large_batches(R, H, kv, n_shared, qt, fmt):
+    """More units of 32 keys than CTAs can merge themselves (52 an SM): rows finished by one warp, rows cut by a range's end, rows whose own keys
+    are none, rows that end inside the shared pages, rows of another's stream, padding."""
+    own = [(0, 1, 31, 32, 33, 64, 65, 90, 17, 128)[i % 10] if i % 7 else 150 for i in range(R)]
+    if n_shared == 0:
+        own = [max(1, x) for x in own]
+    # rows 1, 12: end inside the shared pages (or, without any, early); row 3 reads row 7's stream up to its third key from the end
+    short = [(1, 1, 64 * n_shared // 2 if n_shared else 0), (12, 12, 64 * n_shared - 1 if n_shared else 5), (3, 7, 64 * n_shared + own[7] - 3)]
+    c = Cache(R + n_shared, fmt, kv, n_shared, own, pad=3, same_stream=short)
+    R += 3
+    rpt, pps = 16 // (H // kv), c.args[0].shape[1]
+    units = kv * -(-R // rpt) * (2 * n_shared + 1) + R * kv * (2 * (pps - n_shared) + 1)
+    assert units > 52 * min(160, torch.cuda.get_device_properties(DEV).multi_processor_count)
+    q = _q(R, R, H, qt)
+    got = B.op_attention_shared(q, c.pool, *c.args)
+    c.check(got, q, "large batch")
+    assert torch.all(got[-3:].view(torch.bfloat16) == 0)
+
+
+def test_shared_prefix_attention_of_sixty_rows():
+    c = Cache(11, "bf16", 20, 4, [50 + 7 * i for i in range(60)])
+    q = _q(6, 60, 20, torch.float32)
+    c.check(B.op_attention_shared(q, c.pool, *c.args), q, "sixty rows")
+
+
 # ---------------------------------------------------------------------------------------------
 # strides that address nothing
 # ---------------------------------------------------------------------------------------------
