@@ -334,7 +334,8 @@ int32_t tts_gpt_op_attention(int32_t R, int32_t n_head, const float *q, const vo
  * bf16, sums and accumulators stay fp32).  It has no waits.
  * cluster_size -3: the prefill variant the engine uses for passes of more than 128 rows, same requirement on
  * the rows: 128 consecutive rows per CTA, Q K^T and P V as tcgen05 instructions with the scores and the
- * output in tensor memory (same roundings as -2); its waits are bounded.
+ * output in tensor memory (same roundings as -2); its waits are bounded.  The pages of all streams that have rows among 128
+ * such rows (r / 128 the same) must be 256 at most, as they are in a prefill pass: the rows are NaN otherwise.
  * The waits on the copies of variants 0 and -1 are bounded; this stand-alone entry does not report an
  * expired wait (the engine does, as TTS_GPT_E_TIMEOUT).  q, out and kv_layer must be 16-byte aligned. */
 int32_t tts_gpt_op_attention_cluster(int32_t R, int32_t n_head, const float *q, const void *kv_layer,

@@ -29,7 +29,7 @@ constexpr int kPtRows = 128;
 constexpr int kPtThreads = 352;
 constexpr int kPtSlots = 3;         // pages in shared memory
 constexpr int kPtMergePitch = 65;   // floats per row of the merge buffer: lane = row, conflict-free
-constexpr int kPtMaxJobs = 256;   // two partial long streams + streams of at most 128 rows
+constexpr int kPtMaxJobs = 256;   // two partial long streams + streams of at most 128 rows; a tile with more pages is NaN
 
 __device__ __forceinline__ void pt_cp16(void *smem, const void *gmem, bool real) {
   // a row that does not exist is filled with zeros (stale shared memory may hold NaN, and 0 * NaN must not reach O)
@@ -74,6 +74,7 @@ __global__ void __launch_bounds__(kPtThreads, PAIRED ? 2 : 1) attention_prefill_
   __shared__ int seg_stream[kPtRows], seg_i0[kPtRows], seg_i1[kPtRows], seg_last[kPtRows];
   __shared__ unsigned short jobs[kPtMaxJobs];   // (run << 8) | page, in run order
   __shared__ int n_job_s;
+  __shared__ float one_s;                       // 1, or NaN where the tile's runs have more pages than there are jobs
   __shared__ unsigned run_open[kPtRows / 32];   // bit l of word w: row 32 w + l opens a run
   __shared__ int job_ph[kPtMaxJobs];            // physical page of each job
   __shared__ int2 job_rows[kPtMaxJobs];         // x: rows of the tile the job's run covers, first | end << 16; y: first position of its page
@@ -117,10 +118,13 @@ __global__ void __launch_bounds__(kPtThreads, PAIRED ? 2 : 1) attention_prefill_
   __syncthreads();
   if (threadIdx.x == 0) {
     const int n = __popc(run_open[0]) + __popc(run_open[1]) + __popc(run_open[2]) + __popc(run_open[3]);
-    int nj = 0;
-    for (int sg = 0; sg < n; ++sg)
+    int nj = 0, pages = 0;
+    for (int sg = 0; sg < n; ++sg) {
+      pages += seg_last[sg] / kPageTokens + 1;
       for (int pg = 0; pg <= seg_last[sg] / kPageTokens && nj < kPtMaxJobs; ++pg) jobs[nj++] = (unsigned short)((sg << 8) | pg);
+    }
     n_job_s = nj;
+    one_s = pages <= kPtMaxJobs ? 1.0f : __int_as_float(0x7FFFFFFF);
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -335,7 +339,7 @@ __global__ void __launch_bounds__(kPtThreads, PAIRED ? 2 : 1) attention_prefill_
       const float M = fmaxf(m, m1);
       const float a0 = (m == -INFINITY) ? 0.f : pt_exp2(m - M), a1 = (m1 == -INFINITY) ? 0.f : pt_exp2(m1 - M);
       const float lt = l * a0 + l1 * a1;
-      const float inv = lt > 0.f ? 1.0f / lt : 0.f;
+      const float inv = lt > 0.f ? one_s / lt : one_s - 1.0f;
       const float w0 = a0 * inv, w1 = a1 * inv;
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
