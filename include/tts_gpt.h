@@ -414,12 +414,15 @@ int32_t tts_gpt_op_kv_append(int32_t R, int32_t n_head, int32_t type, const void
                              int64_t v_stride, const int32_t *row_slot, int32_t kv_fmt, int32_t n_pages, void *kv_layer,
                              void *cuda_stream);
 
-/* Attention of a batch whose streams begin with the same pages: as tts_gpt_op_attention (row r attends over keys
- * 0..row_pos[r] of stream row_stream[r], o = softmax(q.K^T / 8) V per head), where the first n_shared entries of the page lists of
+/* Attention of a batch whose streams begin with the same pages: row r attends over keys 0..row_pos[r] of stream row_stream[r],
+ * o = softmax(q.K^T / 8) V per head, as in tts_gpt_op_attention (which keeps fp32 queries and weights whole; roundings here: below), where the first n_shared entries of the page lists of
  * all R rows are the same pages, which are read once for all rows and not once for each.  n_shared may be 0.  Query head
  * h reads the keys of head h / (n_head / n_kv_head), at most 16 to one.  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements
  * apart; out bf16 [R][n_head*64]; neither it nor scratch may overlap anything else that the call is given (E_ARG).  A row with row_pos -1 or a negative row_stream has no keys: its output
- * is zero.  Several rows may belong to one stream.  Keys on a page outside 0..n_pages-1 are left out, as are those behind the
+ * is zero.  Other row_stream are numbers of lists that page_table has.  Several rows may belong to one stream, but each reads
+ * the keys behind the shared pages for itself: for a pass of many rows a stream op_attention_cluster -3 is several times faster (3210 rows of 23
+ * prompts behind 7 shared pages, 20 heads, 73 us against 303), and 2 there for a few single rows (five 5.7 us against 10.8), where
+ * the cache is bf16 and heads are not grouped.  Keys on a page outside 0..n_pages-1 are left out, as are those behind the
  * list's pages_per_stream pages.  K and V of the shared pages must be finite.  fp32 queries enter with 16 bits, the softmax weights are rounded to bf16, sums are fp32; results do
  * not depend on timing.  R <= 4096.
  * scratch (256-byte aligned, >= scratch_bytes; zero before its first use, by this call or op_attention_cross, in any size)
@@ -436,7 +439,7 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
  * k_start[i] .. k_start[i+1]-1 (rows of k and v), all of them, o = softmax(scale q.K^T) V per head.  Lengths are ragged and
  * independent; a sequence without keys has zero outputs, rows outside every sequence are left as they were.  q_start, k_start:
  * ascending (where one does not, nothing is written), n + 1 each, at most q_rows and k_rows; q_max: at least the longest sequence of queries (rows beyond it are not
- * computed).  q, k, v, out of one type, TTS_GPT_T_BF16 or TTS_GPT_T_F16; q rows q_stride elements apart with contiguous heads, k and v with
+ * computed); it decides which kernel serves the whole call, so that sequences of one query go faster in a call of their own than beside one of hundreds.  q, k, v, out of one type, TTS_GPT_T_BF16 or TTS_GPT_T_F16; q rows q_stride elements apart with contiguous heads, k and v with
  * strides of rows and of heads (so both [rows][heads][64], parts of one array, and [heads][rows][64]); out [q_rows][n_head*64]; neither
  * it nor scratch may overlap anything else that the call is given (E_ARG).
  * Heads, roundings and scratch as for op_attention_shared (scratch size independent of the call).  n <= 4096, rows below 2^30. */

@@ -5,8 +5,8 @@
 // warps owns its row t = accumulator lane t.  For each block of 128 keys, which both halves read from one copy in shared memory,
 //     S = Q K^T     tcgen05.mma M=128 x N=128 x K=64, S (fp32) in tensor memory
 //     softmax       S out of tensor memory, running reference m and sum l in fp32, P = 2^(S scale - m) rounded to the inputs' type
-//                   back into tensor memory.  The reference moves, and O with it, only where a score exceeds it by 2^8: weights
-//                   stay below 256 and the rounding of a weight is relative, so nothing is lost
+//                   back into tensor memory.  The reference moves, and O with it, only where a scaled score (log2 units) exceeds it by
+//                   more than 8: weights stay at or below 2^8 and the rounding of a weight is relative, so nothing is lost
 //     O += P V      M=128 x N=64 x K=128, P as the operand in tensor memory, V as stored
 // S takes 128 columns, P 64 and O 64 of each half: all of an SM's tensor memory.  S of block j + 1 is computed while the softmax works on
 // S of block j, which by then is in registers; one half's softmax runs beside the other's.
@@ -14,7 +14,8 @@
 // Bound and measurements.  A block of 256 rows by 128 keys is 1024 tensor cycles, and 2048 cycles of exponentials at 16 a cycle and
 // SM; a quarter of them goes through a polynomial on the FMA pipes (every 8th, 4th, 3rd, 2nd pair: 99, 94, 95, 107 us for 8 sequences
 // of 517 to 1500 queries by 700 to 1500 keys, 20 heads, fp16; none: 99).  With the loads and stores of tensor memory and the maximum a
-// block takes some 2500 cycles, a change of tile 4500.  Those sequences take 94 us, 0.52 PFLOP/s; 1536 by 1536 take 145 us, 0.67 PFLOP/s.
+// block takes some 2500 cycles, a change of tile 4500.  Those sequences take 94.7 us, 0.52 PFLOP/s, the tensor pipe at 27 %, that of the
+// exponentials at 38 %, 43 % of the issue slots; 1536 by 1536 take 145 us, 0.67 PFLOP/s.
 // What came before: S only once P of the block before was there 102 us (3000 cycles a block, though no pipe had more than 2048 to do);
 // 128 rows a CTA, two or four CTAs an SM, K and V out of L2 twice as often 131 us; two threads a row 134 us.
 //

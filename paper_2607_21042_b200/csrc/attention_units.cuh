@@ -24,9 +24,11 @@
 //
 // Bound and measurements.  Where each row has keys of its own, the bytes: 128 rows behind 1024 shared tokens, 3 to 900 of their own,
 // 20 heads, bf16, 302 MB: 64 us, 4.7 TB/s, of which the start and the second kernel take 8; 16 queries of one token by 100 to 1500
-// keys, 20 heads, 65 MB: 20 us, half of them the start, the tickets and the merge.  Where many rows share keys, m16n8k16, which runs at about
-// 1/16 of the tcgen05 rate, and the code around it: 300 rows of 20 heads by 4, 1536 shared tokens, 8 bits: 44 us, 60 TFLOP/s; 16 by 32
-// queries by 90 to 1500 keys: 30 us.  Five rows behind 448 tokens: 10.6 us, latency from end to end.
+// keys, 20 heads, 65 MB: 20 us, half of them the start, the tickets and the merge.  Where many rows share keys, instructions: 300 rows of 20 heads
+// by 4, 1536 shared tokens, 8 bits: 44.5 us, 59 TFLOP/s, 63 % of the issue slots and 54 % of the ALU pipe, which widens the codes anew for each tile
+// of 16 rows; the tensor pipe is at 18 % (m16n8k16 alone gives 555 TFLOP/s here, a third of tcgen05).  16 by 32 queries by 90 to 1500
+// keys: 30 us, latency: 29 % of the issue slots, 15 % of the tensor pipe, K and V read by two warps.  Five rows behind 448 tokens: 10.8 us,
+// latency from end to end.
 // Measured and not kept (us for 128 rows / 300 rows above): tiles of 32 rows 83 / 51; queries as the 8-wide operand 65 and 12.3 for five
 // rows; tickets instead of the second kernel 79 / 56.
 #pragma once

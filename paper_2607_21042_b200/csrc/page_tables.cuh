@@ -11,7 +11,8 @@
 // of the rows and of the list entries, which it finds by bisection: one launch, no CTA waits for another.  What a caller may
 // update in place (contexts, stack height) is then written by the CTA that leaves last, when every CTA has read it.
 // Bound: two dependent reads (ids, contexts), one of the page stack, the launch; 12 bytes a row where there are many.  16 requests of a
-// token 3.5 us, 128 requests 5.3 us, 1000 requests with half a million rows 6.8 us.
+// token 3.5 us, 128 requests with 3315 rows 5.2 us, 1000 requests with half a million rows 6.8 us; updated in place 0.1 us more from one CTA, 0.3 to
+// 1 us from several, whose last one's turn it then is.
 #pragma once
 #include <cuda_fp8.h>
 #include <algorithm>
