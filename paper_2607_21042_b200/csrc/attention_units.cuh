@@ -32,9 +32,8 @@
 // Measured and not kept (us for 128 rows / 300 rows above): tiles of 32 rows 83 / 51; queries as the 8-wide operand 65 and 12.3 for five
 // rows; tickets instead of the second kernel 79 / 56.
 #pragma once
-#include <cuda_fp16.h>
+#include "attention_common.cuh"
 #include "page_tables.cuh"
-#include "tcgen05.cuh"
 #include "tensor_map.cuh"
 
 namespace ttsgpt {
@@ -52,33 +51,6 @@ constexpr int kUnPitch = 68;                // floats of a partial row: o[64], m
 constexpr unsigned long long kUnWaitNs = 2000000000ull;
 
 enum { KV_BF16 = 0, KV_F16 = 1, KV_E4M3 = 2 };   // what the keys and values are stored as
-
-// Division by a number that is the same throughout a launch, in three instructions and not in the thirty of a general one: code is
-// fetched cold in every launch, and these kernels divide in many places.  For 0 <= n < 2^31: with l = ceil(log2 d) and
-// m = ceil(2^(31 + l) / d), n / d = floor(n m / 2^(31 + l)) (m d exceeds 2^(31 + l) by less than d <= 2^l).
-struct Div {
-  uint32_t d, m, s;
-  __host__ __device__ void set(uint32_t by) {
-    d = by; m = 0; s = 0;
-    if (by > 1) {
-      uint32_t q = 0x80000000u / by, r = 0x80000000u - q * by, l = 0;   // 2^31 = q d + r, doubled l times
-      while ((1u << l) < by) {
-        ++l;
-        q <<= 1; r <<= 1;
-        if (r >= by) { r -= by; ++q; }
-      }
-      m = q + (r != 0);
-      s = l - 1;
-    }
-  }
-  __device__ __forceinline__ int of(int n) const {
-#ifdef __CUDA_ARCH__
-    return d == 1 ? n : (int)(__umulhi((uint32_t)n, m) >> s);
-#else
-    return n / (int)d;
-#endif
-  }
-};
 
 struct UnitArgs {
   const void *q;
@@ -129,10 +101,6 @@ template <int KV> inline size_t units_smem_bytes(int n) {
   return (size_t)kUnWarps * UnitLayout<KV>::kStages * UnitLayout<KV>::kStage + 1024 + kUnWarps * UnitLayout<KV>::kStages * 8 + (size_t)(2 * n + 1) * 4 + 64;
 }
 
-__device__ __forceinline__ void un_box(const CUtensorMap *map, int c1, int c2, unsigned char *dst, uint64_t *bar) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-               ::"r"(smem_u32(dst)), "l"(map), "r"(0), "r"(c1), "r"(c2), "r"(smem_u32(bar)) : "memory");
-}
 template <bool F16>
 __device__ __forceinline__ void un_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if constexpr (F16)
@@ -140,20 +108,6 @@ __device__ __forceinline__ void un_mma(float (&c)[4], const uint32_t (&a)[4], ui
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   else mma_bf16_16816(c, a[0], a[1], a[2], a[3], b0, b1);
 }
-template <bool F16>
-__device__ __forceinline__ uint32_t un_pack(float lo, float hi) {
-  if constexpr (F16) { const __half2 v = __floats2half2_rn(lo, hi); return *reinterpret_cast<const uint32_t *>(&v); }
-  else return pack_bf16x2(lo, hi);
-}
-// Two e4m3 codes, in the upper bytes of the halves of x (the lower bytes are ignored), as bf16: the bits moved into place are the
-// value times 2^-120, exactly (denormals too).  The NaN code reads as 480.
-__device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t x) {
-  const uint32_t y = (x & 0x80008000u) | ((x >> 4) & 0x07F007F0u);
-  uint32_t r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(y), "r"(0x7B807B80u));   // 2^120
-  return r;
-}
-
 // First partial row of a part.  A tile's parts are numbered tile + range, which never repeats along the units; sequences, whose
 // tiles only meet where a range ends, have two places a range: for the tile that goes on behind it, and the one that began before.
 __device__ __forceinline__ size_t prefix_part(int tile, int range) { return (size_t)(tile + range) * kUnTile; }

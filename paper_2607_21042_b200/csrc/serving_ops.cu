@@ -4,19 +4,17 @@
 #include <algorithm>
 #include <cmath>
 
-#include "host.cuh"
-#include "page_tables.cuh"
+#include "op_checks.cuh"
 #include "attention_tiles.cuh"
 
 using namespace ttsgpt;
 
-namespace {
+Expire &ttsgpt::op_expire() {
+  static thread_local Expire e = {-1, kUnWaitNs};
+  return e;
+}
 
-#define OP_TRY(expr)                                                                                   \
-  do {                                                                                                 \
-    cudaError_t e_ = (expr);                                                                           \
-    if (e_ != cudaSuccess) return fail_op(TTS_GPT_E_CUDA, "%s: %s", #expr, cudaGetErrorString(e_));   \
-  } while (0)
+namespace {
 
 // Scratch of the two attentions: [error word][tickets][plan][partial rows], the first three of the same size in every call, so
 // that calls of other sizes, of either kind, find the tickets at zero where the call before left them.
@@ -24,25 +22,6 @@ constexpr size_t kOpTicketBytes = kUnTickets * sizeof(unsigned), kOpPlanBytes = 
 constexpr size_t kOpHeaderBytes = 256 + kOpTicketBytes + kOpPlanBytes;
 static_assert(kUnTickets >= kUnMaxWarps && kUnTickets >= kTlTile / 32 * kTlMaxCtas && kUnTickets >= kUnMaxTiles * kUnMaxCtas, "a ticket per range, or per row and group of a call that merges itself");
 size_t scratch_bytes(long long part_rows) { return kOpHeaderBytes + (size_t)part_rows * kUnPitch * sizeof(float); }
-
-bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
-
-// test aid: the CTA of this thread's calls whose copies never count as complete, and how long it waits for them
-struct Expire { int cta = -1; unsigned long long wait_ns = kUnWaitNs; };
-thread_local Expire g_expire;
-
-struct Bytes { const void *p; size_t n; };
-bool overlap(const Bytes &a, const Bytes &b) {
-  return a.p && b.p && a.n && b.n && (uintptr_t)a.p < (uintptr_t)b.p + b.n && (uintptr_t)b.p < (uintptr_t)a.p + a.n;
-}
-// rows of `width` elements, `stride` apart
-Bytes rows_of(const void *p, long long rows, long long stride, long long width, size_t size) {
-  return {p, rows > 0 ? (size_t)((rows - 1) * stride + width) * size : 0};
-}
-
-Bytes pool_of(const void *kv_layer, int32_t kv_fmt, int32_t n_pages, int32_t heads) {
-  return {kv_layer, (size_t)n_pages * 2 * heads * (kv_fmt == TTS_GPT_KV_BF16 ? (size_t)kPageElems * 2 : (size_t)kE4m3BlockBytes)};
-}
 
 int check_heads(const char *op, int32_t n_head, int32_t n_kv_head) {
   if (n_head < 1 || n_kv_head < 1 || n_head % n_kv_head) return fail_op(TTS_GPT_E_ARG, "%s: n_head must be a multiple of n_kv_head", op);
@@ -57,8 +36,7 @@ extern "C" {
 
 int32_t tts_gpt_debug_expire_op(int32_t cta, uint32_t limit_us) {
   if (cta < -1 || (cta >= 0 && (limit_us < 1 || limit_us > 100000))) return fail_op(TTS_GPT_E_ARG, "expire_op: cta must be -1 or more, limit_us in 1..100000");
-  g_expire = Expire();
-  if (cta >= 0) { g_expire.cta = cta; g_expire.wait_ns = (unsigned long long)limit_us * 1000ull; }
+  op_expire() = cta >= 0 ? Expire{cta, (unsigned long long)limit_us * 1000ull} : Expire{-1, kUnWaitNs};
   return TTS_GPT_OK;
 }
 
@@ -173,7 +151,7 @@ int32_t tts_gpt_op_attention_shared(int32_t R, int32_t n_head, int32_t n_kv_head
   a.page_table = page_table; a.row_stream = row_stream; a.row_pos = row_pos; a.pool = (const unsigned char *)kv_layer; a.pps = pages_per_stream;
   a.n_pages = n_pages;
   a.err = (int *)scratch;
-  a.wait_ns = g_expire.wait_ns; a.starve = g_expire.cta;
+  a.wait_ns = op_expire().wait_ns; a.starve = op_expire().cta;
   a.plan = (int *)((char *)scratch + 256 + kOpTicketBytes);
   a.part = (float *)((char *)scratch + kOpHeaderBytes);
   a.suffix_part0 = (int)shared_prefix_part_rows(R, n_kv_head, G);
@@ -250,7 +228,7 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
   const int n_sm = device_sms();
   a.few_rows = (long long)q_max * G <= 4 || n_kv_head * blocks * 16 <= (long long)std::min(n_sm, kUnMaxCtas) * kUnWarps;
   a.err = (int *)scratch;
-  a.wait_ns = g_expire.wait_ns; a.starve = g_expire.cta;
+  a.wait_ns = op_expire().wait_ns; a.starve = op_expire().cta;
   a.tickets = (unsigned *)((char *)scratch + 256);
   a.part = (float *)((char *)scratch + kOpHeaderBytes);
   CUtensorMap k_map = {}, v_map = {};
