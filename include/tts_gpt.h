@@ -450,6 +450,84 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
                                    const int32_t *k_start, int32_t q_max, float scale, void *out, void *scratch,
                                    size_t scratch_bytes, void *cuda_stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Several drafted tokens a step, over the same paged cache.  A draft is a tree: node 0 is the token that the stream has sampled last, every
+ * other node a guess at what follows its parent.  All nodes of all requests are the rows of one pass, whose slots op_page_tables gives
+ * (new_len = nodes); op_tree_tables makes masks and positions of the parents, op_rope_kv_append rotates and writes the rows,
+ * op_attention_tree attends, op_sample says what the model would have said after each node, op_tree_accept keeps the path that agrees with it,
+ * and op_kv_move brings that path's K and V to where the stream goes on.  Rules as for the operators above.  In all of these calls
+ *   tree i (of n) is rows row_start[i] .. row_start[i+1]-1 of R (n + 1 starts, ascending, at most R), of stream stream_ids[i] (NULL: i);
+ *   kv_len[stream] counts the stream's tokens with the tree's nodes, which are the last of them; those before are committed.
+ * ------------------------------------------------------------------------------------------- */
+
+/* How the frequencies of rotary positions are stretched: not at all; all divided by `factor`; the base raised so that the slowest one is (NTK); the
+ * slow ones divided, with a blend between pairs that turn `high` and `low` times in `original` positions, by pair (YARN, which also multiplies
+ * cosine and sine by 0.1 ln(factor) + 1) or by number of turns (BANDS); or as the caller gives them. */
+enum { TTS_GPT_ROPE_NONE = 0, TTS_GPT_ROPE_LINEAR = 1, TTS_GPT_ROPE_NTK = 2, TTS_GPT_ROPE_YARN = 3, TTS_GPT_ROPE_BANDS = 4, TTS_GPT_ROPE_GIVEN = 5 };
+
+/* The table op_rope_kv_append takes, on the host, no CUDA call: pair i of n_rot / 2 (n_rot even, 2..64) turns by w_i radians a position, w_i =
+ * base^(-2 i / n_rot) stretched as `scaling` says, or inv_freq[i] (HOST, only with TTS_GPT_ROPE_GIVEN).  turns (HOST, n_rot / 2 values): w_i / 2 pi modulo 1 in
+ * units of 2^-64, so that the phase of any position is exact to 2^-64 turns times the position.  *magnitude (HOST): what cosine and sine
+ * are to be multiplied by.  Arguments that a scaling does not name are not looked at. */
+int32_t tts_gpt_op_rope_frequencies(int32_t n_rot, int32_t scaling, double base, double factor, double original, double low, double high, const double *inv_freq,
+                                    uint64_t *turns, float *magnitude);
+
+/* A pass's rows rotated by their positions: q to q_out, K (rotated) and V (as it is) into their slots as in op_kv_append, whose rules for strides, slots
+ * and formats hold.  The first n_rot values of a head turn in pairs (i, i + n_rot/2) or, interleaved, (2i, 2i + 1):
+ *   a' = magnitude (a cos - b sin),  b' = magnitude (b cos + a sin)  of the angle row_pos w_i;
+ * the others stay.  Any position is fine, a negative one turns back.  q, K and V of one type, TTS_GPT_T_F32 or TTS_GPT_T_BF16; q_out of either type, rows
+ * out_stride elements apart; it may be q itself (same type and stride).  turns DEVICE, 8-byte aligned.  n_head 0: K and V only, q and q_out are not
+ * looked at.  A row whose slot lies outside the pool is left out, its q_out included.  Sums in fp32, each value rounded once; e4m3 scales are
+ * those of the rotated values. */
+int32_t tts_gpt_op_rope_kv_append(int32_t R, int32_t n_head, int32_t n_kv_head, int32_t type, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                  const void *v, int64_t v_stride, const int32_t *row_pos, const int32_t *row_slot, int32_t n_rot, const uint64_t *turns,
+                                  int32_t interleaved, float magnitude, int32_t out_type, void *q_out, int64_t out_stride, int32_t kv_fmt, int32_t n_pages, void *kv_layer,
+                                  void *cuda_stream);
+
+/* Masks and positions of trees: parent[r] is the number of row r's parent inside its tree, lower than its own, or -1.  tree_mask [R][mask_words]: bit j
+ * (word j / 32, bit j % 32) is set where node j is the row or one of its ancestors, or else zero; row_pos[r] = committed tokens + number of ancestors.
+ * Rows behind the last tree are left as they were, and so are trees with something wrong: info[0] (zero before the first use) becomes the lowest of
+ * the codes of all trees, and stays: E_ARG (starts, parents, fewer tokens than nodes), E_STREAM (an id outside 0..max_streams-1),
+ * E_WORKSPACE (more nodes than 32 mask_words).  n <= 4096, mask_words <= 8, max_streams <= 32768. */
+int32_t tts_gpt_op_tree_tables(int32_t n, int32_t R, const int32_t *row_start, const int32_t *stream_ids, int32_t max_streams, const int32_t *kv_len, const int32_t *parent,
+                               int32_t mask_words, int32_t *tree_mask, int32_t *row_pos, int32_t *info, void *cuda_stream);
+
+/* Attention of trees: row r attends to all committed keys of its stream and, of the tree's nodes j, to those whose bit its mask has (any mask; the row's
+ * own bit counts like the others; bits of nodes that the tree has not, and nodes beyond 32 mask_words, count as not set), o = softmax(scale q.K^T) V per head.
+ * A row without keys is zero; a stream outside 0..max_streams-1 has none.  Keys on a page outside 0..n_pages-1 are left out, as are those behind pages_per_stream
+ * pages.  K and V of committed keys must be finite; those of a node matter only to rows that see it, which become NaN where they are not
+ * finite.  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements apart; out bf16 [R][n_head*64]; neither it nor scratch may overlap anything else that
+ * the call is given (E_ARG).  t_max: at least the largest tree (rows beyond it are not computed); with the heads of a group it decides how a tile's
+ * work is spread, so that small trees go faster in a call of their own than beside large ones.  Rows of no tree are left as they were; where starts do not
+ * ascend, or exceed R, nothing is written.  Heads, roundings, timing and scratch as for op_attention_shared (scratch size independent of the
+ * call).  n <= 2048, mask_words <= 32. */
+int32_t tts_gpt_op_attention_tree_scratch_bytes(size_t *bytes);
+int32_t tts_gpt_op_attention_tree(int32_t n, int32_t R, int32_t n_head, int32_t n_kv_head, int32_t type, const void *q, int64_t q_stride, int32_t kv_fmt, int32_t n_pages,
+                                  const void *kv_layer, int32_t max_streams, const int32_t *page_table, int32_t pages_per_stream, const int32_t *row_start,
+                                  const int32_t *stream_ids, const int32_t *kv_len, int32_t mask_words, const int32_t *tree_mask, int32_t t_max, float scale, void *out,
+                                  void *scratch, size_t scratch_size, void *cuda_stream);
+
+/* The path on which a draft and the model agree: node 0, then again and again the first child (parent[r], as above) whose draft[r] is the token that
+ * target has for its parent.  path[row_start[i] + k] is the row of the k-th accepted node, ascending, and -1 behind the last; n_accepted[i] their number (0: a tree
+ * without nodes); next_token[i] = target of the last one, or -1.  The streams then go back to the accepted nodes: kv_len_out[stream] = committed + accepted, and
+ * the pages behind that many tokens go back onto the stack free_pages (of n_pages places, *free_top filled), request by request in the order of the
+ * call, a list's last page first (they stay in the page list, where op_page_tables overwrites them).  kv_len_out and free_top_out may be kv_len and free_top; nothing else may overlap an
+ * output (E_ARG).  info: int32 [8], zero before its first use: {status, accepted nodes, pages returned, height of the stack, ...}; status E_ARG (starts, parents, fewer
+ * tokens than nodes, a height outside 0..n_pages, more pages than the stack has places), E_STREAM (an id outside 0..max_streams-1, or twice), E_CTX_OVERFLOW (more tokens
+ * than pages_per_stream pages hold), E_WORKSPACE (more than 256 nodes): then lengths, stack and height are left as they were, a tree with wrong parents or too many nodes accepts
+ * nothing, and the others' paths are written.  n <= 4096, max_streams and pages_per_stream <= 32768.  Two calls that share info or update the same
+ * streams must be ordered. */
+int32_t tts_gpt_op_tree_accept(int32_t n, int32_t R, const int32_t *row_start, const int32_t *stream_ids, const int32_t *draft, const int32_t *target, const int32_t *parent,
+                               int32_t max_streams, const int32_t *kv_len, int32_t *kv_len_out, const int32_t *page_table, int32_t pages_per_stream, int32_t n_pages,
+                               int32_t *free_pages, const int32_t *free_top, int32_t *free_top_out, int32_t *path, int32_t *n_accepted, int32_t *next_token, int32_t *info,
+                               void *cuda_stream);
+
+/* K and V of accepted nodes to where they belong, in n_layers layers (their pools layer_bytes apart, a multiple of 16): the k-th row of
+ * path[row_start[i] ..], which ascends and ends at the first -1, from its slot row_slot[row] to the slot of row row_start[i] + k.  Codes and scales move as they are.  A row
+ * that is where it belongs stays; a row whose slot, or the slot that it should go to, lies outside the pool is left out.  Slots must be distinct. */
+int32_t tts_gpt_op_kv_move(int32_t n, int32_t R, const int32_t *row_start, const int32_t *path, const int32_t *row_slot, int32_t n_kv_head, int32_t kv_fmt, int32_t n_pages,
+                           int32_t n_layers, int64_t layer_bytes, void *kv_layers, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

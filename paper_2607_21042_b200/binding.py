@@ -32,17 +32,25 @@ EXPORTS = [
     "tts_gpt_op_sample",
     "tts_gpt_op_page_tables", "tts_gpt_op_kv_append", "tts_gpt_op_attention_shared_scratch_bytes", "tts_gpt_op_attention_shared",
     "tts_gpt_op_attention_cross_scratch_bytes", "tts_gpt_op_attention_cross",
+    "tts_gpt_op_rope_frequencies", "tts_gpt_op_rope_kv_append", "tts_gpt_op_tree_tables", "tts_gpt_op_attention_tree_scratch_bytes", "tts_gpt_op_attention_tree",
+    "tts_gpt_op_tree_accept", "tts_gpt_op_kv_move",
 ]
 T_F32, T_BF16, T_F16 = 0, 1, 2
 _TYPES = {torch.float32: T_F32, torch.bfloat16: T_BF16, torch.int16: T_BF16, torch.float16: T_F16}   # int16: bf16 bits
 # Argument types of the calls below that are made once a step or more: declared, ctypes converts plain numbers itself, several
 # times faster than from objects made for each argument.
-_i, _l, _p = C.c_int32, C.c_int64, C.c_void_p  # noqa: E741
+_i, _l, _p, _f, _d = C.c_int32, C.c_int64, C.c_void_p, C.c_float, C.c_double  # noqa: E741
 _ARGTYPES = {
     "tts_gpt_op_page_tables": [_i, _p, _p, _i, _p, _p, _i, _p, _p, _p, _i, _p, _i, _p, _i, _p, _p, _p, _p, _p, _p],
     "tts_gpt_op_kv_append": [_i, _i, _i, _p, _l, _p, _l, _p, _i, _i, _p, _p],
     "tts_gpt_op_attention_shared": [_i, _i, _i, _i, _p, _l, _i, _i, _p, _i, _p, _i, _p, _p, _p, _p, C.c_size_t, _p],
     "tts_gpt_op_attention_cross": [_i, _i, _i, _i, _i, _p, _l, _i, _p, _l, _l, _p, _l, _l, _p, _p, _i, C.c_float, _p, _p, C.c_size_t, _p],
+    "tts_gpt_op_rope_frequencies": [_i, _i, _d, _d, _d, _d, _d, _p, _p, _p],
+    "tts_gpt_op_rope_kv_append": [_i, _i, _i, _i, _p, _l, _p, _l, _p, _l, _p, _p, _i, _p, _i, _f, _i, _p, _l, _i, _i, _p, _p],
+    "tts_gpt_op_tree_tables": [_i, _i, _p, _p, _i, _p, _p, _i, _p, _p, _p, _p],
+    "tts_gpt_op_attention_tree": [_i, _i, _i, _i, _i, _p, _l, _i, _i, _p, _i, _p, _i, _p, _p, _p, _i, _p, _i, _f, _p, _p, C.c_size_t, _p],
+    "tts_gpt_op_tree_accept": [_i, _i, _p, _p, _p, _p, _p, _i, _p, _p, _p, _i, _i, _p, _p, _p, _p, _p, _p, _p, _p],
+    "tts_gpt_op_kv_move": [_i, _i, _p, _p, _p, _i, _i, _i, _i, _l, _p, _p],
 }
 
 
@@ -633,6 +641,194 @@ def op_attention_cross(q, k, v, q_start, k_start, q_max, scale=0.125, scratch=No
     _run((_lib or load()).tts_gpt_op_attention_cross, d, stream, n, heads, kv_heads, _TYPES[t], rows, q.data_ptr(), qs, k_rows, k.data_ptr(), kr, kh,
          v.data_ptr(), vr, vh, q_start.data_ptr(), k_start.data_ptr(), q_max, scale, out.data_ptr(), sp, sn)
     return out
+
+
+# ---------------------------------------------------------------------------------------------
+# several drafted tokens a step
+# ---------------------------------------------------------------------------------------------
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
+
+
+def op_rope_frequencies(n_rot, base=10000.0, scaling="none", factor=1.0, original=0, low=1.0, high=None, inv_freq=None, device="cuda"):
+    """The table op_rope_kv_append takes for heads whose first n_rot values are rotated, and what cosine and sine are multiplied by.  Pair i turns by
+    base ** (-2 i / n_rot) radians a position, stretched by ``scaling``: "none", "linear", "ntk", "yarn" (high: 32 turns) or "bands" (high: 4); or by
+    inv_freq[i] where that is given (a sequence of n_rot / 2 numbers).  Returns (int64 tensor [n_rot / 2] on `device`, float)."""
+    if not isinstance(n_rot, int) or n_rot < 2 or n_rot > 64 or n_rot % 2:
+        _refuse("n_rot must be even, 2 to 64")
+    given = None
+    if inv_freq is not None:
+        kind, values = 5, [float(w) for w in inv_freq]
+        if len(values) != n_rot // 2:
+            _refuse("inv_freq must have n_rot / 2 values")
+        given = (C.c_double * len(values))(*values)
+    elif scaling in ROPE_SCALINGS:
+        kind = ROPE_SCALINGS[scaling]
+    else:
+        _refuse("scaling must be one of %s" % ", ".join(ROPE_SCALINGS))
+    turns, magnitude = (C.c_uint64 * (n_rot // 2))(), C.c_float(1.0)
+    _check((_lib or load()).tts_gpt_op_rope_frequencies(n_rot, kind, base, factor, original, low, (32.0 if scaling == "yarn" else 4.0) if high is None else high, given, turns,
+                                                        C.byref(magnitude)))
+    table = torch.from_numpy(np.frombuffer(turns, dtype=np.int64).copy())
+    return table.to(device), magnitude.value
+
+
+def op_rope_kv_append(q, k, v, kv_layer, row_slot, row_pos, turns, magnitude=1.0, interleaved=False, q_out=None, stream=None):
+    """A pass's rows rotated by their positions row_pos [R]: q [R, heads * 64] to q_out (None: a new bf16 tensor; q itself is fine), K (rotated) and V [R, heads of
+    the pool * 64] into their slots.  All fp32 or all bf16, rows may be strided; q_out fp32 or bf16.  turns, magnitude: op_rope_frequencies.  Pairs are
+    (i, i + n_rot / 2), or (2i, 2i + 1) where interleaved.  q None: K and V only.  A row without a slot is left out, its q_out included."""
+    d, t, shape = k.get_device(), k.dtype, k.shape
+    fmt, pages, heads = _pool(kv_layer, d)
+    if (t is not _F32 and t is not _BF16 and t is not _I16) or v.dtype is not t or len(shape) != 2 or shape[1] != heads * 64 or v.shape != shape or v.get_device() != d:
+        _refuse("k and v must be [R, %d] of one type, fp32 or bf16, on one device" % (heads * 64))
+    (ks, k1), (vs, v1), R = k.stride(), v.stride(), shape[0]
+    if k1 != 1 or v1 != 1:
+        _refuse("rows of k and v must be contiguous")
+    if R == 1:
+        ks = vs = heads * 64                   # the stride of a single row addresses nothing
+    if not (row_slot.dtype is row_pos.dtype is _I32 and row_slot.get_device() == row_pos.get_device() == d and row_slot.is_contiguous() and row_pos.is_contiguous()
+            and row_slot.numel() >= R and row_pos.numel() >= R):
+        _refuse("row_slot and row_pos must be contiguous int32 tensors of at least R values on the same device")
+    if turns.dtype is not torch.int64 or turns.get_device() != d or not turns.is_contiguous():
+        _refuse("turns must be a contiguous int64 tensor on the same device")
+    qp = op = None
+    qh = qs = os_ = 0
+    ot = _BF16
+    if q is not None:
+        qshape = q.shape
+        if q.dtype is not t or len(qshape) != 2 or qshape[0] != R or qshape[1] % 64 or not qshape[1] or q.get_device() != d:
+            _refuse("q must be [R, heads * 64] of the type of k and v on the same device")
+        if q_out is None:
+            with _on(stream):
+                q_out = torch.empty(qshape, dtype=_BF16, device=q.device)
+        ot = q_out.dtype
+        if (ot is not _F32 and ot is not _BF16 and ot is not _I16) or q_out.shape != qshape or q_out.get_device() != d:
+            _refuse("q_out must be of q's shape, fp32 or bf16, on the same device")
+        (qs, q1), (os_, o1), qh = q.stride(), q_out.stride(), qshape[1] // 64
+        if q1 != 1 or o1 != 1:
+            _refuse("rows of q and q_out must be contiguous")
+        if R == 1:
+            qs = os_ = qh * 64
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None:
+        _refuse("there is no q for q_out")
+    _run((_lib or load()).tts_gpt_op_rope_kv_append, d, stream, R, qh, heads, _TYPES[t], qp, qs, k.data_ptr(), ks, v.data_ptr(), vs, row_pos.data_ptr(), row_slot.data_ptr(),
+         2 * turns.numel(), turns.data_ptr(), 1 if interleaved else 0, magnitude, _TYPES[ot], op, os_, fmt, pages, kv_layer.data_ptr())
+    return q_out
+
+
+def _trees(d, row_start, stream_ids, kv_len):
+    """Number of trees of a call, and the address of their streams' numbers."""
+    n = row_start.numel() - 1
+    if not (row_start.dtype is kv_len.dtype is _I32 and row_start.get_device() == kv_len.get_device() == d and row_start.is_contiguous() and kv_len.is_contiguous() and n >= 1):
+        _refuse_index(d, row_start=row_start, kv_len=kv_len)
+        _refuse("row_start must have one value more than there are trees")
+    if stream_ids is None:
+        return n, None
+    if stream_ids.dtype is not _I32 or stream_ids.get_device() != d or not stream_ids.is_contiguous() or stream_ids.numel() != n:
+        _refuse("stream_ids must be a contiguous int32 tensor with a value for each tree on the same device")
+    return n, stream_ids.data_ptr()
+
+
+def op_tree_tables(parent, row_start, kv_len, tree_mask, row_pos, info, stream_ids=None, stream=None):
+    """Masks [R, words] and positions [R] of trees from the parents [R] (numbers inside the tree, -1: none); everything int32 on one device, written in
+    place.  info[0], zero at first, becomes the lowest code of a tree with something wrong, which is left as it was."""
+    d, R = parent.get_device(), parent.numel()
+    n, ids = _trees(d, row_start, stream_ids, kv_len)
+    shape = tree_mask.shape
+    if not (parent.dtype is tree_mask.dtype is row_pos.dtype is info.dtype is _I32 and tree_mask.get_device() == row_pos.get_device() == info.get_device() == d
+            and parent.is_contiguous() and tree_mask.is_contiguous() and row_pos.is_contiguous() and info.is_contiguous() and len(shape) == 2 and shape[0] == R
+            and row_pos.numel() == R and info.numel() >= 1):
+        _refuse_index(d, parent=parent, tree_mask=tree_mask, row_pos=row_pos, info=info)
+        _refuse("parent and row_pos must have a value, and tree_mask a row, for each row")
+    _run((_lib or load()).tts_gpt_op_tree_tables, d, stream, n, R, row_start.data_ptr(), ids, kv_len.numel(), kv_len.data_ptr(), parent.data_ptr(), shape[1], tree_mask.data_ptr(),
+         row_pos.data_ptr(), info.data_ptr())
+
+
+def op_attention_tree_scratch(device):
+    n = C.c_size_t(0)
+    _check(load().tts_gpt_op_attention_tree_scratch_bytes(C.byref(n)))
+    return torch.zeros(n.value, dtype=torch.uint8, device=device)
+
+
+def op_attention_tree(q, kv_layer, page_table, row_start, kv_len, tree_mask, t_max, stream_ids=None, scale=0.125, scratch=None, out=None, stream=None):
+    """Attention of trees of drafted tokens: rows q [R, heads * 64] (fp32 or bf16), of which tree i has row_start[i] .. row_start[i + 1] - 1, to the committed keys of
+    their streams and to the nodes of the tree that their masks [R, words] name.  kv_len counts a stream's tokens with the tree's nodes; t_max: at least the
+    largest tree.  Returns bf16 [R, heads * 64] (rows of no tree undefined), or `out` (in which they are left as they were).  NaN rows and scratch as for
+    op_attention_shared."""
+    d, t, shape = q.get_device(), q.dtype, q.shape
+    fmt, pages, kv_heads = _pool(kv_layer, d)
+    if len(shape) != 2 or shape[1] % 64 or (t is not _F32 and t is not _BF16 and t is not _I16):
+        _refuse("q must be [R, heads * 64], fp32 or bf16")
+    (qs, q1), R, heads = q.stride(), shape[0], shape[1] // 64
+    if q1 != 1:
+        _refuse("rows of q must be contiguous")
+    if R == 1:
+        qs = heads * 64                        # the stride of a single row addresses nothing
+    n, ids = _trees(d, row_start, stream_ids, kv_len)
+    lists, words = page_table.shape, tree_mask.shape
+    if not (page_table.dtype is tree_mask.dtype is _I32 and page_table.get_device() == tree_mask.get_device() == d and page_table.is_contiguous() and tree_mask.is_contiguous()
+            and len(lists) == 2 and lists[0] == kv_len.numel() and len(words) == 2 and words[0] >= R):
+        _refuse_index(d, page_table=page_table, tree_mask=tree_mask)
+        _refuse("page_table must be [streams, pages of a stream] for the streams of kv_len, tree_mask [R, words]")
+    if out is None:
+        with _on(stream):
+            out = torch.empty(shape, dtype=_BF16, device=q.device)
+    elif out.shape != shape or (out.dtype is not _BF16 and out.dtype is not _I16) or out.get_device() != d or not out.is_contiguous():
+        _refuse("out must be a contiguous bf16 tensor of q's shape on the same device")
+    if scratch is None:
+        with _on(stream):
+            scratch = op_attention_tree_scratch(q.device)
+    sp, sn = _scratch(scratch, d)
+    _run((_lib or load()).tts_gpt_op_attention_tree, d, stream, n, R, heads, kv_heads, _TYPES[t], q.data_ptr(), qs, fmt, pages, kv_layer.data_ptr(), lists[0], page_table.data_ptr(),
+         lists[1], row_start.data_ptr(), ids, kv_len.data_ptr(), words[1], tree_mask.data_ptr(), t_max, scale, out.data_ptr(), sp, sn)
+    return out
+
+
+def op_tree_accept(draft, target, parent, row_start, kv_len, page_table, free_pages, free_top, path, n_accepted, next_token, info, stream_ids=None, kv_len_out=None,
+                   free_top_out=None, stream=None):
+    """The path from node 0 through children whose drafted token is the model's (target, by row) after their parent; everything int32 on one device, written in
+    place: path [R] (rows of accepted nodes at the head of the tree's rows, then -1), n_accepted and next_token by tree, the streams' lengths without the other nodes
+    (kv_len_out, None: kv_len), and unused pages back onto the stack (free_pages, free_top_out, None: free_top).  info: 8 values, zero at first; info[0] is the status."""
+    d, R = draft.get_device(), draft.numel()
+    n, ids = _trees(d, row_start, stream_ids, kv_len)
+    if kv_len_out is None:
+        kv_len_out = kv_len
+    if free_top_out is None:
+        free_top_out = free_top
+    lists = page_table.shape
+    if not (draft.dtype is target.dtype is parent.dtype is page_table.dtype is free_pages.dtype is free_top.dtype is path.dtype is n_accepted.dtype is next_token.dtype is info.dtype
+            is kv_len_out.dtype is free_top_out.dtype is _I32
+            and target.get_device() == parent.get_device() == page_table.get_device() == free_pages.get_device() == free_top.get_device() == path.get_device()
+            == n_accepted.get_device() == next_token.get_device() == info.get_device() == kv_len_out.get_device() == free_top_out.get_device() == d
+            and draft.is_contiguous() and target.is_contiguous() and parent.is_contiguous() and page_table.is_contiguous() and free_pages.is_contiguous() and path.is_contiguous()
+            and n_accepted.is_contiguous() and next_token.is_contiguous() and info.is_contiguous() and kv_len_out.is_contiguous()
+            and target.numel() == parent.numel() == path.numel() == R and len(lists) == 2 and lists[0] == kv_len.numel() == kv_len_out.numel()
+            and n_accepted.numel() >= n and next_token.numel() >= n and info.numel() >= 8 and free_top.numel() and free_top_out.numel()):
+        _refuse_index(d, draft=draft, target=target, parent=parent, page_table=page_table, free_pages=free_pages, free_top=free_top, path=path, n_accepted=n_accepted,
+                      next_token=next_token, info=info, kv_len_out=kv_len_out, free_top_out=free_top_out)
+        _refuse("draft, target, parent and path must be of one length, page_table [streams, pages of a stream] for the streams of kv_len and kv_len_out, n_accepted and "
+                "next_token as long as there are trees, info 8 long")
+    _run((_lib or load()).tts_gpt_op_tree_accept, d, stream, n, R, row_start.data_ptr(), ids, draft.data_ptr(), target.data_ptr(), parent.data_ptr(), lists[0], kv_len.data_ptr(),
+         kv_len_out.data_ptr(), page_table.data_ptr(), lists[1], free_pages.numel(), free_pages.data_ptr(), free_top.data_ptr(), free_top_out.data_ptr(), path.data_ptr(),
+         n_accepted.data_ptr(), next_token.data_ptr(), info.data_ptr())
+
+
+def op_kv_move(kv_layers, row_start, path, row_slot, stream=None):
+    """K and V of accepted nodes to the slots of their tree's first rows, in one layer's pool or in several [layers, ...] (which may be strided)."""
+    d, shape = kv_layers.get_device(), kv_layers.shape
+    layer, layers, stride = kv_layers, 1, 0
+    if len(shape) == (5 if kv_layers.dtype is _U8 else 6):
+        layers, layer = shape[0], kv_layers[0] if shape[0] else None
+        if not layers:
+            _refuse("there must be a layer")
+        stride = kv_layers.stride(0) * kv_layers.element_size()
+    fmt, pages, heads = _pool(layer, d)
+    n, R = row_start.numel() - 1, path.numel()
+    if not (row_start.dtype is path.dtype is row_slot.dtype is _I32 and row_start.get_device() == path.get_device() == row_slot.get_device() == d and row_start.is_contiguous()
+            and path.is_contiguous() and row_slot.is_contiguous() and n >= 1 and row_slot.numel() >= R):
+        _refuse_index(d, row_start=row_start, path=path, row_slot=row_slot)
+        _refuse("row_start must have one value more than there are trees, row_slot one for each of path's")
+    _run((_lib or load()).tts_gpt_op_kv_move, d, stream, n, R, row_start.data_ptr(), path.data_ptr(), row_slot.data_ptr(), heads, fmt, pages, layers, stride, kv_layers.data_ptr())
 
 
 def bf16_bits_tensor_to_f32(t: torch.Tensor) -> torch.Tensor:

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtts_gpt.so")
 EXTRA = os.environ.get("TTS_EXTRA_NVCC", "").split()
-SOURCES = [os.path.join(CSRC, f) for f in ("tts_gpt.cu", "serving_ops.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("tts_gpt.cu", "serving_ops.cu", "draft_ops.cu")]
 
 
 def _deps():
