@@ -28,21 +28,22 @@
 
 namespace ttsgpt {
 
-constexpr int kTrKeys = 128;                // keys of a block
-constexpr int kTrHalf = kTrKeys * 128;      // K or V of a block as bf16: 16 KB
-constexpr int kTrQ = 2 * kTrHalf;           // Q of two tiles (fp32: both parts of one); where a row's copies meet, too
+constexpr int kTrKeys = kPageTokens;        // keys of a step: a page
+constexpr int kTrPage = kTrKeys * 128;      // K or V of a page as bf16: 8 KB
+constexpr int kTrRows = 128 * 128;          // queries of a tile, as often as they stand among the 128 lanes: 16 KB
+constexpr int kTrQ = 2 * kTrRows;           // of two tiles (fp32: both parts of one)
 constexpr int kTrMaxSeq = 2048;
 constexpr int kTrNear = 256;                // trees up to which a CTA keeps what it has read of them
 constexpr int kTrMaxCtas = 320;
 constexpr int kTrPitch = 68;                // floats of a row's part
 constexpr float kTrSlack = 8.0f;            // log2 by which a score may exceed the reference
-constexpr int kTrCostBlock = 2, kTrCostTile = 5;   // what a range is measured in: a block, a tile besides its blocks
-// Parts that the first copying warp may describe ahead.  Every part has a block, and no copy is more than five blocks ahead of the softmax, so
-// that it never waits for a place while the softmax waits for it.
+constexpr int kTrCostTile = 5;              // what a tile costs besides its steps, in steps
+// Parts that the copying warp may describe ahead.  Every part has a step, and no copy is more than six steps ahead of the softmax, so that it
+// never waits for a place while the softmax waits for it.
 constexpr int kTrParts = 8;
-// What the copying warps write beside a block has four places, though K and V have two: block c + 4's is written when Q K^T of block c + 2 is
-// done, which was issued when the softmax was done with block c + 1.
-constexpr int kTrBeside = 4;
+// Places of what is written beside a page: whether it is there (by the copying warp, four pages ahead of the products, which are two ahead of the softmax)
+// and the scales of the 8-bit cache (by the widening warps, two ahead of the products).
+constexpr int kTrThere = 8, kTrScales = 4;
 constexpr unsigned long long kTrWaitNs = 2000000000ull;
 
 struct TreeAttnArgs {
@@ -50,7 +51,6 @@ struct TreeAttnArgs {
   uint16_t *out;                // [R][H * 64]
   long long q_stride;           // elements between rows
   int R, H, Hkv, G, rpt;        // G query heads a head of keys; tree rows of a tile
-  int lg;                       // log2 of how often a row stands among the 128 lanes
   Div by_G, by_rpt;
   float scale;                  // of the scores, in log2 units
   const int *row_start, *stream_ids, *kv_len, *page_table, *mask;
@@ -66,8 +66,8 @@ struct TreeAttnArgs {
 // The part of a tile that lies in a CTA's range.
 struct TreePart {
   int row0, n_i, kvh, next;     // first row, rows times heads, head of keys; where the next tile's cost begins
-  int j0, j1, keys, committed, nodes, stream;   // its blocks here; keys of the stream, of them committed, nodes of the tree
-  int c0, c1;                   // first and last CTA that have blocks of the tile
+  int j0, j1, keys, committed, nodes, stream;   // its pages here; keys of the stream, of them committed, nodes of the tree
+  int c0, c1;                   // first and last CTA that have pages of the tile
 };
 constexpr int kTrPartWords = sizeof(TreePart) / 4;
 
@@ -75,33 +75,43 @@ struct alignas(16) TreeShared {
   TreePart part[kTrParts];
   TreePart mine[4], shared[2][4];   // the softmax warps' own copies: the part at hand; of tiles of several CTAs the one that began before the range, and the last
   uint64_t part_full[kTrParts], part_free[kTrParts];
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], raw_full[2], raw_empty[2];
+  uint64_t k_full[4], v_full[4], k_empty[4], v_empty[4], raw_full[4], raw_empty[4];
   uint64_t q_full[2], q_free[2];
-  uint64_t s_full, p_full, o_full, meet;    // meet: the softmax warps among themselves, bounded like every wait
+  uint64_t s_full[2], p_full[2], o_full[2];   // by step: scores there, weights there, their product done
+  uint64_t meet;                // the softmax warps among themselves, bounded like every wait
   uint32_t tmem;
   int failed;                   // 1: a wait of the CTA has run out; 2: one of an earlier call with the same scratch had
-  int pages_ok[kTrBeside];      // of a block: bit p, its page p is there
-  int found;                    // number (from 1 on) of the last block with a drafted key whose V is not finite
-  unsigned bad[4];              // those keys
+  int there[kTrThere];          // of a step: is its page one?
+  int found;                    // number (from 1 on) of the last step with a drafted key whose V is not finite
+  unsigned bad[2];              // those keys
   float2 ml[4][32];
   Div size;
-  int warp_tot[16];
+  int warp_tot[16], top_cost;   // ... and the most that a tile costs
 };
 
-template <bool E4M3> struct TreeShape {
-  // warps 0-3: softmax, 4: copies, 5: products, 8-bit cache 6 and 7: codes to bf16
-  static constexpr int kCopyWarp = 4, kMmaWarp = 5, kWidenWarp = 6, kWidenWarps = E4M3 ? 2 : 0, kThreads = 32 * (6 + kWidenWarps);
+template <int S, bool E4M3> struct TreeShape {
+  // warps 0-3: softmax, 4: copies, 5: products; 8-bit cache: codes to bf16, two warps (6, 7) where the softmax takes longer than they do, or four (8-11; 6
+  // and 7 only give up their registers)
+  static constexpr int kCopyWarp = 4, kMmaWarp = 5, kWidenWarp = S == 1 ? 6 : 8, kWidenWarps = !E4M3 ? 0 : S == 1 ? 2 : 4;
+  static constexpr int kThreads = !E4M3 ? 192 : S == 1 ? 256 : 384;
+  // 8-bit cache: registers of a thread, which the groups of four warps split anew; at launch each has 128 or 80
+  static constexpr int kRegsLaunch = S == 1 ? 128 : 80, kRegsSoftmax = S == 1 ? 168 : 120, kRegsCopy = S == 1 ? 88 : 64, kRegsWiden = S == 1 ? 0 : 56;
+  static_assert(kRegsSoftmax + kRegsCopy + kRegsWiden <= kRegsLaunch * (S == 1 ? 2 : 3), "a split of more registers than the launch has would wait forever");
   static constexpr int kCtas = 2;            // an SM
-  static constexpr int kRing = E4M3 ? 1 : 2; // blocks of K and of V as the tensor cores take them
-  static constexpr int kRaw = E4M3 ? 2 : 0;  // blocks of K and V as they are in the cache: two pages' codes and scales of each
-  static constexpr int kRawBlock = 4 * kE4m3BlockBytes;
-  static constexpr int kScales = E4M3 ? kTrBeside * 2 * kTrKeys * 4 : 0;
-  static constexpr int kBytes = 2 * kRing * kTrHalf + kTrQ + kRaw * kRawBlock + kScales;
+  static constexpr int kRing = E4M3 ? 2 : 4; // pages of K and of V as the tensor cores take them
+  static constexpr int kRaw = E4M3 ? 4 : 0;  // pages of K and V as they are in the cache, codes and scales
+  static constexpr int kRawPage = 2 * kE4m3BlockBytes;
+  static constexpr int kScales = E4M3 ? kTrScales * 2 * kTrKeys * 4 : 0;
+  static constexpr int kBytes = kTrQ + 2 * kRing * kTrPage + kRaw * kRawPage + kScales;
 };
-template <bool E4M3> inline size_t tree_smem_bytes(int n) {
-  return 1024 + TreeShape<E4M3>::kBytes + sizeof(TreeShared) + (n <= kTrNear ? (size_t)n * sizeof(int4) : 0) + (size_t)(n + 1) * sizeof(int);
+template <int S, bool E4M3> inline size_t tree_smem_bytes(int n) {
+  return 1024 + TreeShape<S, E4M3>::kBytes + sizeof(TreeShared) + (n <= kTrNear ? (size_t)n * sizeof(int4) : 0) + (size_t)(n + 1) * sizeof(int);
 }
 
+__device__ __forceinline__ void tmem_st8_async(uint32_t taddr, const float *v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+}
 // 32 lanes x 16 columns of 32 bits into tensor memory, waited for later
 __device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const float *v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
@@ -110,39 +120,22 @@ __device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const float *v) 
 }
 __device__ __forceinline__ void fence_gpu() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
 
-template <bool E4M3, bool QF32>
-__global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kCtas) attention_tree_kernel(const __grid_constant__ CUtensorMap kv_map,
+template <int S, bool E4M3, bool QF32>
+__global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M3>::kCtas) attention_tree_kernel(const __grid_constant__ CUtensorMap kv_map,
                                                                                                           const __grid_constant__ CUtensorMap q_map, const TreeAttnArgs a) {
-  using Shape = TreeShape<E4M3>;
+  using Shape = TreeShape<S, E4M3>;
   extern __shared__ __align__(16) unsigned char tr_smem_raw[];
   unsigned char *base = tr_smem_raw + ((1024u - (smem_u32(tr_smem_raw) & 1023u)) & 1023u);
-  constexpr int kRing = Shape::kRing;
-  unsigned char *Qs = base, *Ks = base + kTrQ, *Vs = Ks + kRing * kTrHalf;   // 128 rows x 64 [2], 128 keys x 64 [kRing]: 128-byte swizzle
-  unsigned char *raw = Vs + kRing * kTrHalf;                                 // 8-bit cache: [2][K, V][page]
-  float *scales = reinterpret_cast<float *>(raw + Shape::kRaw * Shape::kRawBlock);   // and [kTrBeside][K, V][128]
+  constexpr int kRing = Shape::kRing, kCols = kTrKeys / S, kRgs = 4 / S;   // a thread's keys of a step; groups of 32 rows of a tile
+  unsigned char *Qs = base, *Ks = base + kTrQ, *Vs = Ks + kRing * kTrPage;   // 128 rows x 64 [2], 64 keys x 64 [kRing]: 128-byte swizzle
+  unsigned char *raw = Vs + kRing * kTrPage;                                 // 8-bit cache: [kRaw][K, V]
+  float *scales = reinterpret_cast<float *>(raw + Shape::kRaw * Shape::kRawPage);   // and [kTrScales][K, V][64]
   TreeShared &sh = *reinterpret_cast<TreeShared *>(base + Shape::kBytes);
   int4 *near_s = reinterpret_cast<int4 *>(&sh + 1);   // of each tree: first row, nodes, length and number of the stream
   int *first = reinterpret_cast<int *>(near_s + (a.n_seq <= kTrNear ? a.n_seq : 0));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int *failed = &sh.failed;
 
-  if (warp == Shape::kMmaWarp) tmem_alloc(&sh.tmem, 256);   // S 128 columns, P 64, O 64
-  if (tid == 0) {
-    const int copied = (int)blockIdx.x == a.starve ? 2 : 1, full = E4M3 ? Shape::kWidenWarps : copied;
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.k_full[i], full); mbar_init(&sh.v_full[i], full); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.v_empty[i], 1);
-      mbar_init(&sh.raw_full[i], copied); mbar_init(&sh.raw_empty[i], E4M3 ? Shape::kWidenWarps : 1);
-      mbar_init(&sh.q_full[i], QF32 ? 4 : 1); mbar_init(&sh.q_free[i], 4);
-    }
-    for (int i = 0; i < kTrParts; ++i) { mbar_init(&sh.part_full[i], 1); mbar_init(&sh.part_free[i], 5 + Shape::kWidenWarps); }
-    mbar_init(&sh.s_full, 1); mbar_init(&sh.p_full, 4); mbar_init(&sh.o_full, 1); mbar_init(&sh.meet, 4);
-    sh.found = 0;
-    sh.failed = __ldcg(a.err) ? 2 : 0;
-  }
-  if (warp == Shape::kCopyWarp && lane == 0) {
-    if (!E4M3) asm volatile("prefetch.tensormap [%0];" ::"l"(&kv_map) : "memory");
-    if (!QF32) asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
-  }
   // ---- running sums of cost over the trees ----
   struct Tree { int row0, rows, nodes, keys, committed, stream; };
   auto read_tree = [&](int i) {
@@ -157,20 +150,43 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
     return Tree{x.x, x.y < 0 ? -1 : min(x.y, a.t_max), x.y, min(max(x.z, 0), a.pps * kPageTokens), x.z - x.y, x.w};
   };
   auto tree_of = [&](int i) { return tree_from(a.n_seq <= kTrNear ? near_s[i] : read_tree(i)); };
-  auto tile_cost = [&](int keys) { return kTrCostTile + kTrCostBlock * ((keys + kTrKeys - 1) / kTrKeys); };
+  auto tile_cost = [&](int keys) { return kTrCostTile + (keys + kTrKeys - 1) / kTrKeys; };
+  const int4 own = tid < a.n_seq ? read_tree(tid) : make_int4(0, 0, 0, -1);   // asked for before anything else
+  if (warp == Shape::kMmaWarp) tmem_alloc(&sh.tmem, 256);   // S 2 x 64 columns, P 2 x 32, O 64
+  const int failed_before = tid == 0 ? __ldcg(a.err) : 0;
+  if (tid == 32) {
+    const int copied = (int)blockIdx.x == a.starve ? 2 : 1, full = E4M3 ? Shape::kWidenWarps : copied;
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&sh.k_full[i], full); mbar_init(&sh.v_full[i], full); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.v_empty[i], 1);
+      mbar_init(&sh.raw_full[i], copied); mbar_init(&sh.raw_empty[i], E4M3 ? Shape::kWidenWarps : 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.q_full[i], QF32 ? 4 : 1); mbar_init(&sh.q_free[i], 4); mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 4); mbar_init(&sh.o_full[i], 1);
+    }
+    for (int i = 0; i < kTrParts; ++i) { mbar_init(&sh.part_full[i], 1); mbar_init(&sh.part_free[i], 5 + Shape::kWidenWarps); }
+    mbar_init(&sh.meet, 4);
+    sh.found = 0;
+    sh.top_cost = 0;
+  }
+  if (warp == Shape::kCopyWarp && lane == 0) {
+    if (!E4M3) asm volatile("prefetch.tensormap [%0];" ::"l"(&kv_map) : "memory");
+    if (!QF32) asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
+  }
   int carry = 0, bad = 0;                      // bad: starts that do not ascend, whose rows nothing bounds
 #pragma unroll 1
   for (int i0 = 0; i0 < a.n_seq; i0 += Shape::kThreads) {
     const int i = i0 + tid;
-    int u = 0;
+    int u = 0, cost = 0;
     if (i < a.n_seq) {
-      const int4 read = read_tree(i);
+      const int4 read = i0 == 0 ? own : read_tree(i);
       if (a.n_seq <= kTrNear) near_s[i] = read;
       if (read.w >= 0) prefetch_l2(a.page_table + (size_t)read.w * a.pps);
       const Tree x = tree_from(read);
       bad |= x.rows < 0;
-      u = x.rows > 0 ? a.Hkv * a.by_rpt.of(x.rows + a.rpt - 1) * tile_cost(x.keys) : 0;
+      cost = x.rows > 0 ? tile_cost(x.keys) : 0;
+      u = x.rows > 0 ? a.Hkv * a.by_rpt.of(x.rows + a.rpt - 1) * cost : 0;
     }
+    const int dearest = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)cost);
     int incl = u;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -178,7 +194,7 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
       if (lane >= o) incl += v;
     }
     __syncthreads();
-    if (lane == 31) sh.warp_tot[warp] = incl;
+    if (lane == 31) { sh.warp_tot[warp] = incl; atomicMax(&sh.top_cost, dearest); }
     bad = __syncthreads_or(bad);
     int before = carry;
 #pragma unroll 1
@@ -188,7 +204,9 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
   const int T = bad ? 0 : carry;
   if (tid == 0) {
     first[a.n_seq] = T;
-    sh.size.set(max(kTrCostBlock, (T + (int)gridDim.x - 1) / (int)gridDim.x));
+    // eight pages at least, where a tile has so many: parts of a few cost more than they take off another CTA
+    sh.size.set(max(min(sh.top_cost, kTrCostTile + 8), max(1, (T + (int)gridDim.x - 1) / (int)gridDim.x)));
+    sh.failed = failed_before ? 2 : 0;
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -197,13 +215,16 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
   const Div size = sh.size;
   const int u_begin = blockIdx.x * (int)size.d, u_end = *failed ? u_begin : min(T, u_begin + (int)size.d);
 
-  // The part at unit u or behind it that this CTA has blocks of; false: there is none.  Tiles without keys get their zeros here.
+  // The part at unit u or behind it that this CTA has pages of; false: there is none.  Tiles without keys get their zeros here.
   auto part_at = [&](int u, TreePart &p) {
     while (u < u_end) {
-      int lo = 0, hi = a.n_seq - 1;
-      while (lo < hi) { const int m = (lo + hi + 1) >> 1; if (first[m] <= u) lo = m; else hi = m - 1; }
+      int lo = 0;                              // last tree that begins at or before u: a 32nd at a time
+      for (int span = a.n_seq <= 32 ? 32 : a.n_seq <= 1024 ? 1024 : 32768; span > 1; span >>= 5) {
+        const int at = lo + lane * (span >> 5);
+        lo += (__popc(__ballot_sync(0xFFFFFFFFu, at < a.n_seq && first[at] <= u)) - 1) * (span >> 5);
+      }
       const Tree x = tree_of(lo);
-      const int tiles = a.by_rpt.of(x.rows + a.rpt - 1), blocks = (x.keys + kTrKeys - 1) / kTrKeys, nu = tile_cost(x.keys);
+      const int tiles = a.by_rpt.of(x.rows + a.rpt - 1), pages = (x.keys + kTrKeys - 1) / kTrKeys, nu = tile_cost(x.keys);
       const int k = (int)((unsigned)(u - first[lo]) / (unsigned)nu), u0 = first[lo] + k * nu;
       p.kvh = (int)((unsigned)k / (unsigned)tiles);
       const int tile = k - p.kvh * tiles;
@@ -211,22 +232,22 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
       p.n_i = min(a.rpt, x.rows - tile * a.rpt) * a.G;
       p.keys = x.keys; p.committed = x.committed; p.nodes = x.nodes; p.stream = x.stream;
       p.next = u0 + nu;
-      // Blocks before the border of CTAs c - 1 and c.  A border one or two blocks (an eighth of a range at most) from an end of the tile is moved there: what
+      // Pages before the border of CTAs c - 1 and c.  A border up to four pages (a quarter of a range at most) from an end of the tile is moved there: what
       // they cost is less than another part.
-      const int near_end = min(2, (int)size.d / (8 * kTrCostBlock));
+      const int near_end = min(4, (int)size.d / 4);
       auto border = [&](int c) {
-        const int b = min((max(c * (int)size.d - u0 - kTrCostTile, 0) + kTrCostBlock - 1) / kTrCostBlock, blocks);
-        return b <= near_end && 2 * b <= blocks ? 0 : blocks - b <= near_end ? blocks : b;
+        const int b = min(max(c * (int)size.d - u0 - kTrCostTile, 0), pages);
+        return b <= near_end && 2 * b <= pages ? 0 : pages - b <= near_end ? pages : b;
       };
       const int ca = size.of(u0), cb = size.of(u0 + nu - 1), me = blockIdx.x;
       p.j0 = me == ca ? 0 : border(me);
-      p.j1 = me == cb ? blocks : border(me + 1);
+      p.j1 = me == cb ? pages : border(me + 1);
       if (p.j1 > p.j0) {
         for (p.c0 = ca; p.c0 < cb && border(p.c0 + 1) == 0;) ++p.c0;
-        for (p.c1 = cb; p.c1 > ca && border(p.c1) == blocks;) --p.c1;
+        for (p.c1 = cb; p.c1 > ca && border(p.c1) == pages;) --p.c1;
         return true;
       }
-      if (blocks == 0 && me == ca) {
+      if (pages == 0 && me == ca) {
         uint4 *rows = reinterpret_cast<uint4 *>(a.out);
         for (int i = lane; i < p.n_i * (kHeadDim / 8); i += 32) {
           const int r = a.by_G.of(i >> 3);
@@ -274,87 +295,39 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
     return phys >= 0 && phys < a.n_pages ? phys : -1;
   };
 
-  if (warp == Shape::kCopyWarp) {
-    // ---- copies: 16-bit queries of a tile as often as its rows stand among the lanes, two tiles ahead at most, then its keys and values ----
-    int c = 0;                                 // blocks of this CTA
-    bool fine = true;
-    TreePart p;
-    int u = u_begin;
-#pragma unroll 1
-    for (int n_part = 0; fine; ++n_part) {
-      const bool there = part_at(u, p);
-      if (!there) p.n_i = 0;                   // the part behind the last has no rows
-      fine = give_part(n_part, p) && there;
-      if (!fine) break;
-      u = p.next;
-      if constexpr (!QF32) {
-        const int qb = n_part & 1;
-        if (n_part >= 2) fine = wait_warp(&sh.q_free[qb], (uint32_t)(n_part / 2 - 1) & 1u);
-        if (!fine) break;
-        if (elect_one()) {
-          mbar_expect_tx(&sh.q_full[qb], (uint32_t)((a.rpt * a.G * 128) << a.lg));
-          for (int x = 0; x < 1 << a.lg; ++x) un_box(&q_map, p.kvh * a.G, p.row0, Qs + qb * kTrHalf + x * (kTrHalf >> a.lg), &sh.q_full[qb]);
-        }
-        __syncwarp();
-      }
-      int mine = -1;                           // a page of sixteen blocks each lane
-#pragma unroll 1
-      for (int j = p.j0; j < p.j1 && fine; ++j, ++c) {
-        const int at = (j - p.j0) & 15, s = c & 1;
-        if (at == 0) mine = page_of(p.stream, p.keys, 2 * j + lane);
-        const int p0 = __shfl_sync(0xFFFFFFFFu, mine, 2 * at), p1 = __shfl_sync(0xFFFFFFFFu, mine, 2 * at + 1);
-#pragma unroll 1
-        for (int w = 0; w < 2; ++w) {          // K, V
-          if (c >= 2 && (w == 0 || !E4M3)) fine = wait_warp(E4M3 ? &sh.raw_empty[s] : w ? &sh.v_empty[s] : &sh.k_empty[s], (uint32_t)(c / 2 - 1) & 1u);
-          if (!fine) break;
-          if (w == 0 && lane == 0) sh.pages_ok[c % kTrBeside] = (p0 >= 0) + 2 * (p1 >= 0);
-          __syncwarp();
-          if (elect_one()) {
-            uint64_t *full = E4M3 ? &sh.raw_full[s] : w ? &sh.v_full[s] : &sh.k_full[s];
-            const uint32_t pages = (uint32_t)((p0 >= 0) + (p1 >= 0));
-            if constexpr (E4M3) {
-              if (w == 0) mbar_expect_tx(full, 2 * pages * kE4m3BlockBytes);
-              unsigned char *dst = raw + s * Shape::kRawBlock + 2 * w * kE4m3BlockBytes;
-              const size_t head = (size_t)w * a.Hkv + p.kvh;
-              if (p0 >= 0) bulk_copy_g2s(dst, a.pool + ((size_t)p0 * 2 * a.Hkv + head) * kE4m3BlockBytes, kE4m3BlockBytes, full);
-              if (p1 >= 0) bulk_copy_g2s(dst + kE4m3BlockBytes, a.pool + ((size_t)p1 * 2 * a.Hkv + head) * kE4m3BlockBytes, kE4m3BlockBytes, full);
-            } else {
-              mbar_expect_tx(full, pages * (kTrHalf / 2));
-              unsigned char *dst = (w ? Vs : Ks) + s * kTrHalf;
-              if (p0 >= 0) un_box(&kv_map, 0, (p0 * 2 + w) * a.Hkv + p.kvh, dst, full);
-              if (p1 >= 0) un_box(&kv_map, 0, (p1 * 2 + w) * a.Hkv + p.kvh, dst + kTrHalf / 2, full);
-            }
-          }
-          __syncwarp();
-        }
-      }
-    }
-  } else if (E4M3 && warp >= Shape::kWidenWarp) {
-    // ---- codes to bf16, 16 of a row at a time, as soon as the products are done with the block before; and the scales ----
+  auto widen = [&]() {
+    // ---- codes to bf16, 16 of a row at a time, as soon as the products are done with the page two before; and the scales ----
+    constexpr int kThreads = 32 * (E4M3 ? Shape::kWidenWarps : 1), kIter = 4 * kTrKeys / kThreads;   // 16 codes a thread and turn
     const int t = tid - 32 * Shape::kWidenWarp, quad = t & 3;
     int word, c = 0;
     bool fine = true;
 #pragma unroll 1
     for (int n_part = 0; fine && take_part(n_part, word); ++n_part) {
-      const int nb = TR_FIELD(word, j1) - TR_FIELD(word, j0);
+      const int steps = TR_FIELD(word, j1) - TR_FIELD(word, j0);
 #pragma unroll 1
-      for (int b = 0; b < nb && fine; ++b, ++c) {
-        const unsigned char *from = raw + (c & 1) * Shape::kRawBlock;
-        fine = wait_warp(&sh.raw_full[c & 1], (uint32_t)(c / 2) & 1u);
+      for (int b = 0; b < steps && fine; ++b, ++c) {
+        const int s = c & 1;
+        fine = wait_warp(&sh.raw_full[c & 3], (uint32_t)(c / 4) & 1u);
 #pragma unroll 1
         for (int w = 0; w < 2 && fine; ++w) {
-          if (c > 0) fine = wait_warp(w ? &sh.v_empty[0] : &sh.k_empty[0], (uint32_t)(c - 1) & 1u);
+          const unsigned char *from = raw + (c & 3) * Shape::kRawPage + w * kE4m3BlockBytes;
+          if (c >= 2) fine = wait_warp(w ? &sh.v_empty[s] : &sh.k_empty[s], (uint32_t)(c / 2 - 1) & 1u);
+          // sums of the tile before met in both places of V
+          if (S > 1 && !QF32 && w == 1 && b < 2 && n_part > 0 && fine) fine = wait_warp(&sh.q_free[(n_part - 1) & 1], (uint32_t)((n_part - 1) / 2) & 1u);
           if (!fine) break;
-          if (w == 0) {                        // (both with K: the weights want V's before V is waited for)
+          if (w == 0) {                        // K's and V's
 #pragma unroll
-            for (int e = 0; e < 4; ++e)        // [K, V][page]: 64 scales behind the codes
-              scales[(c % kTrBeside) * 2 * kTrKeys + 64 * e + t] = *reinterpret_cast<const float *>(from + e * kE4m3BlockBytes + kPageElems + 4 * t);
+            for (int x = t; x < 2 * kTrKeys; x += kThreads)
+              scales[(c % kTrScales) * 2 * kTrKeys + x] = *reinterpret_cast<const float *>(from + (x >> 6) * kE4m3BlockBytes + kPageElems + 4 * (x & 63));
           }
-          unsigned char *dst = w ? Vs : Ks;
-#pragma unroll 2
-          for (int r = t >> 2; r < kTrKeys; r += 16) {
-            const uint4 code = *reinterpret_cast<const uint4 *>(from + (2 * w + (r >> 6)) * kE4m3BlockBytes + (r & 63) * kHeadDim + 16 * quad);
-            const uint32_t x[4] = {code.x, code.y, code.z, code.w};
+          unsigned char *dst = (w ? Vs : Ks) + s * kTrPage;
+          uint4 code[kIter];
+#pragma unroll
+          for (int i = 0; i < kIter; ++i) code[i] = *reinterpret_cast<const uint4 *>(from + ((t >> 2) + kThreads / 4 * i) * kHeadDim + 16 * quad);
+#pragma unroll
+          for (int i = 0; i < kIter; ++i) {
+            const int r = (t >> 2) + kThreads / 4 * i;
+            const uint32_t x[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
             uint32_t y[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -367,75 +340,161 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            mbar_arrive(w ? &sh.v_full[0] : &sh.k_full[0]);
-            if (w) mbar_arrive(&sh.raw_empty[c & 1]);
+            mbar_arrive(w ? &sh.v_full[s] : &sh.k_full[s]);
+            if (w) mbar_arrive(&sh.raw_empty[c & 3]);
           }
         }
       }
     }
-  } else if (warp == Shape::kMmaWarp) {
-    // ---- products: Q K^T of a tile's first block, then, each time the softmax has block c's weights in tensor memory (and is done with its scores), Q K^T of
-    //      block c + 1 and P V of block c, whichever's copy is there first ----
+  };
+
+  if (warp >= 4 && (!E4M3 || warp < 8)) {
+    if constexpr (E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kRegsCopy));
+    if constexpr (E4M3 && S == 1)
+      if (warp >= Shape::kWidenWarp) widen();
+    if (warp == Shape::kCopyWarp) {
+    // ---- copies: 16-bit queries of a tile as often as its rows stand among the lanes, two tiles ahead at most, then its keys and values ----
+    int c = 0;                                 // pages of this CTA
+    bool fine = true;
+    TreePart p;
+    int u = u_begin;
+    unsigned long long ended = 0;              // of each place of V, 16 bits: 1 + the tile whose sums meet there (modulo 2^15; one of the last six)
+#pragma unroll 1
+    for (int n_part = 0; fine; ++n_part) {
+      const bool there = part_at(u, p);
+      if (!there) p.n_i = 0;                   // the part behind the last has no rows
+      fine = give_part(n_part, p) && there;
+      if (!fine) break;
+      u = p.next;
+      int mine = page_of(p.stream, p.keys, p.j0 + lane);   // a page each lane
+      if constexpr (!QF32) {
+        const int qb = n_part & 1;
+        if (n_part >= 2) fine = wait_warp(&sh.q_free[qb], (uint32_t)(n_part / 2 - 1) & 1u);
+        if (!fine) break;
+        if (elect_one()) {
+          mbar_expect_tx(&sh.q_full[qb], (uint32_t)(S * a.rpt * a.G * 128));
+#pragma unroll
+          for (int x = 0; x < S; ++x) un_box(&q_map, p.kvh * a.G, p.row0, Qs + qb * kTrRows + x * (kTrRows / S), &sh.q_full[qb]);
+        }
+        __syncwarp();
+      }
+#pragma unroll 1
+      for (int j = p.j0; j < p.j1 && fine; ++j, ++c) {
+        const int at = (j - p.j0) & 31, s = c & 3;
+        if (at == 0 && j > p.j0) mine = page_of(p.stream, p.keys, j + lane);
+        const int page = __shfl_sync(0xFFFFFFFFu, mine, at);
+        if (c >= 4) fine = wait_warp(E4M3 ? &sh.raw_empty[s] : &sh.k_empty[s], (uint32_t)(c / 4 - 1) & 1u);
+        if (!fine) break;
+        if (lane == 0) sh.there[c % kTrThere] = page >= 0;
+        __syncwarp();
+        if constexpr (E4M3) {
+          if (elect_one()) {
+            mbar_expect_tx(&sh.raw_full[s], page >= 0 ? 2 * kE4m3BlockBytes : 0);
+            if (page >= 0) {
+              const unsigned char *from = a.pool + ((size_t)page * 2 * a.Hkv + p.kvh) * kE4m3BlockBytes;
+              bulk_copy_g2s(raw + s * Shape::kRawPage, from, kE4m3BlockBytes, &sh.raw_full[s]);
+              bulk_copy_g2s(raw + s * Shape::kRawPage + kE4m3BlockBytes, from + (size_t)a.Hkv * kE4m3BlockBytes, kE4m3BlockBytes, &sh.raw_full[s]);
+            }
+          }
+        } else {
+          if (elect_one()) {
+            mbar_expect_tx(&sh.k_full[s], page >= 0 ? kTrPage : 0);
+            if (page >= 0) un_box(&kv_map, 0, page * 2 * a.Hkv + p.kvh, Ks + s * kTrPage, &sh.k_full[s]);
+          }
+          __syncwarp();
+          if (c >= 4) fine = wait_warp(&sh.v_empty[s], (uint32_t)(c / 4 - 1) & 1u);
+          if (S > 1 && !QF32) {                // is there a tile whose sums meet in this place?
+            const int tile = (int)(ended >> (16 * s) & 0xFFFF) - 1;
+            if (tile >= 0 && fine) fine = wait_warp(&sh.q_free[tile & 1], (uint32_t)(tile / 2) & 1u);
+            ended &= ~(0xFFFFull << (16 * s));
+            if (j + 1 == p.j1) {               // the sums of this one meet here and where the page before was
+              const unsigned long long mark = (unsigned long long)((n_part & 0x7FFF) + 1), before = (unsigned)(c - 1) & 3u;
+              ended = (ended & ~(0xFFFFull << (16 * before))) | mark << (16 * s) | mark << (16 * before);
+            }
+          }
+          if (!fine) break;
+          if (elect_one()) {
+            mbar_expect_tx(&sh.v_full[s], page >= 0 ? kTrPage : 0);
+            if (page >= 0) un_box(&kv_map, 0, (page * 2 + 1) * a.Hkv + p.kvh, Vs + s * kTrPage, &sh.v_full[s]);
+          }
+        }
+        __syncwarp();
+      }
+    }
+    } else if (warp == Shape::kMmaWarp) {
+    // ---- products: each time the softmax has step c's weights in tensor memory (and its scores in registers), P V of step c and Q K^T of step c + 2,
+    //      over the borders of tiles too.  Scores and weights have two places, by turns ----
     const uint32_t idesc_qk = tc_instr_desc(128, kTrKeys), idesc_pv = tc_instr_desc(128, kHeadDim) | (1u << 16);   // V is MN-major
     const uint64_t dqs = tc_smem_desc(Qs), dks = tc_smem_desc(Ks), dvs = tc_smem_desc(Vs);
-    int n_tile = 0, c = 0, word;               // tiles, and blocks whose weights were waited for
-    bool fine = true;
-    auto scores = [&](int ck) {                // of block ck
-      fine = wait_warp(&sh.k_full[ck % kRing], (uint32_t)(ck / kRing) & 1u);
+    int n_part = 0, left = 0, c_qk = 0, word;  // parts, steps of the last of them that are still to be asked for, steps that were
+    bool fine = true, more = true;
+    unsigned first_bits = 0;                   // bit c % 32: step c is the first of its tile
+    auto scores = [&]() {                      // of the next step, if there is one
+      if (more && left == 0) {
+        more = take_part(n_part, word);
+        if (more) {
+          left = TR_FIELD(word, j1) - TR_FIELD(word, j0);
+          const int qb = QF32 ? 0 : n_part & 1;
+          fine = wait_warp(&sh.q_full[qb], (uint32_t)(QF32 ? n_part : n_part / 2) & 1u);
+          first_bits |= 1u << (c_qk & 31);
+          ++n_part;
+        }
+      }
+      if (!more || !fine) return;
+      const int s = c_qk % kRing;
+      fine = wait_warp(&sh.k_full[s], (uint32_t)(c_qk / kRing) & 1u);
       if (!fine) return;
       tc_fence_after_sync();
       if (elect_one()) {
-        const uint64_t dk = dks + (uint64_t)(ck % kRing) * (kTrHalf >> 4), dq = dqs + (uint64_t)(QF32 ? 0 : n_tile & 1) * (kTrHalf >> 4);
+        const uint64_t dk = dks + (uint64_t)s * (kTrPage >> 4), dq = dqs + (uint64_t)(QF32 ? 0 : (n_part - 1) & 1) * (kTrRows >> 4);
 #pragma unroll
-        for (int q = 0; q < (QF32 ? 8 : 4); ++q) tc_mma(tmem, dq + (uint64_t)(q >> 2) * (kTrHalf >> 4) + 2 * (q & 3), dk + 2 * (q & 3), idesc_qk, q == 0 ? 0u : 1u);
-        tc_commit(&sh.k_empty[ck % kRing]);
-        tc_commit(&sh.s_full);
+        for (int q = 0; q < (QF32 ? 8 : 4); ++q)
+          tc_mma(tmem + 64u * (c_qk & 1), dq + (uint64_t)(q >> 2) * (kTrRows >> 4) + 2 * (q & 3), dk + 2 * (q & 3), idesc_qk, q == 0 ? 0u : 1u);
+        tc_commit(&sh.k_empty[s]);
+        tc_commit(&sh.s_full[c_qk & 1]);
       }
       __syncwarp();
+      ++c_qk; --left;
     };
+    scores();
+    // (fp32 queries have one place: a tile's are written when the one before has left, so that nothing is asked for across that border here)
+    if (fine && (!QF32 || left > 0)) scores();
 #pragma unroll 1
-    for (int n_part = 0; fine && take_part(n_part, word); ++n_part, ++n_tile) {
-      const int nb = TR_FIELD(word, j1) - TR_FIELD(word, j0);
-      fine = wait_warp(&sh.q_full[QF32 ? 0 : n_tile & 1], (uint32_t)(QF32 ? n_tile : n_tile / 2) & 1u);
-#pragma unroll 1
-      for (int k = -1; k < nb && fine; ++k) {
-        // (the scores first where their keys are there, else the values)
-        bool asked = k + 1 == nb;
-        if (k >= 0) {
-          fine = wait_warp(&sh.p_full, (uint32_t)c & 1u);
-          if (!fine) break;
-          tc_fence_after_sync();
-          const bool now = !asked && __all_sync(0xFFFFFFFFu, mbar_try_wait(&sh.k_full[(c + 1) % kRing], (uint32_t)((c + 1) / kRing) & 1u));
-          if (now) { scores(c + 1); asked = true; }
-          if (fine) fine = wait_warp(&sh.v_full[c % kRing], (uint32_t)(c / kRing) & 1u);
-          if (!fine) break;
-          tc_fence_after_sync();
-          if (elect_one()) {
-            const uint64_t dv = dvs + (uint64_t)(c % kRing) * (kTrHalf >> 4);
+    for (int c = 0; fine && c < c_qk; ++c) {
+      fine = wait_warp(&sh.p_full[c & 1], (uint32_t)(c / 2) & 1u) && wait_warp(&sh.v_full[c % kRing], (uint32_t)(c / kRing) & 1u);
+      if (!fine) break;
+      tc_fence_after_sync();
+      if (elect_one()) {
+        const uint64_t dv = dvs + (uint64_t)(c % kRing) * (kTrPage >> 4);
+        const bool opens = first_bits >> (c & 31) & 1u;
 #pragma unroll
-            for (int q = 0; q < kTrKeys / 16; ++q)   // 16 keys an instruction: 8 columns of P, two groups of 8 rows of V
-              tc_mma_ts(tmem + 192u, tmem + 128u + 8u * q, dv + 128 * q, idesc_pv, k == 0 && q == 0 ? 0u : 1u);
-            tc_commit(&sh.v_empty[c % kRing]);
-            tc_commit(&sh.o_full);
-          }
-          __syncwarp();
-          ++c;
-        }
-        if (!asked) scores(c);
+        for (int q = 0; q < kTrKeys / 16; ++q)   // 16 keys an instruction: 8 columns of P, two groups of 8 rows of V
+          tc_mma_ts(tmem + 192u, tmem + 128u + 32u * (c & 1) + 8u * q, dv + 128 * q, idesc_pv, opens && q == 0 ? 0u : 1u);
+        tc_commit(&sh.v_empty[c % kRing]);
+        tc_commit(&sh.o_full[c & 1]);
       }
+      __syncwarp();
+      first_bits &= ~(1u << (c & 31));
+      if (!QF32 || left > 0) scores();
+      else if (c + 1 == c_qk) { scores(); if (fine && left > 0) scores(); }
     }
+    }
+  } else if (E4M3 && S > 1 && warp >= Shape::kWidenWarp) {
+    if constexpr (E4M3 && S > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kRegsWiden));
+    widen();
   } else {
+    if constexpr (E4M3) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Shape::kRegsSoftmax));
     // ---- softmax ----
-    const int copies = 1 << a.lg, rgs = 4 >> a.lg, rg = warp & (rgs - 1), rep = warp >> (2 - a.lg);   // which 32 rows of the tile, and which copy of them
-    const int i_row = 32 * rg + lane, chunks = rgs, col0 = rep * 32 * chunks;                         // the thread's row, and its first key of a block
+    constexpr int kChunks = kRgs;              // 16 values each, that a thread finishes of its row
+    const int rg = warp % kRgs, rep = warp / kRgs, i_row = 32 * rg + lane, col0 = rep * kCols;   // which 32 rows of the tile and which copy of them; the row, its first key of a step
     const uint32_t t_lane = tmem + ((uint32_t)(32 * warp) << 16);
-    int n_meet = 0, c = 0, n_tile = 0, word;                 // waits for meet, blocks, tiles
+    int n_meet = 0, c = 0, n_tile = 0, word;                 // waits for meet, steps, tiles
     bool fine = true;
     // Of the tile that began before the CTA's range, and of its last one, where other CTAs share them: how many had a ticket when this CTA took its own (0: it has
     // no part, or none yet), and which of the two tickets is still to be taken.
     int came[2] = {0, 0}, due = -1;
     TreePart &p = sh.mine[warp];
-    if (copies > 1) {                          // weights of the other copies' keys: zero throughout
+    if (S > 1) {                               // weights of the other copies' keys: zero throughout
       float z[32];
 #pragma unroll
       for (int e = 0; e < 32; ++e) z[e] = 0.f;
@@ -450,7 +509,7 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
     // A tile that several CTAs share has a place in each: by warp, its values' columns of four for 32 rows, then reference and sum.  A CTA has
     // two places: for the tile that began before its range, and the one that goes on behind it.
     auto place = [&](int cta, int c0) { return a.part + (size_t)(2 * cta + (cta == c0)) * 128 * kTrPitch; };
-    auto at_values = [&](int x) { return (warp * chunks + x) * 4 * 128 + lane * 4; };   // of 16 values x of the thread's row
+    auto at_values = [&](int x) { return (warp * kChunks + x) * 4 * 128 + lane * 4; };   // of 16 values x of the thread's row
     // those of CTAs c .. c1, in the order of their keys, onto o, m, l; the sum of weights
     auto add_parts = [&](int c0, int cta, int c1, int x, float (&o)[16], float m, float l) {
 #pragma unroll 1
@@ -476,7 +535,7 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
       if (i_row >= p.n_i) return;
       const float inv = l == 0.f ? 0.f : 1.0f / l;
       const int r = a.by_G.of(i_row);
-      uint4 *dst = reinterpret_cast<uint4 *>(a.out + ((size_t)(p.row0 + r) * a.H + (p.kvh - r) * a.G + i_row) * kHeadDim + 16 * (rep * chunks + x));
+      uint4 *dst = reinterpret_cast<uint4 *>(a.out + ((size_t)(p.row0 + r) * a.H + (p.kvh - r) * a.G + i_row) * kHeadDim + 16 * (rep * kChunks + x));
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         dst[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
@@ -494,7 +553,7 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
     for (int n_part = 0; fine && take_part(n_part, word); ++n_part, ++n_tile) {
       if (lane < kTrPartWords) reinterpret_cast<int *>(&p)[lane] = word;
       __syncwarp();
-      const int j0 = p.j0, nb = p.j1 - j0;
+      const int j0 = p.j0, steps = p.j1 - j0;
       const bool mine = i_row < p.n_i, live = 32 * rg < p.n_i;   // the thread's row exists, some row of the warp does
       float m = -INFINITY, l = 0.f;
       if constexpr (QF32) {                    // the row's queries, as often as it stands among the lanes
@@ -515,7 +574,7 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
             lo[e] = pack_bf16x2(x[2 * e] - f0, x[2 * e + 1] - f1);
           }
           *reinterpret_cast<uint4 *>(Qs + to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4 *>(Qs + kTrHalf + to) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          *reinterpret_cast<uint4 *>(Qs + kTrRows + to) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -524,131 +583,127 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
       const int *row_mask = a.mask + (size_t)(p.row0 + a.by_G.of(min(i_row, p.n_i - 1))) * a.words;
       const unsigned mask0 = (unsigned)row_mask[0], mask1 = a.words > 1 ? (unsigned)row_mask[1] : 0u;   // asked for here, wanted where drafted keys begin
 #pragma unroll 1
-      for (int b = 0; b < nb; ++b, ++c) {
-        const int key0 = (j0 + b) * kTrKeys, n = min(kTrKeys, p.keys - key0), committed = p.committed;
-        fine = wait_warp(&sh.s_full, (uint32_t)c & 1u);
+      for (int b = 0; b < steps; ++b, ++c) {
+        const int key0 = (j0 + b) * kTrKeys, n = min(kTrKeys, p.keys - key0), committed = p.committed, turn = c & 1;
+        fine = wait_warp(&sh.s_full[turn], (uint32_t)(c / 2) & 1u);
         if (!fine) break;
         tc_fence_after_sync();
-        const int pages = *reinterpret_cast<volatile int *>(&sh.pages_ok[c % kTrBeside]);
-        const bool drafted = key0 + kTrKeys > committed, special = drafted || n < kTrKeys || pages != 3;
-        const float *ks = scales + (2 * (c % kTrBeside)) * kTrKeys + col0, *vs = ks + kTrKeys;   // 8-bit cache: of K and V
-        auto visible = [&](int x) {            // bits of the thread's keys 32 x .. 32 x + 31 that its row sees
+        float s[kCols];
+        if (live) {
+          const uint32_t from = t_lane + 64u * turn + col0;
+          if constexpr (kCols == 16) tmem_ld16(from, s);
+          else {
+#pragma unroll
+            for (int e = 0; e < kCols; e += 32) tmem_ld32_async(from + (uint32_t)e, s + e);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < kCols; e += 32) tmem_landed32(s + e);
+          }
+        }
+        const bool there = *reinterpret_cast<volatile int *>(&sh.there[c % kTrThere]) != 0, drafted = key0 + kTrKeys > committed;
+        const bool special = drafted || n < kTrKeys || !there;
+        const float *ks = scales + (c % kTrScales) * 2 * kTrKeys + col0, *vs = ks + kTrKeys;   // 8-bit cache: of K and V
+        auto visible = [&](int k0) {           // bits of keys k0 .. k0 + 31 of the step that the row sees
           const int nodes = p.nodes;
           auto bits = [&](int w) {
             if (w >= a.words || 32 * w >= nodes) return 0u;
             const unsigned v = w == 0 ? mask0 : w == 1 ? mask1 : (unsigned)row_mask[w];
             return nodes - 32 * w < 32 ? v & ((1u << (nodes - 32 * w)) - 1u) : v;
           };
-          const int k0 = col0 + 32 * x, d = key0 + k0 - committed;   // number of the first of these keys among the drafted
+          const int d = key0 + k0 - committed; // number of the first of these keys among the drafted
           unsigned v = ~0u;
           if (d >= 0) v = __funnelshift_r(bits(d >> 5), d & 31 ? bits((d >> 5) + 1) : 0u, d & 31);
           else if (d > -32) v = (bits(0) << -d) | ((1u << -d) - 1u);
-          const int there = pages >> (k0 >> 6) & 1 ? n - k0 : 0;
-          return there <= 0 ? 0u : there < 32 ? v & ((1u << there) - 1u) : v;
+          const int left = there ? n - k0 : 0;
+          return left <= 0 ? 0u : left < 32 ? v & ((1u << left) - 1u) : v;
         };
+        unsigned seen[kCols > 32 ? 2 : 1];
         if (live) {
-          float s[32];
-          unsigned seen = ~0u;
-          auto scores = [&](int x) {           // of the thread's keys 32 x .. 32 x + 31
-            tmem_ld32_async(t_lane + (uint32_t)(col0 + 32 * x), s);
-            if (special) seen = visible(x);
-            tmem_wait_ld();
-            tmem_landed32(s);
-            if constexpr (E4M3) {
+          if constexpr (E4M3) {
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                const ulonglong2 f = *reinterpret_cast<const ulonglong2 *>(ks + 32 * x + e);
-                unpack_f32x2(mul_f32x2(pack_f32x2(s[e], s[e + 1]), f.x), s[e], s[e + 1]);
-                unpack_f32x2(mul_f32x2(pack_f32x2(s[e + 2], s[e + 3]), f.y), s[e + 2], s[e + 3]);
-              }
+            for (int e = 0; e < kCols; e += 4) {
+              const ulonglong2 f = *reinterpret_cast<const ulonglong2 *>(ks + e);
+              unpack_f32x2(mul_f32x2(pack_f32x2(s[e], s[e + 1]), f.x), s[e], s[e + 1]);
+              unpack_f32x2(mul_f32x2(pack_f32x2(s[e + 2], s[e + 3]), f.y), s[e + 2], s[e + 3]);
             }
-            if (special) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) s[e] = seen >> e & 1u ? s[e] : -INFINITY;
-            }
-          };
-          float top = -INFINITY, sc = 1.f;
-#pragma unroll 1
-          for (int x = 0; x < chunks; ++x) {
-            scores(x);
-            float mx[4] = {top, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-#pragma unroll
-              for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], s[e + 2 * q], s[e + 2 * q + 1]);
-            }
-            top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
           }
-          top *= a.scale;
+          if (special) {
+#pragma unroll
+            for (int x = 0; x < (kCols > 32 ? 2 : 1); ++x) {
+              seen[x] = visible(col0 + 32 * x);
+#pragma unroll
+              for (int e = 0; e < (kCols < 32 ? kCols : 32); ++e) s[32 * x + e] = seen[x] >> e & 1u ? s[32 * x + e] : -INFINITY;
+            }
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, sc = 1.f;
+#pragma unroll
+          for (int e = 0; e < kCols; e += 8) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], s[e + 2 * q], s[e + 2 * q + 1]);
+          }
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale;
           if (m == -INFINITY) { sc = 0.f; m = top; }   // nothing seen yet; O, where there is one, is zero
           else if (top > m + kTrSlack) { sc = pt_exp2(m - top); m = top; }
           if (!mine) { sc = 1.f; m = 0.f; }            // a row that does not exist holds anything
-          // P V of the block before, to which P and O belong
-          if (b > 0) {
-            fine = wait_warp(&sh.o_full, (uint32_t)(c - 1) & 1u);
-            if (!fine) break;
-            tc_fence_after_sync();
-            if (__any_sync(0xFFFFFFFFu, sc != 1.f)) {
-              float keep[32];                          // (the scores stay where there is one chunk of them)
-#pragma unroll 1
-              for (int d = 0; d < kHeadDim; d += 32) {
-                tmem_ld32(t_lane + 192u + (uint32_t)d, keep);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) keep[e] *= sc;
-                tmem_st32(t_lane + 192u + (uint32_t)d, keep);
-              }
-            }
-          }
           const float ref = m == -INFINITY ? 0.f : m;
           const unsigned long long scale2 = pack_f32x2(a.scale, a.scale), ref2 = pack_f32x2(-ref, -ref);
           unsigned long long sum2[2] = {0ull, 0ull};
-#pragma unroll 1
-          for (int x = 0; x < chunks; ++x) {
-            if (chunks > 1) scores(x);
+          float w[kCols / 2];                          // weights, two to a column
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              float y, z;
-              const unsigned long long d2 = fma_f32x2(pack_f32x2(s[e], s[e + 1]), scale2, ref2);
-              if ((e >> 1) % 4 == 3) {                 // a quarter of the exponentials on the FMA pipes
-                unpack_f32x2(poly_exp2(d2), y, z);
-              } else {
-                unpack_f32x2(d2, y, z);
-                y = pt_exp2(y); z = pt_exp2(z);
+          for (int e = 0; e < kCols; e += 2) {
+            float y, z;
+            unpack_f32x2(fma_f32x2(pack_f32x2(s[e], s[e + 1]), scale2, ref2), y, z);
+            y = pt_exp2(y); z = pt_exp2(z);
+            sum2[(e >> 1) & 1] = add_f32x2(sum2[(e >> 1) & 1], pack_f32x2(y, z));
+            if constexpr (E4M3) {
+              float fy, fz;
+              unpack_f32x2(*reinterpret_cast<const unsigned long long *>(vs + e), fy, fz);
+              if (special) {                           // a key that is not seen may have any scale
+                fy = seen[e >> 5] >> (e & 31) & 1u ? fy : 0.f;
+                fz = seen[e >> 5] >> ((e & 31) + 1) & 1u ? fz : 0.f;
               }
-              sum2[(e >> 1) & 1] = add_f32x2(sum2[(e >> 1) & 1], pack_f32x2(y, z));
-              if constexpr (E4M3) {
-                float fy, fz;
-                unpack_f32x2(*reinterpret_cast<const unsigned long long *>(vs + 32 * x + e), fy, fz);
-                if (special) {                         // a key that is not seen may have any scale
-                  fy = seen >> e & 1u ? fy : 0.f;
-                  fz = seen >> (e + 1) & 1u ? fz : 0.f;
-                }
-                y *= fy; z *= fz;
-              }
-              s[e >> 1] = __uint_as_float(pack_bf16x2(y, z));
+              y *= fy; z *= fz;
             }
-            tmem_st16_async(t_lane + 128u + (uint32_t)(col0 / 2 + 16 * x), s);
+            w[e >> 1] = __uint_as_float(pack_bf16x2(y, z));
           }
           float s0, s1;
           unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
           l = fmaf(l, sc, s0 + s1);
-          tmem_wait_st();
-        } else if (b > 0) {
-          fine = wait_warp(&sh.o_full, (uint32_t)(c - 1) & 1u);
+          // this place of P is free when the product of the step before last is done; O holds still when the last one's is
+          if (c >= 2) fine = wait_warp(&sh.o_full[turn], (uint32_t)(c / 2 - 1) & 1u);
+          if (b > 0 && fine && __any_sync(0xFFFFFFFFu, sc != 1.f)) {
+            fine = wait_warp(&sh.o_full[turn ^ 1], (uint32_t)((c - 1) / 2) & 1u);
+            if (!fine) break;
+            tc_fence_after_sync();
+#pragma unroll 1
+            for (int d = 0; d < kHeadDim; d += 16) {
+              float keep[16];
+              tmem_ld16(t_lane + 192u + (uint32_t)d, keep);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) keep[e] *= sc;
+              tmem_st16_async(t_lane + 192u + (uint32_t)d, keep);
+            }
+          }
           if (!fine) break;
+          tc_fence_after_sync();
+          const uint32_t to = t_lane + 128u + 32u * turn + col0 / 2;
+          if constexpr (kCols == 64) tmem_st32_async(to, w);
+          else if constexpr (kCols == 32) tmem_st16_async(to, w);
+          else tmem_st8_async(to, w);
+          tmem_wait_st();
         }
         if constexpr (!E4M3) {
           if (special) {
             // V rows without a key hold anything, and so may those of drafted tokens that no row sees (a tree padded to a size): 0 * NaN
             // must not reach O.  They become zero, and rows that do see one that is not finite NaN.
-            if (!wait_warp(&sh.v_full[c & 1], (uint32_t)(c / 2) & 1u)) { fine = false; break; }
-            unsigned char *v = Vs + (c & 1) * kTrHalf;
+            if (!wait_warp(&sh.v_full[c % kRing], (uint32_t)(c / kRing) & 1u)) { fine = false; break; }
+            unsigned char *v = Vs + (c % kRing) * kTrPage;
             unsigned found = 0;
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
+            for (int x = 0; x < 4; ++x) {
               const int k = (tid >> 3) + 16 * x;
               uint4 *piece = reinterpret_cast<uint4 *>(v + k * 128 + (tid & 7) * 16);
-              if (k >= n || !(pages >> (k >> 6) & 1)) *piece = make_uint4(0, 0, 0, 0);
+              if (k >= n || !there) *piece = make_uint4(0, 0, 0, 0);
               else if (key0 + k >= committed) {
                 const uint4 y = *piece;
                 auto odd = [](uint32_t z) { return (z & 0x7F80u) == 0x7F80u || (z & 0x7F800000u) == 0x7F800000u; };
@@ -660,18 +715,18 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
               if (found) sh.found = c + 1;     // (whoever writes writes the same)
               fine = meet();
               if (fine && *reinterpret_cast<volatile int *>(&sh.found) == c + 1) {   // rare: which keys, and who sees them
-                if (tid < 4) sh.bad[tid] = 0u;
+                if (tid < 2) sh.bad[tid] = 0u;
                 fine = meet();
 #pragma unroll 1
-                for (int x = 0; x < 8; ++x)
+                for (int x = 0; x < 4; ++x)
                   if (found >> x & 1) { const int k = (tid >> 3) + 16 * x; atomicOr(&sh.bad[k >> 5], 1u << (k & 31)); }
                 fine = meet() && fine;
                 if (live) {
 #pragma unroll 1
-                  for (int x = 0; x < chunks; ++x)
-                    if (visible(x) & *reinterpret_cast<volatile unsigned *>(&sh.bad[col0 / 32 + x])) l = __int_as_float(0x7FFFFFFF);
+                  for (int x = 0; x < 2; ++x)  // (all keys of the step: a row's copies end up as one)
+                    if (visible(32 * x) & *reinterpret_cast<volatile unsigned *>(&sh.bad[x])) l = __int_as_float(0x7FFFFFFF);
                 }
-                fine = meet() && fine;         // before the next block's are written
+                fine = meet() && fine;         // before the next step's are written
               }
               if (!fine) break;
             }
@@ -679,18 +734,24 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_full);
+        if (lane == 0) mbar_arrive(&sh.p_full[turn]);
         if (due >= 0) take_ticket();
       }
       if (!fine) break;
       // ---- the tile's sums ----
-      fine = wait_warp(&sh.o_full, (uint32_t)(c - 1) & 1u);
+      fine = wait_warp(&sh.o_full[(c - 1) & 1], (uint32_t)((c - 1) / 2) & 1u);
       if (!fine) break;
       tc_fence_after_sync();
       float met[16];                           // where a row stands several times: its sums, or a half or a quarter of them at a time
-      float4 *stage = reinterpret_cast<float4 *>(Qs + (QF32 ? 0 : (n_tile & 1) * kTrHalf));   // where the queries were, which no product reads any more
-      if (copies > 1 && live) sh.ml[warp][lane] = make_float2(m, l);
-      float mine_f[4];                         // what each copy's sums are multiplied by
+      // Copies of a row meet where the tile's queries and (16-bit ones) the values of the last two steps were, which no product reads any more: half of a
+      // row's values each.
+      auto stage = [&](int h, int w) -> float4 * {   // of warp w's rows, half h
+        if (h == 0) return reinterpret_cast<float4 *>(Qs + (QF32 ? 0 : (n_tile & 1) * kTrRows)) + w * 256;
+        if (QF32) return reinterpret_cast<float4 *>(Qs + kTrRows) + w * 256;
+        return reinterpret_cast<float4 *>(Vs + ((c - 1 - (w >> 1)) & (kRing - 1)) * kTrPage) + (w & 1) * 256;
+      };
+      if (S > 1 && live) sh.ml[warp][lane] = make_float2(m, l);
+      float mine_f[S];                         // what each copy's sums are multiplied by
       const int c0 = p.c0, c1 = p.c1;
       const bool begins = c0 == (int)blockIdx.x;
       bool whole = c0 == c1, others = false;   // others: their parts are there
@@ -712,66 +773,65 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
           for (int e = 0; e < 4; ++e) *reinterpret_cast<float4 *>(to + at_values(x) + 128 * e) = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
         }
       };
-      if (copies == 1) {
+      if constexpr (S == 1) {
 #pragma unroll 1
         for (int x = 0; x < 4; ++x) {
           if (live) tmem_ld16(t_lane + 192u + 16u * x, met);
           pass_on(x, met);
         }
       } else {
-        // half of the values at a time: that is what one tile's queries took
+        if (live) {
 #pragma unroll 1
-        for (int h = 0; h < 2 && fine; ++h) {
-          if (live) {
+          for (int h = 0; h < 2; ++h) {
             float x[32];
             tmem_ld32(t_lane + 192u + 32u * h, x);
+            float4 *to4 = stage(h, warp);
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) stage[(warp * 8 + e / 4) * 32 + lane] = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+            for (int e = 0; e < 32; e += 4) to4[e / 4 * 32 + lane] = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
           }
-          fine = meet();
-          if (!fine) break;
-          if (h == 0) {
-            float M = -INFINITY, ly[4];
+        }
+        fine = meet();
+        if (!fine) break;
+        if (live) {
+          float M = -INFINITY, ly[S];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const float2 ml = x < copies && live ? sh.ml[rg + x * rgs][lane] : make_float2(-INFINITY, 0.f);
-              mine_f[x] = ml.x; ly[x] = ml.y;
-              if (ml.y != 0.f) M = fmaxf(M, ml.x);
-            }
-            m = M; l = 0.f;
+          for (int x = 0; x < S; ++x) {
+            const float2 ml = sh.ml[rg + x * kRgs][lane];
+            mine_f[x] = ml.x; ly[x] = ml.y;
+            if (ml.y != 0.f) M = fmaxf(M, ml.x);
+          }
+          m = M; l = 0.f;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              mine_f[x] = ly[x] == 0.f ? 0.f : pt_exp2(mine_f[x] - M);   // no key in it
-              l = fmaf(ly[x], mine_f[x], l);
-            }
+          for (int x = 0; x < S; ++x) {
+            mine_f[x] = ly[x] == 0.f ? 0.f : pt_exp2(mine_f[x] - M);   // no key in it
+            l = fmaf(ly[x], mine_f[x], l);
           }
 #pragma unroll 1
-          for (int x = 0; x < chunks; ++x) {
-            const int d16 = rep * chunks + x;  // which 16 values of the 64
-            if (d16 >> 1 != h) continue;
+          for (int x = 0; x < kChunks; ++x) {
+            const int d16 = rep * kChunks + x; // which 16 values of the 64
 #pragma unroll
             for (int e = 0; e < 16; ++e) met[e] = 0.f;
-            if (live) {
 #pragma unroll
-              for (int y = 0; y < 4; ++y) {
-                if (y >= copies) continue;
-                const float f = mine_f[y];
+            for (int y = 0; y < S; ++y) {
+              const float f = mine_f[y];
+              const float4 *from4 = stage(d16 >> 1, rg + y * kRgs) + (d16 & 1) * 128 + lane;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float4 v = stage[((rg + y * rgs) * 8 + (d16 & 1) * 4 + e) * 32 + lane];
-                  met[4 * e] = fmaf(v.x, f, met[4 * e]); met[4 * e + 1] = fmaf(v.y, f, met[4 * e + 1]);
-                  met[4 * e + 2] = fmaf(v.z, f, met[4 * e + 2]); met[4 * e + 3] = fmaf(v.w, f, met[4 * e + 3]);
-                }
+              for (int e = 0; e < 4; ++e) {
+                const float4 v = from4[e * 32];
+                met[4 * e] = fmaf(v.x, f, met[4 * e]); met[4 * e + 1] = fmaf(v.y, f, met[4 * e + 1]);
+                met[4 * e + 2] = fmaf(v.z, f, met[4 * e + 2]); met[4 * e + 3] = fmaf(v.w, f, met[4 * e + 3]);
               }
             }
             pass_on(x, met);
           }
-          fine = meet();                       // before the other half, or the next queries, are written there
         }
-        if (!fine) break;
+        if constexpr (QF32) {                  // the next tile's queries are written there
+          fine = meet();
+          if (!fine) break;
+        }
       }
       tc_fence_before_sync();                  // O may be overwritten once this thread's next P is announced
-      if constexpr (!QF32) {                   // the queries of the tile after next are copied over these
+      if constexpr (!QF32) {                   // queries of the tile after next, and values of the next one, are written there
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.q_free[n_tile & 1]);
@@ -796,7 +856,7 @@ __global__ void __launch_bounds__(TreeShape<E4M3>::kThreads, TreeShape<E4M3>::kC
       if (lane == 0) a.tickets[4 * q.c0 + warp] = 0u;
       fence_gpu();
 #pragma unroll 1
-      for (int x = 0; x < chunks; ++x) {
+      for (int x = 0; x < kChunks; ++x) {
         float o[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[e] = 0.f;
@@ -845,20 +905,23 @@ inline cudaError_t tree_q_map(CUtensorMap *map, const TreeAttnArgs &a) {
   return tensor_map_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.q, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <bool E4M3, bool QF32>
-inline cudaError_t launch_tree(const CUtensorMap &map, TreeAttnArgs a, int n_sm, cudaStream_t st) {
-  using Shape = TreeShape<E4M3>;
+template <int S, bool E4M3, bool QF32>
+inline cudaError_t launch_tree_as(const CUtensorMap &map, TreeAttnArgs a, int n_sm, cudaStream_t st) {
+  using Shape = TreeShape<S, E4M3>;
   static SmemOptIn opt_in;
-  if (const cudaError_t e = opt_in(attention_tree_kernel<E4M3, QF32>, tree_smem_bytes<E4M3>(kTrMaxSeq))) return e;
-  const long long rows = (long long)a.t_max * a.G;
-  a.lg = rows <= 32 ? 2 : rows <= 64 ? 1 : 0;
-  a.rpt = (128 >> a.lg) / a.G;
+  if (const cudaError_t e = opt_in(attention_tree_kernel<S, E4M3, QF32>, tree_smem_bytes<S, E4M3>(kTrMaxSeq))) return e;
+  a.rpt = 128 / S / a.G;
   a.by_rpt.set((uint32_t)a.rpt);
   CUtensorMap q_map = {};
   if (!QF32)
     if (const cudaError_t e = tree_q_map(&q_map, a)) return e;
-  return launch_kernel(attention_tree_kernel<E4M3, QF32>, dim3((unsigned)min(Shape::kCtas * n_sm, kTrMaxCtas)), dim3(Shape::kThreads), tree_smem_bytes<E4M3>(a.n_seq), st, false,
+  return launch_kernel(attention_tree_kernel<S, E4M3, QF32>, dim3((unsigned)min(Shape::kCtas * n_sm, kTrMaxCtas)), dim3(Shape::kThreads), tree_smem_bytes<S, E4M3>(a.n_seq), st, false,
                        map, q_map, a);
+}
+template <bool E4M3, bool QF32>
+inline cudaError_t launch_tree(const CUtensorMap &map, const TreeAttnArgs &a, int n_sm, cudaStream_t st) {
+  const long long rows = (long long)a.t_max * a.G;
+  return rows <= 32 ? launch_tree_as<4, E4M3, QF32>(map, a, n_sm, st) : rows <= 64 ? launch_tree_as<2, E4M3, QF32>(map, a, n_sm, st) : launch_tree_as<1, E4M3, QF32>(map, a, n_sm, st);
 }
 
 }  // namespace ttsgpt

@@ -169,7 +169,7 @@ int32_t tts_gpt_op_attention_tree(int32_t n, int32_t R, int32_t n_head, int32_t 
   t_max = std::min(t_max, R);
   // what ranges are measured in is counted in 31 bits; so are blocks of the pool
   const int G = n_head / n_kv_head;
-  const long long tiles = (long long)n_kv_head * (R / (32 / G) + (long long)n), cost = kTrCostTile + kTrCostBlock * (pages_per_stream / 2 + 1ll);
+  const long long tiles = (long long)n_kv_head * (R / (32 / G) + (long long)n), cost = kTrCostTile + pages_per_stream + 1ll;
   if (n > kTrMaxSeq || R >= (1 << 28) || mask_words > kTreeWords * 4 || pages_per_stream > (1 << 24) || tiles * cost >= (1ll << 30) || 2ll * n_pages * n_kv_head >= (1ll << 31))
     return fail_op(TTS_GPT_E_UNSUPPORTED, "op_attention_tree: too many trees (%d at most), rows, nodes or pages", kTrMaxSeq);
   if (scratch_size < tree_scratch_bytes()) return fail_op(TTS_GPT_E_WORKSPACE, "op_attention_tree: scratch of %zu bytes, %zu needed", scratch_size, tree_scratch_bytes());
