@@ -37,13 +37,14 @@ constexpr int kTrNear = 256;                // trees up to which a CTA keeps wha
 constexpr int kTrMaxCtas = 320;
 constexpr int kTrPitch = 68;                // floats of a row's part
 constexpr float kTrSlack = 8.0f;            // log2 by which a score may exceed the reference
-constexpr int kTrCostTile = 5;              // what a tile costs besides its steps, in steps
+constexpr int kTrCostTile = 3;              // what a tile costs besides its steps, in steps (the same calls: 1, 2, 3, 5, 7: 31.8 / 77.1, 32.0 / 77.9, 32.2 / 77.2, 32.9 / 80.7, 33.2 / 81.6)
 // Parts that the copying warp may describe ahead.  Every part has a step, and no copy is more than six steps ahead of the softmax, so that it
 // never waits for a place while the softmax waits for it.
 constexpr int kTrParts = 8;
 // Places of what is written beside a page: whether it is there (by the copying warp, four pages ahead of the products, which are two ahead of the softmax)
 // and the scales of the 8-bit cache (by the widening warps, two ahead of the products).
 constexpr int kTrThere = 8, kTrScales = 4;
+constexpr int kTrNodes = 1024;              // of a tree that masks can name
 constexpr unsigned long long kTrWaitNs = 2000000000ull;
 
 struct TreeAttnArgs {
@@ -75,15 +76,15 @@ struct alignas(16) TreeShared {
   TreePart part[kTrParts];
   TreePart mine[4], shared[2][4];   // the softmax warps' own copies: the part at hand; of tiles of several CTAs the one that began before the range, and the last
   uint64_t part_full[kTrParts], part_free[kTrParts];
-  uint64_t k_full[4], v_full[4], k_empty[4], v_empty[4], raw_full[4], raw_empty[4];
+  uint64_t k_full[4], v_full[4], raw_full[4], raw_empty[4];
   uint64_t q_full[2], q_free[2];
-  uint64_t s_full[2], p_full[2], o_full[2];   // by step: scores there, weights there, their product done
+  uint64_t s_full[4], p_full[2], o_full[4];   // by step: scores there (and K read), weights there, their product done (and V read)
   uint64_t meet;                // the softmax warps among themselves, bounded like every wait
   uint32_t tmem;
   int failed;                   // 1: a wait of the CTA has run out; 2: one of an earlier call with the same scratch had
   int there[kTrThere];          // of a step: is its page one?
-  int found;                    // number (from 1 on) of the last step with a drafted key whose V is not finite
-  unsigned bad[2];              // those keys
+  int found;                    // number (from 1 on) of the last tile that has a drafted key whose V is not finite
+  unsigned bad[kTrNodes / 32];  // those keys; zero between tiles
   float2 ml[4][32];
   Div size;
   int warp_tot[16], top_cost;   // ... and the most that a tile costs
@@ -155,17 +156,18 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
   if (warp == Shape::kMmaWarp) tmem_alloc(&sh.tmem, 256);   // S 2 x 64 columns, P 2 x 32, O 64
   const int failed_before = tid == 0 ? __ldcg(a.err) : 0;
   if (tid == 32) {
-    const int copied = (int)blockIdx.x == a.starve ? 2 : 1, full = E4M3 ? Shape::kWidenWarps : copied;
+    const int copied = (int)blockIdx.x == a.starve ? 2 : 1, full = E4M3 ? Shape::kWidenWarps / 2 : copied;
     for (int i = 0; i < 4; ++i) {
-      mbar_init(&sh.k_full[i], full); mbar_init(&sh.v_full[i], full); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.v_empty[i], 1);
+      mbar_init(&sh.k_full[i], full); mbar_init(&sh.v_full[i], full); mbar_init(&sh.s_full[i], 1); mbar_init(&sh.o_full[i], 1);
       mbar_init(&sh.raw_full[i], copied); mbar_init(&sh.raw_empty[i], E4M3 ? Shape::kWidenWarps : 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.q_full[i], QF32 ? 4 : 1); mbar_init(&sh.q_free[i], 4); mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 4); mbar_init(&sh.o_full[i], 1);
+      mbar_init(&sh.q_full[i], QF32 ? 4 : 1); mbar_init(&sh.q_free[i], 4); mbar_init(&sh.p_full[i], 4);
     }
     for (int i = 0; i < kTrParts; ++i) { mbar_init(&sh.part_full[i], 1); mbar_init(&sh.part_free[i], 5 + Shape::kWidenWarps); }
     mbar_init(&sh.meet, 4);
     sh.found = 0;
+    for (int i = 0; i < kTrNodes / 32; ++i) sh.bad[i] = 0u;
     sh.top_cost = 0;
   }
   if (warp == Shape::kCopyWarp && lane == 0) {
@@ -232,9 +234,9 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
       p.n_i = min(a.rpt, x.rows - tile * a.rpt) * a.G;
       p.keys = x.keys; p.committed = x.committed; p.nodes = x.nodes; p.stream = x.stream;
       p.next = u0 + nu;
-      // Pages before the border of CTAs c - 1 and c.  A border up to four pages (a quarter of a range at most) from an end of the tile is moved there: what
-      // they cost is less than another part.
-      const int near_end = min(4, (int)size.d / 4);
+      // Pages before the border of CTAs c - 1 and c.  A border a page from an end of the tile is moved there: another part costs more (us, 16 trees of 64
+      // nodes by 20 heads / 128 of 25 by 4 of the 8-bit cache: no, one, two, four pages: 33.0 / 80.3, 32.8 / 80.5, 32.9 / 80.7, 33.7 / 82.3).
+      const int near_end = min(1, (int)size.d / 4);
       auto border = [&](int c) {
         const int b = min(max(c * (int)size.d - u0 - kTrCostTile, 0), pages);
         return b <= near_end && 2 * b <= pages ? 0 : pages - b <= near_end ? pages : b;
@@ -296,38 +298,39 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
   };
 
   auto widen = [&]() {
-    // ---- codes to bf16, 16 of a row at a time, as soon as the products are done with the page two before; and the scales ----
-    constexpr int kThreads = 32 * (E4M3 ? Shape::kWidenWarps : 1), kIter = 4 * kTrKeys / kThreads;   // 16 codes a thread and turn
-    const int t = tid - 32 * Shape::kWidenWarp, quad = t & 3;
+    // ---- codes to bf16, 16 of a row at a time, by one half of these warps those of K (and the scales), by the other those of V, as soon as the products
+    //      are done with the page two before ----
+    constexpr int kWarps = E4M3 ? Shape::kWidenWarps / 2 : 1, kThreads = 32 * kWarps, kIter = 4 * kTrKeys / kThreads;   // 16 codes a thread and turn
+    const int w = (warp - Shape::kWidenWarp) / kWarps, t = (tid - 32 * Shape::kWidenWarp) % kThreads, quad = t & 3;
     int word, c = 0;
     bool fine = true;
 #pragma unroll 1
     for (int n_part = 0; fine && take_part(n_part, word); ++n_part) {
       const int steps = TR_FIELD(word, j1) - TR_FIELD(word, j0);
 #pragma unroll 1
-      for (int b = 0; b < steps && fine; ++b, ++c) {
+      for (int b = 0; b < steps; ++b, ++c) {
         const int s = c & 1;
+        const unsigned char *from = raw + (c & 3) * Shape::kRawPage + w * kE4m3BlockBytes;
         fine = wait_warp(&sh.raw_full[c & 3], (uint32_t)(c / 4) & 1u);
+        if (c >= 2 && fine) fine = wait_warp(w ? &sh.o_full[(c - 2) & 3] : &sh.s_full[(c - 2) & 3], (uint32_t)((c - 2) / 4) & 1u);
+        // sums of the tile before met in both places of V
+        if (S > 1 && !QF32 && w == 1 && b < 2 && n_part > 0 && fine) fine = wait_warp(&sh.q_free[(n_part - 1) & 1], (uint32_t)((n_part - 1) / 2) & 1u);
+        if (!fine) break;
+        if (w == 0) {                          // K's and V's
+#pragma unroll
+          for (int x = t; x < 2 * kTrKeys; x += kThreads)
+            scales[(c % kTrScales) * 2 * kTrKeys + x] = *reinterpret_cast<const float *>(from + (x >> 6) * kE4m3BlockBytes + kPageElems + 4 * (x & 63));
+        }
+        unsigned char *dst = (w ? Vs : Ks) + s * kTrPage;
 #pragma unroll 1
-        for (int w = 0; w < 2 && fine; ++w) {
-          const unsigned char *from = raw + (c & 3) * Shape::kRawPage + w * kE4m3BlockBytes;
-          if (c >= 2) fine = wait_warp(w ? &sh.v_empty[s] : &sh.k_empty[s], (uint32_t)(c / 2 - 1) & 1u);
-          // sums of the tile before met in both places of V
-          if (S > 1 && !QF32 && w == 1 && b < 2 && n_part > 0 && fine) fine = wait_warp(&sh.q_free[(n_part - 1) & 1], (uint32_t)((n_part - 1) / 2) & 1u);
-          if (!fine) break;
-          if (w == 0) {                        // K's and V's
+        for (int k0 = 0; k0 < kIter; k0 += 4) {
+          uint4 code[4];
 #pragma unroll
-            for (int x = t; x < 2 * kTrKeys; x += kThreads)
-              scales[(c % kTrScales) * 2 * kTrKeys + x] = *reinterpret_cast<const float *>(from + (x >> 6) * kE4m3BlockBytes + kPageElems + 4 * (x & 63));
-          }
-          unsigned char *dst = (w ? Vs : Ks) + s * kTrPage;
-          uint4 code[kIter];
+          for (int k = 0; k < 4; ++k) code[k] = *reinterpret_cast<const uint4 *>(from + ((t >> 2) + kThreads / 4 * (k0 + k)) * kHeadDim + 16 * quad);
 #pragma unroll
-          for (int i = 0; i < kIter; ++i) code[i] = *reinterpret_cast<const uint4 *>(from + ((t >> 2) + kThreads / 4 * i) * kHeadDim + 16 * quad);
-#pragma unroll
-          for (int i = 0; i < kIter; ++i) {
-            const int r = (t >> 2) + kThreads / 4 * i;
-            const uint32_t x[4] = {code[i].x, code[i].y, code[i].z, code[i].w};
+          for (int k = 0; k < 4; ++k) {
+            const int r = (t >> 2) + kThreads / 4 * (k0 + k);
+            const uint32_t x[4] = {code[k].x, code[k].y, code[k].z, code[k].w};
             uint32_t y[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -337,12 +340,12 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
             *reinterpret_cast<uint4 *>(dst + r * 128 + (((2 * quad) ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
             *reinterpret_cast<uint4 *>(dst + r * 128 + (((2 * quad + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
           }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(w ? &sh.v_full[s] : &sh.k_full[s]);
-            if (w) mbar_arrive(&sh.raw_empty[c & 3]);
-          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(w ? &sh.v_full[s] : &sh.k_full[s]);
+          mbar_arrive(&sh.raw_empty[c & 3]);
         }
       }
     }
@@ -383,7 +386,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
         const int at = (j - p.j0) & 31, s = c & 3;
         if (at == 0 && j > p.j0) mine = page_of(p.stream, p.keys, j + lane);
         const int page = __shfl_sync(0xFFFFFFFFu, mine, at);
-        if (c >= 4) fine = wait_warp(E4M3 ? &sh.raw_empty[s] : &sh.k_empty[s], (uint32_t)(c / 4 - 1) & 1u);
+        if (c >= 4) fine = wait_warp(E4M3 ? &sh.raw_empty[s] : &sh.s_full[s], (uint32_t)(c / 4 - 1) & 1u);
         if (!fine) break;
         if (lane == 0) sh.there[c % kTrThere] = page >= 0;
         __syncwarp();
@@ -402,7 +405,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
             if (page >= 0) un_box(&kv_map, 0, page * 2 * a.Hkv + p.kvh, Ks + s * kTrPage, &sh.k_full[s]);
           }
           __syncwarp();
-          if (c >= 4) fine = wait_warp(&sh.v_empty[s], (uint32_t)(c / 4 - 1) & 1u);
+          if (c >= 4) fine = wait_warp(&sh.o_full[s], (uint32_t)(c / 4 - 1) & 1u);
           if (S > 1 && !QF32) {                // is there a tile whose sums meet in this place?
             const int tile = (int)(ended >> (16 * s) & 0xFFFF) - 1;
             if (tile >= 0 && fine) fine = wait_warp(&sh.q_free[tile & 1], (uint32_t)(tile / 2) & 1u);
@@ -434,31 +437,29 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
         more = take_part(n_part, word);
         if (more) {
           left = TR_FIELD(word, j1) - TR_FIELD(word, j0);
-          const int qb = QF32 ? 0 : n_part & 1;
-          fine = wait_warp(&sh.q_full[qb], (uint32_t)(QF32 ? n_part : n_part / 2) & 1u);
+          fine = wait_warp(&sh.q_full[QF32 ? 0 : n_part & 1], (uint32_t)(QF32 ? n_part : n_part / 2) & 1u);
           first_bits |= 1u << (c_qk & 31);
           ++n_part;
         }
       }
       if (!more || !fine) return;
-      const int s = c_qk % kRing;
-      fine = wait_warp(&sh.k_full[s], (uint32_t)(c_qk / kRing) & 1u);
+      fine = wait_warp(&sh.k_full[c_qk % kRing], (uint32_t)(c_qk / kRing) & 1u);
       if (!fine) return;
       tc_fence_after_sync();
       if (elect_one()) {
-        const uint64_t dk = dks + (uint64_t)s * (kTrPage >> 4), dq = dqs + (uint64_t)(QF32 ? 0 : (n_part - 1) & 1) * (kTrRows >> 4);
+        const uint64_t dk = dks + (uint64_t)(c_qk % kRing) * (kTrPage >> 4), dq = dqs + (uint64_t)(QF32 ? 0 : (n_part - 1) & 1) * (kTrRows >> 4);
 #pragma unroll
         for (int q = 0; q < (QF32 ? 8 : 4); ++q)
           tc_mma(tmem + 64u * (c_qk & 1), dq + (uint64_t)(q >> 2) * (kTrRows >> 4) + 2 * (q & 3), dk + 2 * (q & 3), idesc_qk, q == 0 ? 0u : 1u);
-        tc_commit(&sh.k_empty[s]);
-        tc_commit(&sh.s_full[c_qk & 1]);
+        tc_commit(&sh.s_full[c_qk & 3]);
       }
       __syncwarp();
       ++c_qk; --left;
     };
-    scores();
-    // (fp32 queries have one place: a tile's are written when the one before has left, so that nothing is asked for across that border here)
-    if (fine && (!QF32 || left > 0)) scores();
+    // (fp32 queries have one place: a tile's are written when the one before has left, so that nothing is asked for across that border before)
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k)
+      if (fine && (!QF32 || k == 0 || left > 0)) scores();
 #pragma unroll 1
     for (int c = 0; fine && c < c_qk; ++c) {
       fine = wait_warp(&sh.p_full[c & 1], (uint32_t)(c / 2) & 1u) && wait_warp(&sh.v_full[c % kRing], (uint32_t)(c / kRing) & 1u);
@@ -470,8 +471,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
 #pragma unroll
         for (int q = 0; q < kTrKeys / 16; ++q)   // 16 keys an instruction: 8 columns of P, two groups of 8 rows of V
           tc_mma_ts(tmem + 192u, tmem + 128u + 32u * (c & 1) + 8u * q, dv + 128 * q, idesc_pv, opens && q == 0 ? 0u : 1u);
-        tc_commit(&sh.v_empty[c % kRing]);
-        tc_commit(&sh.o_full[c & 1]);
+        tc_commit(&sh.o_full[c & 3]);
       }
       __syncwarp();
       first_bits &= ~(1u << (c & 31));
@@ -490,9 +490,10 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
     const uint32_t t_lane = tmem + ((uint32_t)(32 * warp) << 16);
     int n_meet = 0, c = 0, n_tile = 0, word;                 // waits for meet, steps, tiles
     bool fine = true;
-    // Of the tile that began before the CTA's range, and of its last one, where other CTAs share them: how many had a ticket when this CTA took its own (0: it has
-    // no part, or none yet), and which of the two tickets is still to be taken.
-    int came[2] = {0, 0}, due = -1;
+    // Of the tile that began before the CTA's range, and of the last one where it goes on behind it: is there a part whose ticket is still to be taken, and how
+    // many had one then, this CTA among them?
+    bool due0 = false, due1 = false;
+    int came0 = 0, came1 = 0;
     TreePart &p = sh.mine[warp];
     if (S > 1) {                               // weights of the other copies' keys: zero throughout
       float z[32];
@@ -541,14 +542,6 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
         dst[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
                             pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
     };
-    auto take_ticket = [&]() {                 // for the part written some time ago
-      fence_gpu();
-      __syncwarp();
-      int n = 0;
-      if (lane == 0) n = (int)atomicAdd(a.tickets + 4 * sh.shared[due][warp].c0 + warp, 1u) + 1;
-      if (due == 0) came[0] = n; else came[1] = n;
-      due = -1;
-    };
 #pragma unroll 1
     for (int n_part = 0; fine && take_part(n_part, word); ++n_part, ++n_tile) {
       if (lane < kTrPartWords) reinterpret_cast<int *>(&p)[lane] = word;
@@ -585,7 +578,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
 #pragma unroll 1
       for (int b = 0; b < steps; ++b, ++c) {
         const int key0 = (j0 + b) * kTrKeys, n = min(kTrKeys, p.keys - key0), committed = p.committed, turn = c & 1;
-        fine = wait_warp(&sh.s_full[turn], (uint32_t)(c / 2) & 1u);
+        fine = wait_warp(&sh.s_full[c & 3], (uint32_t)(c / 4) & 1u);
         if (!fine) break;
         tc_fence_after_sync();
         float s[kCols];
@@ -657,7 +650,8 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
             sum2[(e >> 1) & 1] = add_f32x2(sum2[(e >> 1) & 1], pack_f32x2(y, z));
             if constexpr (E4M3) {
               float fy, fz;
-              unpack_f32x2(*reinterpret_cast<const unsigned long long *>(vs + e), fy, fz);
+              const ulonglong2 f = *reinterpret_cast<const ulonglong2 *>(vs + (e & ~3));
+              unpack_f32x2(e & 2 ? f.y : f.x, fy, fz);
               if (special) {                           // a key that is not seen may have any scale
                 fy = seen[e >> 5] >> (e & 31) & 1u ? fy : 0.f;
                 fz = seen[e >> 5] >> ((e & 31) + 1) & 1u ? fz : 0.f;
@@ -670,9 +664,9 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
           unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
           l = fmaf(l, sc, s0 + s1);
           // this place of P is free when the product of the step before last is done; O holds still when the last one's is
-          if (c >= 2) fine = wait_warp(&sh.o_full[turn], (uint32_t)(c / 2 - 1) & 1u);
+          if (c >= 2) fine = wait_warp(&sh.o_full[(c - 2) & 3], (uint32_t)((c - 2) / 4) & 1u);
           if (b > 0 && fine && __any_sync(0xFFFFFFFFu, sc != 1.f)) {
-            fine = wait_warp(&sh.o_full[turn ^ 1], (uint32_t)((c - 1) / 2) & 1u);
+            fine = wait_warp(&sh.o_full[(c - 1) & 3], (uint32_t)((c - 1) / 4) & 1u);
             if (!fine) break;
             tc_fence_after_sync();
 #pragma unroll 1
@@ -698,50 +692,46 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
             // must not reach O.  They become zero, and rows that do see one that is not finite NaN.
             if (!wait_warp(&sh.v_full[c % kRing], (uint32_t)(c / kRing) & 1u)) { fine = false; break; }
             unsigned char *v = Vs + (c % kRing) * kTrPage;
-            unsigned found = 0;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-              const int k = (tid >> 3) + 16 * x;
+              const int k = (tid >> 3) + 16 * x, d = key0 + k - committed;
               uint4 *piece = reinterpret_cast<uint4 *>(v + k * 128 + (tid & 7) * 16);
               if (k >= n || !there) *piece = make_uint4(0, 0, 0, 0);
-              else if (key0 + k >= committed) {
+              else if (d >= 0) {
                 const uint4 y = *piece;
                 auto odd = [](uint32_t z) { return (z & 0x7F80u) == 0x7F80u || (z & 0x7F800000u) == 0x7F800000u; };
-                if (odd(y.x) || odd(y.y) || odd(y.z) || odd(y.w)) { *piece = make_uint4(0, 0, 0, 0); found |= 1u << x; }
+                if (odd(y.x) || odd(y.y) || odd(y.z) || odd(y.w)) {
+                  *piece = make_uint4(0, 0, 0, 0);
+                  if (d < kTrNodes) { atomicOr(&sh.bad[d >> 5], 1u << (d & 31)); *reinterpret_cast<volatile int *>(&sh.found) = n_tile + 1; }
+                }
               }
             }
             fence_proxy_async_smem();
-            if (drafted) {
-              if (found) sh.found = c + 1;     // (whoever writes writes the same)
-              fine = meet();
-              if (fine && *reinterpret_cast<volatile int *>(&sh.found) == c + 1) {   // rare: which keys, and who sees them
-                if (tid < 2) sh.bad[tid] = 0u;
-                fine = meet();
-#pragma unroll 1
-                for (int x = 0; x < 4; ++x)
-                  if (found >> x & 1) { const int k = (tid >> 3) + 16 * x; atomicOr(&sh.bad[k >> 5], 1u << (k & 31)); }
-                fine = meet() && fine;
-                if (live) {
-#pragma unroll 1
-                  for (int x = 0; x < 2; ++x)  // (all keys of the step: a row's copies end up as one)
-                    if (visible(32 * x) & *reinterpret_cast<volatile unsigned *>(&sh.bad[x])) l = __int_as_float(0x7FFFFFFF);
-                }
-                fine = meet() && fine;         // before the next step's are written
-              }
-              if (!fine) break;
-            }
           }
         }
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.p_full[turn]);
-        if (due >= 0) take_ticket();
+        if (due0) {                            // the part was written a step ago; what the ticket says is looked at in the end
+          fence_gpu();
+          __syncwarp();
+          if (lane == 0) came0 = (int)atomicAdd(a.tickets + 4 * sh.shared[0][warp].c0 + warp, 1u) + 1;
+          due0 = false;
+        }
       }
       if (!fine) break;
       // ---- the tile's sums ----
-      fine = wait_warp(&sh.o_full[(c - 1) & 1], (uint32_t)((c - 1) / 2) & 1u);
+      fine = wait_warp(&sh.o_full[(c - 1) & 3], (uint32_t)((c - 1) / 4) & 1u);
       if (!fine) break;
       tc_fence_after_sync();
+      if (!E4M3 && *reinterpret_cast<volatile int *>(&sh.found) == n_tile + 1) {   // rare: rows that see a V that is not finite
+        for (int w = 0; w < a.words && 32 * w < p.nodes; ++w)
+          if ((unsigned)row_mask[w] & (p.nodes - 32 * w < 32 ? (1u << (p.nodes - 32 * w)) - 1u : ~0u) & *reinterpret_cast<volatile unsigned *>(&sh.bad[w])) l = __int_as_float(0x7FFFFFFF);
+        fine = meet();
+        if (tid < kTrNodes / 32) sh.bad[tid] = 0u;
+        fine = meet() && fine;                 // before those of the next tile
+        if (!fine) break;
+      }
       float met[16];                           // where a row stands several times: its sums, or a half or a quarter of them at a time
       // Copies of a row meet where the tile's queries and (16-bit ones) the values of the last two steps were, which no product reads any more: half of a
       // row's values each.
@@ -841,15 +831,20 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
         continue;
       }
       if (mine) *reinterpret_cast<float2 *>(to + 128 * kHeadDim + 64 * warp + 2 * lane) = make_float2(m, l);
-      due = begins;
-      if (lane < kTrPartWords) reinterpret_cast<int *>(&sh.shared[due][warp])[lane] = word;
+      due0 = !begins; due1 = begins;
+      if (lane < kTrPartWords) reinterpret_cast<int *>(&sh.shared[begins][warp])[lane] = word;
       __syncwarp();
     }
     // ---- the tiles that other CTAs share, where this CTA came last: the one that began before its range, and its last ----
-    if (fine && due >= 0) take_ticket();
+    if (fine && (due0 || due1)) {
+      fence_gpu();
+      __syncwarp();
+      if (due0 && lane == 0) came0 = (int)atomicAdd(a.tickets + 4 * sh.shared[0][warp].c0 + warp, 1u) + 1;
+      if (due1 && lane == 0) came1 = (int)atomicAdd(a.tickets + 4 * sh.shared[1][warp].c0 + warp, 1u) + 1;
+    }
 #pragma unroll 1
     for (int which = 0; fine && which < 2; ++which) {
-      const int n = __shfl_sync(0xFFFFFFFFu, which ? came[1] : came[0], 0);
+      const int n = __shfl_sync(0xFFFFFFFFu, which ? came1 : came0, 0);
       if (n == 0) continue;
       const TreePart &q = sh.shared[which][warp];
       if (n != q.c1 - q.c0 + 1) continue;
