@@ -316,10 +316,14 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
         // sums of the tile before met in both places of V
         if (S > 1 && !QF32 && w == 1 && b < 2 && n_part > 0 && fine) fine = wait_warp(&sh.q_free[(n_part - 1) & 1], (uint32_t)((n_part - 1) / 2) & 1u);
         if (!fine) break;
-        if (w == 0) {                          // K's and V's
+        if (w == 0) {                          // K's and V's; a V scale that is not finite is put into the score, since 0 * NaN must not reach rows that do not see its key
 #pragma unroll
-          for (int x = t; x < 2 * kTrKeys; x += kThreads)
-            scales[(c % kTrScales) * 2 * kTrKeys + x] = *reinterpret_cast<const float *>(from + (x >> 6) * kE4m3BlockBytes + kPageElems + 4 * (x & 63));
+          for (int x = t; x < kTrKeys; x += kThreads) {
+            const float ks = *reinterpret_cast<const float *>(from + kPageElems + 4 * x), vs = *reinterpret_cast<const float *>(from + kE4m3BlockBytes + kPageElems + 4 * x);
+            const bool sound = fabsf(vs) < INFINITY;
+            scales[(c % kTrScales) * 2 * kTrKeys + x] = sound ? ks : __int_as_float(0x7FFFFFFF);
+            scales[(c % kTrScales) * 2 * kTrKeys + kTrKeys + x] = sound ? vs : 0.f;
+          }
         }
         unsigned char *dst = (w ? Vs : Ks) + s * kTrPage;
 #pragma unroll 1
@@ -610,7 +614,6 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
           const int left = there ? n - k0 : 0;
           return left <= 0 ? 0u : left < 32 ? v & ((1u << left) - 1u) : v;
         };
-        unsigned seen[kCols > 32 ? 2 : 1];
         if (live) {
           if constexpr (E4M3) {
 #pragma unroll
@@ -623,9 +626,9 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
           if (special) {
 #pragma unroll
             for (int x = 0; x < (kCols > 32 ? 2 : 1); ++x) {
-              seen[x] = visible(col0 + 32 * x);
+              const unsigned seen = visible(col0 + 32 * x);
 #pragma unroll
-              for (int e = 0; e < (kCols < 32 ? kCols : 32); ++e) s[32 * x + e] = seen[x] >> e & 1u ? s[32 * x + e] : -INFINITY;
+              for (int e = 0; e < (kCols < 32 ? kCols : 32); ++e) s[32 * x + e] = seen >> e & 1u ? s[32 * x + e] : -INFINITY;
             }
           }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, sc = 1.f;
@@ -649,14 +652,8 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
             y = pt_exp2(y); z = pt_exp2(z);
             sum2[(e >> 1) & 1] = add_f32x2(sum2[(e >> 1) & 1], pack_f32x2(y, z));
             if constexpr (E4M3) {
-              float fy, fz;
               const ulonglong2 f = *reinterpret_cast<const ulonglong2 *>(vs + (e & ~3));
-              unpack_f32x2(e & 2 ? f.y : f.x, fy, fz);
-              if (special) {                           // a key that is not seen may have any scale
-                fy = seen[e >> 5] >> (e & 31) & 1u ? fy : 0.f;
-                fz = seen[e >> 5] >> ((e & 31) + 1) & 1u ? fz : 0.f;
-              }
-              y *= fy; z *= fz;
+              unpack_f32x2(mul_f32x2(pack_f32x2(y, z), e & 2 ? f.y : f.x), y, z);
             }
             w[e >> 1] = __uint_as_float(pack_bf16x2(y, z));
           }
