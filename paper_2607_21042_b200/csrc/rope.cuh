@@ -9,17 +9,24 @@
 // modulo one, to 2^-64 of a turn a position, however far p is (in fp32 the angle of position 10^5 is off by 2^-8 radians).  The nearest quarter turn is taken
 // off in integers; what is left, at most an eighth of a turn either way, is rounded to fp32 (2^-27 half turns) and goes to sincospif.
 //
-// Split.  Eight lanes take the 64 values of a (row, head), eight values each; a CTA takes whole rows, whose sines and cosines it computes
-// once for all heads while their values are on the way.  Bound: bytes in and out.
+// Split.  A thread takes two times 16 bytes of a (row, head): eight lanes of fp32 or four of bf16 have its 64 values, and where pairs lie half the rotated
+// values apart, a thread's are those of four or eight pairs, so that no lane asks another.  A CTA takes as many (row, head) pieces at once as it has such groups
+// of lanes, in rows as wide as a power of two that holds the heads, and computes its rows' sines and cosines once for all heads while the values are under way.
+// Bound: bytes in and out.  Measured: 16 fp32 rows of 20 heads 2.2 us (a launch), 3584 of them 15.6 us (5.3 TB/s; 21.4 with eight lanes a head that exchange halves by
+// shuffles), 777 bf16 rows of 20 + 4 + 4 heads into the 8-bit cache 3.3 us, 3584 bf16 rows of 60 heads 16.6 us (17.4 with 8 bytes a time; CTAs that stay for more
+// rows and load the next ahead: 16.4, and 18.7 instead of 15.7 from fp32).  CTAs an SM by registers: one more or less costs 3 to 7 %.
 #pragma once
 #include "attention_common.cuh"
 #include "page_tables.cuh"
 
 namespace ttsgpt {
 
-constexpr int kRopeThreads = 256, kRopeSlots = kRopeThreads / 8;
-constexpr int kRopePer = 2;                    // (row, head) pieces of a thread under way at once
-constexpr int kRopeRows = 16;                  // rows of a CTA at most
+constexpr int kRopeThreads = 256;
+template <typename Src> struct RopeShape {
+  static constexpr int kVals = 16 / sizeof(Src), kLanes = kHeadDim / (2 * kVals), kSlots = kRopeThreads / kLanes;   // (row, head) pieces of a CTA
+  static constexpr int kPer = sizeof(Src) == 4 ? 2 : 1;   // of a thread under way at once, where a row has more heads
+  static constexpr int kRows = kSlots / 2;     // of a CTA at most
+};
 
 struct RopeArgs {
   const void *q, *k, *v;
@@ -29,10 +36,9 @@ struct RopeArgs {
   void *q_out;
   unsigned char *pool;
   int R, H, K, pairs, n_slots;                 // heads of q and of the pool; slots: 64 n_pages
-  int rows;                                    // of a CTA
+  int lg;                                      // log2 of the slots of a row: as many as it has heads, as far as there are slots
   int out_f32;
   float magnitude;
-  Div by_heads;                                // H + 2 K
 };
 
 // cosine and sine of a phase, in 2^-64 turns
@@ -45,112 +51,187 @@ __device__ __forceinline__ float2 cos_sin_of_phase(unsigned long long phase) {
   return make_float2((quarter + 1) & 2 ? -x : x, quarter & 2 ? -y : y);
 }
 
-enum { ROPE_HALF8 = 0, ROPE_HALF = 1, ROPE_NEIGHBOURS = 2 };   // pairs (i, i + r/2) with r/2 a multiple of 8, with any r/2; pairs (2i, 2i + 1)
+enum { ROPE_HALVES = 0, ROPE_HALF = 1, ROPE_NEIGHBOURS = 2 };   // pairs (i, i + r/2) with r/2 a multiple of 16 bytes' values, with any r/2; pairs (2i, 2i + 1)
+
+// 16 bytes as values
+__device__ __forceinline__ void values_of(const uint4 &w, float (&x)[4]) { x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w); }
+__device__ __forceinline__ void values_of(const uint4 &w, float (&x)[8]) {
+  x[0] = bf16_lo(w.x); x[1] = bf16_hi(w.x); x[2] = bf16_lo(w.y); x[3] = bf16_hi(w.y);
+  x[4] = bf16_lo(w.z); x[5] = bf16_hi(w.z); x[6] = bf16_lo(w.w); x[7] = bf16_hi(w.w);
+}
+// N values as bf16, as fp32, as e4m3 codes of scale s
+template <int N> __device__ __forceinline__ void store_bf16(uint16_t *p, const float (&v)[N]) {
+  if constexpr (N == 4) *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  else *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+}
+template <int N> __device__ __forceinline__ void store_f32(float *p, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+}
+template <int N> __device__ __forceinline__ void store_e4m3(unsigned char *p, const float (&v)[N], float s) {
+  uint32_t w[N / 4];
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(__fdiv_rn(v[i], s), __fdiv_rn(v[i + 1], s)), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(__fdiv_rn(v[i + 2], s), __fdiv_rn(v[i + 3], s)), __NV_SATFINITE, __NV_E4M3);
+    w[i / 4] = lo | (hi << 16);
+  }
+  if constexpr (N == 4) *reinterpret_cast<uint32_t *>(p) = w[0];
+  else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+}
+
+template <typename Src, bool E4M3, int ORDER> __host__ __device__ constexpr int rope_ctas() { return ORDER == ROPE_HALF ? (sizeof(Src) == 2 ? 2 : 3) : sizeof(Src) == 2 ? 3 : E4M3 ? 4 : 5; }   // of an SM
 
 template <typename Src, bool E4M3, int ORDER>
-__global__ void __launch_bounds__(kRopeThreads) rope_kv_append_kernel(const RopeArgs a) {
-  __shared__ __align__(16) float cos_s[kRopeRows][kHeadDim], sin_s[kRopeRows][kHeadDim];   // by value of the head; the sine with its sign
-  const int tid = threadIdx.x, e = tid & 7, heads = a.H + 2 * a.K, rot = 2 * a.pairs;
-  const int row0 = blockIdx.x * a.rows, n_rows = min(a.rows, a.R - row0), n = n_rows * heads;
-#pragma unroll 1
-  for (int base = 0; base < n; base += kRopePer * kRopeSlots) {
-    float x[kRopePer][8], y[kRopePer][8];
-    int slot[kRopePer], rl[kRopePer], head[kRopePer];
+__global__ void __launch_bounds__(kRopeThreads, rope_ctas<Src, E4M3, ORDER>()) rope_kv_append_kernel(const RopeArgs a) {
+  using Shape = RopeShape<Src>;
+  constexpr int kVals = Shape::kVals, kLanes = Shape::kLanes, kSlots = Shape::kSlots, kPer = Shape::kPer;
+  __shared__ __align__(16) float cos_s[Shape::kRows][kHeadDim / 2], sin_s[Shape::kRows][kHeadDim / 2];   // by pair
+  const int tid = threadIdx.x, e = tid % kLanes, heads = a.H + 2 * a.K, rot = 2 * a.pairs;
+  const int rows = kSlots >> a.lg, rl = (tid / kLanes) >> a.lg, h0 = (tid / kLanes) & ((1 << a.lg) - 1);
+  // the thread's values, kVals from d0 and from d1 on: of as many pairs, or of what is not rotated
+  const int groups = a.pairs / kVals;
+  const bool turns_half = ORDER == ROPE_HALVES && e < groups;
+  const int d0 = ORDER != ROPE_HALVES || turns_half ? kVals * e : 2 * kVals * e, d1 = ORDER != ROPE_HALVES ? kVals * e + 32 : turns_half ? kVals * e + a.pairs : 2 * kVals * e + kVals;
+  auto source = [&](int r, int h) {
+    return h < a.H ? reinterpret_cast<const Src *>(a.q) + (size_t)r * a.q_stride + h * kHeadDim
+           : h < a.H + a.K ? reinterpret_cast<const Src *>(a.k) + (size_t)r * a.k_stride + (h - a.H) * kHeadDim
+                           : reinterpret_cast<const Src *>(a.v) + (size_t)r * a.v_stride + (h - a.H - a.K) * kHeadDim;
+  };
+  const int row0 = blockIdx.x * rows, r = row0 + rl;
+  uint4 now[kPer][2];
+  auto load = [&](int base) {
 #pragma unroll
-    for (int p = 0; p < kRopePer; ++p) {
-      const int item = base + p * kRopeSlots + (tid >> 3);
-      const bool live = item < n;
-      rl[p] = live ? a.by_heads.of(item) : 0;
-      head[p] = live ? item - rl[p] * heads : 0;
-      const int r = row0 + rl[p], h = head[p];
-      slot[p] = live ? a.row_slot[r] : -1;
-      const Src *src = h < a.H ? reinterpret_cast<const Src *>(a.q) + (size_t)r * a.q_stride + h * kHeadDim
-                       : h < a.H + a.K ? reinterpret_cast<const Src *>(a.k) + (size_t)r * a.k_stride + (h - a.H) * kHeadDim
-                                       : reinterpret_cast<const Src *>(a.v) + (size_t)r * a.v_stride + (h - a.H - a.K) * kHeadDim;
-      load8(src + 8 * e, x[p]);
-      if constexpr (ORDER == ROPE_HALF) {      // the partners one by one
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int d = 8 * e + i, o = d < a.pairs ? d + a.pairs : d < rot ? d - a.pairs : d;
-          if constexpr (sizeof(Src) == 4) y[p][i] = src[o];
-          else y[p][i] = bf16_bits_to_float(src[o]);
-        }
+    for (int p = 0; p < kPer; ++p) {
+      const int h = base + p * kSlots + h0;
+      now[p][0] = now[p][1] = make_uint4(0, 0, 0, 0);
+      if (r < a.R && h < heads) {
+        const Src *src = source(r, h);
+        now[p][0] = *reinterpret_cast<const uint4 *>(src + d0);
+        now[p][1] = *reinterpret_cast<const uint4 *>(src + d1);
       }
     }
-    if (base == 0) {
-      for (int i = tid; i < n_rows * a.pairs; i += kRopeThreads) {
-        const int r = i / a.pairs, j = i - r * a.pairs;
-        const float2 cs = cos_sin_of_phase((unsigned long long)(long long)a.row_pos[row0 + r] * a.turns[j]);
-        const int d0 = ORDER == ROPE_NEIGHBOURS ? 2 * j : j, d1 = ORDER == ROPE_NEIGHBOURS ? 2 * j + 1 : j + a.pairs;
-        const float c = cs.x * a.magnitude, s = cs.y * a.magnitude;
-        cos_s[r][d0] = c; cos_s[r][d1] = c;
-        sin_s[r][d0] = -s; sin_s[r][d1] = s;
-      }
-      __syncthreads();
-    }
-    // (the output may lie over the queries: all lanes of a head have read it)
-    __syncwarp();
+  };
+  load(0);
+  const int slot = r < a.R ? a.row_slot[r] : -1;
+  for (int i = tid; i < rows * a.pairs; i += kRopeThreads) {   // beside the loads
+    const int k = i / a.pairs, j = i - k * a.pairs;
+    if (row0 + k >= a.R) break;
+    const float2 cs = cos_sin_of_phase((unsigned long long)(long long)a.row_pos[row0 + k] * a.turns[j]);
+    cos_s[k][j] = cs.x * a.magnitude; sin_s[k][j] = cs.y * a.magnitude;
+  }
+  __syncthreads();
+  const bool there = slot >= 0 && slot < a.n_slots;
+  const int page = there ? slot / kPageTokens : 0, off = there ? slot % kPageTokens : 0;
+  constexpr int kTurns = ORDER == ROPE_HALF ? 2 * kVals : kVals;
+  float c[kTurns], s[kTurns];                // of the pairs of the thread's values; with any r/2 of each value, the second of a pair with its sign
+  const float *cs = cos_s[rl], *sn = sin_s[rl];
+  if constexpr (ORDER == ROPE_HALVES) {
+    if (turns_half) {
 #pragma unroll
-    for (int p = 0; p < kRopePer; ++p) {
-      const bool turn = head[p] < a.H + a.K, there = slot[p] >= 0 && slot[p] < a.n_slots;
-      if constexpr (ORDER == ROPE_HALF8) {     // the partners are another lane's; lanes that turn nothing have themselves
-        const int half = a.pairs >> 3, at = e < half ? e + half : e < 2 * half ? e - half : e, from = (tid & 24) | at;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[p][i] = __shfl_sync(0xFFFFFFFFu, x[p][i], from);
-      }
-      if constexpr (ORDER == ROPE_NEIGHBOURS) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[p][i] = x[p][i ^ 1];
-      }
-      float c[8], s[8];
-#pragma unroll
-      for (int i = 0; i < 8; i += 4) {
-        const float4 c4 = *reinterpret_cast<const float4 *>(&cos_s[rl[p]][8 * e + i]), s4 = *reinterpret_cast<const float4 *>(&sin_s[rl[p]][8 * e + i]);
+      for (int i = 0; i < kVals; i += 4) {
+        const float4 c4 = *reinterpret_cast<const float4 *>(cs + d0 + i), s4 = *reinterpret_cast<const float4 *>(sn + d0 + i);
         c[i] = c4.x; c[i + 1] = c4.y; c[i + 2] = c4.z; c[i + 3] = c4.w;
         s[i] = s4.x; s[i + 1] = s4.y; s[i + 2] = s4.z; s[i + 3] = s4.w;
       }
-      float v[8];
+    }
+  } else if constexpr (ORDER == ROPE_NEIGHBOURS) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = turn && 8 * e + i < rot ? fmaf(x[p][i], c[i], y[p][i] * s[i]) : x[p][i];
-      const int r = row0 + rl[p], h = head[p];
+    for (int i = 0; i < kVals; ++i) {        // (of what is not rotated: not used)
+      const int j = ((i < kVals / 2 ? d0 : d1) >> 1) + i % (kVals / 2);
+      c[i] = cs[j]; s[i] = sn[j];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2 * kVals; ++i) {
+      const int d = i < kVals ? d0 + i : d1 + i - kVals, j = d < a.pairs ? d : d < rot ? d - a.pairs : 0;
+      c[i] = cs[j];
+      s[i] = d < a.pairs ? -sn[j] : sn[j];
+    }
+  }
+#pragma unroll 1
+  for (int base = 0; base < heads; base += kPer * kSlots) {   // the same for all threads
+    if (base > 0) load(base);
+    float y[ORDER == ROPE_HALF ? kPer : 1][2 * kVals];
+    if constexpr (ORDER == ROPE_HALF) {      // the partners one by one
+#pragma unroll
+      for (int p = 0; p < kPer; ++p) {
+        const int h = base + p * kSlots + h0;
+#pragma unroll
+        for (int i = 0; i < 2 * kVals; ++i) {
+          const int d = i < kVals ? d0 + i : d1 + i - kVals, o = d < a.pairs ? d + a.pairs : d < rot ? d - a.pairs : d;
+          if constexpr (sizeof(Src) == 4) y[p][i] = r < a.R && h < heads ? source(r, h)[o] : 0.f;
+          else y[p][i] = r < a.R && h < heads ? bf16_bits_to_float(source(r, h)[o]) : 0.f;
+        }
+      }
+    }
+    __syncwarp();                            // (the output may lie over the queries: all lanes of a head have read it)
+#pragma unroll
+    for (int p = 0; p < kPer; ++p) {
+      if (base + p * kSlots >= heads) break;         // the same for all threads
+      const int h = base + p * kSlots + h0;
+      float x[2][kVals], v[2][kVals];
+      values_of(now[p][0], x[0]);
+      values_of(now[p][1], x[1]);
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) { v[0][i] = x[0][i]; v[1][i] = x[1][i]; }
+      if (h < a.H + a.K) {
+        if constexpr (ORDER == ROPE_HALVES) {
+          if (turns_half) {
+#pragma unroll
+            for (int i = 0; i < kVals; ++i) {
+              v[0][i] = fmaf(x[0][i], c[i], -(x[1][i] * s[i]));
+              v[1][i] = fmaf(x[1][i], c[i], x[0][i] * s[i]);
+            }
+          }
+        } else if constexpr (ORDER == ROPE_NEIGHBOURS) {
+#pragma unroll
+          for (int i = 0; i < kVals; ++i) {
+            const int k = i / (kVals / 2), o = 2 * (i % (kVals / 2));
+            if ((k ? d1 : d0) + o < rot) {
+              v[k][o] = fmaf(x[k][o], c[i], -(x[k][o + 1] * s[i]));
+              v[k][o + 1] = fmaf(x[k][o + 1], c[i], x[k][o] * s[i]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2 * kVals; ++i)
+            if ((i < kVals ? d0 + i : d1 + i - kVals) < rot) v[i / kVals][i % kVals] = fmaf(x[i / kVals][i % kVals], c[i], y[p][i] * s[i]);
+        }
+      }
       float scale = 1.f;
-      if constexpr (E4M3) {                    // of the rotated values; all lanes of the warp take part
-        float m = fabsf(v[0]);
+      if constexpr (E4M3) {                  // of the rotated values; all lanes of the warp take part
+        float m = 0.f;
 #pragma unroll
-        for (int i = 1; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
+        for (int i = 0; i < kVals; ++i) m = fmaxf(m, fmaxf(fabsf(v[0][i]), fabsf(v[1][i])));
 #pragma unroll
-        for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        for (int o = 1; o < kLanes; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
         const float quotient = m / 448.0f;
         scale = quotient > 0.f ? quotient : 1.0f;   // below 448 2^-150 it is zero though m is not
       }
-      if (!there) continue;
+      if (!there || h >= heads) continue;
       if (h < a.H) {
         if (a.out_f32) {
-          float4 *dst = reinterpret_cast<float4 *>(reinterpret_cast<float *>(a.q_out) + (size_t)r * a.out_stride + h * kHeadDim + 8 * e);
-          dst[0] = make_float4(v[0], v[1], v[2], v[3]);
-          dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+          float *dst = reinterpret_cast<float *>(a.q_out) + (size_t)r * a.out_stride + h * kHeadDim;
+          store_f32(dst + d0, v[0]);
+          store_f32(dst + d1, v[1]);
         } else {
-          *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(a.q_out) + (size_t)r * a.out_stride + h * kHeadDim + 8 * e) =
-              make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+          uint16_t *dst = reinterpret_cast<uint16_t *>(a.q_out) + (size_t)r * a.out_stride + h * kHeadDim;
+          store_bf16(dst + d0, v[0]);
+          store_bf16(dst + d1, v[1]);
         }
         continue;
       }
-      const int kv = h - a.H, which = kv >= a.K, page = slot[p] / kPageTokens, off = slot[p] % kPageTokens;
-      const size_t block = ((size_t)page * 2 + which) * a.K + (kv - which * a.K);
+      const size_t block = (size_t)page * 2 * a.K + (h - a.H);   // K's heads, then V's
       if constexpr (E4M3) {
-        uint32_t w[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(__fdiv_rn(v[4 * i], scale), __fdiv_rn(v[4 * i + 1], scale)), __NV_SATFINITE, __NV_E4M3);
-          const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(__fdiv_rn(v[4 * i + 2], scale), __fdiv_rn(v[4 * i + 3], scale)), __NV_SATFINITE, __NV_E4M3);
-          w[i] = lo | (hi << 16);
-        }
         unsigned char *blk = a.pool + block * kE4m3BlockBytes;
-        *reinterpret_cast<uint2 *>(blk + off * kHeadDim + 8 * e) = make_uint2(w[0], w[1]);
+        store_e4m3(blk + off * kHeadDim + d0, v[0], scale);
+        store_e4m3(blk + off * kHeadDim + d1, v[1], scale);
         if (e == 0) *reinterpret_cast<float *>(blk + kPageTokens * kHeadDim + 4 * off) = scale;
       } else {
-        *reinterpret_cast<uint4 *>(a.pool + block * (kPageElems * 2) + off * (kHeadDim * 2) + 16 * e) =
-            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+        uint16_t *dst = reinterpret_cast<uint16_t *>(a.pool + block * (kPageElems * 2)) + off * kHeadDim;
+        store_bf16(dst + d0, v[0]);
+        store_bf16(dst + d1, v[1]);
       }
     }
   }
@@ -158,15 +239,13 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kv_append_kernel(const Rope
 
 template <typename Src, bool E4M3>
 inline cudaError_t launch_rope_as(const RopeArgs &a, bool neighbours, cudaStream_t st) {
-  const dim3 grid((unsigned)((a.R + a.rows - 1) / a.rows)), block(kRopeThreads);
+  const dim3 grid((unsigned)((a.R - 1) / (RopeShape<Src>::kSlots >> a.lg) + 1)), block(kRopeThreads);
   if (neighbours) return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_NEIGHBOURS>, grid, block, 0, st, false, a);
-  if (a.pairs % 8 == 0) return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_HALF8>, grid, block, 0, st, false, a);
+  if (a.pairs % RopeShape<Src>::kVals == 0) return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_HALVES>, grid, block, 0, st, false, a);
   return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_HALF>, grid, block, 0, st, false, a);
 }
 inline cudaError_t launch_rope(RopeArgs a, bool src_f32, bool e4m3, bool neighbours, cudaStream_t st) {
-  const int heads = a.H + 2 * a.K;
-  a.by_heads.set((uint32_t)heads);
-  a.rows = max(1, min(kRopeRows, kRopePer * kRopeSlots / heads));   // pieces for all threads where a row has few
+  for (a.lg = 1; (1 << a.lg) < (src_f32 ? RopeShape<float>::kSlots : RopeShape<uint16_t>::kSlots) && (1 << a.lg) < a.H + 2 * a.K;) ++a.lg;
   if (src_f32) return e4m3 ? launch_rope_as<float, true>(a, neighbours, st) : launch_rope_as<float, false>(a, neighbours, st);
   return e4m3 ? launch_rope_as<uint16_t, true>(a, neighbours, st) : launch_rope_as<uint16_t, false>(a, neighbours, st);
 }
