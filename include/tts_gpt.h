@@ -268,7 +268,7 @@ int32_t tts_gpt_debug_expire_wait(tts_gpt_t *h, uint32_t limit_us);
  * after the 2 s that every wait has, and its cluster stores nothing.  Nothing hangs or faults. */
 int32_t tts_gpt_debug_expire_linear(tts_gpt_t *h, int32_t kernel, int32_t rows, int32_t tile, uint32_t limit_us, float *out);
 
-/* Test aid for the same path inside op_attention_shared and op_attention_cross: in the calls that this thread makes from now
+/* Test aid for the same path inside op_attention_shared, op_attention_cross and op_attention_tree: in the calls that this thread makes from now
  * on, the copies of CTA number `cta` (0 on) never count as complete, and waits give up after limit_us microseconds (1..100000; in
  * op_attention_cross, where its tiles have 256 rows, after the 2 s that every wait has).  cta -1: as usual again, limit_us is
  * ignored.  Nothing hangs or faults. */
@@ -458,6 +458,8 @@ int32_t tts_gpt_op_attention_cross(int32_t n, int32_t n_head, int32_t n_kv_head,
  * and op_kv_move brings that path's K and V to where the stream goes on.  Rules as for the operators above.  In all of these calls
  *   tree i (of n) is rows row_start[i] .. row_start[i+1]-1 of R (n + 1 starts, ascending, at most R), of stream stream_ids[i] (NULL: i);
  *   kv_len[stream] counts the stream's tokens with the tree's nodes, which are the last of them; those before are committed.
+ * A pass of a fixed number of rows, a captured one for instance, may have more than its trees: op_page_tables leaves the slots of those behind the last
+ * tree as they were, and where they are -1 op_rope_kv_append leaves these rows out.
  * ------------------------------------------------------------------------------------------- */
 
 /* How the frequencies of rotary positions are stretched: not at all; all divided by `factor`; the base raised so that the slowest one is (NTK); the
@@ -494,7 +496,7 @@ int32_t tts_gpt_op_tree_tables(int32_t n, int32_t R, const int32_t *row_start, c
 
 /* Attention of trees: row r attends to all committed keys of its stream and, of the tree's nodes j, to those whose bit its mask has (any mask; the row's
  * own bit counts like the others; bits of nodes that the tree has not, and nodes beyond 32 mask_words, count as not set), o = softmax(scale q.K^T) V per head.
- * A row without keys is zero; a stream outside 0..max_streams-1 has none.  Keys on a page outside 0..n_pages-1 are left out, as are those behind pages_per_stream
+ * A row without keys is zero; a stream outside 0..max_streams-1 has none, and one of fewer tokens than the tree has nodes has the last nodes' keys.  Keys on a page outside 0..n_pages-1 are left out, as are those behind pages_per_stream
  * pages.  K and V of committed keys must be finite; those of a node matter only to rows that see it, which become NaN where they are not
  * finite.  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements apart; out bf16 [R][n_head*64]; neither it nor scratch may overlap anything else that
  * the call is given (E_ARG).  t_max: at least the largest tree (rows beyond it are not computed); with the heads of a group it decides how a tile's

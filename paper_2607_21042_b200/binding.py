@@ -815,14 +815,23 @@ def op_tree_accept(draft, target, parent, row_start, kv_len, page_table, free_pa
 
 def op_kv_move(kv_layers, row_start, path, row_slot, stream=None):
     """K and V of accepted nodes to the slots of their tree's first rows, in one layer's pool or in several [layers, ...] (which may be strided)."""
-    d, shape = kv_layers.get_device(), kv_layers.shape
-    layer, layers, stride = kv_layers, 1, 0
-    if len(shape) == (5 if kv_layers.dtype is _U8 else 6):
-        layers, layer = shape[0], kv_layers[0] if shape[0] else None
-        if not layers:
-            _refuse("there must be a layer")
-        stride = kv_layers.stride(0) * kv_layers.element_size()
-    fmt, pages, heads = _pool(layer, d)
+    d, shape, u8 = kv_layers.get_device(), kv_layers.shape, kv_layers.dtype is _U8
+    if len(shape) == (5 if u8 else 6):
+        layers, pages, heads = shape[0], shape[1], shape[3]
+        strides = kv_layers.stride()
+        # of a layer that is contiguous and has a format's shape
+        sound = ((shape[2:] == (2, heads, 4352) and strides[1:] == (8704 * heads, 4352 * heads, 4352, 1)) if u8 else
+                 (shape[2:] == (2, heads, 64, 64) and strides[1:] == (8192 * heads, 4096 * heads, 4096, 64, 1) and kv_layers.dtype in (_BF16, _I16)))
+        if sound and layers:
+            fmt, stride = (1, strides[0]) if u8 else (0, 2 * strides[0])
+        else:                                  # (a size of one may have any stride)
+            if not layers:
+                _refuse("there must be a layer")
+            fmt, pages, heads = _pool(kv_layers[0], d)
+            stride = strides[0] * kv_layers.element_size()
+    else:
+        layers, stride = 1, 0
+        fmt, pages, heads = _pool(kv_layers, d)
     n, R = row_start.numel() - 1, path.numel()
     if not (row_start.dtype is path.dtype is row_slot.dtype is _I32 and row_start.get_device() == path.get_device() == row_slot.get_device() == d and row_start.is_contiguous()
             and path.is_contiguous() and row_slot.is_contiguous() and n >= 1 and row_slot.numel() >= R):

@@ -4,26 +4,34 @@
 // Row r of tree i is a node.  It attends to all committed keys of its stream and to those of the stream's last T_i keys whose bits its
 // mask has:  o = sum_j p_j v_j,  p_j = 2^(s_j - m) / sum 2^(s_j - m),  s_j = scale log2(e) q.k_j.  A row that sees no key is zero.
 //
-// Tile.  Rows of one tree times the G query heads of a head of keys, at most 128 / S of them, over blocks of 128 keys (two pages):
-//     S = Q K^T     tcgen05.mma M=128 x N=128 x K=64, fp32 in tensor memory (fp32 queries as two bf16 parts, 16 bits)
+// Tile.  Rows of one tree times the G query heads of a head of keys, at most 128 / S of them, a step a page of 64 keys:
+//     S = Q K^T     tcgen05.mma M=128 x N=64 x K=64, fp32 in tensor memory (fp32 queries as two bf16 parts, 16 bits)
 //     softmax       a thread a lane of tensor memory: reference m and sum l in fp32, P rounded to bf16 back into tensor memory; the
-//                   reference moves, and O with it, only where a score exceeds it by more than 8 (log2)
-//     O += P V      M=128 x N=64 x K=128, V as stored
-// Where a tile has at most 64 or 32 rows, they stand S = 2 or 4 times among the 128 lanes, and each copy's threads take only their half or
-// quarter of a block's keys (their P is zero elsewhere): the exponentials, which would otherwise be one warp's, are spread over all four,
-// and a row's S sums meet in shared memory at the end of the tile.
+//                   reference moves, and O with it, only where a score exceeds it by more than 8 (log2): weights stay below 2^8, sums below 2^8 per key
+//     O += P V      M=128 x N=64 x K=64, V as stored
+// Scores and weights have two places each, by turns, so that the products of a step run beside the softmax of the next: S 2 x 64, P 2 x 32, O 64 columns, 256 in
+// all, two CTAs an SM.  Where a tile has at most 64 or 32 rows, they stand S = 2 or 4 times among the 128 lanes, and each copy's threads take only their half or quarter of a
+// step's keys (their P is zero elsewhere): the exponentials, which would otherwise be one or two warps', are spread over all four, and a row's S sums meet
+// in shared memory at the end of the tile.  (S = 4, 2, 1: 16 trees of up to 32 nodes, 20 heads 28.0, 31.1, 35.8 us; 128 trees of up to 6, 5 heads to each of 4 35.5,
+// 37.9, 42.7; S = 2, 1: 64 nodes 32.6, 37.3.)
 //
-// K and V come page by page: bf16 by copies of 64 rows with the 128-byte swizzle, K a block ahead of V since it is needed a block earlier; of
-// the 8-bit cache four more warps load codes, widen them to bf16 (exact) and store them as the tensor cores want them; K's scales multiply
-// the scores and V's the weights.  Two CTAs an SM (one where 8-bit keys meet tiles of 128 rows), each with two blocks of K and of V.
+// Warps.  Four of softmax; one that finds the CTA's tiles, describes them to the others and copies queries and pages by TMA, four pages ahead; one that issues
+// the products, over the borders of tiles too.  Blocks of the 8-bit cache come as they are by bulk copies, four ahead, and two or four more warps widen the
+// codes to bf16 (exact) where the tensor cores take them, two ahead; K's scales multiply the scores and V's the weights, in fp32, before those are rounded.
 //
 // Work split.  Tiles are laid end to end by what they cost and cut into equal ranges, one a CTA, wherever the cut falls; parts of a tile that
 // several CTAs share go to scratch with a ticket, and the CTA that comes last adds them in the order of their keys, so that results do not
 // depend on timing.  Every wait is bounded.
+//
+// Bound.  One tree of 8 nodes, 20 heads, 341 keys: 10.9 us, of which 4.5 pass before the first scores (tensor memory, the trees, the first copy); then come steps of
+// 0.7 us, the end of a tile and the parts' joining, 3 us.  16 trees of up to 64 nodes, 20 heads, 88 MB of keys and values: 32.1 us against 14.2 of reading; steps of 0.65 to 0.8 us each,
+// of which scores to weights take most (tensor memory there and back, 2^x, the two products' latency), not bytes.  128 trees of 25 nodes by 5 heads to each of 4 heads of the
+// 8-bit cache: 66 us, the softmax warps' instructions (512 tiles of up to 125 rows); tensor cores and memory wait.
 #pragma once
 #include "attention_common.cuh"
 #include "draft_trees.cuh"
 #include "tensor_map.cuh"
+#include <atomic>
 #include <cstddef>
 
 namespace ttsgpt {
@@ -902,6 +910,15 @@ inline cudaError_t launch_tree_as(const CUtensorMap &map, TreeAttnArgs a, int n_
   using Shape = TreeShape<S, E4M3>;
   static SmemOptIn opt_in;
   if (const cudaError_t e = opt_in(attention_tree_kernel<S, E4M3, QF32>, tree_smem_bytes<S, E4M3>(kTrMaxSeq))) return e;
+  if constexpr (E4M3) {                        // the kernel splits the launch's registers anew: has a thread as many as the split counts on?
+    static std::atomic<bool> enough{false};
+    if (!enough.load(std::memory_order_acquire)) {
+      cudaFuncAttributes at;
+      if (const cudaError_t e = cudaFuncGetAttributes(&at, attention_tree_kernel<S, E4M3, QF32>)) return e;
+      if ((at.numRegs + 7) / 8 * 8 < Shape::kRegsLaunch) return cudaErrorInvalidKernelImage;
+      enough.store(true, std::memory_order_release);
+    }
+  }
   a.rpt = 128 / S / a.G;
   a.by_rpt.set((uint32_t)a.rpt);
   CUtensorMap q_map = {};
