@@ -87,11 +87,13 @@ struct alignas(16) TreeShared {
   uint64_t k_full[4], v_full[4], raw_full[4], raw_empty[4];
   uint64_t q_full[2], q_free[2];
   uint64_t s_full[4], p_full[2], o_full[4];   // by step: scores there (and K read), weights there, their product done (and V read)
+  uint64_t written, came_full;  // the first tile's part is in scratch; its tickets are taken
   uint64_t meet;                // the softmax warps among themselves, bounded like every wait
   uint32_t tmem;
   int failed;                   // 1: a wait of the CTA has run out; 2: one of an earlier call with the same scratch had
   int there[kTrThere];          // of a step: is its page one?
   int found;                    // number (from 1 on) of the last tile that has a drafted key whose V is not finite
+  int came[4];                  // how many CTAs had a ticket then, of each warp's rows
   unsigned bad[kTrNodes / 32];  // those keys; zero between tiles
   float2 ml[4][32];
   Div size;
@@ -102,7 +104,8 @@ template <int S, bool E4M3> struct TreeShape {
   // warps 0-3: softmax, 4: copies, 5: products; 8-bit cache: codes to bf16, two warps (6, 7) where the softmax takes longer than they do, or four (8-11; 6
   // and 7 only give up their registers)
   static constexpr int kCopyWarp = 4, kMmaWarp = 5, kWidenWarp = S == 1 ? 6 : 8, kWidenWarps = !E4M3 ? 0 : S == 1 ? 2 : 4;
-  static constexpr int kThreads = !E4M3 ? 192 : S == 1 ? 256 : 384;
+  static constexpr bool kTicketWarp = S > 1;  // warp 6 takes the first tile's tickets; else the copying warp does
+  static constexpr int kThreads = !E4M3 ? (S == 1 ? 192 : 224) : S == 1 ? 256 : 384;
   // 8-bit cache: registers of a thread, which the groups of four warps split anew; at launch each has 128 or 80
   static constexpr int kRegsLaunch = S == 1 ? 128 : 80, kRegsSoftmax = S == 1 ? 168 : 120, kRegsCopy = S == 1 ? 88 : 64, kRegsWiden = S == 1 ? 0 : 56;
   static_assert(kRegsSoftmax + kRegsCopy + kRegsWiden <= kRegsLaunch * (S == 1 ? 2 : 3), "a split of more registers than the launch has would wait forever");
@@ -126,6 +129,12 @@ __device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const float *v) 
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
                ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]),
                "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]) : "memory");
+}
+// has the phase ended?  (does not suspend the thread, as mbar_try_wait may)
+__device__ __forceinline__ bool mbar_test_wait(uint64_t *bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+  return done != 0;
 }
 __device__ __forceinline__ void fence_gpu() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
 
@@ -172,8 +181,8 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.q_full[i], QF32 ? 4 : 1); mbar_init(&sh.q_free[i], 4); mbar_init(&sh.p_full[i], 4);
     }
-    for (int i = 0; i < kTrParts; ++i) { mbar_init(&sh.part_full[i], 1); mbar_init(&sh.part_free[i], 5 + Shape::kWidenWarps); }
-    mbar_init(&sh.meet, 4);
+    for (int i = 0; i < kTrParts; ++i) { mbar_init(&sh.part_full[i], 1); mbar_init(&sh.part_free[i], 5 + Shape::kWidenWarps + Shape::kTicketWarp); }
+    mbar_init(&sh.meet, 4); mbar_init(&sh.written, 4); mbar_init(&sh.came_full, 1);
     sh.found = 0;
     for (int i = 0; i < kTrNodes / 32; ++i) sh.bad[i] = 0u;
     sh.top_cost = 0;
@@ -367,12 +376,32 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
     if constexpr (E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Shape::kRegsCopy));
     if constexpr (E4M3 && S == 1)
       if (warp >= Shape::kWidenWarp) widen();
+    // The tickets of the first tile, c0 its first CTA, where it began before the CTA's range.  Not the softmax warps' work: the fence takes microseconds
+    // while copies are under way (16 trees of up to 32 nodes 28.0 us with it, 26.6 without).
+    auto tickets = [&](int c0) {
+      if (!wait_warp(&sh.written, 0)) return false;
+      fence_gpu();
+      if (lane < 4) sh.came[lane] = (int)atomicAdd(a.tickets + 4 * c0 + lane, 1u) + 1;
+      fence_gpu();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.came_full);
+      return true;
+    };
+    if (Shape::kTicketWarp && warp == 6) {
+      int word;
+#pragma unroll 1
+      for (int n_part = 0; take_part(n_part, word); ++n_part) {
+        const int c0 = TR_FIELD(word, c0);
+        if (n_part == 0 && c0 != (int)blockIdx.x && !tickets(c0)) break;
+      }
+    }
     if (warp == Shape::kCopyWarp) {
     // ---- copies: 16-bit queries of a tile as often as its rows stand among the lanes, two tiles ahead at most, then its keys and values ----
     int c = 0;                                 // pages of this CTA
     bool fine = true;
     TreePart p;
     int u = u_begin;
+    int due = -1;                              // first CTA of the first tile, where its tickets are to be taken here
     unsigned long long ended = 0;              // of each place of V, 16 bits: 1 + the tile whose sums meet there (modulo 2^15; one of the last six)
 #pragma unroll 1
     for (int n_part = 0; fine; ++n_part) {
@@ -381,6 +410,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
       fine = give_part(n_part, p) && there;
       if (!fine) break;
       u = p.next;
+      if (!Shape::kTicketWarp && n_part == 0 && p.c0 != (int)blockIdx.x) due = p.c0;
       int mine = page_of(p.stream, p.keys, p.j0 + lane);   // a page each lane
       if constexpr (!QF32) {
         const int qb = n_part & 1;
@@ -434,8 +464,10 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
           }
         }
         __syncwarp();
+        if (due >= 0 && mbar_test_wait(&sh.written, 0)) { fine = tickets(due) && fine; due = -1; }
       }
     }
+    if (due >= 0) tickets(due);
     } else if (warp == Shape::kMmaWarp) {
     // ---- products: each time the softmax has step c's weights in tensor memory (and its scores in registers), P V of step c and Q K^T of step c + 2,
     //      over the borders of tiles too.  Scores and weights have two places, by turns ----
@@ -502,8 +534,8 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
     const uint32_t t_lane = tmem + ((uint32_t)(32 * warp) << 16);
     int n_meet = 0, c = 0, n_tile = 0, word;                 // waits for meet, steps, tiles
     bool fine = true;
-    // Of the tile that began before the CTA's range, and of the last one where it goes on behind it: is there a part whose ticket is still to be taken, and how
-    // many had one then, this CTA among them?
+    // Of the tile that began before the CTA's range, and of the last one where it goes on behind it: is there a part in scratch, and how many CTAs had a ticket
+    // when this one took its own?
     bool due0 = false, due1 = false;
     int came0 = 0, came1 = 0;
     TreePart &p = sh.mine[warp];
@@ -717,12 +749,6 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.p_full[turn]);
-        if (due0) {                            // the part was written a step ago; what the ticket says is looked at in the end
-          fence_gpu();
-          __syncwarp();
-          if (lane == 0) came0 = (int)atomicAdd(a.tickets + 4 * sh.shared[0][warp].c0 + warp, 1u) + 1;
-          due0 = false;
-        }
       }
       if (!fine) break;
       // ---- the tile's sums ----
@@ -756,7 +782,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
         if (lane == 0) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(came) : "l"(ticket) : "memory");
         others = __shfl_sync(0xFFFFFFFFu, came, 0) == (unsigned)(c1 - c0);
         whole = others;
-        if (others) fence_gpu();
+        __syncwarp();                          // what lane 0 has acquired the others see
       }
       float *to = place(blockIdx.x, c0);
       auto pass_on = [&](int x, float (&o)[16]) {   // 16 values x of the thread's row leave, or go to scratch
@@ -836,16 +862,20 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
         continue;
       }
       if (mine) *reinterpret_cast<float2 *>(to + 128 * kHeadDim + 64 * warp + 2 * lane) = make_float2(m, l);
-      due0 = !begins; due1 = begins;
+      (begins ? due1 : due0) = true;
       if (lane < kTrPartWords) reinterpret_cast<int *>(&sh.shared[begins][warp])[lane] = word;
       __syncwarp();
+      if (!begins && lane == 0) mbar_arrive(&sh.written);
     }
     // ---- the tiles that other CTAs share, where this CTA came last: the one that began before its range, and its last ----
-    if (fine && (due0 || due1)) {
+    if (fine && due1) {
       fence_gpu();
       __syncwarp();
-      if (due0 && lane == 0) came0 = (int)atomicAdd(a.tickets + 4 * sh.shared[0][warp].c0 + warp, 1u) + 1;
-      if (due1 && lane == 0) came1 = (int)atomicAdd(a.tickets + 4 * sh.shared[1][warp].c0 + warp, 1u) + 1;
+      if (lane == 0) came1 = (int)atomicAdd(a.tickets + 4 * sh.shared[1][warp].c0 + warp, 1u) + 1;
+    }
+    if (fine && due0) {
+      fine = wait_warp(&sh.came_full, 0);
+      came0 = *reinterpret_cast<volatile int *>(&sh.came[warp]);
     }
 #pragma unroll 1
     for (int which = 0; fine && which < 2; ++which) {
@@ -910,7 +940,7 @@ inline cudaError_t launch_tree_as(const CUtensorMap &map, TreeAttnArgs a, int n_
   using Shape = TreeShape<S, E4M3>;
   static SmemOptIn opt_in;
   if (const cudaError_t e = opt_in(attention_tree_kernel<S, E4M3, QF32>, tree_smem_bytes<S, E4M3>(kTrMaxSeq))) return e;
-  if constexpr (E4M3) {                        // the kernel splits the launch's registers anew: has a thread as many as the split counts on?
+  if constexpr (E4M3) {               // the kernel splits the launch's registers anew: has a thread as many as the split counts on?
     static std::atomic<bool> enough{false};
     if (!enough.load(std::memory_order_acquire)) {
       cudaFuncAttributes at;
