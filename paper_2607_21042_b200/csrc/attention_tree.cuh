@@ -728,20 +728,17 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
             // V rows without a key hold anything, and so may those of drafted tokens that no row sees (a tree padded to a size): 0 * NaN
             // must not reach O.  They become zero, and rows that do see one that is not finite NaN.
             if (!wait_warp(&sh.v_full[c % kRing], (uint32_t)(c / kRing) & 1u)) { fine = false; break; }
-            unsigned char *v = Vs + (c % kRing) * kTrPage;
+            unsigned char *v = Vs + (c % kRing) * kTrPage + (tid >> 3) * 128 + (tid & 7) * 16;   // every 16th row, from the thread's on
+            uint4 y[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[x] = *reinterpret_cast<const uint4 *>(v + x * 2048);
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const int k = (tid >> 3) + 16 * x, d = key0 + k - committed;
-              uint4 *piece = reinterpret_cast<uint4 *>(v + k * 128 + (tid & 7) * 16);
-              if (k >= n || !there) *piece = make_uint4(0, 0, 0, 0);
-              else if (d >= 0) {
-                const uint4 y = *piece;
-                auto odd = [](uint32_t z) { return (z & 0x7F80u) == 0x7F80u || (z & 0x7F800000u) == 0x7F800000u; };
-                if (odd(y.x) || odd(y.y) || odd(y.z) || odd(y.w)) {
-                  *piece = make_uint4(0, 0, 0, 0);
-                  if (d < kTrNodes) { atomicOr(&sh.bad[d >> 5], 1u << (d & 31)); *reinterpret_cast<volatile int *>(&sh.found) = n_tile + 1; }
-                }
-              }
+              auto odd = [](uint32_t z) { return (z & 0x7F807F80u) + 0x00800080u; };   // bits 15 and 31: an exponent of ones
+              const bool none = k >= n || !there, bad = ((odd(y[x].x) | odd(y[x].y) | odd(y[x].z) | odd(y[x].w)) & 0x80008000u) != 0 && d >= 0;
+              if (none || bad) *reinterpret_cast<uint4 *>(v + x * 2048) = make_uint4(0, 0, 0, 0);
+              if (bad && !none && d < kTrNodes) { atomicOr(&sh.bad[d >> 5], 1u << (d & 31)); *reinterpret_cast<volatile int *>(&sh.found) = n_tile + 1; }
             }
             fence_proxy_async_smem();
           }
