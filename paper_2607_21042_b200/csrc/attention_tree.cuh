@@ -169,6 +169,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
   };
   auto tree_of = [&](int i) { return tree_from(a.n_seq <= kTrNear ? near_s[i] : read_tree(i)); };
   auto tile_cost = [&](int keys) { return kTrCostTile + (keys + kTrKeys - 1) / kTrKeys; };
+  pdl_wait();                                  // nothing of memory is touched before
   const int4 own = tid < a.n_seq ? read_tree(tid) : make_int4(0, 0, 0, -1);   // asked for before anything else
   if (warp == Shape::kMmaWarp) tmem_alloc(&sh.tmem, 256);   // S 2 x 64 columns, P 2 x 32, O 64
   const int failed_before = tid == 0 ? __ldcg(a.err) : 0;
@@ -231,6 +232,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = sh.tmem;
+  pdl_launch_dependents();                     // the CTA has its tensor memory: the next kernel can take none from under it
   const Div size = sh.size;
   const int u_begin = blockIdx.x * (int)size.d, u_end = *failed ? u_begin : min(T, u_begin + (int)size.d);
 
@@ -951,7 +953,7 @@ inline cudaError_t launch_tree_as(const CUtensorMap &map, TreeAttnArgs a, int n_
   CUtensorMap q_map = {};
   if (!QF32)
     if (const cudaError_t e = tree_q_map(&q_map, a)) return e;
-  return launch_kernel(attention_tree_kernel<S, E4M3, QF32>, dim3((unsigned)min(Shape::kCtas * n_sm, kTrMaxCtas)), dim3(Shape::kThreads), tree_smem_bytes<S, E4M3>(a.n_seq), st, false,
+  return launch_kernel(attention_tree_kernel<S, E4M3, QF32>, dim3((unsigned)min(Shape::kCtas * n_sm, kTrMaxCtas)), dim3(Shape::kThreads), tree_smem_bytes<S, E4M3>(a.n_seq), st, true,
                        map, q_map, a);
 }
 template <bool E4M3, bool QF32>

@@ -38,6 +38,8 @@ template <int WORDS>
 __global__ void __launch_bounds__(32 * WORDS) tree_tables_kernel(const TreeTableArgs a) {
   __shared__ unsigned set_s[WORDS][32 * WORDS];
   __shared__ int up_s[32 * WORDS];
+  pdl_launch_dependents();
+  pdl_wait();                                  // nothing of memory is touched before (in all of these kernels)
   const int i = blockIdx.x, j = threadIdx.x;
   int first, n;
   const bool sound = tree_rows(a.row_start, i, a.R, first, n);
@@ -80,10 +82,10 @@ __global__ void __launch_bounds__(32 * WORDS) tree_tables_kernel(const TreeTable
 
 inline cudaError_t launch_tree_tables(const TreeTableArgs &a, cudaStream_t st) {
   const dim3 grid((unsigned)a.n);
-  if (a.words <= 1) return launch_kernel(tree_tables_kernel<1>, grid, dim3(32), 0, st, false, a);
-  if (a.words <= 2) return launch_kernel(tree_tables_kernel<2>, grid, dim3(64), 0, st, false, a);
-  if (a.words <= 4) return launch_kernel(tree_tables_kernel<4>, grid, dim3(128), 0, st, false, a);
-  return launch_kernel(tree_tables_kernel<8>, grid, dim3(256), 0, st, false, a);
+  if (a.words <= 1) return launch_kernel(tree_tables_kernel<1>, grid, dim3(32), 0, st, true, a);
+  if (a.words <= 2) return launch_kernel(tree_tables_kernel<2>, grid, dim3(64), 0, st, true, a);
+  if (a.words <= 4) return launch_kernel(tree_tables_kernel<4>, grid, dim3(128), 0, st, true, a);
+  return launch_kernel(tree_tables_kernel<8>, grid, dim3(256), 0, st, true, a);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -118,6 +120,8 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) tree_accept_kernel(const Tr
   int *child_s = accept_smem, *target_s = child_s + kAcceptWarps * kTreeNodes;   // of each warp's tree, by node: its first child on the path, what the model says
   unsigned *seen_s = reinterpret_cast<unsigned *>(target_s + kAcceptWarps * kTreeNodes);   // a bit a stream
   __shared__ int bad_s, last_s, warp_s[kAcceptWarps], acc_s[kAcceptWarps], count_s[kAcceptWarps];
+  pdl_launch_dependents();
+  pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool alone = gridDim.x == 1;
   // ---- paths ----
@@ -288,11 +292,11 @@ inline cudaError_t launch_tree_accept(const TreeAcceptArgs &a, cudaStream_t st) 
   if (ctas > 1 && ctas <= kAcceptCluster) {
     static SmemOptIn opt_in;
     if (const cudaError_t e = opt_in(tree_accept_kernel<true>, tree_accept_smem_bytes(kTabMaxStreams))) return e;
-    return launch_kernel_cluster_dims(tree_accept_kernel<true>, dim3((unsigned)ctas), dim3(kAcceptThreads), smem, dim3((unsigned)ctas), st, false, a);
+    return launch_kernel_cluster_dims(tree_accept_kernel<true>, dim3((unsigned)ctas), dim3(kAcceptThreads), smem, dim3((unsigned)ctas), st, true, a);
   }
   static SmemOptIn opt_in;
   if (const cudaError_t e = opt_in(tree_accept_kernel<false>, tree_accept_smem_bytes(kTabMaxStreams))) return e;
-  return launch_kernel(tree_accept_kernel<false>, dim3((unsigned)ctas), dim3(kAcceptThreads), smem, st, false, a);
+  return launch_kernel(tree_accept_kernel<false>, dim3((unsigned)ctas), dim3(kAcceptThreads), smem, st, true, a);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -316,6 +320,8 @@ template <bool E4M3>
 __global__ void __launch_bounds__(kMoveMaxThreads) kv_move_kernel(const KvMoveArgs a) {
   __shared__ int2 move_s[kMoveMaxThreads];     // {from, to}, slots
   __shared__ int warp_s[kMoveMaxThreads / 32];
+  pdl_launch_dependents();
+  pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
   int first, n;
   if (!tree_rows(a.row_start, blockIdx.x, a.R, first, n)) return;
@@ -368,7 +374,7 @@ __global__ void __launch_bounds__(kMoveMaxThreads) kv_move_kernel(const KvMoveAr
 inline cudaError_t launch_kv_move(const KvMoveArgs &a, bool e4m3, cudaStream_t st) {
   const int pieces = 2 * a.K * (e4m3 ? 4 : 8);   // a thread each, where there are not too many
   return launch_kernel(e4m3 ? kv_move_kernel<true> : kv_move_kernel<false>, dim3((unsigned)a.n, (unsigned)a.layers),
-                       dim3((unsigned)std::min(kMoveMaxThreads, std::max(64, (pieces + 31) / 32 * 32))), 0, st, false, a);
+                       dim3((unsigned)std::min(kMoveMaxThreads, std::max(64, (pieces + 31) / 32 * 32))), 0, st, true, a);
 }
 
 }  // namespace ttsgpt

@@ -87,6 +87,8 @@ __global__ void __launch_bounds__(kRopeThreads, rope_ctas<Src, E4M3, ORDER>()) r
   using Shape = RopeShape<Src>;
   constexpr int kVals = Shape::kVals, kLanes = Shape::kLanes, kSlots = Shape::kSlots, kPer = Shape::kPer;
   __shared__ __align__(16) float cos_s[Shape::kRows][kHeadDim / 2], sin_s[Shape::kRows][kHeadDim / 2];   // by pair
+  pdl_launch_dependents();
+  pdl_wait();                                  // nothing of memory is touched before
   const int tid = threadIdx.x, e = tid % kLanes, heads = a.H + 2 * a.K, rot = 2 * a.pairs;
   const int rows = kSlots >> a.lg, rl = (tid / kLanes) >> a.lg, h0 = (tid / kLanes) & ((1 << a.lg) - 1);
   // the thread's values, kVals from d0 and from d1 on: of as many pairs, or of what is not rotated
@@ -240,9 +242,9 @@ __global__ void __launch_bounds__(kRopeThreads, rope_ctas<Src, E4M3, ORDER>()) r
 template <typename Src, bool E4M3>
 inline cudaError_t launch_rope_as(const RopeArgs &a, bool neighbours, cudaStream_t st) {
   const dim3 grid((unsigned)((a.R - 1) / (RopeShape<Src>::kSlots >> a.lg) + 1)), block(kRopeThreads);
-  if (neighbours) return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_NEIGHBOURS>, grid, block, 0, st, false, a);
-  if (a.pairs % RopeShape<Src>::kVals == 0) return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_HALVES>, grid, block, 0, st, false, a);
-  return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_HALF>, grid, block, 0, st, false, a);
+  if (neighbours) return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_NEIGHBOURS>, grid, block, 0, st, true, a);
+  if (a.pairs % RopeShape<Src>::kVals == 0) return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_HALVES>, grid, block, 0, st, true, a);
+  return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_HALF>, grid, block, 0, st, true, a);
 }
 inline cudaError_t launch_rope(RopeArgs a, bool src_f32, bool e4m3, bool neighbours, cudaStream_t st) {
   for (a.lg = 1; (1 << a.lg) < (src_f32 ? RopeShape<float>::kSlots : RopeShape<uint16_t>::kSlots) && (1 << a.lg) < a.H + 2 * a.K;) ++a.lg;
