@@ -12,21 +12,21 @@
 // Scores and weights have two places each, by turns, so that the products of a step run beside the softmax of the next: S 2 x 64, P 2 x 32, O 64 columns, 256 in
 // all, two CTAs an SM.  Where a tile has at most 64 or 32 rows, they stand S = 2 or 4 times among the 128 lanes, and each copy's threads take only their half or quarter of a
 // step's keys (their P is zero elsewhere): the exponentials, which would otherwise be one or two warps', are spread over all four, and a row's S sums meet
-// in shared memory at the end of the tile.  (S = 4, 2, 1: 16 trees of up to 32 nodes, 20 heads 28.0, 31.1, 35.8 us; 128 trees of up to 6, 5 heads to each of 4 35.5,
-// 37.9, 42.7; S = 2, 1: 64 nodes 32.6, 37.3.)
+// in shared memory at the end of the tile.  (S = 4, 2, 1: 16 trees of up to 32 nodes, 20 heads 26.2, 28.3, 35.3 us; 128 trees of up to 6, 5 heads to each of 4 32.6,
+// 34.2, 40.1; S = 2, 1: 64 nodes 31.0, 37.0.)
 //
 // Warps.  Four of softmax; one that finds the CTA's tiles, describes them to the others and copies queries and pages by TMA, four pages ahead; one that issues
-// the products, over the borders of tiles too.  Blocks of the 8-bit cache come as they are by bulk copies, four ahead, and two or four more warps widen the
+// the products, over the borders of tiles too; one that takes tickets (below).  Blocks of the 8-bit cache come as they are by bulk copies, four ahead, and two or four more warps widen the
 // codes to bf16 (exact) where the tensor cores take them, two ahead; K's scales multiply the scores and V's the weights, in fp32, before those are rounded.
 //
 // Work split.  Tiles are laid end to end by what they cost and cut into equal ranges, one a CTA, wherever the cut falls; parts of a tile that
 // several CTAs share go to scratch with a ticket, and the CTA that comes last adds them in the order of their keys, so that results do not
 // depend on timing.  Every wait is bounded.
 //
-// Bound.  One tree of 8 nodes, 20 heads, 341 keys: 10.9 us, of which 4.5 pass before the first scores (tensor memory, the trees, the first copy); then come steps of
-// 0.7 us, the end of a tile and the parts' joining, 3 us.  16 trees of up to 64 nodes, 20 heads, 88 MB of keys and values: 32.1 us against 14.2 of reading; steps of 0.65 to 0.8 us each,
+// Bound.  One tree of 8 nodes, 20 heads, 341 keys: 10.4 us, of which 4.5 pass before the first scores (tensor memory, the trees, the first copy); then come steps of
+// 0.7 us, the end of a tile and the parts' joining, 3 us.  16 trees of up to 64 nodes, 20 heads, 88 MB of keys and values: 30.6 us against 14.2 of reading; steps of 0.65 to 0.8 us each,
 // of which scores to weights take most (tensor memory there and back, 2^x, the two products' latency), not bytes.  128 trees of 25 nodes by 5 heads to each of 4 heads of the
-// 8-bit cache: 66 us, the softmax warps' instructions (512 tiles of up to 125 rows); tensor cores and memory wait.
+// 8-bit cache: 64 us, the softmax warps' instructions (512 tiles of up to 125 rows); tensor cores and memory wait.
 #pragma once
 #include "attention_common.cuh"
 #include "draft_trees.cuh"
@@ -45,7 +45,7 @@ constexpr int kTrNear = 256;                // trees up to which a CTA keeps wha
 constexpr int kTrMaxCtas = 320;
 constexpr int kTrPitch = 68;                // floats of a row's part
 constexpr float kTrSlack = 8.0f;            // log2 by which a score may exceed the reference
-constexpr int kTrCostTile = 3;              // what a tile costs besides its steps, in steps (the same calls: 1, 2, 3, 5, 7: 31.8 / 77.1, 32.0 / 77.9, 32.2 / 77.2, 32.9 / 80.7, 33.2 / 81.6)
+constexpr int kTrCostTile = 3;              // what a tile costs besides its steps, in steps (us of 16 trees of 64 nodes by 20 heads / 128 of 25 by 5 heads to each of 4, bf16: 1, 2, 3, 5: 30.6 / 49.4, 30.4 / 46.8, 30.6 / 45.3, 31.7 / 46.8)
 // Parts that the copying warp may describe ahead.  Every part has a step, and no copy is more than six steps ahead of the softmax, so that it
 // never waits for a place while the softmax waits for it.
 constexpr int kTrParts = 8;
@@ -224,7 +224,8 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
   const int T = bad ? 0 : carry;
   if (tid == 0) {
     first[a.n_seq] = T;
-    // eight pages at least, where a tile has so many: parts of a few cost more than they take off another CTA
+    // eight pages at least, where a tile has so many: parts of a few cost more than they take off another CTA (a tree of 8 nodes, 341 keys 10.4 us, cut into
+    // single pages 11.6)
     sh.size.set(max(min(sh.top_cost, kTrCostTile + 8), max(1, (T + (int)gridDim.x - 1) / (int)gridDim.x)));
     sh.failed = failed_before ? 2 : 0;
   }
@@ -253,13 +254,8 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
       p.n_i = min(a.rpt, x.rows - tile * a.rpt) * a.G;
       p.keys = x.keys; p.committed = x.committed; p.nodes = x.nodes; p.stream = x.stream;
       p.next = u0 + nu;
-      // Pages before the border of CTAs c - 1 and c.  A border a page from an end of the tile is moved there: another part costs more (us, 16 trees of 64
-      // nodes by 20 heads / 128 of 25 by 4 of the 8-bit cache: no, one, two, four pages: 33.0 / 80.3, 32.8 / 80.5, 32.9 / 80.7, 33.7 / 82.3).
-      const int near_end = min(1, (int)size.d / 4);
-      auto border = [&](int c) {
-        const int b = min(max(c * (int)size.d - u0 - kTrCostTile, 0), pages);
-        return b <= near_end && 2 * b <= pages ? 0 : pages - b <= near_end ? pages : b;
-      };
+      // pages before the border of CTAs c - 1 and c (a border near an end of the tile is not moved there: a page 66.0 us, none 64.6, in 128 trees of 25 nodes)
+      auto border = [&](int c) { return min(max(c * (int)size.d - u0 - kTrCostTile, 0), pages); };
       const int ca = size.of(u0), cb = size.of(u0 + nu - 1), me = blockIdx.x;
       p.j0 = me == ca ? 0 : border(me);
       p.j1 = me == cb ? pages : border(me + 1);
@@ -379,7 +375,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
     if constexpr (E4M3 && S == 1)
       if (warp >= Shape::kWidenWarp) widen();
     // The tickets of the first tile, c0 its first CTA, where it began before the CTA's range.  Not the softmax warps' work: the fence takes microseconds
-    // while copies are under way (16 trees of up to 32 nodes 28.0 us with it, 26.6 without).
+    // while copies are under way (16 trees of up to 32 nodes 28.0 us with it on them, 26.6 so).
     auto tickets = [&](int c0) {
       if (!wait_warp(&sh.written, 0)) return false;
       fence_gpu();
