@@ -224,9 +224,11 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
   const int T = bad ? 0 : carry;
   if (tid == 0) {
     first[a.n_seq] = T;
-    // eight pages at least, where a tile has so many: parts of a few cost more than they take off another CTA (a tree of 8 nodes, 341 keys 10.4 us, cut into
-    // single pages 11.6)
-    sh.size.set(max(min(sh.top_cost, kTrCostTile + 8), max(1, (T + (int)gridDim.x - 1) / (int)gridDim.x)));
+    // Few tiles are cut into ranges of three pages at least, and not at all where they have no more than eight: parts cost more than they take off another CTA (20
+    // heads, ranges of 1, 2, 3, 4, 8 pages: a tree of 256 nodes, 856 keys 21.9, 21.2, 21.8, 21.3, 28.3 us, of 8 nodes, 1908 keys 13.5, 13.5, 13.4, 13.6, 14.7; of 8
+    // nodes, 341 keys, uncut 9.5, cut 10.0 to 11.9).
+    const int least = sh.top_cost <= kTrCostTile + 8 ? sh.top_cost : kTrCostTile + 3;
+    sh.size.set(max(least, max(1, (T + (int)gridDim.x - 1) / (int)gridDim.x)));
     sh.failed = failed_before ? 2 : 0;
   }
   tc_fence_before_sync();
