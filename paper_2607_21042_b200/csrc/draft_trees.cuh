@@ -26,7 +26,7 @@ __device__ __forceinline__ bool tree_rows(const int *row_start, int i, int R, in
 // Ancestors and positions.  With A_j the set {j} and up_j the parent of j, a round takes  A_j |= A_(up_j), up_j = up_(up_j):  after k rounds
 // A_j has 2^k ancestors and up_j is the one behind them, so that the sets are complete when every up_j is -1.  A CTA a tree, a thread a
 // node, sets in shared memory.  Depth: |A_j| - 1.  Bound: launch, two dependent reads, log2(depth) rounds of two barriers.
-// Measured: 16 trees of up to 40 nodes 2.0 us (a launch), 128 of up to 200 3.1 us.
+// Measured: 16 trees of up to 40 nodes 1.6 us (a launch), 128 of up to 200 2.9 us.
 // ---------------------------------------------------------------------------------------------
 struct TreeTableArgs {
   int n, R, max_streams, words;
@@ -93,7 +93,7 @@ inline cudaError_t launch_tree_tables(const TreeTableArgs &a, cudaStream_t st) {
 // child is found at once (a minimum in shared memory), then a path is a walk along them.  A warp a tree.  One CTA then takes the streams' lengths back to the
 // accepted nodes and returns the pages behind them: request by request in the order of the call, the last page of a list first.  It is the only one up to 32
 // trees, the first of a cluster up to 256, which finds the others' counts in their shared memory, and else the one that comes last.
-// Bound: launch, two dependent reads, two sums over the requests and a read of the pages.  Measured: 16 trees of up to 40 nodes 5.2 us, 128 of up to 200 7.5 us
+// Bound: launch, two dependent reads, two sums over the requests and a read of the pages.  Measured: 16 trees of up to 40 nodes 4.9 us, 128 of up to 200 7.1 us
 // (8.0 and 12.5 with a search of the children at every step of the path, 256 threads and tickets; 7.1 and 11.6 with parents and tokens in registers).
 // ---------------------------------------------------------------------------------------------
 struct TreeAcceptArgs {
@@ -304,7 +304,7 @@ inline cudaError_t launch_tree_accept(const TreeAcceptArgs &a, cudaStream_t st) 
 // tree and a layer; its threads own 16 bytes of a (K|V, head) row each and move it for all rows of the path, eight read before they are
 // written.  Row k comes from a row behind it (path[k] > k where it moves at all, and path ascends), which is behind every place that
 // rows before it go to: nothing is written before it has been read.
-// Bound: three dependent reads of indices, then bytes.  Measured: a layer of 16 trees' paths 3.0 us; 24 layers of 32 10.1 us, 3.8 TB/s (12.4 with the pieces of all rows
+// Bound: three dependent reads of indices, then bytes.  Measured: a layer of 16 trees' paths 2.7 us; 24 layers of 32 9.5 us, 4.0 TB/s (12.4 with the pieces of all rows
 // spread over the threads and a barrier between reads and writes).
 // ---------------------------------------------------------------------------------------------
 struct KvMoveArgs {

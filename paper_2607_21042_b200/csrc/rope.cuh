@@ -12,8 +12,8 @@
 // Split.  A thread takes two times 16 bytes of a (row, head): eight lanes of fp32 or four of bf16 have its 64 values, and where pairs lie half the rotated
 // values apart, a thread's are those of four or eight pairs, so that no lane asks another.  A CTA takes as many (row, head) pieces at once as it has such groups
 // of lanes, in rows as wide as a power of two that holds the heads, and computes its rows' sines and cosines once for all heads while the values are under way.
-// Bound: bytes in and out.  Measured: 16 fp32 rows of 20 heads 2.2 us (a launch), 3584 of them 15.6 us (5.3 TB/s; 21.4 with eight lanes a head that exchange halves by
-// shuffles), 777 bf16 rows of 20 + 4 + 4 heads into the 8-bit cache 3.3 us, 3584 bf16 rows of 60 heads 16.6 us (17.4 with 8 bytes a time; CTAs that stay for more
+// Bound: bytes in and out.  Measured: 16 fp32 rows of 20 heads 2.0 us (a launch), 3584 of them 15.2 us (5.4 TB/s; 21.4 with eight lanes a head that exchange halves by
+// shuffles), 777 bf16 rows of 20 + 4 + 4 heads into the 8-bit cache 2.8 us, 3584 bf16 rows of 60 heads 16.6 us (17.4 with 8 bytes a time; CTAs that stay for more
 // rows and load the next ahead: 16.4, and 18.7 instead of 15.7 from fp32).  CTAs an SM by registers: one more or less costs 3 to 7 %.
 #pragma once
 #include "attention_common.cuh"
