@@ -480,7 +480,7 @@ int32_t tts_gpt_op_rope_frequencies(int32_t n_rot, int32_t scaling, double base,
  * the others stay.  Any position is fine, a negative one turns back.  q, K and V of one type, TTS_GPT_T_F32 or TTS_GPT_T_BF16; q_out of either type, rows
  * out_stride elements apart; it may be q itself (same type and stride).  turns DEVICE, 8-byte aligned.  n_head 0: K and V only, q and q_out are not
  * looked at.  A row whose slot lies outside the pool is left out, its q_out included.  Sums in fp32, each value rounded once; e4m3 scales are
- * those of the rotated values. */
+ * those of the rotated values, NaN where one of the 64 is. */
 int32_t tts_gpt_op_rope_kv_append(int32_t R, int32_t n_head, int32_t n_kv_head, int32_t type, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                                   const void *v, int64_t v_stride, const int32_t *row_pos, const int32_t *row_slot, int32_t n_rot, const uint64_t *turns,
                                   int32_t interleaved, float magnitude, int32_t out_type, void *q_out, int64_t out_stride, int32_t kv_fmt, int32_t n_pages, void *kv_layer,
@@ -498,7 +498,7 @@ int32_t tts_gpt_op_tree_tables(int32_t n, int32_t R, const int32_t *row_start, c
  * own bit counts like the others; bits of nodes that the tree has not, and nodes beyond 32 mask_words, count as not set), o = softmax(scale q.K^T) V per head.
  * A row without keys is zero; a stream outside 0..max_streams-1 has none, and one of fewer tokens than the tree has nodes has the last nodes' keys.  Keys on a page outside 0..n_pages-1 are left out, as are those behind pages_per_stream
  * pages.  K and V of committed keys must be finite; those of a node matter only to rows that see it, which become NaN where they are not
- * finite.  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements apart; out bf16 [R][n_head*64]; neither it nor scratch may overlap anything else that
+ * finite (8-bit cache: where a scale is not).  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements apart; out bf16 [R][n_head*64]; neither it nor scratch may overlap anything else that
  * the call is given (E_ARG).  t_max: at least the largest tree (rows beyond it are not computed); with the heads of a group it decides how a tile's
  * work is spread, so that small trees go faster in a call of their own than beside large ones.  Rows of no tree are left as they were; where starts do not
  * ascend, or exceed R, nothing is written.  Heads, roundings, timing and scratch as for op_attention_shared (scratch size independent of the

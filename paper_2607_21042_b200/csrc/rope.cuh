@@ -205,11 +205,11 @@ __global__ void __launch_bounds__(kRopeThreads, rope_ctas<Src, E4M3, ORDER>()) r
       if constexpr (E4M3) {                  // of the rotated values; all lanes of the warp take part
         float m = 0.f;
 #pragma unroll
-        for (int i = 0; i < kVals; ++i) m = fmaxf(m, fmaxf(fabsf(v[0][i]), fabsf(v[1][i])));
+        for (int i = 0; i < kVals; ++i) m = max_nan(m, max_nan(fabsf(v[0][i]), fabsf(v[1][i])));
 #pragma unroll
-        for (int o = 1; o < kLanes; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        for (int o = 1; o < kLanes; o <<= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
         const float quotient = m / 448.0f;
-        scale = quotient > 0.f ? quotient : 1.0f;   // below 448 2^-150 it is zero though m is not
+        scale = quotient == 0.f ? 1.0f : quotient;   // below 448 2^-150 it is zero though m is not; NaN (and so the whole row) where a value is: codes have none that attention knows
       }
       if (!there || h >= heads) continue;
       if (h < a.H) {

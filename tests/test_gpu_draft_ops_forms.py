@@ -211,6 +211,24 @@ def test_calls_on_a_stream_that_is_not_the_current_one():
 # ---------------------------------------------------------------------------------------------
 # forms of the arguments
 # ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("src", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("n_rot", [64, 30])
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them(fmt, n_rot, interleaved, src):
+    """A chain of six nodes behind nothing: from the node on whose key or value is not finite, the head's rows are NaN, and no others."""
+    x = torch.randn(6, 3 * 128, generator=_gen(4)).to(src).to(DEV)
+    q, k, v = x.split(128, 1)
+    k[3, 64 + 17], v[1, 5], v[4, 64 + 60] = float("nan"), float("nan"), float("inf")
+    pool, table = _empty_pool(fmt, 2, 2), _i32([[1]])
+    slot, pos = torch.arange(64, 70, dtype=torch.int32, device=DEV), torch.arange(6, dtype=torch.int32, device=DEV)
+    q_out = B.op_rope_kv_append(q, k, v, pool, slot, pos, B.op_rope_frequencies(n_rot, device=DEV)[0], interleaved=interleaved)
+    out = B.op_attention_tree(q_out, pool, table, _i32([0, 6]), _i32([6]), _masks([np.tril(np.ones((6, 6), bool))], 1, extra=0), 6).view(6, 2, 64)
+    bad = torch.isnan(out)
+    for head, first in ((0, 1), (1, 3)):
+        assert not bad[:first, head].any() and bad[first:, head].all()
+
+
 @pytest.mark.parametrize("fmt", [0, 1])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("H,K,lens,ctx", [(4, 4, [20, 31], [70, 200]), (6, 2, [20, 9], [130, 64]), (2, 2, [100, 3], [0, 300]), (3, 3, [1], [90])])
