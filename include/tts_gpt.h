@@ -502,9 +502,9 @@ int32_t tts_gpt_op_tree_tables(int32_t n, int32_t R, const int32_t *row_start, c
  * the call is given (E_ARG).  t_max: at least the largest tree (rows beyond it are not computed); with the heads of a group it decides how a tile's
  * work is spread, so that small trees go faster in a call of their own than beside large ones.  Rows of no tree are left as they were; where starts do not
  * ascend, or exceed R, nothing is written.  Heads, roundings, timing and scratch as for op_attention_shared (scratch size independent of the
- * call).  For trees of one node op_attention_shared is faster (16 streams of about 1000 tokens, 20 heads 20 us against 28), for one chain of hundreds of
- * nodes, where the cache is bf16 and heads are not grouped, op_attention_cluster -3 (256 nodes 16 us against 23); bf16 queries are faster than fp32 ones (16 trees of
- * 64 nodes 31 us against 40).  n <= 2048, mask_words <= 32. */
+ * call).  For trees of one node op_attention_shared is faster (16 streams of about 1000 tokens, 20 heads 20 us against 27), for one chain of hundreds of
+ * nodes, where the cache is bf16 and heads are not grouped, op_attention_cluster -3 (256 nodes 16 us against 22); bf16 queries are faster than fp32 ones (16 trees of
+ * 64 nodes 31 us against 34).  n <= 2048, mask_words <= 32. */
 int32_t tts_gpt_op_attention_tree_scratch_bytes(size_t *bytes);
 int32_t tts_gpt_op_attention_tree(int32_t n, int32_t R, int32_t n_head, int32_t n_kv_head, int32_t type, const void *q, int64_t q_stride, int32_t kv_fmt, int32_t n_pages,
                                   const void *kv_layer, int32_t max_streams, const int32_t *page_table, int32_t pages_per_stream, const int32_t *row_start,

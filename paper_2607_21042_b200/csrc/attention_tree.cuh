@@ -23,7 +23,7 @@
 // several CTAs share go to scratch with a ticket, and the CTA that comes last adds them in the order of their keys, so that results do not
 // depend on timing.  Every wait is bounded.
 //
-// Bound.  One tree of 8 nodes, 20 heads, 341 keys: 10.4 us, of which 4.5 pass before the first scores (tensor memory, the trees, the first copy); then come steps of
+// Bound.  One tree of 8 nodes, 20 heads, 341 keys: 9.9 us, of which 4 pass before the first scores (tensor memory, the trees, the first copy); then come steps of
 // 0.7 us, the end of a tile and the parts' joining, 3 us.  16 trees of up to 64 nodes, 20 heads, 88 MB of keys and values: 30.6 us against 14.2 of reading; steps of 0.65 to 0.8 us each,
 // of which scores to weights take most (tensor memory there and back, 2^x, the two products' latency), not bytes.  128 trees of 25 nodes by 5 heads to each of 4 heads of the
 // 8-bit cache: 64 us, the softmax warps' instructions (512 tiles of up to 125 rows); tensor cores and memory wait.
@@ -593,25 +593,39 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
       const int j0 = p.j0, steps = p.j1 - j0;
       const bool mine = i_row < p.n_i, live = 32 * rg < p.n_i;   // the thread's row exists, some row of the warp does
       float m = -INFINITY, l = 0.f;
-      if constexpr (QF32) {                    // the row's queries, as often as it stands among the lanes
-        const int r = a.by_G.of(i_row);
-        const size_t at = mine ? (size_t)(p.row0 + r) * a.q_stride + (size_t)((p.kvh - r) * a.G + i_row) * kHeadDim : 0;
-#pragma unroll 4
-        for (int e8 = 0; e8 < 8; ++e8) {
-          const int to = tid * 128 + ((e8 ^ (tid & 7)) << 4);
-          float x[8];
+      if constexpr (QF32) {                    // the tile's queries, 16 rows a turn and 8 values a thread, as often as they stand among the lanes
+        constexpr int kTileRows = 128 / S, kTurns = kTileRows / 16;
+        // Turns whose loads are under way together, as many as registers allow (us, tiles of 128, 64 rows, bf16: 8 59.7, -; 4 55.1, 35.5; 2 59.3, 38.2; 8-bit: 8 69.6, -; 4
+        // 74.4, 60.2; 2 74.1, 54.6).
+        constexpr int kAhead = !E4M3 ? (kTurns < 4 ? kTurns : 4) : S == 1 ? kTurns : 2;
+        const int e8 = tid & 7;
+#pragma unroll 1
+        for (int y0 = 0; y0 < kTurns; y0 += kAhead) {
+          float x[kAhead][8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = 0.f;
-          if (mine) load8(reinterpret_cast<const float *>(a.q) + at + 8 * e8, x);
-          uint32_t hi[4], lo[4];
+          for (int y = 0; y < kAhead; ++y) {
+            const int i = (tid >> 3) + 16 * (y0 + y), r = a.by_G.of(i);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float f0 = __uint_as_float(__float_as_uint(x[2 * e]) & 0xFFFF0000u), f1 = __uint_as_float(__float_as_uint(x[2 * e + 1]) & 0xFFFF0000u);
-            hi[e] = pack_bf16x2(f0, f1);
-            lo[e] = pack_bf16x2(x[2 * e] - f0, x[2 * e + 1] - f1);
+            for (int e = 0; e < 8; ++e) x[y][e] = 0.f;
+            if (i < p.n_i) load8(reinterpret_cast<const float *>(a.q) + (size_t)(p.row0 + r) * a.q_stride + (size_t)((p.kvh - r) * a.G + i) * kHeadDim + 8 * e8, x[y]);
           }
-          *reinterpret_cast<uint4 *>(Qs + to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4 *>(Qs + kTrRows + to) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+#pragma unroll
+          for (int y = 0; y < kAhead; ++y) {
+            const int i = (tid >> 3) + 16 * (y0 + y);
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float f0 = __uint_as_float(__float_as_uint(x[y][2 * e]) & 0xFFFF0000u), f1 = __uint_as_float(__float_as_uint(x[y][2 * e + 1]) & 0xFFFF0000u);
+              hi[e] = pack_bf16x2(f0, f1);
+              lo[e] = pack_bf16x2(x[y][2 * e] - f0, x[y][2 * e + 1] - f1);
+            }
+#pragma unroll
+            for (int z = 0; z < S; ++z) {
+              const int to = (i + z * kTileRows) * 128 + ((e8 ^ (i & 7)) << 4);
+              *reinterpret_cast<uint4 *>(Qs + to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+              *reinterpret_cast<uint4 *>(Qs + kTrRows + to) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            }
+          }
         }
         fence_proxy_async_smem();
         __syncwarp();
