@@ -714,9 +714,9 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
           float s0, s1;
           unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
           l = fmaf(l, sc, s0 + s1);
-          // this place of P is free when the product of the step before last is done; O holds still when the last one's is
-          if (c >= 2) fine = wait_warp(&sh.o_full[(c - 2) & 3], (uint32_t)((c - 2) / 4) & 1u);
-          if (b > 0 && fine && __any_sync(0xFFFFFFFFu, sc != 1.f)) {
+          // This place of P is free: the product of the step before last was issued ahead of this step's scores, by the same thread, whose commit counts all before it (a
+          // wait for it costs 3 %).  O holds still when the last step's product is done.
+          if (b > 0 && __any_sync(0xFFFFFFFFu, sc != 1.f)) {
             fine = wait_warp(&sh.o_full[(c - 1) & 3], (uint32_t)((c - 1) / 4) & 1u);
             if (!fine) break;
             tc_fence_after_sync();
@@ -729,8 +729,6 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
               tmem_st16_async(t_lane + 192u + (uint32_t)d, keep);
             }
           }
-          if (!fine) break;
-          tc_fence_after_sync();
           const uint32_t to = t_lane + 128u + 32u * turn + col0 / 2;
           if constexpr (kCols == 64) tmem_st32_async(to, w);
           else if constexpr (kCols == 32) tmem_st16_async(to, w);
