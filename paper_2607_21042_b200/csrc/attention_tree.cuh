@@ -12,8 +12,8 @@
 // Scores and weights have two places each, by turns, so that the products of a step run beside the softmax of the next: S 2 x 64, P 2 x 32, O 64 columns, 256 in
 // all, two CTAs an SM.  Where a tile has at most 64 or 32 rows, they stand S = 2 or 4 times among the 128 lanes, and each copy's threads take only their half or quarter of a
 // step's keys (their P is zero elsewhere): the exponentials, which would otherwise be one or two warps', are spread over all four, and a row's S sums meet
-// in shared memory at the end of the tile.  (S = 4, 2, 1: 16 trees of up to 32 nodes, 20 heads 26.2, 28.3, 35.3 us; 128 trees of up to 6, 5 heads to each of 4 32.6,
-// 34.2, 40.1; S = 2, 1: 64 nodes 31.0, 37.0.)
+// in shared memory at the end of the tile.  (S = 4, 2, 1: 16 trees of up to 32 nodes, 20 heads 25.7, 27.7, 33.8 us; 128 trees of up to 6, 5 heads to each of 4 32.2,
+// 33.7, 38.0; S = 2, 1: 64 nodes 29.8, 35.7.)
 //
 // Warps.  Four of softmax; one that finds the CTA's tiles, describes them to the others and copies queries and pages by TMA, four pages ahead; one that issues
 // the products, over the borders of tiles too; one that takes tickets (below).  Blocks of the 8-bit cache come as they are by bulk copies, four ahead, and two or four more warps widen the
@@ -23,10 +23,10 @@
 // several CTAs share go to scratch with a ticket, and the CTA that comes last adds them in the order of their keys, so that results do not
 // depend on timing.  Every wait is bounded.
 //
-// Bound.  One tree of 8 nodes, 20 heads, 341 keys: 9.9 us, of which 4 pass before the first scores (tensor memory, the trees, the first copy); then come steps of
-// 0.7 us, the end of a tile and the parts' joining, 3 us.  16 trees of up to 64 nodes, 20 heads, 88 MB of keys and values: 30.6 us against 14.2 of reading; steps of 0.65 to 0.8 us each,
+// Bound.  One tree of 8 nodes, 20 heads, 341 keys: 9.6 us, of which 4 pass before the first scores (tensor memory, the trees, the first copy); then come steps of
+// 0.7 us, the end of a tile and the parts' joining, 3 us.  16 trees of up to 64 nodes, 20 heads, 88 MB of keys and values: 29.4 us against 14.2 of reading; steps of 0.6 to 0.75 us each,
 // of which scores to weights take most (tensor memory there and back, 2^x, the two products' latency), not bytes.  128 trees of 25 nodes by 5 heads to each of 4 heads of the
-// 8-bit cache: 64 us, the softmax warps' instructions (512 tiles of up to 125 rows); tensor cores and memory wait.
+// 8-bit cache: 62 us, the softmax warps' instructions (512 tiles of up to 125 rows); tensor cores and memory wait.
 #pragma once
 #include "attention_common.cuh"
 #include "draft_trees.cuh"
@@ -45,7 +45,7 @@ constexpr int kTrNear = 256;                // trees up to which a CTA keeps wha
 constexpr int kTrMaxCtas = 320;
 constexpr int kTrPitch = 68;                // floats of a row's part
 constexpr float kTrSlack = 8.0f;            // log2 by which a score may exceed the reference
-constexpr int kTrCostTile = 3;              // what a tile costs besides its steps, in steps (us of 16 trees of 64 nodes by 20 heads / 128 of 25 by 5 heads to each of 4, bf16: 1, 2, 3, 5: 30.6 / 49.4, 30.4 / 46.8, 30.6 / 45.3, 31.7 / 46.8)
+constexpr int kTrCostTile = 3;              // what a tile costs besides its steps, in steps (us of 16 trees of 64 nodes by 20 heads / 128 of 25 by 5 heads to each of 4, bf16: 1, 2, 3, 4, 5: 29.1 / 47.9, 29.4 / 44.6, 29.4 / 43.2, 29.7 / 44.5, 29.9 / 44.5)
 // Parts that the copying warp may describe ahead.  Every part has a step, and no copy is more than six steps ahead of the softmax, so that it
 // never waits for a place while the softmax waits for it.
 constexpr int kTrParts = 8;
