@@ -26,7 +26,7 @@
 // Bound.  One tree of 8 nodes, 20 heads, 341 keys: 9.6 us, of which 4 pass before the first scores (tensor memory, the trees, the first copy); then come steps of
 // 0.7 us, the end of a tile and the parts' joining, 3 us.  16 trees of up to 64 nodes, 20 heads, 88 MB of keys and values: 29.4 us against 14.2 of reading; steps of 0.6 to 0.75 us each,
 // of which scores to weights take most (tensor memory there and back, 2^x, the two products' latency), not bytes.  128 trees of 25 nodes by 5 heads to each of 4 heads of the
-// 8-bit cache: 62 us, the softmax warps' instructions (512 tiles of up to 125 rows); tensor cores and memory wait.
+// 8-bit cache: 58 us, the softmax warps' instructions (512 tiles of up to 125 rows); tensor cores and memory wait.
 #pragma once
 #include "attention_common.cuh"
 #include "draft_trees.cuh"
@@ -106,8 +106,9 @@ template <int S, bool E4M3> struct TreeShape {
   static constexpr int kCopyWarp = 4, kMmaWarp = 5, kWidenWarp = S == 1 ? 6 : 8, kWidenWarps = !E4M3 ? 0 : S == 1 ? 2 : 4;
   static constexpr bool kTicketWarp = S > 1;  // warp 6 takes the first tile's tickets; else the copying warp does
   static constexpr int kThreads = !E4M3 ? (S == 1 ? 192 : 224) : S == 1 ? 256 : 384;
-  // 8-bit cache: registers of a thread, which the groups of four warps split anew; at launch each has 128 or 80
-  static constexpr int kRegsLaunch = S == 1 ? 128 : 80, kRegsSoftmax = S == 1 ? 168 : 120, kRegsCopy = S == 1 ? 88 : 64, kRegsWiden = S == 1 ? 0 : 56;
+  // 8-bit cache: registers of a thread, which the groups of four warps split anew; at launch each has 128 or 80 (tiles of 128 rows: softmax 168, 176, 184, 192, 200: 62.4, 61.1, 58.5,
+  // 59.6, 59.6 us; of 64: 120, 136: 45.6, 45.0)
+  static constexpr int kRegsLaunch = S == 1 ? 128 : 80, kRegsSoftmax = S == 1 ? 184 : 136, kRegsCopy = S == 1 ? 72 : 56, kRegsWiden = S == 1 ? 0 : 48;
   static_assert(kRegsSoftmax + kRegsCopy + kRegsWiden <= kRegsLaunch * (S == 1 ? 2 : 3), "a split of more registers than the launch has would wait forever");
   static constexpr int kCtas = 2;            // an SM
   static constexpr int kRing = E4M3 ? 2 : 4; // pages of K and of V as the tensor cores take them
