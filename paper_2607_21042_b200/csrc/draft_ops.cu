@@ -121,7 +121,7 @@ int32_t tts_gpt_op_rope_kv_append(int32_t R, int32_t n_head, int32_t n_kv_head, 
   a.row_pos = row_pos; a.row_slot = row_slot; a.turns = (const unsigned long long *)turns; a.q_out = q_out; a.pool = (unsigned char *)kv_layer;
   a.R = R; a.H = n_head; a.K = n_kv_head; a.pairs = n_rot / 2; a.n_slots = n_pages * kPageTokens;
   a.out_f32 = out_type == TTS_GPT_T_F32; a.magnitude = magnitude;
-  OP_TRY(launch_rope(a, type == TTS_GPT_T_F32, kv_fmt == TTS_GPT_KV_FP8_E4M3, interleaved != 0, (cudaStream_t)cuda_stream));
+  OP_TRY(launch_rope(a, type == TTS_GPT_T_F32, kv_fmt == TTS_GPT_KV_FP8_E4M3, interleaved != 0, device_sms(), (cudaStream_t)cuda_stream));
   return TTS_GPT_OK;
 }
 

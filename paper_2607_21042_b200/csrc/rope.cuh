@@ -13,17 +13,16 @@
 // values apart, a thread's are those of four or eight pairs, so that no lane asks another.  A CTA takes as many (row, head) pieces at once as it has such groups
 // of lanes, in rows as wide as a power of two that holds the heads, and computes its rows' sines and cosines once for all heads while the values are under way.
 // Bound: bytes in and out.  Measured: 16 fp32 rows of 20 heads 2.0 us (a launch), 3584 of them 15.2 us (5.4 TB/s; 21.4 with eight lanes a head that exchange halves by
-// shuffles), 777 bf16 rows of 20 + 4 + 4 heads into the 8-bit cache 2.8 us, 3584 bf16 rows of 60 heads 16.6 us (17.4 with 8 bytes a time; CTAs that stay for more
-// rows and load the next ahead: 16.4, and 18.7 instead of 15.7 from fp32).  CTAs an SM by registers: one more or less costs 3 to 7 %.
+// shuffles), 777 bf16 rows of 20 + 4 + 4 heads into the 8-bit cache 2.8 us, 3584 bf16 rows of 60 heads 13.3 us (in CTAs of 256 threads 16.0, with 8 bytes a time 17.4; CTAs that stay
+// for more rows and load the next ahead: no faster, and 18.7 instead of 15.7 from fp32).  CTAs an SM by registers: one more or less costs 3 to 7 %.
 #pragma once
 #include "attention_common.cuh"
 #include "page_tables.cuh"
 
 namespace ttsgpt {
 
-constexpr int kRopeThreads = 256;
-template <typename Src> struct RopeShape {
-  static constexpr int kVals = 16 / sizeof(Src), kLanes = kHeadDim / (2 * kVals), kSlots = kRopeThreads / kLanes;   // (row, head) pieces of a CTA
+template <typename Src, int THREADS> struct RopeShape {
+  static constexpr int kVals = 16 / sizeof(Src), kLanes = kHeadDim / (2 * kVals), kSlots = THREADS / kLanes;   // (row, head) pieces of a CTA
   static constexpr int kPer = sizeof(Src) == 4 ? 2 : 1;   // of a thread under way at once, where a row has more heads
   static constexpr int kRows = kSlots / 2;     // of a CTA at most
 };
@@ -80,11 +79,14 @@ template <int N> __device__ __forceinline__ void store_e4m3(unsigned char *p, co
   else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
 }
 
-template <typename Src, bool E4M3, int ORDER> __host__ __device__ constexpr int rope_ctas() { return ORDER == ROPE_HALF ? (sizeof(Src) == 2 ? 2 : 3) : sizeof(Src) == 2 ? 3 : E4M3 ? 4 : 5; }   // of an SM
+// CTAs an SM by registers
+template <typename Src, bool E4M3, int ORDER, int THREADS> __host__ __device__ constexpr int rope_ctas() {
+  return 256 / THREADS * (ORDER == ROPE_HALF ? (sizeof(Src) == 2 ? 2 : 3) : sizeof(Src) == 2 ? 3 : E4M3 ? 4 : 5);
+}
 
-template <typename Src, bool E4M3, int ORDER>
-__global__ void __launch_bounds__(kRopeThreads, rope_ctas<Src, E4M3, ORDER>()) rope_kv_append_kernel(const RopeArgs a) {
-  using Shape = RopeShape<Src>;
+template <typename Src, bool E4M3, int ORDER, int THREADS>
+__global__ void __launch_bounds__(THREADS, rope_ctas<Src, E4M3, ORDER, THREADS>()) rope_kv_append_kernel(const RopeArgs a) {
+  using Shape = RopeShape<Src, THREADS>;
   constexpr int kVals = Shape::kVals, kLanes = Shape::kLanes, kSlots = Shape::kSlots, kPer = Shape::kPer;
   __shared__ __align__(16) float cos_s[Shape::kRows][kHeadDim / 2], sin_s[Shape::kRows][kHeadDim / 2];   // by pair
   pdl_launch_dependents();
@@ -116,7 +118,7 @@ __global__ void __launch_bounds__(kRopeThreads, rope_ctas<Src, E4M3, ORDER>()) r
   };
   load(0);
   const int slot = r < a.R ? a.row_slot[r] : -1;
-  for (int i = tid; i < rows * a.pairs; i += kRopeThreads) {   // beside the loads
+  for (int i = tid; i < rows * a.pairs; i += THREADS) {   // beside the loads
     const int k = i / a.pairs, j = i - k * a.pairs;
     if (row0 + k >= a.R) break;
     const float2 cs = cos_sin_of_phase((unsigned long long)(long long)a.row_pos[row0 + k] * a.turns[j]);
@@ -239,17 +241,31 @@ __global__ void __launch_bounds__(kRopeThreads, rope_ctas<Src, E4M3, ORDER>()) r
   }
 }
 
-template <typename Src, bool E4M3>
-inline cudaError_t launch_rope_as(const RopeArgs &a, bool neighbours, cudaStream_t st) {
-  const dim3 grid((unsigned)((a.R - 1) / (RopeShape<Src>::kSlots >> a.lg) + 1)), block(kRopeThreads);
-  if (neighbours) return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_NEIGHBOURS>, grid, block, 0, st, true, a);
-  if (a.pairs % RopeShape<Src>::kVals == 0) return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_HALVES>, grid, block, 0, st, true, a);
-  return launch_kernel(rope_kv_append_kernel<Src, E4M3, ROPE_HALF>, grid, block, 0, st, true, a);
+template <typename Src, bool E4M3, int ORDER, int THREADS>
+inline cudaError_t launch_rope_with(RopeArgs a, cudaStream_t st) {
+  constexpr int kSlots = RopeShape<Src, THREADS>::kSlots;
+  for (a.lg = 1; (1 << a.lg) < kSlots && (1 << a.lg) < a.H + 2 * a.K;) ++a.lg;
+  return launch_kernel(rope_kv_append_kernel<Src, E4M3, ORDER, THREADS>, dim3((unsigned)((a.R - 1) / (kSlots >> a.lg) + 1)), dim3(THREADS), 0, st, true, a);
 }
-inline cudaError_t launch_rope(RopeArgs a, bool src_f32, bool e4m3, bool neighbours, cudaStream_t st) {
-  for (a.lg = 1; (1 << a.lg) < (src_f32 ? RopeShape<float>::kSlots : RopeShape<uint16_t>::kSlots) && (1 << a.lg) < a.H + 2 * a.K;) ++a.lg;
-  if (src_f32) return e4m3 ? launch_rope_as<float, true>(a, neighbours, st) : launch_rope_as<float, false>(a, neighbours, st);
-  return e4m3 ? launch_rope_as<uint16_t, true>(a, neighbours, st) : launch_rope_as<uint16_t, false>(a, neighbours, st);
+// CTAs of 256 threads have the shortest way through a row, CTAs of 128 wait less for one another where there are more than fit at once (3584 rows: of 60 bf16 heads 16.0 against 13.2 us,
+// of 60 fp32 heads into the 8-bit cache 20.1, 18.5, 30 values rotated 27.8, 23.5; 16 fp32 rows 2.0, 2.6), but not where fp32 goes to 16 bits (60 heads 15.2, 15.0; 12 heads 5.0, 5.5).
+template <typename Src, bool E4M3, int ORDER>
+inline cudaError_t launch_rope_in(const RopeArgs &a, int n_sm, cudaStream_t st) {
+  if constexpr (sizeof(Src) == 2 || E4M3 || ORDER == ROPE_HALF) {
+    const long long pieces = (long long)a.R * (a.H + 2 * a.K);
+    if (pieces > (long long)rope_ctas<Src, E4M3, ORDER, 256>() * n_sm * RopeShape<Src, 256>::kSlots) return launch_rope_with<Src, E4M3, ORDER, 128>(a, st);
+  }
+  return launch_rope_with<Src, E4M3, ORDER, 256>(a, st);
+}
+template <typename Src, bool E4M3>
+inline cudaError_t launch_rope_as(const RopeArgs &a, bool neighbours, int n_sm, cudaStream_t st) {
+  if (neighbours) return launch_rope_in<Src, E4M3, ROPE_NEIGHBOURS>(a, n_sm, st);
+  if (a.pairs % (16 / sizeof(Src)) == 0) return launch_rope_in<Src, E4M3, ROPE_HALVES>(a, n_sm, st);
+  return launch_rope_in<Src, E4M3, ROPE_HALF>(a, n_sm, st);
+}
+inline cudaError_t launch_rope(const RopeArgs &a, bool src_f32, bool e4m3, bool neighbours, int n_sm, cudaStream_t st) {
+  if (src_f32) return e4m3 ? launch_rope_as<float, true>(a, neighbours, n_sm, st) : launch_rope_as<float, false>(a, neighbours, n_sm, st);
+  return e4m3 ? launch_rope_as<uint16_t, true>(a, neighbours, n_sm, st) : launch_rope_as<uint16_t, false>(a, neighbours, n_sm, st);
 }
 
 }  // namespace ttsgpt

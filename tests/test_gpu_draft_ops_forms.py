@@ -211,6 +211,28 @@ def test_calls_on_a_stream_that_is_not_the_current_one():
 # ---------------------------------------------------------------------------------------------
 # forms of the arguments
 # ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("H,K", [(12, 4), (0, 12), (40, 40)])
+@pytest.mark.parametrize("src", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n_rot,interleaved", [(64, False), (30, False), (62, True)])
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_rope_of_a_large_pass_is_that_of_its_parts(fmt, n_rot, interleaved, src, H, K):
+    """More rows than CTAs of the other size have place for: bit for bit what calls of 100 rows give."""
+    g, rows = _gen(n_rot + H), 30000 // (H + 2 * K) * 2 + 77
+    pages = (rows + 63) // 64 + 1
+    q, k, v = torch.randn(rows, (H + 2 * K) * 64, generator=g).to(src).to(DEV).split([H * 64, K * 64, K * 64], 1)
+    slot = torch.randperm(pages * 64, generator=g)[:rows].to(torch.int32)
+    slot[::17] = -1
+    slot, pos = slot.to(DEV), torch.randint(-10 ** 6, 10 ** 6, (rows,), generator=g, dtype=torch.int32).to(DEV)
+    turns, _ = B.op_rope_frequencies(n_rot, device=DEV)
+    pools, outs = [_empty_pool(fmt, pages, K) for _ in range(2)], [torch.full((rows, H * 64), 5.0, dtype=src, device=DEV) if H else None for _ in range(2)]
+    for pool, out, step in zip(pools, outs, (rows, 100)):
+        for i in range(0, rows, step):
+            s = slice(i, i + step)
+            B.op_rope_kv_append(q[s] if H else None, k[s], v[s], pool, slot[s], pos[s], turns, interleaved=interleaved, q_out=out[s] if H else None)
+    assert torch.equal(pools[0].view(torch.uint8), pools[1].view(torch.uint8))
+    assert not H or torch.equal(outs[0], outs[1]) and torch.all(outs[0][::17] == 5.0) and not torch.any((outs[0] == 5.0).all(-1)[torch.arange(rows) % 17 != 0])
+
+
 @pytest.mark.parametrize("src", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("n_rot", [64, 30])
