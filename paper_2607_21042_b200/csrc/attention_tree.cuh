@@ -131,11 +131,12 @@ __device__ __forceinline__ void tmem_st16_async(uint32_t taddr, const float *v) 
                ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]),
                "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]) : "memory");
 }
-// has the phase ended?  (does not suspend the thread, as mbar_try_wait may)
-__device__ __forceinline__ bool mbar_test_wait(uint64_t *bar, uint32_t parity) {
+// Has the phase ended?  (Does not suspend the thread, as mbar_try_wait may.)  The whole warp asks and has one answer: lanes that look at a barrier while
+// others arrive may see different things, and what follows has votes of all lanes in it.
+__device__ __forceinline__ bool mbar_test_warp(uint64_t *bar, uint32_t parity) {
   uint32_t done;
   asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(smem_u32(bar)), "r"(parity) : "memory");
-  return done != 0;
+  return __any_sync(0xFFFFFFFFu, done != 0);
 }
 __device__ __forceinline__ void fence_gpu() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
 
@@ -238,7 +239,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
   const uint32_t tmem = sh.tmem;
   pdl_launch_dependents();                     // the CTA has its tensor memory: the next kernel can take none from under it
   const Div size = sh.size;
-  const int u_begin = blockIdx.x * (int)size.d, u_end = *failed ? u_begin : min(T, u_begin + (int)size.d);
+  const int u_begin = blockIdx.x * (int)size.d, u_end = __any_sync(0xFFFFFFFFu, *failed) ? u_begin : min(T, u_begin + (int)size.d);   // one for the warp: part_at votes
 
   // The part at unit u or behind it that this CTA has pages of; false: there is none.  Tiles without keys get their zeros here.
   auto part_at = [&](int u, TreePart &p) {
@@ -465,7 +466,7 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
           }
         }
         __syncwarp();
-        if (due >= 0 && mbar_test_wait(&sh.written, 0)) { fine = tickets(due) && fine; due = -1; }
+        if (due >= 0 && mbar_test_warp(&sh.written, 0)) { fine = tickets(due) && fine; due = -1; }
       }
     }
     if (due >= 0) tickets(due);
