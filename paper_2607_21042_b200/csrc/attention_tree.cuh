@@ -100,6 +100,12 @@ struct alignas(16) TreeShared {
   int warp_tot[16], top_cost;   // ... and the most that a tile costs
 };
 
+// The tile whose sums may still stand in the place of V that page `i` (from 0 on) of part n_part takes, where there are four places; -1: none.  A tile's sums meet in the
+// places of its last page and of the one before, which are those of the next part's fourth and third page: the third waits for both.  Older tiles have left: the part's
+// queries are copied behind the end of the tile two before.  To wait for one of those could go wrong, because its barrier serves every second tile: when the next
+// of these has left too, the phase that is asked for looks as if it had not ended.
+__host__ __device__ constexpr int tree_tile_in_place(int n_part, int i) { return i == 2 ? n_part - 1 : -1; }
+
 template <int S, bool E4M3> struct TreeShape {
   // warps 0-3: softmax, 4: copies, 5: products; 8-bit cache: codes to bf16, two warps (6, 7) where the softmax takes longer than they do, or four (8-11; 6
   // and 7 only give up their registers)
@@ -404,7 +410,6 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
     TreePart p;
     int u = u_begin;
     int due = -1;                              // first CTA of the first tile, where its tickets are to be taken here
-    unsigned long long ended = 0;              // of each place of V, 16 bits: 1 + the tile whose sums meet there (modulo 2^15; one of the last six)
 #pragma unroll 1
     for (int n_part = 0; fine; ++n_part) {
       const bool there = part_at(u, p);
@@ -450,14 +455,9 @@ __global__ void __launch_bounds__(TreeShape<S, E4M3>::kThreads, TreeShape<S, E4M
           }
           __syncwarp();
           if (c >= 4) fine = wait_warp(&sh.o_full[s], (uint32_t)(c / 4 - 1) & 1u);
-          if (S > 1 && !QF32) {                // is there a tile whose sums meet in this place?
-            const int tile = (int)(ended >> (16 * s) & 0xFFFF) - 1;
+          if (S > 1 && !QF32) {
+            const int tile = tree_tile_in_place(n_part, j - p.j0);
             if (tile >= 0 && fine) fine = wait_warp(&sh.q_free[tile & 1], (uint32_t)(tile / 2) & 1u);
-            ended &= ~(0xFFFFull << (16 * s));
-            if (j + 1 == p.j1) {               // the sums of this one meet here and where the page before was
-              const unsigned long long mark = (unsigned long long)((n_part & 0x7FFF) + 1), before = (unsigned)(c - 1) & 3u;
-              ended = (ended & ~(0xFFFFull << (16 * before))) | mark << (16 * s) | mark << (16 * before);
-            }
           }
           if (!fine) break;
           if (elect_one()) {
