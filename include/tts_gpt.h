@@ -518,8 +518,9 @@ int32_t tts_gpt_op_attention_tree(int32_t n, int32_t R, int32_t n_head, int32_t 
  * call, a list's last page first (they stay in the page list, where op_page_tables overwrites them).  kv_len_out and free_top_out may be kv_len and free_top; nothing else may overlap an
  * output (E_ARG).  info: int32 [8], zero before its first use: {status, accepted nodes, pages returned, height of the stack, ...}; status E_ARG (starts, parents, fewer
  * tokens than nodes, a height outside 0..n_pages, more pages than the stack has places), E_STREAM (an id outside 0..max_streams-1, or twice), E_CTX_OVERFLOW (more tokens
- * than pages_per_stream pages hold), E_WORKSPACE (more than 256 nodes): then lengths, stack and height are left as they were, a tree with wrong parents or too many nodes accepts
- * nothing, and the others' paths are written.  n <= 4096, max_streams and pages_per_stream <= 32768.  Two calls that share info or update the same
+ * than pages_per_stream pages hold), E_WORKSPACE (more than 256 nodes): then lengths, stack and height are left as they were, and path is -1 in the rows of all trees, so that
+ * op_kv_move moves nothing behind such a call; n_accepted and next_token are 0 and -1 of a tree with wrong starts, wrong parents or too many nodes, and of the others what they would
+ * have been.  n <= 4096, max_streams and pages_per_stream <= 32768.  Two calls that share info or update the same
  * streams must be ordered. */
 int32_t tts_gpt_op_tree_accept(int32_t n, int32_t R, const int32_t *row_start, const int32_t *stream_ids, const int32_t *draft, const int32_t *target, const int32_t *parent,
                                int32_t max_streams, const int32_t *kv_len, int32_t *kv_len_out, const int32_t *page_table, int32_t pages_per_stream, int32_t n_pages,

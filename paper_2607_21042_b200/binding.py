@@ -788,7 +788,8 @@ def op_tree_accept(draft, target, parent, row_start, kv_len, page_table, free_pa
                    free_top_out=None, stream=None):
     """The path from node 0 through children whose drafted token is the model's (target, by row) after their parent; everything int32 on one device, written in
     place: path [R] (rows of accepted nodes at the head of the tree's rows, then -1), n_accepted and next_token by tree, the streams' lengths without the other nodes
-    (kv_len_out, None: kv_len), and unused pages back onto the stack (free_pages, free_top_out, None: free_top).  info: 8 values, zero at first; info[0] is the status."""
+    (kv_len_out, None: kv_len), and unused pages back onto the stack (free_pages, free_top_out, None: free_top).  info: 8 values, zero at first; info[0] is the status:
+    where it is not 0, path is -1 in all trees' rows and lengths and stack are as they were."""
     d, R = draft.get_device(), draft.numel()
     n, ids = _trees(d, row_start, stream_ids, kv_len)
     if kv_len_out is None:

@@ -91,7 +91,8 @@ inline cudaError_t launch_tree_tables(const TreeTableArgs &a, cudaStream_t st) {
 // ---------------------------------------------------------------------------------------------
 // Acceptance.  From node 0 on, the first child whose drafted token is what the model says after its parent, as long as there is one: every node's first such
 // child is found at once (a minimum in shared memory), then a path is a walk along them.  A warp a tree.  One CTA then takes the streams' lengths back to the
-// accepted nodes and returns the pages behind them: request by request in the order of the call, the last page of a list first.  It is the only one up to 32
+// accepted nodes and returns the pages behind them: request by request in the order of the call, the last page of a list first; or, where something is wrong, takes all
+// paths back.  It is the only one up to 32
 // trees, the first of a cluster up to 256, which finds the others' counts in their shared memory, and else the one that comes last.
 // Bound: launch, two dependent reads, two sums over the requests and a read of the pages.  Measured: 16 trees of up to 40 nodes 4.9 us, 128 of up to 200 7.1 us
 // (8.0 and 12.5 with a search of the children at every step of the path, 256 threads and tickets; 7.1 and 11.6 with parents and tokens in registers).
@@ -268,6 +269,14 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) tree_accept_kernel(const Tr
       freed_all = carry;
       accepted = __reduce_add_sync(0xFFFFFFFFu, acc_s[lane]);
       if (bad_s) break;
+    }
+  }
+  if (bad_s) {   // nothing is accepted: no path is left, not this call's nor what stood there, so that moves behind it move nothing
+#pragma unroll 1
+    for (int x = warp; x < a.n; x += kAcceptWarps) {
+      const int r0 = max(a.row_start[x], 0), r1 = min(max(a.row_start[x + 1], 0), a.R);   // starts may be anything
+#pragma unroll 1
+      for (unsigned k = lane; k < (unsigned)max(r1 - r0, 0); k += 32) a.path[r0 + k] = -1;
     }
   }
   if (tid == 0) {

@@ -5,7 +5,7 @@ import torch
 
 from paper_2607_21042_b200 import binding as B
 from test_gpu_draft_ops import Drafts, _forest, _masks, _sees
-from test_gpu_serving_ops import HALF, _bound, _check
+from test_gpu_serving_ops import HALF, _bound, _check, _gen, _i32
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -58,3 +58,54 @@ def test_tiles_of_few_pages(fmt, dtype, t, H, K, ctx):
         else:
             _check_tree(d, i, out[0], q, sees[i])
     assert torch.all(out[0][d.start[-1]:] == 9.0)
+
+
+# ---------------------------------------------------------------------------------------------
+# acceptance that is refused, and what follows it
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n", [3, 40, 300])
+@pytest.mark.parametrize("code,what", [(B.E_ARG, "parent"), (B.E_ARG, "short"), (B.E_STREAM, "stream"), (B.E_STREAM, "twice"), (B.E_CTX_OVERFLOW, "long"), (B.E_WORKSPACE, "nodes"),
+                                       (B.E_ARG, "height"), (B.E_ARG, "places"), (B.E_ARG, "starts"), (B.E_ARG, "end")])
+def test_a_refused_acceptance_leaves_no_path(code, what, n):
+    """Rows of trees that a step before would have moved: behind a refused call there is no path, and the same step's moves leave the cache as it is."""
+    lens = [4] * n
+    if what == "nodes":
+        lens[1] = 257
+    start, parent = _forest(1, lens)
+    ids, kv, top, places, R = list(range(n)), [66] * n, 3, 3 + n, sum(lens) + 2
+    path = np.full(R, -9)
+    for a, b in zip(start[:-1], start[1:]):
+        path[a:b - 1], path[b - 1] = np.arange(a + 1, b), -1       # every row to the place before
+    if what == "nodes":
+        kv[1] = 257 + 62
+    if what == "parent":
+        parent[4 + 2] = 2
+    if what == "short":
+        kv[1] = 3
+    if what == "stream":
+        ids[1] = n
+    if what == "twice":
+        ids[1] = 0
+    if what == "long":
+        kv[1] = 8 * 64 + 1
+    if what == "height":
+        top = places + 1
+    if what == "places":                       # some pages come back, for which there is no place
+        places = top
+    if what == "starts":
+        start[2] = 3
+    if what == "end":
+        start[n] += 3
+    pages = (R + 63) // 64
+    pool = torch.randint(0, 255, (2, pages, 2, 3, 8192), generator=_gen(1), dtype=torch.uint8).to(DEV).view(torch.bfloat16).unflatten(-1, (64, 64))
+    before, slot = pool.clone(), torch.randperm(pages * 64, generator=_gen(2))[:R].to(torch.int32).to(DEV)
+    start_d, path_d, kv_d, free, top_d = _i32(start.tolist()), _i32(path.tolist()), _i32(kv), _i32([0] * places), _i32([top])
+    acc, nxt, info = _i32([-9] * n), _i32([-9] * n), _i32([0] * 8)
+    # every drafted token agrees with what is said after its parent, so that other trees have paths that move
+    B.op_tree_accept(_i32([1] * R), _i32([1] * R), _i32(parent.tolist() + [0, 0]), start_d, kv_d, torch.arange(8 * n, dtype=torch.int32, device=DEV).view(n, 8), free, top_d, path_d, acc, nxt,
+                     info, stream_ids=_i32(ids))
+    B.op_kv_move(pool, start_d, path_d, slot)
+    assert info.tolist() == [code, 0, 0, top, 0, 0, 0, 0] and kv_d.tolist() == kv and top_d.item() == top and not free.any()
+    last = min(int(start[n]), R)
+    assert torch.all(path_d[:last] == -1) and torch.all(path_d[last:] == -9)
+    assert torch.equal(pool.view(torch.int16), before.view(torch.int16))
