@@ -528,7 +528,7 @@ int32_t tts_gpt_op_tree_accept(int32_t n, int32_t R, const int32_t *row_start, c
                                void *cuda_stream);
 
 /* K and V of accepted nodes to where they belong, in n_layers layers (their pools layer_bytes apart, a multiple of 16): the k-th row of
- * path[row_start[i] ..], which ascends and ends at the first -1, from its slot row_slot[row] to the slot of row row_start[i] + k.  Codes and scales move as they are.  A row
+ * path[row_start[i] ..], which ascends and ends at the first -1 (or other negative number; what stands behind it does not matter), from its slot row_slot[row] to the slot of row row_start[i] + k.  Codes and scales move as they are.  A row
  * that is where it belongs stays; a row whose slot, or the slot that it should go to, lies outside the pool is left out.  Slots must be distinct. */
 int32_t tts_gpt_op_kv_move(int32_t n, int32_t R, const int32_t *row_start, const int32_t *path, const int32_t *row_slot, int32_t n_kv_head, int32_t kv_fmt, int32_t n_pages,
                            int32_t n_layers, int64_t layer_bytes, void *kv_layers, void *cuda_stream);

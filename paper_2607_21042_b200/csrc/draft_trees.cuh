@@ -328,26 +328,32 @@ constexpr int kMoveMaxThreads = 512, kMoveBatch = 8;
 template <bool E4M3>
 __global__ void __launch_bounds__(kMoveMaxThreads) kv_move_kernel(const KvMoveArgs a) {
   __shared__ int2 move_s[kMoveMaxThreads];     // {from, to}, slots
-  __shared__ int warp_s[kMoveMaxThreads / 32];
+  __shared__ int2 warp_s[kMoveMaxThreads / 32];   // {rows that move, does the path end}
   pdl_launch_dependents();
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
   int first, n;
   if (!tree_rows(a.row_start, blockIdx.x, a.R, first, n)) return;
   unsigned char *pool = a.pool + (size_t)blockIdx.y * a.layer_bytes;
-  bool more = true;
+  bool more = true;                            // the path has not ended
 #pragma unroll 1
   for (int k0 = 0; k0 < n && more; k0 += threads) {
     const int k = k0 + tid, r = k < n ? a.path[first + k] : -1;
-    const bool on = k < n && r > first + k && r < first + n;     // a row that is where it belongs stays
+    const unsigned ends = __ballot_sync(0xFFFFFFFFu, r < 0);
+    const bool on = r > first + k && r < first + n && (ends & ((1u << lane) - 1)) == 0;   // a row that is where it belongs stays; nothing behind an end moves
     const int from = on ? a.row_slot[r] : -1, to = on ? a.row_slot[first + k] : -1;
-    const bool moves = from >= 0 && from < a.n_slots && to >= 0 && to < a.n_slots;
+    bool moves = from >= 0 && from < a.n_slots && to >= 0 && to < a.n_slots;
     const unsigned votes = __ballot_sync(0xFFFFFFFFu, moves);
-    if (lane == 0) warp_s[warp] = __popc(votes);
-    more = __syncthreads_or(k < n && r >= 0);  // nothing behind a path's end
+    if (lane == 0) warp_s[warp] = make_int2(__popc(votes), ends != 0);
+    __syncthreads();
     int at = __popc(votes & ((1u << lane) - 1)), count = 0;
 #pragma unroll 1
-    for (int w = 0; w < threads / 32; ++w) { const int x = warp_s[w]; if (w < warp) at += x; count += x; }
+    for (int w = 0; w < threads / 32 && more; ++w) {
+      const int2 x = warp_s[w];
+      if (w < warp) { at += x.x; moves = moves && !x.y; }
+      count += x.x;
+      more = !x.y;
+    }
     if (moves) move_s[at] = make_int2(from, to);
     __syncthreads();
     constexpr int kLanes = E4M3 ? 4 : 8;       // 16-byte pieces of a row

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2607_21042_b200 import binding as B
-from test_gpu_draft_ops import Drafts, _forest, _masks, _sees
+from test_gpu_draft_ops import E4M3_BLOCK, Drafts, _forest, _masks, _sees
 from test_gpu_serving_ops import HALF, _bound, _check, _gen, _i32
 
 pytestmark = pytest.mark.gpu
@@ -109,3 +109,31 @@ def test_a_refused_acceptance_leaves_no_path(code, what, n):
     last = min(int(start[n]), R)
     assert torch.all(path_d[:last] == -1) and torch.all(path_d[last:] == -9)
     assert torch.equal(pool.view(torch.int16), before.view(torch.int16))
+
+
+# ---------------------------------------------------------------------------------------------
+# moves
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt,heads,lens,ends", [(0, 1, [9], [1]), (0, 20, [9, 30, 64], [1, 29, 0]), (1, 1, [130, 200, 3], [1, 64, 0]), (1, 20, [300, 257], [63, 161]), (0, 4, [700, 2], [65, 1]),
+                                                 (0, 40, [700, 600], [513, 511])])
+def test_a_path_ends_at_its_first_hole(fmt, heads, lens, ends):
+    """Whatever stands behind the first -1 (or another negative number), in the same reach of a CTA's threads or a later one, moves nothing."""
+    start = np.concatenate([[0], np.cumsum(lens)])
+    R = int(start[-1])
+    pages = (R + 63) // 64 + 1
+    path = np.full(R, -1)
+    for i, (t, end) in enumerate(zip(lens, ends)):
+        path[start[i]:start[i + 1] - 1] = np.arange(start[i] + 1, start[i + 1])      # all rows one place on
+        path[start[i] + end] = -1 - 5 * (i % 2)
+    slot = np.random.default_rng(3).permutation(pages * 64)[:R]
+    pool = torch.randint(0, 255, (pages, 2, heads, E4M3_BLOCK if fmt else 8192), generator=_gen(1), dtype=torch.uint8).to(DEV)
+    want = pool.clone()
+    views = (lambda x: [x[..., :4096].unflatten(-1, (64, 64)), x[..., 4096:].unflatten(-1, (64, 4))]) if fmt else (lambda x: [x.unflatten(-1, (64, 128))])  # noqa: E731
+    for v in views(want):
+        old = v.clone()
+        for i, end in enumerate(ends):
+            for k in range(min(end, lens[i] - 1)):
+                a, b = slot[path[start[i] + k]], slot[start[i] + k]
+                v[b // 64, :, :, b % 64] = old[a // 64, :, :, a % 64]
+    B.op_kv_move(pool if fmt else pool.view(torch.bfloat16).unflatten(-1, (64, 64)), _i32(start.tolist()), _i32(path.tolist()), _i32(slot.tolist()))
+    assert torch.equal(pool, want)
