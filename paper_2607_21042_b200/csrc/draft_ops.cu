@@ -12,7 +12,7 @@ using namespace ttsgpt;
 
 namespace {
 
-constexpr double kTwoPi = 6.283185307179586476925286766559;
+constexpr long double kTwoPi = 6.28318530717958647692528676655900576839L;
 
 // Do rows of `wa` bytes, `sa` apart, share a byte with others?  Rows of the same distance may lie side by side, as parts of one array.
 bool rows_overlap(const void *pa, long long na, long long wa, long long sa, const void *pb, long long nb, long long wb, long long sb) {
@@ -56,29 +56,32 @@ int32_t tts_gpt_op_rope_frequencies(int32_t n_rot, int32_t scaling, double base,
       !(std::isfinite(original) && original > 0.0 && std::isfinite(low) && std::isfinite(high) && low > 0.0 && high > low))
     return fail_op(TTS_GPT_E_ARG, "op_rope_frequencies: original must be positive, and 0 < low < high");
   if (scaling == TTS_GPT_ROPE_NTK && n_rot < 4) return fail_op(TTS_GPT_E_ARG, "op_rope_frequencies: a base can be raised for 4 values or more");
+  // In long double, whose last place is 2^-64 of a value: in double a frequency is off by 2^-53 of itself, some 200 units of the table.
   const int n = n_rot / 2;
-  if (scaling == TTS_GPT_ROPE_NTK) base *= std::pow(factor, (double)n_rot / (n_rot - 2));
-  double first = 0.0, last = 0.0;              // of the pairs between which yarn blends
+  const long double stretch = factor;
+  long double from = base;
+  if (scaling == TTS_GPT_ROPE_NTK) from *= std::pow(stretch, (long double)n_rot / (n_rot - 2));
+  double first = 0.0, last = 0.0;              // of the pairs between which yarn blends: whole numbers
   if (scaling == TTS_GPT_ROPE_YARN) {
-    auto pair_of = [&](double rotations) { return n_rot * std::log(original / (rotations * kTwoPi)) / (2.0 * std::log(base)); };   // that turns so often
+    auto pair_of = [&](double rotations) { return n_rot * std::log(original / (rotations * (double)kTwoPi)) / (2.0 * std::log(base)); };   // that turns so often
     first = std::max(std::floor(pair_of(high)), 0.0);
     last = std::min(std::ceil(pair_of(low)), (double)n_rot - 1.0);
     if (last - first < 0.001) last = first + 0.001;
   }
   for (int i = 0; i < n; ++i) {
-    double w = scaling == TTS_GPT_ROPE_GIVEN ? inv_freq[i] : std::pow(base, -2.0 * i / n_rot);
-    if (scaling == TTS_GPT_ROPE_LINEAR) w /= factor;
+    long double w = scaling == TTS_GPT_ROPE_GIVEN ? (long double)inv_freq[i] : std::pow(from, -2.0L * i / n_rot);
+    if (scaling == TTS_GPT_ROPE_LINEAR) w /= stretch;
     if (scaling == TTS_GPT_ROPE_YARN) {
-      const double slow = std::min(std::max((i - first) / (last - first), 0.0), 1.0);
-      w = w / factor * slow + w * (1.0 - slow);
+      const long double slow = std::min(std::max(((long double)i - first) / ((long double)last - first), 0.0L), 1.0L);
+      w = w / stretch * slow + w * (1.0L - slow);
     }
     if (scaling == TTS_GPT_ROPE_BANDS) {
-      const double rotations = original * w / kTwoPi;
-      const double fast = std::min(std::max((rotations - low) / (high - low), 0.0), 1.0);   // 0: slow, divided; 1: fast, as it is
-      w = w / factor * (1.0 - fast) + w * fast;
+      const long double rotations = original * w / kTwoPi;
+      const long double fast = std::min(std::max((rotations - low) / ((long double)high - low), 0.0L), 1.0L);   // 0: slow, divided; 1: fast, as it is
+      w = w / stretch * (1.0L - fast) + w * fast;
     }
     if (!std::isfinite(w)) return fail_op(TTS_GPT_E_ARG, "op_rope_frequencies: frequency %d is not finite", i);
-    const long double t = (long double)w / (2.0L * 3.14159265358979323846264338327950288L), part = t - std::floor(t);   // turns a position, modulo one
+    const long double t = w / kTwoPi, part = t - std::floor(t);   // turns a position, modulo one
     turns[i] = part >= 1.0L - 0x1p-64L ? 0u : (uint64_t)std::ldexp(part, 64);
   }
   *magnitude = scaling == TTS_GPT_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;

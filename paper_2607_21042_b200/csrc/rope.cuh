@@ -6,7 +6,7 @@
 // where the pair is (i, i + r/2) or (2i, 2i + 1) of the first r values; the others stay.  V stays.
 //
 // Angles.  The table holds w_i / 2 pi as a fraction of 2^64, so that p times it, in 64-bit integers that wrap, is the phase in turns
-// modulo one, to 2^-64 of a turn a position, however far p is (in fp32 the angle of position 10^5 is off by 2^-8 radians).  The nearest quarter turn is taken
+// modulo one, to two units of that a position, however far p is (in fp32 the angle of position 10^5 is off by 2^-8 radians).  The nearest quarter turn is taken
 // off in integers; what is left, at most an eighth of a turn either way, is rounded to fp32 (2^-27 half turns) and goes to sincospif.
 //
 // Split.  A thread takes two times 16 bytes of a (row, head): eight lanes of fp32 or four of bf16 have its 64 values, and where pairs lie half the rotated

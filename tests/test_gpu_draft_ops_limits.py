@@ -1,10 +1,12 @@
 """The draft operators where short things follow one another and where long ones end.  Tolerances as in test_gpu_draft_ops."""
+from decimal import Decimal as D, localcontext
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2607_21042_b200 import binding as B
-from test_gpu_draft_ops import E4M3_BLOCK, Drafts, _forest, _masks, _sees
+from test_gpu_draft_ops import E4M3_BLOCK, Drafts, _empty_pool, _forest, _masks, _sees
 from test_gpu_serving_ops import HALF, _bound, _check, _gen, _i32
 
 pytestmark = pytest.mark.gpu
@@ -137,3 +139,28 @@ def test_a_path_ends_at_its_first_hole(fmt, heads, lens, ends):
                 v[b // 64, :, :, b % 64] = old[a // 64, :, :, a % 64]
     B.op_kv_move(pool if fmt else pool.view(torch.bfloat16).unflatten(-1, (64, 64)), _i32(start.tolist()), _i32(path.tolist()), _i32(slot.tolist()))
     assert torch.equal(pool, want)
+
+
+# ---------------------------------------------------------------------------------------------
+# far positions
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n_rot", [4, 26, 64])
+@pytest.mark.parametrize("base", [10000.0, 500000.0])
+def test_cosine_and_sine_of_far_positions(base, n_rot):
+    """Pairs (1, 0) turn into cosine and sine.  The phase is that of the formula with 60 digits, modulo a turn, in whole numbers.  Off by: the table's two units of 2^-64 turns a
+    position, 2^31 times, 2 pi 2^-32 radians or 0.025 2^-24; what is left of the angle rounded to fp32, pi 2^-27 or 0.4 2^-24; an ulp of sincospif, 2^-24 (the product with a
+    magnitude of 1 is exact)."""
+    rows, g = 400, np.random.default_rng(n_rot)
+    pos = np.concatenate([[2 ** 31 - 1, -2 ** 31, 0, 1, -1, 2 ** 30], g.integers(-2 ** 31, 2 ** 31, rows - 6)])
+    with localcontext() as c:
+        c.prec = 60
+        two_pi = 2 * D("3.14159265358979323846264338327950288419716939937510582097494459")
+        turn = [int((-D(2 * i) / D(n_rot) * D(base).ln()).exp() / two_pi * 2 ** 128) for i in range(n_rot // 2)]
+    part = np.array([[int(p) * t % 2 ** 128 / 2 ** 128 for t in turn] for p in pos])
+    q = torch.zeros(rows, 64, device=DEV)
+    q[:, :n_rot // 2] = 1.0
+    got = B.op_rope_kv_append(q, q, q, _empty_pool(0, 8, 1), torch.arange(rows, dtype=torch.int32, device=DEV), _i32(pos.tolist()), B.op_rope_frequencies(n_rot, base=base, device=DEV)[0],
+                              q_out=torch.empty_like(q)).double().cpu().numpy()
+    off = max(np.abs(got[:, :n_rot // 2] - np.cos(2 * np.pi * part)).max(), np.abs(got[:, n_rot // 2:n_rot] - np.sin(2 * np.pi * part)).max())
+    assert off <= 1.43 * 2.0 ** -24, off * 2 ** 24
+    assert not got[:, n_rot:].any()
