@@ -498,8 +498,8 @@ int32_t tts_gpt_op_tree_tables(int32_t n, int32_t R, const int32_t *row_start, c
 /* Attention of trees: row r attends to all committed keys of its stream and, of the tree's nodes j, to those whose bit its mask has (any mask; the row's
  * own bit counts like the others; bits of nodes that the tree has not, and nodes beyond 32 mask_words, count as not set), o = softmax(scale q.K^T) V per head.
  * A row without keys is zero; a stream outside 0..max_streams-1 has none, and one of fewer tokens than the tree has nodes has the last nodes' keys.  Keys on a page outside 0..n_pages-1 are left out, as are those behind pages_per_stream
- * pages.  K and V of committed keys must be finite; those of a node matter only to rows that see it, which become NaN where they are not
- * finite (8-bit cache: where a scale is not).  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements apart; out bf16 [R][n_head*64]; neither it nor scratch may overlap anything else that
+ * pages.  K and V of committed keys must be finite; those of a node matter only to rows that see it.  These become NaN where its V is not
+ * finite (8-bit cache: V's scale), and where its K makes the score NaN or infinity; a score of -infinity has weight zero.  q: TTS_GPT_T_F32 or TTS_GPT_T_BF16, rows q_stride elements apart; out bf16 [R][n_head*64]; neither it nor scratch may overlap anything else that
  * the call is given (E_ARG).  t_max: at least the largest tree (rows beyond it are not computed); with the heads of a group it decides how a tile's
  * work is spread, so that small trees go faster in a call of their own than beside large ones.  Rows of no tree are left as they were; where starts do not
  * ascend, or exceed R, nothing is written.  Heads, roundings, timing and scratch as for op_attention_shared (scratch size independent of the

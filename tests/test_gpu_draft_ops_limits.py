@@ -164,3 +164,32 @@ def test_cosine_and_sine_of_far_positions(base, n_rot):
     off = max(np.abs(got[:, :n_rot // 2] - np.cos(2 * np.pi * part)).max(), np.abs(got[:, n_rot // 2:n_rot] - np.sin(2 * np.pi * part)).max())
     assert off <= 1.43 * 2.0 ** -24, off * 2 ** 24
     assert not got[:, n_rot:].any()
+
+
+# ---------------------------------------------------------------------------------------------
+# keys that are not finite
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("lens,ctx", [([20, 7], [33, 200]), ([64, 50], [10, 0]), ([100, 128], [70, 1])])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_a_key_that_is_not_finite(fmt, lens, ctx, value):
+    """Queries are positive, so that an infinite key has an infinite score: NaN in the rows that see it, or no weight where it is -infinity."""
+    d = Drafts(12, fmt, 2, lens, ctx)
+    _, parent = _forest(4, lens)
+    sees = [_sees(parent[a:b]) for a, b in zip(d.start[:-1], d.start[1:])]
+    q = d.queries(9, 4, torch.bfloat16).abs()
+    mask, odd = _masks(sees, (max(lens) + 31) // 32), [t // 3 for t in lens]
+    for i, j in enumerate(odd):
+        page, off = int(d.table[d.ids[i], (ctx[i] + j) // 64]), (ctx[i] + j) % 64
+        if fmt:
+            d.pool[page, 0, :, 64 * off:64 * off + 64] = 0xB8 if value < 0 else 0x38                       # minus or plus one
+            d.pool[page, 0, :, 4096:].view(torch.float32)[:, off] = abs(value)
+        else:
+            d.pool[page, 0, :, off, 17] = value
+    out = d.run(q, mask)
+    rows = [r for i, (a, b) in enumerate(zip(d.start[:-1], d.start[1:])) for r in range(a, b) if value < 0 or not sees[i][r - a, odd[i]]]
+    others = [r for r in range(int(d.start[-1])) if r not in set(rows)]
+    for i, m in enumerate(sees):
+        m[:, odd[i]] = False
+    d.check(out, q, sees, rows=rows)
+    assert bool(others) == (not value < 0) and torch.all(torch.isnan(out[others]))
