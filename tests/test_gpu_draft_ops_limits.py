@@ -193,3 +193,52 @@ def test_a_key_that_is_not_finite(fmt, lens, ctx, value):
         m[:, odd[i]] = False
     d.check(out, q, sees, rows=rows)
     assert bool(others) == (not value < 0) and torch.all(torch.isnan(out[others]))
+
+
+# ---------------------------------------------------------------------------------------------
+# large trees
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt,H,K,dtype,lens,ctx,words", [
+    (0, 2, 2, torch.bfloat16, [257, 1], [100, 30], 9), (1, 1, 1, torch.bfloat16, [500, 300], [0, 77], 16), (0, 1, 1, torch.float32, [1024, 40], [65, 500], 32),
+    (1, 4, 1, torch.float32, [700], [300], 22), (0, 5, 1, torch.bfloat16, [1023, 1, 513], [1, 900, 128], 32), (1, 3, 1, torch.bfloat16, [1100, 20], [50, 64], 32)])
+def test_trees_of_hundreds_of_nodes(fmt, H, K, dtype, lens, ctx, words):
+    """Masks of up to 32 words; nodes behind the 1024th count as not seen, and the rows of such nodes see others all the same."""
+    d = Drafts(sum(lens), fmt, K, lens, ctx)
+    rng = np.random.default_rng(3)
+    _, parent = _forest(sum(lens) + 1, lens, 9)
+    sees = [_sees(parent[a:b]) for a, b in zip(d.start[:-1], d.start[1:])]
+    for m in sees:
+        m[rng.random(len(m)) < 0.05] = False   # some see nothing of the tree, some all before them
+        m[rng.random(len(m)) < 0.05] = True
+        m[:, 32 * words:] = False
+    q, mask = d.queries(5, H, dtype), _masks([m[:, :32 * words] for m in sees], words)
+    out = d.run(q, mask)
+    for i, m in enumerate(sees):
+        _check_tree(d, i, out, q, m)
+    assert torch.all(out[d.start[-1]:] == 9.0)
+
+
+@pytest.mark.parametrize("n,words", [(1024, 32), (1100, 32), (600, 19), (600, 10)])
+def test_values_of_far_nodes_that_are_not_finite(n, words):
+    """Only rows whose masks name such a node see it, in the last words too; nodes that the masks cannot name are seen by none."""
+    d = Drafts(n, 0, 1, [n], [40])
+    rng = np.random.default_rng(4)
+    bad = [0, 31, 32, 300, min(n, 32 * words) - 1] + [j for j in (550, 1023, 1024, 1099) if j < n]
+    for j, value in zip(bad, [float("nan"), float("inf"), -float("inf")] * 3):
+        d.pool[int(d.table[0, (40 + j) // 64]), 1, 0, (40 + j) % 64, j % 64] = value
+    m = rng.random((n, n)) < 0.02
+    m[:, bad] = False
+    named = [j for j in bad if j < 32 * words]
+    for k, j in enumerate(named):
+        m[20 + 50 * k:24 + 50 * k, j] = True
+    m[:, 32 * words:] = False
+    q = d.queries(5, 2, torch.bfloat16)
+    out = d.run(q, _masks([m[:, :32 * words]], words))
+    lost = m[:, named].any(1)
+    want = np.isnan(out[:n].double().cpu().numpy()).reshape(n, -1)
+    assert np.array_equal(want.all(1), lost) and np.array_equal(want.any(1), lost) and lost.sum() == 4 * len(named)
+    for r in np.flatnonzero(~lost)[::7]:
+        k, v = d.keys_of(0)
+        on = np.concatenate([np.ones(40, bool), m[r]])
+        ref, tol = _bound(q[r].double().cpu().numpy().reshape(2, 64), k[on, 0], v[on, 0], 0.125, HALF[torch.bfloat16])
+        _check(out[r].view(2, 64), ref, tol, r)
