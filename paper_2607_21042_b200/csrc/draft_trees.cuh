@@ -94,7 +94,7 @@ inline cudaError_t launch_tree_tables(const TreeTableArgs &a, cudaStream_t st) {
 // accepted nodes and returns the pages behind them: request by request in the order of the call, the last page of a list first; or, where something is wrong, takes all
 // paths back.  It is the only one up to 32
 // trees, the first of a cluster up to 256, which finds the others' counts in their shared memory, and else the one that comes last.
-// Bound: launch, two dependent reads, two sums over the requests and a read of the pages.  Measured: 16 trees of up to 40 nodes 4.9 us, 128 of up to 200 7.1 us
+// Bound: launch, two dependent reads, two sums over the requests and a read of the pages.  Measured: 16 trees of up to 40 nodes 4.9 us, 128 of up to 200 7.0 us
 // (8.0 and 12.5 with a search of the children at every step of the path, 256 threads and tickets; 7.1 and 11.6 with parents and tokens in registers).
 // ---------------------------------------------------------------------------------------------
 struct TreeAcceptArgs {
@@ -313,7 +313,7 @@ inline cudaError_t launch_tree_accept(const TreeAcceptArgs &a, cudaStream_t st) 
 // tree and a layer; its threads own 16 bytes of a (K|V, head) row each and move it for all rows of the path, eight read before they are
 // written.  Row k comes from a row behind it (path[k] > k where it moves at all, and path ascends), which is behind every place that
 // rows before it go to: nothing is written before it has been read.
-// Bound: three dependent reads of indices, then bytes.  Measured: a layer of 16 trees' paths 2.7 us; 24 layers of 32 9.5 us, 4.0 TB/s (12.4 with the pieces of all rows
+// Bound: three dependent reads of indices, then bytes.  Measured: a layer of 16 trees' paths 2.7 us; 24 layers of 32 9.2 us, 4.1 TB/s (12.4 with the pieces of all rows
 // spread over the threads and a barrier between reads and writes).
 // ---------------------------------------------------------------------------------------------
 struct KvMoveArgs {
