@@ -118,6 +118,7 @@ template <int S, bool E4M3> struct TreeShape {
   static_assert(kRegsSoftmax + kRegsCopy + kRegsWiden <= kRegsLaunch * (S == 1 ? 2 : 3), "a split of more registers than the launch has would wait forever");
   static constexpr int kCtas = 2;            // an SM
   static constexpr int kRing = E4M3 ? 2 : 4; // pages of K and of V as the tensor cores take them
+  static_assert(E4M3 || kRing == 4, "tree_tile_in_place counts on four places");
   static constexpr int kRaw = E4M3 ? 4 : 0;  // pages of K and V as they are in the cache, codes and scales
   static constexpr int kRawPage = 2 * kE4m3BlockBytes;
   static constexpr int kScales = E4M3 ? kTrScales * 2 * kTrKeys * 4 : 0;
