@@ -469,8 +469,8 @@ enum { TTS_GPT_ROPE_NONE = 0, TTS_GPT_ROPE_LINEAR = 1, TTS_GPT_ROPE_NTK = 2, TTS
 
 /* The table op_rope_kv_append takes, on the host, no CUDA call: pair i of n_rot / 2 (n_rot even, 2..64) turns by w_i radians a position, w_i =
  * base^(-2 i / n_rot) stretched as `scaling` says, or inv_freq[i] (HOST, only with TTS_GPT_ROPE_GIVEN).  turns (HOST, n_rot / 2 values): w_i / 2 pi modulo 1 in
- * units of 2^-64, two units off at most (frequencies are formed with 64-bit significands; of given ones beyond a turn a position the last place of those counts), so that the phase of
- * position p is good to 2^-63 p turns.  *magnitude (HOST): what cosine and sine
+ * units of 2^-64, two units off at most, so that the phase of position p is good to 2^-63 p turns.  (Frequencies are formed with 64-bit significands.  Of given ones beyond a turn a
+ * position the last place of those counts; by number of turns, 20 high^2 / (original (high - low)) units come on top, for the rounded number between the two.)  *magnitude (HOST): what cosine and sine
  * are to be multiplied by.  Arguments that a scaling does not name are not looked at. */
 int32_t tts_gpt_op_rope_frequencies(int32_t n_rot, int32_t scaling, double base, double factor, double original, double low, double high, const double *inv_freq,
                                     uint64_t *turns, float *magnitude);

@@ -51,3 +51,14 @@ def test_blends(base, n_rot):
     fast = [min(max((original * x / TWO_PI - 1) / 3, D(0)), D(1)) for x in w]
     # (the number of turns is 4 at most where it counts, and a third of its rounding comes in)
     _near([x / factor * (1 - s) + x * s for x, s in zip(w, fast)], 2, n_rot=n_rot, base=base, scaling="bands", factor=16.0, original=4096)
+
+
+@pytest.mark.parametrize("low,high,original", [(1.0, 32.0, 100), (1.0, 1.001, 8192), (3.0, 3.5, 20), (0.01, 50.0, 4096)])
+def test_narrow_bands(low, high, original):
+    """The number of turns is off by 5 + ln(1 / w), at most 20, last places of itself (a power, three operations); by the band's width it moves the blend, and by r / original the turns."""
+    for n_rot in (32, 64):
+        w = _power(500000.0, n_rot)
+        fast = [min(max((original * x / TWO_PI - D(low)) / (D(high) - D(low)), D(0)), D(1)) for x in w]
+        assert any(0 < s < 1 for s in fast) or high - low < 0.01
+        _near([x / 8 * (1 - s) + x * s for x, s in zip(w, fast)], 2 + 20 * D(high) ** 2 / (D(original) * (D(high) - D(low))), n_rot=n_rot, base=500000.0, scaling="bands", factor=8.0,
+              original=original, low=low, high=high)
